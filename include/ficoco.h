@@ -13,7 +13,7 @@
  *     thread's current device (checked: FICOCO_EINVAL otherwise).  The library allocates no
  *     device memory and frees nothing of the caller's.  Outputs must not alias inputs
  *     (X_out overlapping X or the workspace is rejected with FICOCO_EINVAL; the small index
- *     and edge outputs are not checked).
+ *     and edge outputs are not checked).  The arrays of a ficoco_cache are read and changed in place.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  All work is
  *     enqueued on it asynchronously; no call synchronises the device or copies to the host.
  *   - Return value: a ficoco_status.  Argument errors are found on the host before anything
@@ -372,6 +372,118 @@ int ficoco_v_step_static(ficoco_ctx *ctx, const ficoco_problem *p, void *X_out, 
                          int32_t *keep_idx, int32_t *discard_idx, int32_t *edge_cnt,
                          int32_t *edge_tgt, double *edge_alpha, double *scores, int32_t *overflow,
                          void *stream);
+
+/* ---- The decoder's key / value cache ---------------------------------------------------------------
+ *
+ * A cache in pages of 8 bits for a decoder whose prompt is reduced by ficoco_l_step: pages are handed out,
+ * shared between the sequences that continue one prompt, rewritten without the tokens that a step discarded, given
+ * back, and attended to.  Everything it consists of is device memory of the caller:
+ *
+ *   k, v          [layers][n_pages][heads][page_size][d_head] E4M3 (OCP, 4 exponent and 3 mantissa bits), 16-byte aligned
+ *   k_exp, v_exp  [layers][n_pages][heads] uint8: the scale of a block (one page of one head) is 2^(byte - 127)
+ *   table         [n_seqs][max_pages] int32: page of tokens [i page_size, (i + 1) page_size) of a sequence, -1 = none
+ *   len           [n_seqs] int32: tokens of a sequence
+ *   refs          [n_pages] int32: sequences that hold a page, 0 = free
+ *
+ * An empty cache is table = -1, len = 0, refs = 0; pages and exponents need no value.  One table serves all
+ * layers.  The library keeps no state of its own: calls on one cache belong on one stream (or are ordered by the
+ * caller).  Only whole pages are ever shared, so a page that is written has one holder.
+ *
+ * Values: a block's exponent byte e is the smallest with max|x| <= 448 * 2^(e - 127), at least 17 (2^-110, also the
+ * byte of a block of zeros); x is stored as the E4M3 number nearest to x * 2^(127 - e), ties to even.  Infinities
+ * are stored as the largest number and, like NaN, do not count for the maximum; NaN stays NaN (byte 127).
+ *
+ * Sequences are named by slots 0 .. n_seqs - 1 in arrays on the device, which no call can check on the host:
+ * entries that are out of range, or that name a slot a second time where that has no meaning, are left out as each
+ * function says; page numbers out of range are taken for -1.  Limits: page_size 16, 32, 64 or 128; d_head 64 or 128
+ * (others FICOCO_EUNSUPPORTED); n_seqs <= 8192; at most 1024 sequences in a call of reserve, fork or compact.
+ */
+typedef struct {
+  int32_t layers, n_pages, page_size, heads, d_head, n_seqs, max_pages;
+  void *k, *v;
+  uint8_t *k_exp, *v_exp;
+  int32_t *table, *len, *refs;
+} ficoco_cache;
+
+/* Tokens of n sequences on their way into a cache or out of it: K[b][h][t], t < n_new[b] <= n_max, is the token at position
+ * start[b] + t of slot seq[b].  seq NULL = slot b; n_new NULL = n_max.  Strides in elements, d_head contiguous. */
+typedef struct {
+  int32_t n, n_max;
+  int32_t dtype;                    /* ficoco_dtype of K and V                              */
+  const int32_t *seq, *start, *n_new; /* [n] each                                           */
+  void *K, *V;                      /* [n][heads][n_max][d_head]                            */
+  int64_t k_stride_b, k_stride_h, k_stride_n;
+  int64_t v_stride_b, v_stride_h, v_stride_n;
+} ficoco_tokens;
+
+/* Attention problem.  Query t < q_len[b] of sequence b stands at position p = q_start[b] + t and sees key j where
+ *   j < k_len[b],  j <= p,  and (window = 0 or j > p - window or j < sinks):
+ * O[b][h][t] = sum_j softmax_j(scale * Q[b][h][t] . K[j]) V[j], zeros where no key is seen.  Rows t >= q_len[b] are left
+ * as they are.  Query head h reads key / value head h / (H / H_kv).  NULL arrays: q_len = n_q, q_start = k_len - q_len
+ * (the queries are the last tokens; a negative position sees nothing).  bfloat16; logits, exponentials and sums in single precision, the
+ * weights are rounded to bfloat16 for the product with V.  Strides in elements, d_head contiguous, any element alignment. */
+typedef struct {
+  int32_t B, H, H_kv, n_q, n_k, d_head;
+  const void *Q; /* [B][H][n_q][d_head] */
+  int64_t q_stride_b, q_stride_h, q_stride_n;
+  const void *K, *V; /* [B][H_kv][n_k][d_head]: ficoco_window_attention alone */
+  int64_t k_stride_b, k_stride_h, k_stride_n;
+  int64_t v_stride_b, v_stride_h, v_stride_n;
+  void *O; /* [B][H][n_q][d_head] */
+  int64_t o_stride_b, o_stride_h, o_stride_n;
+  const int32_t *seq;                     /* [B] slots, NULL = b: ficoco_cache_attention alone */
+  const int32_t *q_len, *k_len, *q_start; /* [B] each, or NULL                                 */
+  float scale;
+  int32_t window, sinks;
+  int32_t max_len; /* ficoco_cache_attention: about how many tokens the longest sequence has, 0 = as many as the
+                      table has room for.  It decides how the work is cut, never the result's meaning. */
+} ficoco_attention;
+
+/* Pages for n_new[b] more tokens of each sequence (n_new NULL: n_each), the free ones with the lowest numbers, in the
+ * order of the call; len grows by as much.  start[b], out: position of the first of them, for ficoco_cache_append.
+ * start[b] = -1 and nothing changes where the slot is out of range or named before in this call, n_new[b] < 0, the table's row
+ * is too short, or pages run out: from the first sequence that finds too few on, only those that need none are served. */
+int ficoco_cache_reserve(ficoco_ctx *ctx, const ficoco_cache *c, int32_t n, const int32_t *seq, const int32_t *n_new,
+                         int32_t n_each, int32_t *start, void *stream);
+
+/* Writes the tokens of one layer into their pages.  A page that is begun inside keeps what lies before: it takes the larger of
+ * its exponent and that of the new tokens, the older ones rewritten to it (exactly, but for E4M3's denormals).  What lies behind
+ * the new tokens in a page is void.  Sequences with start[b] < 0 are left out, and so are positions that have no page. */
+int ficoco_cache_append(ficoco_ctx *ctx, const ficoco_cache *c, int32_t layer, const ficoco_tokens *t, void *stream);
+
+/* The values that a layer's pages hold, as bfloat16 (exact) or single precision; K or V may be NULL.  start NULL = 0.  Positions
+ * that have no page give zeros, sequences with start[b] < 0 are left out.  (With K: the keys of ficoco_l_step's query/key form.) */
+int ficoco_cache_read(ficoco_ctx *ctx, const ficoco_cache *c, int32_t layer, const ficoco_tokens *t, void *stream);
+
+/* Sequence dst[b] continues src[b]: it shares its whole pages and has a copy, in all layers, of the page that is not full, or of every
+ * page (whole != 0).  done[b], out: 1, or 0 and nothing changes where a slot is out of range, dst[b] is not empty or named before in this
+ * call, src[b] is a dst of this call, or pages run out (as ficoco_cache_reserve). */
+int ficoco_cache_fork(ficoco_ctx *ctx, const ficoco_cache *c, int32_t n, const int32_t *src, const int32_t *dst,
+                      int32_t whole, int32_t *done, void *stream);
+
+/* The selection of a reduction step applied to sequences of the cache (see ficoco_gather_tokens): dst[b] becomes src[b]
+ * without the visual tokens that keep_idx [n][n_keep] (ascending) does not name, for layers [layer_begin, layer_begin + n_layers); the
+ * visual span is [vis_begin, vis_begin + N).  dst[b] = src[b] replaces the sequence; otherwise dst[b] must be empty.  Whole pages
+ * before the first token that moves are kept (shared); the others are written anew into free pages, each
+ * block with the exponent of what it holds, and src's own are given back if it is replaced.  Other layers of the new
+ * pages are void.  done[b], out: as ficoco_cache_fork (a src may be replaced, not read, by another entry), also 0 where src[b] has fewer than
+ * vis_begin + N tokens.  ws: ficoco_cache_workspace_bytes, 256-byte aligned. */
+int ficoco_cache_workspace_bytes(const ficoco_cache *c, int32_t n, size_t *out_bytes);
+int ficoco_cache_compact(ficoco_ctx *ctx, const ficoco_cache *c, int32_t layer_begin, int32_t n_layers, int32_t n, const int32_t *src,
+                         const int32_t *dst, int32_t vis_begin, int32_t N, int32_t n_keep, const int32_t *keep_idx,
+                         int32_t *done, void *ws, size_t ws_bytes, void *stream);
+
+/* Gives back the pages of the sequences, which are empty then.  Slots out of range or named twice are harmless. */
+int ficoco_cache_free(ficoco_ctx *ctx, const ficoco_cache *c, int32_t n, const int32_t *seq, void *stream);
+
+/* Attention over one layer of the cache; k_len NULL = len (a given k_len never reaches beyond it).  Any n_q: single tokens and whole
+ * questions.  Positions that have no page, or a slot out of range, hold no key.  The workspace may be used by one call at a time. */
+int ficoco_cache_attention_workspace_bytes(const ficoco_cache *c, const ficoco_attention *a, size_t *out_bytes);
+int ficoco_cache_attention(ficoco_ctx *ctx, const ficoco_cache *c, int32_t layer, const ficoco_attention *a, void *ws,
+                           size_t ws_bytes, void *stream);
+
+/* Attention of dense prompts (k_len NULL = n_k), with or without a window.  Keys that no query of a block sees are not read. */
+int ficoco_window_attention(ficoco_ctx *ctx, const ficoco_attention *a, void *stream);
 
 #ifdef __cplusplus
 }

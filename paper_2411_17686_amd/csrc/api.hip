@@ -2,11 +2,10 @@
 // declared in include/ficoco.h.  Host code only; every launch goes to the caller's stream.
 #include <algorithm>
 #include <cmath>
-#include <cstdio>
 #include <cstring>
 #include <new>
 
-#include "common.hpp"
+#include "ctx.hpp"
 
 // Scratch of the allocation-free entry point (ficoco_v_step_static): the workspace of a step
 // lives in this file-scope device array instead of caller memory.  Every GPU the library runs
@@ -20,13 +19,6 @@ static_assert(kStaticScratchBytes == (size_t)48 << 20, "the size that ficoco.h s
 static __device__ __align__(256) unsigned char g_static_scratch[kStaticScratchBytes];
 constexpr int kMaxDevices = 64;
 static void* g_static_ws[kMaxDevices];    // per device, filled by ficoco_create (written once per device with the same value)
-
-struct ficoco_ctx {
-  int device;
-  hipEvent_t probe_start, probe_stop;   // measurement hook, both null when off
-  int probe_kernel;
-  char err[512];
-};
 
 namespace ficoco {
 
@@ -368,26 +360,6 @@ int make_plan(const ficoco_problem& p, Plan& pl, const char** why, size_t scratc
   return FICOCO_OK;
 }
 
-static int fail(ficoco_ctx* ctx, int code, const char* what, const char* detail) {
-  if (ctx) std::snprintf(ctx->err, sizeof(ctx->err), "%s: %s", what, detail ? detail : "");
-  return code;
-}
-
-// The calling thread's current device must be the one the ctx was created for: every launch
-// goes to the current device, and the caller's pointers and stream belong to it.
-static int check_device(ficoco_ctx* ctx, const char* fn) {
-  int cur = -1;
-  if (hipGetDevice(&cur) != hipSuccess) return fail(ctx, FICOCO_EHIP, fn, "hipGetDevice failed");
-  if (cur != ctx->device) return fail(ctx, FICOCO_EINVAL, fn, "the current device is not the device this ctx was created for");
-  return FICOCO_OK;
-}
-
-// Do the byte ranges [a, a + na) and [b, b + nb) overlap?
-static bool ranges_overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
-  return a && b && na && nb && a0 < b0 + nb && b0 < a0 + na;
-}
-
 // Bytes from X to the end of its last row, and of the dense X_out.
 static size_t x_extent(const ficoco_problem& p) {
   const size_t es = p.dtype == FICOCO_BF16 ? 2 : 4;
@@ -408,12 +380,6 @@ static int prepare(ficoco_ctx* ctx, const ficoco_problem* p, const void* ws, siz
   if (rc != FICOCO_OK) return fail(ctx, rc, fn, why);
   if (!ws || ((uintptr_t)ws & 255)) return fail(ctx, FICOCO_EINVAL, fn, "workspace is NULL or not 256-byte aligned");
   if (ws_bytes < pl.total) return fail(ctx, FICOCO_ENOMEM, fn, "workspace smaller than ficoco_workspace_bytes()");
-  return FICOCO_OK;
-}
-
-static int finish(ficoco_ctx* ctx, const char* fn) {
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return fail(ctx, FICOCO_EHIP, fn, hipGetErrorString(e));
   return FICOCO_OK;
 }
 

@@ -1,0 +1,114 @@
+// What the two attention kernels share: the rows of a workgroup, which keys they see, and the parts of a result whose
+// keys are cut over several workgroups.
+#pragma once
+#include "cache.hpp"
+
+namespace ficoco {
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+// A key / value head serves `group` query heads; their rows are taken together, row r = query r / group of head
+// r % group, so that a block's keys are read once for all of them.
+struct AttendArgs {
+  const bf16_t* Q;
+  int64_t q_sb, q_sh, q_sn;
+  bf16_t* O;
+  int64_t o_sb, o_sh, o_sn;
+  const int32_t *seq, *q_len, *k_len, *q_start;
+  int B, H_kv, group, n_q, n_k, splits, row_tiles;
+  float scale_log2e;
+  int window, sinks;
+  // pages of the layer
+  const uint8_t *k, *v, *k_exp, *v_exp;
+  const int32_t *table, *len;
+  int n_pages, n_seqs, max_pages, page_shift;
+  // dense keys and values
+  const bf16_t *K, *V;
+  int64_t k_sb, k_sh, k_sn, v_sb, v_sh, v_sn;
+  // parts of cut rows: [B * H_kv][splits][rows] of (maximum, sum) and of sums of values
+  float2* part_ms;
+  float* part_o;
+  int part_rows;                      // row_tiles * rows of a workgroup
+};
+
+constexpr float kNoLogit = -3.402823466e38f;     // maximum of a row that has seen nothing (a finite one: differences stay numbers)
+
+// What the rows of one sequence see.
+struct Sight {
+  int first;        // position of query 0
+  int queries;      // that count
+  int keys;         // keys there are
+};
+template <bool PAGED>
+__device__ __forceinline__ Sight sight_of(const AttendArgs& a, int b, int& slot) {
+  Sight s;
+  slot = b;
+  if constexpr (PAGED) {
+    slot = a.seq ? a.seq[b] : b;
+    const bool ok = slot >= 0 && slot < a.n_seqs;
+    slot = ok ? slot : 0;
+    s.keys = ok ? a.len[slot] : 0;
+    const int64_t room = (int64_t)a.max_pages << a.page_shift;
+    s.keys = s.keys < room ? s.keys : (int)room;
+  } else {
+    s.keys = a.n_k;
+  }
+  if (a.k_len) s.keys = a.k_len[b] < s.keys ? a.k_len[b] : s.keys;
+  s.keys = s.keys > 0 ? s.keys : 0;
+  s.queries = a.q_len ? a.q_len[b] : a.n_q;
+  s.first = a.q_start ? a.q_start[b] : s.keys - s.queries;
+  s.queries = s.queries < a.n_q ? s.queries : a.n_q;
+  return s;
+}
+
+// Blocks of KEYS keys that queries at positions lo .. hi of a sequence see: `head` blocks from key 0 on (the first tokens),
+// then the blocks from `near` on.
+template <int KEYS>
+struct Blocks {
+  int head, near, count;
+  int near_key, first_keys;       // keys below near_key are seen by no row unless they are below first_keys
+  int end;                        // keys behind the last one seen
+  __device__ __forceinline__ Blocks(const AttendArgs& a, const Sight& s, int lo, int hi) {
+    end = hi + 1 < s.keys ? hi + 1 : s.keys;
+    end = end > 0 ? end : 0;
+    near_key = a.window > 0 && lo >= a.window ? lo - a.window + 1 : 0;
+    near_key = near_key < end ? near_key : end;
+    first_keys = a.sinks < near_key ? a.sinks : near_key;
+    near = near_key / KEYS;
+    head = (first_keys + KEYS - 1) / KEYS;
+    head = head < near ? head : near;
+    count = head + (end + KEYS - 1) / KEYS - near;
+  }
+  __device__ __forceinline__ int block(int i) const { return i < head ? i : near + (i - head); }
+};
+
+__device__ __forceinline__ bool key_seen(const AttendArgs& a, int key, int pos, int keys) {
+  return key < keys && key <= pos && (a.window <= 0 || (int64_t)key > (int64_t)pos - a.window || key < a.sinks);
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, bf16x2_t{(__bf16)a, (__bf16)b});
+}
+// Four E4M3 numbers times a power of two as four bfloat16 (exact).
+__device__ __forceinline__ uint2 widen_e4m3(uint32_t q, float scale) {
+  return uint2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q, scale, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q, scale, true))};
+}
+
+// How the keys of a call are cut: few workgroups otherwise leave compute units idle.
+struct AttendPlan {
+  bool few;            // single tokens (cache_attn.hip), else tiles of 128 rows (tile_attn.hip)
+  int rows;            // rows of a workgroup
+  int row_tiles, splits;
+  size_t part_ms, part_o, total;
+};
+AttendPlan attend_plan(const ficoco_attention& a, int heads, int64_t max_keys, bool paged);
+
+void launch_few_rows(const AttendArgs& a, const AttendPlan& pl, int d_head, hipStream_t s);
+void launch_tile_rows(const AttendArgs& a, int d_head, bool paged, hipStream_t s);
+void launch_join_rows(const AttendArgs& a, int d_head, hipStream_t s);
+
+}  // namespace ficoco

@@ -1,0 +1,537 @@
+// Pages of the decoder's key / value cache: handing them out, sharing, rewriting and giving them back, and the blocks
+// of 8 bits that hold the tokens.
+//
+// A call that hands out pages is two launches: one workgroup decides (a thread per sequence: what it needs, prefix sums
+// over the call, the free pages with the lowest numbers found by a scan of `refs`), then the chip moves the bytes.
+// Nothing is decided by the order in which workgroups run: every result is the same in every run.
+#include "cache.hpp"
+
+namespace ficoco {
+namespace {
+
+constexpr int kPlanThreads = kMaxCall;
+constexpr int kNone = 0x7fffffff;
+constexpr int kMoveThreads = 256;
+
+struct PlanLds {
+  int owner[kMaxSlots];      // the first entry of the call that names a slot
+  int end[kMaxCall];         // pages needed by entries 0 .. b
+  int scratch[kPlanThreads / kWave];
+  int served;
+};
+
+__device__ __forceinline__ bool slot_ok(const ficoco_cache& c, int s) { return s >= 0 && s < c.n_seqs; }
+__device__ __forceinline__ bool page_ok(const ficoco_cache& c, int p) { return p >= 0 && p < c.n_pages; }
+__device__ __forceinline__ int pages_of(const ficoco_cache& c, int64_t tokens) { return (int)((tokens + c.page_size - 1) / c.page_size); }
+
+// owner[s] = the first entry b of the call with slot(b) == s
+template <typename F>
+__device__ __forceinline__ void find_owners(const ficoco_cache& c, PlanLds& l, int n, F slot) {
+  for (int i = threadIdx.x; i < c.n_seqs; i += kPlanThreads) l.owner[i] = kNone;
+  if (threadIdx.x == 0) l.served = 0;
+  __syncthreads();
+  if ((int)threadIdx.x < n) {
+    const int s = slot(threadIdx.x);
+    if (slot_ok(c, s)) atomicMin(&l.owner[s], (int)threadIdx.x);
+  }
+  __syncthreads();
+}
+
+// Eight refs of a thread, page i0 on: their free ones as a bit mask.
+__device__ __forceinline__ int free_mask(const ficoco_cache& c, int i0) {
+  int m = 0;
+  if (i0 + 8 <= c.n_pages) {
+    int r[8];
+    __builtin_memcpy(r, c.refs + i0, 32);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m |= (r[j] == 0) << j;
+  } else {
+    for (int j = 0; i0 + j < c.n_pages; ++j) m |= (c.refs[i0 + j] == 0) << j;
+  }
+  return m;
+}
+
+// Every entry's thread (tid < n, others need = 0) asks for `need` pages; take(b, k, page) gets page k of entry b, the free pages
+// in ascending order.  Entries are served in order as long as the pages last.  Returns whether this thread's entry is.
+template <typename F>
+__device__ __forceinline__ bool hand_out(const ficoco_cache& c, PlanLds& l, int n, int need, F take) {
+  int total;
+  const int end = block_scan_inclusive(need, l.scratch, &total);
+  if ((int)threadIdx.x < n) l.end[threadIdx.x] = end;
+  if (total == 0) return true;                            // (uniform)
+  int n_free = 0;
+  for (int base = 0; base < c.n_pages && n_free < total; base += 8 * kPlanThreads) {
+    int t;
+    (void)block_scan_inclusive(__popc(free_mask(c, base + 8 * (int)threadIdx.x)), l.scratch, &t);
+    n_free += t;
+  }
+  const bool ok = need == 0 || end <= n_free;
+  if (need > 0 && ok) atomicMax(&l.served, end);
+  __syncthreads();
+  const int give = l.served;
+  int given = 0;
+  for (int base = 0; base < c.n_pages && given < give; base += 8 * kPlanThreads) {
+    const int i0 = base + 8 * (int)threadIdx.x, m = free_mask(c, i0);
+    int t;
+    int r = given + block_scan_inclusive(__popc(m), l.scratch, &t) - __popc(m);
+    for (int j = 0; j < 8; ++j) {
+      if (!(m >> j & 1)) continue;
+      if (r < give) {
+        int lo = 0, hi = n - 1;                           // first entry whose end lies behind r
+        while (lo < hi) {
+          const int mid = (lo + hi) / 2;
+          if (l.end[mid] > r) hi = mid; else lo = mid + 1;
+        }
+        take(lo, r - (lo ? l.end[lo - 1] : 0), i0 + j);
+      }
+      ++r;
+    }
+    given += t;
+  }
+  return ok;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void cache_reserve_kernel(ficoco_cache c, int n, const int32_t* __restrict__ seq,
+                                                                     const int32_t* __restrict__ n_new, int n_each, int32_t* __restrict__ start) {
+  __shared__ PlanLds l;
+  __shared__ int slot[kMaxCall], have[kMaxCall];
+  const int b = threadIdx.x;
+  auto slot_of = [&](int i) { return seq ? seq[i] : i; };
+  find_owners(c, l, n, slot_of);
+  int need = 0, len = 0, add = 0;
+  bool ok = false;
+  if (b < n) {
+    const int s = slot_of(b);
+    add = n_new ? n_new[b] : n_each;
+    ok = slot_ok(c, s) && l.owner[s] == b && add >= 0;
+    if (ok) {
+      len = c.len[s];
+      ok = len >= 0 && (int64_t)len + add <= (int64_t)c.max_pages * c.page_size;
+    }
+    if (ok) {
+      have[b] = pages_of(c, len);
+      need = pages_of(c, (int64_t)len + add) - have[b];
+    }
+    slot[b] = s;
+  }
+  __syncthreads();
+  const bool served = hand_out(c, l, n, need, [&](int e, int k, int page) {
+    c.table[(int64_t)slot[e] * c.max_pages + have[e] + k] = page;
+    c.refs[page] = 1;
+  });
+  if (b < n) {
+    if (ok && served) c.len[slot[b]] = len + add;
+    start[b] = ok && served ? len : -1;
+  }
+}
+
+// ---- tokens in and out of blocks ----------------------------------------------------------------------------
+__device__ __forceinline__ void load8f(const bf16_t* p, float (&x)[8]) {
+  uint4 r;
+  __builtin_memcpy(&r, p, 16);
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void load8f(const float* p, float (&x)[8]) { __builtin_memcpy(x, p, 32); }
+__device__ __forceinline__ void store8f(float* p, const float (&x)[8]) { __builtin_memcpy(p, x, 32); }
+__device__ __forceinline__ void store8f(bf16_t* p, const float (&x)[8]) {      // (exact: three mantissa bits)
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = (__float_as_uint(x[2 * i]) >> 16) | (__float_as_uint(x[2 * i + 1]) & 0xffff0000u);
+  __builtin_memcpy(p, w, 16);
+}
+
+struct TokenSide {       // K or V of a call
+  const void* x;
+  int64_t sb, sh, sn;
+  uint8_t* pool;
+  uint8_t* exps;
+};
+
+__device__ __forceinline__ float block_max(float v, float* scratch) {
+  v = wave_reduce(v, [](float a, float b) { return fmaxf(a, b); });
+  const int nw = blockDim.x / kWave;
+  __syncthreads();
+  if (threadIdx.x % kWave == 0) scratch[threadIdx.x / kWave] = v;
+  __syncthreads();
+  for (int w = 0; w < nw; ++w) v = fmaxf(v, scratch[w]);
+  return v;
+}
+
+// One workgroup per touched page, head, sequence and K / V.  GPT: groups of eight values a thread.
+template <typename T, int GPT>
+__global__ __launch_bounds__(kMoveThreads) void cache_append_kernel(ficoco_cache c, int64_t layer_pages, TokenSide ks, TokenSide vs, int n_max,
+                                                                    const int32_t* __restrict__ seq, const int32_t* __restrict__ start,
+                                                                    const int32_t* __restrict__ n_new) {
+  __shared__ float scratch[kMoveThreads / kWave];
+  const int b = blockIdx.z >> 1, h = blockIdx.y, P = c.page_size, per_row = c.d_head / 8;
+  const TokenSide& side = blockIdx.z & 1 ? vs : ks;
+  const int s = seq ? seq[b] : b, first = start[b];
+  int n = n_new ? n_new[b] : n_max;
+  n = n < n_max ? n : n_max;
+  if (!slot_ok(c, s) || first < 0 || n <= 0) return;
+  const int64_t stop = (int64_t)first + n;
+  const int64_t at = first / P + (int64_t)blockIdx.x;
+  if (at * P >= stop || at >= c.max_pages) return;
+  const int page = c.table[(int64_t)s * c.max_pages + at];
+  if (!page_ok(c, page)) return;
+  const int64_t block = (layer_pages + page) * c.heads + h;
+  uint8_t* pool = side.pool + block * P * c.d_head;
+  const T* x = (const T*)side.x + (int64_t)b * side.sb + (int64_t)h * side.sh;
+
+  float v[GPT][8];
+  float top = 0.0f;
+#pragma unroll
+  for (int j = 0; j < GPT; ++j) {
+    const int g = threadIdx.x + j * kMoveThreads, row = g / per_row;
+    const int64_t pos = at * P + row;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[j][i] = 0.0f;
+    if (row < P && pos >= first && pos < stop) load8f(x + (pos - first) * side.sn + g % per_row * 8, v[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < GPT; ++j) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_magnitude(v[j][i]));
+  }
+  int e = block_exponent(block_max(top, scratch));
+  const bool begun = at * P < first;
+  const int old = begun ? side.exps[block] : 0;
+  e = e > old ? e : old;
+  const float inv = exp_inverse(e);
+  __syncthreads();                                         // the byte is read before it is written
+#pragma unroll
+  for (int j = 0; j < GPT; ++j) {
+    const int g = threadIdx.x + j * kMoveThreads, row = g / per_row;
+    const int64_t pos = at * P + row;
+    if (row >= P || pos >= stop) continue;
+    uint8_t* to = pool + (int64_t)g * 8;
+    if (pos < first) {
+      if (e == old) continue;
+      uint2 q;
+      __builtin_memcpy(&q, to, 8);
+      from_e4m3(q, exp_scale(old), v[j]);
+    }
+    const uint2 q = to_e4m3(v[j], inv);
+    __builtin_memcpy(to, &q, 8);
+  }
+  if (threadIdx.x == 0) side.exps[block] = (uint8_t)e;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kMoveThreads) void cache_read_kernel(ficoco_cache c, int64_t layer_pages, TokenSide ks, TokenSide vs, int n_max,
+                                                                  const int32_t* __restrict__ seq, const int32_t* __restrict__ start,
+                                                                  const int32_t* __restrict__ n_new) {
+  const int b = blockIdx.z >> 1, h = blockIdx.y, P = c.page_size, per_row = c.d_head / 8;
+  const TokenSide& side = blockIdx.z & 1 ? vs : ks;
+  if (!side.x) return;
+  const int s = seq ? seq[b] : b, first = start ? start[b] : 0;
+  int n = n_new ? n_new[b] : n_max;
+  n = n < n_max ? n : n_max;
+  if (first < 0) return;
+  const int g = threadIdx.x % per_row;
+  const int t = (int)(blockIdx.x * (kMoveThreads / per_row) + threadIdx.x / per_row);
+  if (t >= n) return;
+  const int64_t pos = (int64_t)first + t, at = pos / P;
+  float v[8] = {};
+  const int page = slot_ok(c, s) && at < c.max_pages ? c.table[(int64_t)s * c.max_pages + at] : -1;
+  if (page_ok(c, page)) {
+    const int64_t block = (layer_pages + page) * c.heads + h;
+    uint2 q;
+    __builtin_memcpy(&q, side.pool + (block * P + pos % P) * c.d_head + g * 8, 8);
+    from_e4m3(q, exp_scale(side.exps[block]), v);
+  }
+  store8f((T*)const_cast<void*>(side.x) + (int64_t)b * side.sb + (int64_t)h * side.sh + (int64_t)t * side.sn + g * 8, v);
+}
+
+// ---- fork -------------------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(kPlanThreads) void cache_fork_kernel(ficoco_cache c, int n, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
+                                                                  int whole, int32_t* __restrict__ done) {
+  __shared__ PlanLds l;
+  __shared__ int from[kMaxCall], to[kMaxCall], shared[kMaxCall];
+  const int b = threadIdx.x;
+  find_owners(c, l, n, [&](int i) { return dst[i]; });
+  int need = 0, len = 0;
+  bool ok = false;
+  if (b < n) {
+    const int s = src[b], d = dst[b];
+    ok = slot_ok(c, s) && slot_ok(c, d) && l.owner[d] == b && l.owner[s] == kNone;
+    if (ok) {
+      len = c.len[s];
+      ok = c.len[d] == 0 && len >= 0 && pages_of(c, len) <= c.max_pages;
+    }
+    from[b] = s;
+    to[b] = d;
+    shared[b] = ok && !whole ? len / c.page_size : 0;
+    need = ok ? pages_of(c, len) - shared[b] : 0;
+  }
+  __syncthreads();
+  const bool served = ok & hand_out(c, l, n, need, [&](int e, int k, int page) {
+    c.table[(int64_t)to[e] * c.max_pages + shared[e] + k] = page;
+    c.refs[page] = 1;
+  });
+  if (b < n) {
+    if (served) c.len[to[b]] = len;
+    done[b] = served;
+    if (!served) shared[b] = 0;
+  }
+  __syncthreads();                                         // (also: the scans are over before refs change below)
+  for (int e = threadIdx.x / kWave; e < n; e += kPlanThreads / kWave) {
+    for (int i = threadIdx.x % kWave; i < shared[e]; i += kWave) {
+      const int page = c.table[(int64_t)from[e] * c.max_pages + i];
+      c.table[(int64_t)to[e] * c.max_pages + i] = page;
+      if (page_ok(c, page)) atomicAdd(&c.refs[page], 1);
+    }
+  }
+}
+
+// Whole pages of all layers, as they are.  Workgroups of one sequence, layer, head and K / V walk its copied pages.
+__global__ __launch_bounds__(kMoveThreads) void cache_copy_kernel(ficoco_cache c, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
+                                                                  int whole, const int32_t* __restrict__ done) {
+  const int b = blockIdx.z >> 1;
+  if (!done[b]) return;
+  const int from = src[b], to = dst[b], len = c.len[to], pages = pages_of(c, len);
+  const int layer = blockIdx.y / c.heads, h = blockIdx.y % c.heads;
+  uint8_t* pool = (uint8_t*)(blockIdx.z & 1 ? c.v : c.k);
+  uint8_t* exps = blockIdx.z & 1 ? c.v_exp : c.k_exp;
+  const int block_bytes = c.page_size * c.d_head;
+  for (int i = (whole ? 0 : len / c.page_size) + blockIdx.x; i < pages; i += gridDim.x) {
+    const int p = c.table[(int64_t)from * c.max_pages + i], q = c.table[(int64_t)to * c.max_pages + i];
+    if (!page_ok(c, p) || !page_ok(c, q)) continue;
+    const int64_t bp = ((int64_t)layer * c.n_pages + p) * c.heads + h, bq = ((int64_t)layer * c.n_pages + q) * c.heads + h;
+    const uint4* x = (const uint4*)(pool + bp * block_bytes);
+    uint4* y = (uint4*)(pool + bq * block_bytes);
+    for (int j = threadIdx.x; j < block_bytes / 16; j += kMoveThreads) y[j] = x[j];
+    if (threadIdx.x == 0) exps[bq] = exps[bp];
+  }
+}
+
+// ---- compact ------------------------------------------------------------------------------------------------------
+struct CompactMeta { int first, pages, tokens, pad; };
+
+__global__ __launch_bounds__(kPlanThreads) void cache_compact_plan_kernel(ficoco_cache c, int n, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
+                                                                          int vis_begin, int N, int n_keep, const int32_t* __restrict__ keep_idx,
+                                                                          int32_t* __restrict__ done, CompactMeta* __restrict__ meta, int32_t* __restrict__ rows) {
+  __shared__ PlanLds l;
+  __shared__ int from[kMaxCall], to[kMaxCall], moved[kMaxCall], first[kMaxCall], had[kMaxCall], now[kMaxCall];
+  const int b = threadIdx.x, lane = threadIdx.x % kWave;
+  find_owners(c, l, n, [&](int i) { return dst[i]; });
+  // the first preserved token that moves: its rank among the preserved ones
+  for (int e = threadIdx.x / kWave; e < n; e += kPlanThreads / kWave) {
+    const int32_t* k = keep_idx + (int64_t)e * n_keep;
+    int at = n_keep;
+    for (int i0 = 0; i0 < n_keep; i0 += kWave) {
+      const int i = i0 + lane;
+      const uint64_t m = __ballot(i < n_keep && k[i] != i);
+      if (m) {
+        at = i0 + __ffsll((long long)m) - 1;
+        break;
+      }
+    }
+    if (lane == 0) moved[e] = at;
+  }
+  __syncthreads();
+  int need = 0, new_len = 0;
+  bool ok = false;
+  if (b < n) {
+    const int s = src[b], d = dst[b];
+    ok = slot_ok(c, s) && slot_ok(c, d) && l.owner[d] == b && (s == d || l.owner[s] == kNone);
+    int f = 0, pages = 0, have = 0;
+    if (ok) {
+      const int len = c.len[s];
+      have = pages_of(c, len > 0 ? len : 0);
+      ok = (int64_t)len >= (int64_t)vis_begin + N && have <= c.max_pages && (s == d || c.len[d] == 0);
+      new_len = len - (N - n_keep);
+      pages = pages_of(c, new_len > 0 ? new_len : 0);
+      const int change = moved[b] < n_keep ? vis_begin + moved[b] : n_keep == N ? new_len : vis_begin + n_keep;
+      f = s == d && moved[b] == n_keep && n_keep == N ? pages : change / c.page_size;
+    }
+    from[b] = s;
+    to[b] = d;
+    first[b] = ok ? f : 0;
+    had[b] = ok ? have : 0;
+    now[b] = ok ? pages : 0;
+    need = ok ? pages - f : 0;
+  }
+  __syncthreads();
+  for (int e = threadIdx.x / kWave; e < n; e += kPlanThreads / kWave)
+    for (int i = lane; i < had[e]; i += kWave) rows[(int64_t)e * c.max_pages + i] = c.table[(int64_t)from[e] * c.max_pages + i];
+  __syncthreads();                                         // the rows are saved before new pages go into them
+  const bool served = ok & hand_out(c, l, n, need, [&](int e, int k, int page) {
+    c.table[(int64_t)to[e] * c.max_pages + first[e] + k] = page;
+    c.refs[page] = 1;
+  });
+  if (b < n) {
+    if (served) c.len[to[b]] = new_len;
+    done[b] = served;
+    meta[b] = CompactMeta{first[b], served ? now[b] : 0, new_len, 0};
+    if (!served) had[b] = 0;
+  }
+  __syncthreads();
+  for (int e = threadIdx.x / kWave; e < n; e += kPlanThreads / kWave) {
+    const int32_t* row = rows + (int64_t)e * c.max_pages;
+    const bool in_place = from[e] == to[e];
+    for (int i = lane; i < had[e]; i += kWave) {
+      const int page = row[i];
+      if (i < first[e]) {
+        if (!in_place) {
+          c.table[(int64_t)to[e] * c.max_pages + i] = page;
+          if (page_ok(c, page)) atomicAdd(&c.refs[page], 1);
+        }
+      } else if (in_place) {
+        if (page_ok(c, page)) atomicSub(&c.refs[page], 1);
+        if (i >= now[e]) c.table[(int64_t)to[e] * c.max_pages + i] = -1;
+      }
+    }
+  }
+}
+
+// The new pages of one sequence, layer, head and K / V, a workgroup each in turn: rows gathered from the pages before,
+// with their exponents, the block's own exponent, and back to 8 bits.  The pages read are not among those written: they are
+// held until the plan of a later call.
+template <int GPT>
+__global__ __launch_bounds__(kMoveThreads) void cache_compact_kernel(ficoco_cache c, int layer_begin, int vis_begin, int N, int n_keep,
+                                                                     const int32_t* __restrict__ dst, const int32_t* __restrict__ keep_idx,
+                                                                     const CompactMeta* __restrict__ meta, const int32_t* __restrict__ rows) {
+  __shared__ float scratch[kMoveThreads / kWave];
+  const int b = blockIdx.z >> 1;
+  const CompactMeta m = meta[b];
+  const int P = c.page_size, per_row = c.d_head / 8, block_bytes = P * c.d_head;
+  const int64_t layer = layer_begin + blockIdx.y / c.heads, h = blockIdx.y % c.heads;
+  uint8_t* pool = (uint8_t*)(blockIdx.z & 1 ? c.v : c.k);
+  uint8_t* exps = blockIdx.z & 1 ? c.v_exp : c.k_exp;
+  for (int page_at = m.first + blockIdx.x; page_at < m.pages; page_at += gridDim.x) {
+    const int page = c.table[(int64_t)dst[b] * c.max_pages + page_at];
+    if (!page_ok(c, page)) continue;                       // (uniform)
+    uint2 q[GPT];
+    int e_old[GPT];
+#pragma unroll
+    for (int j = 0; j < GPT; ++j) {
+      const int g = threadIdx.x + j * kMoveThreads, row = g / per_row;
+      const int64_t r = (int64_t)page_at * P + row;
+      q[j] = uint2{0, 0};
+      e_old[j] = kExpMin;
+      if (row < P && r < m.tokens) {
+        int64_t t = r;
+        if (r >= vis_begin + n_keep) {
+          t = r + (N - n_keep);
+        } else if (r >= vis_begin) {
+          const int k = keep_idx[(int64_t)b * n_keep + (r - vis_begin)];
+          t = vis_begin + (k < 0 ? 0 : k < N ? k : N - 1);
+        }
+        const int old = rows[(int64_t)b * c.max_pages + t / P];
+        if (page_ok(c, old)) {
+          const int64_t block = (layer * c.n_pages + old) * c.heads + h;
+          __builtin_memcpy(&q[j], pool + block * block_bytes + t % P * c.d_head + g % per_row * 8, 8);
+          e_old[j] = exps[block];
+        }
+      }
+    }
+    float v[GPT][8];
+    float top = 0.0f;
+#pragma unroll
+    for (int j = 0; j < GPT; ++j) {
+      from_e4m3(q[j], exp_scale(e_old[j]), v[j]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_magnitude(v[j][i]));
+    }
+    const int e = block_exponent(block_max(top, scratch));
+    const int64_t block = (layer * c.n_pages + page) * c.heads + h;
+#pragma unroll
+    for (int j = 0; j < GPT; ++j) {
+      const int g = threadIdx.x + j * kMoveThreads, row = g / per_row;
+      if (row >= P || (int64_t)page_at * P + row >= m.tokens) continue;
+      const uint2 w = to_e4m3(v[j], exp_inverse(e));
+      __builtin_memcpy(pool + block * block_bytes + (int64_t)g * 8, &w, 8);
+    }
+    if (threadIdx.x == 0) exps[block] = (uint8_t)e;
+  }
+}
+
+// ---- free -----------------------------------------------------------------------------------------------------------
+// A workgroup per entry; an entry of the table is taken out by one exchange, so a slot named twice gives its pages back once.
+__global__ __launch_bounds__(kMoveThreads) void cache_free_kernel(ficoco_cache c, const int32_t* __restrict__ seq) {
+  const int s = seq ? seq[blockIdx.x] : (int)blockIdx.x;
+  if (!slot_ok(c, s)) return;
+  for (int i = threadIdx.x; i < c.max_pages; i += kMoveThreads) {
+    int32_t* at = c.table + (int64_t)s * c.max_pages + i;
+    if (*at < 0) continue;
+    const int page = atomicExch(at, -1);
+    if (page_ok(c, page)) atomicSub(&c.refs[page], 1);
+  }
+  if (threadIdx.x == 0) c.len[s] = 0;
+}
+
+TokenSide side_of(const ficoco_cache& c, const ficoco_tokens& t, int layer, bool v) {
+  (void)layer;
+  return v ? TokenSide{t.V, t.v_stride_b, t.v_stride_h, t.v_stride_n, (uint8_t*)c.v, c.v_exp}
+           : TokenSide{t.K, t.k_stride_b, t.k_stride_h, t.k_stride_n, (uint8_t*)c.k, c.k_exp};
+}
+
+// Workgroups that walk the pages of one sequence, layer, head and K / V.
+int page_walkers(const ficoco_cache& c, int64_t others) {
+  const int64_t want = (8192 + others - 1) / others;
+  return (int)(want < 1 ? 1 : want < c.max_pages ? want : c.max_pages);
+}
+
+template <typename T>
+void append_groups(const ficoco_cache& c, int layer, const ficoco_tokens& t, hipStream_t s) {
+  const int touched = (t.n_max + c.page_size - 2) / c.page_size + 1;
+  const dim3 grid(touched, c.heads, 2 * t.n);
+  const TokenSide k = side_of(c, t, layer, false), v = side_of(c, t, layer, true);
+  const int64_t lp = (int64_t)layer * c.n_pages;
+  const int groups = c.page_size * c.d_head / 8;
+  if (groups <= 256) hipLaunchKernelGGL((cache_append_kernel<T, 1>), grid, dim3(kMoveThreads), 0, s, c, lp, k, v, t.n_max, t.seq, t.start, t.n_new);
+  else if (groups <= 512) hipLaunchKernelGGL((cache_append_kernel<T, 2>), grid, dim3(kMoveThreads), 0, s, c, lp, k, v, t.n_max, t.seq, t.start, t.n_new);
+  else if (groups <= 1024) hipLaunchKernelGGL((cache_append_kernel<T, 4>), grid, dim3(kMoveThreads), 0, s, c, lp, k, v, t.n_max, t.seq, t.start, t.n_new);
+  else hipLaunchKernelGGL((cache_append_kernel<T, 8>), grid, dim3(kMoveThreads), 0, s, c, lp, k, v, t.n_max, t.seq, t.start, t.n_new);
+}
+
+}  // namespace
+
+void launch_cache_reserve(const ficoco_cache& c, int n, const int32_t* seq, const int32_t* n_new, int n_each, int32_t* start, hipStream_t s) {
+  hipLaunchKernelGGL(cache_reserve_kernel, dim3(1), dim3(kPlanThreads), 0, s, c, n, seq, n_new, n_each, start);
+}
+
+void launch_cache_append(const ficoco_cache& c, int layer, const ficoco_tokens& t, hipStream_t s) {
+  if (t.dtype == FICOCO_BF16) append_groups<bf16_t>(c, layer, t, s); else append_groups<float>(c, layer, t, s);
+}
+
+void launch_cache_read(const ficoco_cache& c, int layer, const ficoco_tokens& t, hipStream_t s) {
+  const int rows = kMoveThreads / (c.d_head / 8);
+  const dim3 grid((t.n_max + rows - 1) / rows, c.heads, 2 * t.n);
+  const TokenSide k = side_of(c, t, layer, false), v = side_of(c, t, layer, true);
+  const int64_t lp = (int64_t)layer * c.n_pages;
+  if (t.dtype == FICOCO_BF16) hipLaunchKernelGGL(cache_read_kernel<bf16_t>, grid, dim3(kMoveThreads), 0, s, c, lp, k, v, t.n_max, t.seq, t.start, t.n_new);
+  else hipLaunchKernelGGL(cache_read_kernel<float>, grid, dim3(kMoveThreads), 0, s, c, lp, k, v, t.n_max, t.seq, t.start, t.n_new);
+}
+
+void launch_cache_fork(const ficoco_cache& c, int n, const int32_t* src, const int32_t* dst, bool whole, int32_t* done, hipStream_t s) {
+  hipLaunchKernelGGL(cache_fork_kernel, dim3(1), dim3(kPlanThreads), 0, s, c, n, src, dst, (int)whole, done);
+  const int walkers = whole ? page_walkers(c, (int64_t)c.layers * c.heads * n * 2) : 1;
+  hipLaunchKernelGGL(cache_copy_kernel, dim3(walkers, c.layers * c.heads, 2 * n), dim3(kMoveThreads), 0, s, c, src, dst, (int)whole, done);
+}
+
+void launch_cache_compact(const ficoco_cache& c, int layer_begin, int n_layers, int n, const int32_t* src, const int32_t* dst, int vis_begin, int N,
+                          int n_keep, const int32_t* keep_idx, int32_t* done, char* ws, hipStream_t s) {
+  CompactMeta* meta = (CompactMeta*)ws;
+  int32_t* rows = (int32_t*)(ws + (size_t)n * sizeof(CompactMeta));
+  hipLaunchKernelGGL(cache_compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, c, n, src, dst, vis_begin, N, n_keep, keep_idx, done, meta, rows);
+  if (n_layers == 0) return;
+  const dim3 grid(page_walkers(c, (int64_t)n_layers * c.heads * n * 2), n_layers * c.heads, 2 * n);
+  const int groups = c.page_size * c.d_head / 8;
+  if (groups <= 256) hipLaunchKernelGGL((cache_compact_kernel<1>), grid, dim3(kMoveThreads), 0, s, c, layer_begin, vis_begin, N, n_keep, dst, keep_idx, meta, rows);
+  else if (groups <= 512) hipLaunchKernelGGL((cache_compact_kernel<2>), grid, dim3(kMoveThreads), 0, s, c, layer_begin, vis_begin, N, n_keep, dst, keep_idx, meta, rows);
+  else if (groups <= 1024) hipLaunchKernelGGL((cache_compact_kernel<4>), grid, dim3(kMoveThreads), 0, s, c, layer_begin, vis_begin, N, n_keep, dst, keep_idx, meta, rows);
+  else hipLaunchKernelGGL((cache_compact_kernel<8>), grid, dim3(kMoveThreads), 0, s, c, layer_begin, vis_begin, N, n_keep, dst, keep_idx, meta, rows);
+}
+
+void launch_cache_free(const ficoco_cache& c, int n, const int32_t* seq, hipStream_t s) {
+  hipLaunchKernelGGL(cache_free_kernel, dim3(n), dim3(kMoveThreads), 0, s, c, seq);
+}
+
+}  // namespace ficoco

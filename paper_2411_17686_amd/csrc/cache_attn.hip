@@ -1,0 +1,328 @@
+// Attention over pages of 8 bits for few rows: single tokens of a decoder (and the few of a draft), all query heads
+// of a key / value head together.
+#include "attend.hpp"
+
+namespace ficoco {
+namespace {
+
+constexpr int kFewWaves = 4;
+constexpr int kFewKeys = 32;                 // keys of a step
+constexpr float kSlack = 8.0f;               // (units of log2) growth of a row's maximum that is put up with
+
+// One step's keys and values of a lane as they come out of memory.
+template <int D> struct FewRaw {
+  uint4 k[2][D / 64];
+  uint32_t v[2][4][D / 64];
+};
+
+// Four dwords of four keys, each four features, as four dwords of four features, each four keys.
+__device__ __forceinline__ void transpose4(const uint32_t (&a)[4], uint32_t (&t)[4]) {
+  const uint32_t x = __builtin_amdgcn_perm(a[1], a[0], 0x05010400u), y = __builtin_amdgcn_perm(a[1], a[0], 0x07030602u);
+  const uint32_t z = __builtin_amdgcn_perm(a[3], a[2], 0x05010400u), w = __builtin_amdgcn_perm(a[3], a[2], 0x07030602u);
+  t[0] = __builtin_amdgcn_perm(z, x, 0x05040100u);
+  t[1] = __builtin_amdgcn_perm(z, x, 0x07060302u);
+  t[2] = __builtin_amdgcn_perm(w, y, 0x05040100u);
+  t[3] = __builtin_amdgcn_perm(w, y, 0x07060302u);
+}
+
+__device__ __forceinline__ float quarters_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float quarters_sum(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
+// o = sum_j softmax_j(scale q . k_j) v_j for 16 * CT rows, in one pass with a running maximum and sum.  Every wavefront takes steps of
+// 32 keys of its own, straight from memory into registers, the next step's loads in flight while one is computed:
+//   S^T[key][row] = K Q^T      operand A a lane's 32 bytes of key lane % 16 (the features of a lane are not in order: Q has them alike)
+//   O^T[feature][row] += V^T P^T   contraction over 32 keys in the order in which a lane holds its logits, so that the weights
+//                                  stay where they are; operand A eight keys of one feature, out of a byte transposition
+// 8 bits become bfloat16 (exactly, the block's scale with them) in front of the products.  A row's maximum is the reference of its
+// exponentials as long as no logit lies more than 2^8 above it.
+//
+// Bound by memory: 2 d_head bytes a token and head.
+template <int D, int CT>
+__global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendArgs a) {
+  constexpr int L = D / 64;                  // 16-byte loads of a key
+  constexpr int M = D / 16;                  // blocks of 16 features; features of a lane's value load
+  constexpr int R = 16 * CT;
+  __shared__ float so[kFewWaves][R][D + 4];
+  __shared__ float sm[kFewWaves][R], ss[kFewWaves][R];
+  const int lane = threadIdx.x % kWave, wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int c16 = lane % 16, q4 = lane / 16;
+  const int split = blockIdx.x % a.splits, bh = blockIdx.x / a.splits, h = bh % a.H_kv, b = bh / a.H_kv;
+  int slot;
+  const Sight s = sight_of<true>(a, b, slot);
+  if (s.queries <= 0) return;
+  const int rows = s.queries * a.group;
+  const Blocks<kFewKeys> blocks(a, s, s.first, s.first + s.queries - 1);
+  int per = (blocks.count + a.splits - 1) / a.splits;
+  per = (per + kFewWaves - 1) / kFewWaves * kFewWaves;
+  const int begin = split * per, end = begin + per < blocks.count ? begin + per : blocks.count;
+
+  // queries: row CT * 16 + c16, features 64 l + 16 q4 + 8 u .. + 8
+  bf16x8_t qf[CT][L][2];
+  int pos[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    int r = ct * 16 + c16;
+    r = r < rows ? r : rows - 1;
+    const int t = r / a.group, g = r % a.group;
+    pos[ct] = s.first + t;
+    const bf16_t* q = a.Q + (int64_t)b * a.q_sb + (int64_t)(h * a.group + g) * a.q_sh + (int64_t)t * a.q_sn;
+#pragma unroll
+    for (int l = 0; l < L; ++l) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) __builtin_memcpy(&qf[ct][l][u], q + 64 * l + 16 * q4 + 8 * u, 16);
+    }
+  }
+  f32x4_t o[CT][M];
+  float top[CT], sum[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    top[ct] = kNoLogit;
+    sum[ct] = 0.0f;
+#pragma unroll
+    for (int m = 0; m < M; ++m) o[ct][m] = f32x4_t{0, 0, 0, 0};
+  }
+
+  // Pages and exponents of 32 steps (64 half steps of 16 keys, one a lane): the page or -1, and both bytes.
+  struct Meta { int page, exps; };
+  const int32_t* row = a.table + (int64_t)slot * a.max_pages;
+  auto meta_of = [&](int chunk) {
+    Meta m{-1, 0};
+    const int i = begin + wv + (chunk * 32 + lane / 2) * kFewWaves;
+    if (i < end) {
+      const int at = (blocks.block(i) * kFewKeys + 16 * (lane & 1)) >> a.page_shift;
+      int p = at < a.max_pages ? row[at] : -1;
+      p = p < a.n_pages ? p : -1;
+      if (p >= 0) m.exps = a.k_exp[(int64_t)p * a.H_kv + h] | a.v_exp[(int64_t)p * a.H_kv + h] << 8;
+      m.page = p;
+    }
+    return m;
+  };
+  const int steps = begin + wv < end ? (end - begin - wv + kFewWaves - 1) / kFewWaves : 0;
+  Meta now = meta_of(0), next = steps > 32 ? meta_of(1) : Meta{-1, 0};
+  const int page_bytes = D << a.page_shift;
+  auto load = [&](FewRaw<D>& raw, int step, const Meta& m) {
+    const int key0 = blocks.block(begin + wv + step * kFewWaves) * kFewKeys;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int p = __builtin_amdgcn_readlane(m.page, (step & 31) * 2 + u);
+      const int64_t at = ((int64_t)(p < 0 ? 0 : p) * a.H_kv + h) * page_bytes + ((key0 + 16 * u) & ((1 << a.page_shift) - 1)) * D;
+      const uint8_t* k = a.k + at;
+      const uint8_t* v = a.v + at;
+#pragma unroll
+      for (int l = 0; l < L; ++l) raw.k[u][l] = *(const uint4*)(k + (c16 * D + 16 * q4) + 64 * l);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (L == 2) {
+          const uint2 x = *(const uint2*)(v + (4 * q4 * D + c16 * M) + i * D);
+          raw.v[u][i][0] = x.x;
+          raw.v[u][i][1] = x.y;
+        } else {
+          raw.v[u][i][0] = *(const uint32_t*)(v + (4 * q4 * D + c16 * M) + i * D);
+        }
+      }
+    }
+  };
+  auto compute = [&](FewRaw<D>& raw, int step, const Meta& m) {
+    const int key0 = blocks.block(begin + wv + step * kFewWaves) * kFewKeys;
+    float ks[2], vs[2];
+    bool there = true, have[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int e = __builtin_amdgcn_readlane(m.exps, (step & 31) * 2 + u);
+      have[u] = __builtin_amdgcn_readlane(m.page, (step & 31) * 2 + u) >= 0;
+      there &= have[u];
+      ks[u] = exp_scale(e & 255);
+      vs[u] = exp_scale(e >> 8);
+    }
+    f32x4_t S[CT][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int l = 0; l < L; ++l) {
+        const uint32_t w[4] = {raw.k[u][l].x, raw.k[u][l].y, raw.k[u][l].z, raw.k[u][l].w};
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const uint2 x = widen_e4m3(w[2 * half], ks[u]), y = widen_e4m3(w[2 * half + 1], ks[u]);
+          const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, uint4{x.x, x.y, y.x, y.y});
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+            S[ct][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[ct][l][half], l + half == 0 ? f32x4_t{0, 0, 0, 0} : S[ct][u], 0, 0, 0);
+        }
+      }
+    }
+    const int last = key0 + kFewKeys - 1, lo = s.first, hi = s.first + s.queries - 1;
+    const bool all_seen = there && last < s.keys && last <= lo && (a.window <= 0 || (int64_t)key0 > (int64_t)hi - a.window || last < a.sinks);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) S[ct][u] *= a.scale_log2e;
+    }
+    if (!all_seen) {                                      // (uniform)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int key = key0 + 16 * u + 4 * q4 + i;
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) S[ct][u][i] = have[u] && key_seen(a, key, pos[ct], s.keys) ? S[ct][u][i] : -__builtin_huge_valf();
+          // what no row sees may hold anything, and 0 * NaN is NaN
+          if (!have[u] || key >= blocks.end || (key < blocks.near_key && key >= blocks.first_keys)) {
+#pragma unroll
+            for (int l = 0; l < L; ++l) raw.v[u][i][l] = 0;
+          }
+        }
+      }
+    }
+    bf16x8_t P[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      float t = fmaxf(fmaxf(S[ct][0][0], S[ct][0][1]), fmaxf(S[ct][0][2], S[ct][0][3]));
+      t = fmaxf(t, fmaxf(fmaxf(S[ct][1][0], S[ct][1][1]), fmaxf(S[ct][1][2], S[ct][1][3])));
+      if (__any(t > top[ct] + kSlack)) {
+        const float m = fmaxf(top[ct], quarters_max(t)), f = __builtin_amdgcn_exp2f(top[ct] - m);
+        top[ct] = m;
+        sum[ct] *= f;
+#pragma unroll
+        for (int i = 0; i < M; ++i) o[ct][i] *= f;
+      }
+      float p[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(S[ct][i / 4][i % 4] - top[ct]);
+        sum[ct] += p[i];
+      }
+      P[ct] = __builtin_bit_cast(bf16x8_t, uint4{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])});
+    }
+#pragma unroll
+    for (int w = 0; w < M / 4; ++w) {                     // four features of the lane at a time
+      uint32_t t[2][4];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const uint32_t x[4] = {raw.v[u][0][w], raw.v[u][1][w], raw.v[u][2][w], raw.v[u][3][w]};
+        transpose4(x, t[u]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint2 x = widen_e4m3(t[0][i], vs[0]), y = widen_e4m3(t[1][i], vs[1]);
+        const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, uint4{x.x, x.y, y.x, y.y});
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) o[ct][4 * w + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, P[ct], o[ct][4 * w + i], 0, 0, 0);
+      }
+    }
+  };
+
+  FewRaw<D> r0, r1;
+  if (steps > 0) load(r0, 0, now);
+  for (int i = 0; i < steps; i += 2) {
+    // (a chunk is 32 steps: an even step and the next one are of the same chunk)
+    if (i + 1 < steps) load(r1, i + 1, now);
+    compute(r0, i, now);
+    if (i + 1 >= steps) break;
+    const bool turn = ((i + 2) & 31) == 0;
+    if (i + 2 < steps) load(r0, i + 2, turn ? next : now);
+    compute(r1, i + 1, now);
+    if (turn) {
+      now = next;
+      if (i + 34 < steps) next = meta_of((i + 34) / 32);
+    }
+  }
+
+  // the wavefronts' parts
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int r = ct * 16 + c16;
+    const float total = quarters_sum(sum[ct]);
+    if (q4 == 0) {
+      sm[wv][r] = top[ct];
+      ss[wv][r] = total;
+    }
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) so[wv][r][(4 * q4 + i) * M + m] = o[ct][m][i];
+    }
+  }
+  __syncthreads();
+  for (int j = threadIdx.x; j < R * D / 8; j += kFewWaves * kWave) {
+    const int r = j / (D / 8), d = j % (D / 8) * 8;
+    if (r >= rows) continue;
+    float m = sm[0][r];
+#pragma unroll
+    for (int w = 1; w < kFewWaves; ++w) m = fmaxf(m, sm[w][r]);
+    float total = 0.0f, x[8] = {};
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(sm[w][r] - m);
+      total += f * ss[w][r];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] += f * so[w][r][d + i];
+    }
+    if (a.splits > 1) {
+      const int64_t at = ((int64_t)bh * a.splits + split) * a.part_rows + r;
+      if (d == 0) a.part_ms[at] = float2{m, total};
+      __builtin_memcpy(a.part_o + at * D + d, x, 32);
+    } else {
+      const float inv = total > 0.0f ? 1.0f / total : 0.0f;
+      const uint4 w = {pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv), pack_bf16(x[4] * inv, x[5] * inv),
+                       pack_bf16(x[6] * inv, x[7] * inv)};
+      __builtin_memcpy(a.O + (int64_t)b * a.o_sb + (int64_t)(h * a.group + r % a.group) * a.o_sh + (int64_t)(r / a.group) * a.o_sn + d, &w, 16);
+    }
+  }
+}
+
+// Rows whose keys were cut: the parts, relative to their largest maximum.  A wavefront a row.
+template <int D>
+__global__ __launch_bounds__(4 * kWave) void join_rows_kernel(AttendArgs a) {
+  constexpr int E = D / kWave;
+  const int lane = threadIdx.x % kWave;
+  const int64_t rows = (int64_t)a.n_q * a.group;
+  const int64_t at = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+  if (at >= rows * a.B * a.H_kv) return;
+  const int r = (int)(at % rows), bh = (int)(at / rows), h = bh % a.H_kv, b = bh / a.H_kv;
+  const int t = r / a.group;
+  if (a.q_len && t >= a.q_len[b]) return;
+  const int64_t part = (int64_t)bh * a.splits * a.part_rows + r;
+  float m = kNoLogit;
+  for (int i = lane; i < a.splits; i += kWave) m = fmaxf(m, a.part_ms[part + (int64_t)i * a.part_rows].x);
+  m = wave_reduce(m, [](float x, float y) { return fmaxf(x, y); });
+  float total = 0.0f, x[E] = {};
+  for (int i = 0; i < a.splits; ++i) {
+    const int64_t p = part + (int64_t)i * a.part_rows;
+    const float2 ms = a.part_ms[p];
+    const float f = __builtin_amdgcn_exp2f(ms.x - m);
+    total += f * ms.y;
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] += f * a.part_o[p * D + lane * E + e];
+  }
+  const float inv = total > 0.0f ? 1.0f / total : 0.0f;
+  bf16_t* o = a.O + (int64_t)b * a.o_sb + (int64_t)(h * a.group + r % a.group) * a.o_sh + (int64_t)t * a.o_sn + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = (bf16_t)__builtin_bit_cast(uint16_t, (__bf16)(x[e] * inv));
+}
+
+}  // namespace
+
+void launch_few_rows(const AttendArgs& a, const AttendPlan& pl, int d_head, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)a.B * a.H_kv * a.splits)), threads(kFewWaves * kWave);
+  if (d_head == 128) {
+    if (pl.rows <= 16) hipLaunchKernelGGL((few_rows_kernel<128, 1>), grid, threads, 0, s, a);
+    else hipLaunchKernelGGL((few_rows_kernel<128, 2>), grid, threads, 0, s, a);
+  } else {
+    if (pl.rows <= 16) hipLaunchKernelGGL((few_rows_kernel<64, 1>), grid, threads, 0, s, a);
+    else hipLaunchKernelGGL((few_rows_kernel<64, 2>), grid, threads, 0, s, a);
+  }
+}
+
+void launch_join_rows(const AttendArgs& a, int d_head, hipStream_t s) {
+  const dim3 grid((unsigned)(((int64_t)a.B * a.H_kv * a.n_q * a.group + 3) / 4));
+  if (d_head == 128) hipLaunchKernelGGL(join_rows_kernel<128>, grid, dim3(4 * kWave), 0, s, a);
+  else hipLaunchKernelGGL(join_rows_kernel<64>, grid, dim3(4 * kWave), 0, s, a);
+}
+
+}  // namespace ficoco

@@ -26,7 +26,10 @@ COMPRESS_SELF, COMPRESS_AVERAGE = 0, 1
 EXPORTS = ["ficoco_create", "ficoco_destroy", "ficoco_last_error", "ficoco_version",
            "ficoco_set_probe", "ficoco_workspace_bytes", "ficoco_out_rows", "ficoco_reduce", "ficoco_score",
            "ficoco_filter", "ficoco_correlate", "ficoco_correlation_gap", "ficoco_compress", "ficoco_v_step",
-           "ficoco_l_step", "ficoco_schedule", "ficoco_gather_tokens", "ficoco_v_step_static"]
+           "ficoco_l_step", "ficoco_schedule", "ficoco_gather_tokens", "ficoco_v_step_static",
+           "ficoco_cache_reserve", "ficoco_cache_append", "ficoco_cache_read", "ficoco_cache_fork",
+           "ficoco_cache_workspace_bytes", "ficoco_cache_compact", "ficoco_cache_free",
+           "ficoco_cache_attention_workspace_bytes", "ficoco_cache_attention", "ficoco_window_attention"]
 STATIC_SCRATCH_BYTES = 32 << 20
 
 
@@ -67,6 +70,35 @@ class ScheduleProblem(C.Structure):
                 ("min_keep", C.c_int32), ("budget_flops", C.c_double)]
 
 
+class CacheProblem(C.Structure):
+    """Mirror of `ficoco_cache`."""
+    _fields_ = [("layers", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("heads", C.c_int32),
+                ("d_head", C.c_int32), ("n_seqs", C.c_int32), ("max_pages", C.c_int32),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p),
+                ("table", C.c_void_p), ("len", C.c_void_p), ("refs", C.c_void_p)]
+
+
+class TokensProblem(C.Structure):
+    """Mirror of `ficoco_tokens`."""
+    _fields_ = [("n", C.c_int32), ("n_max", C.c_int32), ("dtype", C.c_int32),
+                ("seq", C.c_void_p), ("start", C.c_void_p), ("n_new", C.c_void_p), ("K", C.c_void_p), ("V", C.c_void_p),
+                ("k_stride_b", C.c_int64), ("k_stride_h", C.c_int64), ("k_stride_n", C.c_int64),
+                ("v_stride_b", C.c_int64), ("v_stride_h", C.c_int64), ("v_stride_n", C.c_int64)]
+
+
+class AttentionProblem(C.Structure):
+    """Mirror of `ficoco_attention`."""
+    _fields_ = [("B", C.c_int32), ("H", C.c_int32), ("H_kv", C.c_int32), ("n_q", C.c_int32), ("n_k", C.c_int32),
+                ("d_head", C.c_int32),
+                ("Q", C.c_void_p), ("q_stride_b", C.c_int64), ("q_stride_h", C.c_int64), ("q_stride_n", C.c_int64),
+                ("K", C.c_void_p), ("V", C.c_void_p),
+                ("k_stride_b", C.c_int64), ("k_stride_h", C.c_int64), ("k_stride_n", C.c_int64),
+                ("v_stride_b", C.c_int64), ("v_stride_h", C.c_int64), ("v_stride_n", C.c_int64),
+                ("O", C.c_void_p), ("o_stride_b", C.c_int64), ("o_stride_h", C.c_int64), ("o_stride_n", C.c_int64),
+                ("seq", C.c_void_p), ("q_len", C.c_void_p), ("k_len", C.c_void_p), ("q_start", C.c_void_p),
+                ("scale", C.c_float), ("window", C.c_int32), ("sinks", C.c_int32), ("max_len", C.c_int32)]
+
+
 _lib = None
 
 
@@ -100,6 +132,17 @@ def lib():
         L.ficoco_v_step_static.argtypes = step[:2] + step[4:]
         L.ficoco_gather_tokens.argtypes = [vp, pp, i32p, vp, C.c_int64, C.c_int64, C.c_int32, vp, vp]
         L.ficoco_schedule.argtypes = [C.POINTER(ScheduleProblem), C.POINTER(C.c_int32), C.POINTER(C.c_double)]
+        cp, tp, ap, i32 = C.POINTER(CacheProblem), C.POINTER(TokensProblem), C.POINTER(AttentionProblem), C.c_int32
+        L.ficoco_cache_reserve.argtypes = [vp, cp, i32, i32p, i32p, i32, i32p, vp]
+        L.ficoco_cache_append.argtypes = [vp, cp, i32, tp, vp]
+        L.ficoco_cache_read.argtypes = [vp, cp, i32, tp, vp]
+        L.ficoco_cache_fork.argtypes = [vp, cp, i32, i32p, i32p, i32, i32p, vp]
+        L.ficoco_cache_workspace_bytes.argtypes = [cp, i32, C.POINTER(C.c_size_t)]
+        L.ficoco_cache_compact.argtypes = [vp, cp, i32, i32, i32, i32p, i32p, i32, i32, i32, i32p, i32p, vp, C.c_size_t, vp]
+        L.ficoco_cache_free.argtypes = [vp, cp, i32, i32p, vp]
+        L.ficoco_cache_attention_workspace_bytes.argtypes = [cp, ap, C.POINTER(C.c_size_t)]
+        L.ficoco_cache_attention.argtypes = [vp, cp, i32, ap, vp, C.c_size_t, vp]
+        L.ficoco_window_attention.argtypes = [vp, ap, vp]
         for name in EXPORTS:
             getattr(L, name)            # fail loudly here if the build lacks a symbol
         _lib = L
@@ -341,3 +384,163 @@ def ficoco_schedule(variant, layers, start_layer, N, M, D, F, min_keep, budget_f
     if rc not in (OK, EUNSUPPORTED):
         raise FicocoError(rc, "ficoco_schedule rejected the arguments")
     return rc, list(out)[:layers], total.value
+
+
+# ---- the decoder's key / value cache -----------------------------------------------------------
+class Cache:
+    """Tensors of a `ficoco_cache` (shapes as in include/ficoco.h) and its description, filled once."""
+
+    def __init__(self, k, v, k_exp, v_exp, table, length, refs):
+        layers, n_pages, heads, page_size, d_head = k.shape
+        n_seqs, max_pages = table.shape
+        for t, dtype, shape in ((k, torch.uint8, k.shape), (v, torch.uint8, k.shape),
+                                (k_exp, torch.uint8, k.shape[:3]), (v_exp, torch.uint8, k.shape[:3]),
+                                (table, torch.int32, table.shape), (length, torch.int32, (n_seqs,)),
+                                (refs, torch.int32, (n_pages,))):
+            if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != k.device:
+                raise TypeError("the tensors of a cache are contiguous, on one device, of the types and shapes in ficoco.h")
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self.table, self.len, self.refs = table, length, refs
+        self.c = CacheProblem(layers, n_pages, page_size, heads, d_head, n_seqs, max_pages, k.data_ptr(), v.data_ptr(),
+                              k_exp.data_ptr(), v_exp.data_ptr(), table.data_ptr(), length.data_ptr(), refs.data_ptr())
+
+    @classmethod
+    def empty(cls, layers, n_pages, page_size, heads, d_head, n_seqs, max_pages, device="cuda"):
+        """A cache of n_seqs empty sequences."""
+        pages = [torch.zeros(layers, n_pages, heads, page_size, d_head, dtype=torch.uint8, device=device) for _ in range(2)]
+        exps = [torch.zeros(layers, n_pages, heads, dtype=torch.uint8, device=device) for _ in range(2)]
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(*pages, *exps, torch.full((n_seqs, max_pages), -1, **i32), torch.zeros(n_seqs, **i32),
+                   torch.zeros(n_pages, **i32))
+
+
+class Workspace:
+    """Device memory for one call at a time, 256-byte aligned."""
+
+    def __init__(self, n, device):
+        self.bytes = n
+        self.t = torch.empty(n + 256, dtype=torch.uint8, device=device)
+        self.ptr = self.t.data_ptr() + (-self.t.data_ptr()) % 256
+
+
+def _i32(t, n, name):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != n:
+        raise TypeError("%s must be %d contiguous int32 values" % (name, n))
+    return C.c_void_p(t.data_ptr())
+
+
+def cache_workspace(cache, n):
+    """Workspace of ficoco_cache_compact for n sequences."""
+    out = C.c_size_t()
+    rc = lib().ficoco_cache_workspace_bytes(C.byref(cache.c), n, C.byref(out))
+    if rc != OK:
+        raise FicocoError(rc, "ficoco_cache_workspace_bytes rejected the arguments")
+    return Workspace(out.value, cache.k.device)
+
+
+def ficoco_cache_reserve(ctx, cache, start, n_new, seq=None):
+    """n_new: tokens of every sequence (int32 tensor), or one number for all."""
+    n = start.numel()
+    each = isinstance(n_new, int)
+    ctx.check(lib().ficoco_cache_reserve(ctx._h, C.byref(cache.c), n, _i32(seq, n, "seq"),
+                                         None if each else _i32(n_new, n, "n_new"), n_new if each else 0,
+                                         _i32(start, n, "start"), ctx.stream()))
+
+
+def _tokens(cache, K, V, start, n_new, seq):
+    some = K if K is not None else V
+    if some is None:
+        raise TypeError("K and V are both None")
+    n, heads, n_max, d = some.shape
+    if heads != cache.c.heads or d != cache.c.d_head:
+        raise TypeError("tokens are [n][heads][n_max][d_head] of the cache")
+    for t in (K, V):
+        if t is not None and (t.shape != some.shape or t.dtype != some.dtype or (t.stride(3) != 1 and t.numel())):
+            raise TypeError("K and V are of one shape and type, d_head contiguous")
+    p = TokensProblem(n=n, n_max=n_max, dtype=_dtype_code(some))
+    p.seq, p.start, p.n_new = _i32(seq, n, "seq"), _i32(start, n, "start"), _i32(n_new, n, "n_new")
+    if K is not None:
+        p.K, p.k_stride_b, p.k_stride_h, p.k_stride_n = K.data_ptr(), K.stride(0), K.stride(1), K.stride(2)
+    if V is not None:
+        p.V, p.v_stride_b, p.v_stride_h, p.v_stride_n = V.data_ptr(), V.stride(0), V.stride(1), V.stride(2)
+    return p
+
+
+def ficoco_cache_append(ctx, cache, layer, K, V, start, n_new=None, seq=None):
+    t = _tokens(cache, K, V, start, n_new, seq)
+    ctx.check(lib().ficoco_cache_append(ctx._h, C.byref(cache.c), layer, C.byref(t), ctx.stream()))
+
+
+def ficoco_cache_read(ctx, cache, layer, K, V, start=None, n_new=None, seq=None):
+    """Into K and V (either may be None)."""
+    t = _tokens(cache, K, V, start, n_new, seq)
+    ctx.check(lib().ficoco_cache_read(ctx._h, C.byref(cache.c), layer, C.byref(t), ctx.stream()))
+
+
+def ficoco_cache_fork(ctx, cache, src, dst, done, whole=False):
+    n = done.numel()
+    ctx.check(lib().ficoco_cache_fork(ctx._h, C.byref(cache.c), n, _i32(src, n, "src"), _i32(dst, n, "dst"), int(whole),
+                                      _i32(done, n, "done"), ctx.stream()))
+
+
+def ficoco_cache_compact(ctx, cache, layer_begin, n_layers, src, dst, vis_begin, N, keep_idx, done, ws):
+    """keep_idx [n][n_keep] int32, as the filter of a step leaves it."""
+    n = done.numel()
+    if keep_idx.dim() != 2 or keep_idx.shape[0] != n:
+        raise TypeError("keep_idx must be [n][n_keep]")
+    ctx.check(lib().ficoco_cache_compact(ctx._h, C.byref(cache.c), layer_begin, n_layers, n, _i32(src, n, "src"),
+                                         _i32(dst, n, "dst"), vis_begin, N, keep_idx.shape[1],
+                                         _i32(keep_idx, keep_idx.numel(), "keep_idx"), _i32(done, n, "done"),
+                                         C.c_void_p(ws.ptr), ws.bytes, ctx.stream()))
+
+
+def ficoco_cache_free(ctx, cache, seq):
+    n = seq.numel()
+    ctx.check(lib().ficoco_cache_free(ctx._h, C.byref(cache.c), n, _i32(seq, n, "seq"), ctx.stream()))
+
+
+def _attention(Q, O, scale, window, sinks, q_len, k_len, q_start):
+    B, H, n_q, d = Q.shape
+    if O.shape != Q.shape or Q.dtype != torch.bfloat16 or O.dtype != torch.bfloat16 or \
+            ((Q.stride(3) != 1 or O.stride(3) != 1) and Q.numel()):
+        raise TypeError("Q and O are bfloat16 [B][H][n_q][d_head], d_head contiguous")
+    a = AttentionProblem(B=B, H=H, n_q=n_q, d_head=d, window=window, sinks=sinks)
+    a.Q, a.q_stride_b, a.q_stride_h, a.q_stride_n = Q.data_ptr(), Q.stride(0), Q.stride(1), Q.stride(2)
+    a.O, a.o_stride_b, a.o_stride_h, a.o_stride_n = O.data_ptr(), O.stride(0), O.stride(1), O.stride(2)
+    a.scale = float(d) ** -0.5 if scale is None else scale
+    a.q_len, a.k_len, a.q_start = _i32(q_len, B, "q_len"), _i32(k_len, B, "k_len"), _i32(q_start, B, "q_start")
+    return a
+
+
+def attention_workspace(cache, Q, O, window=0, sinks=0, max_len=0):
+    """Workspace of ficoco_cache_attention for calls of these shapes."""
+    a = _attention(Q, O, None, window, sinks, None, None, None)
+    a.max_len = max_len
+    out = C.c_size_t()
+    rc = lib().ficoco_cache_attention_workspace_bytes(C.byref(cache.c), C.byref(a), C.byref(out))
+    if rc != OK:
+        raise FicocoError(rc, "ficoco_cache_attention_workspace_bytes rejected the arguments")
+    return Workspace(out.value, cache.k.device)
+
+
+def ficoco_cache_attention(ctx, cache, layer, Q, O, ws, scale=None, window=0, sinks=0, q_len=None, k_len=None,
+                           q_start=None, seq=None, max_len=0):
+    """Into O; scale None = d_head ** -0.5."""
+    a = _attention(Q, O, scale, window, sinks, q_len, k_len, q_start)
+    a.seq, a.max_len = _i32(seq, a.B, "seq"), max_len
+    ctx.check(lib().ficoco_cache_attention(ctx._h, C.byref(cache.c), layer, C.byref(a), C.c_void_p(ws.ptr), ws.bytes,
+                                           ctx.stream()))
+
+
+def ficoco_window_attention(ctx, Q, K, V, O, scale=None, window=0, sinks=0, q_len=None, k_len=None, q_start=None):
+    """Into O; scale None = d_head ** -0.5."""
+    a = _attention(Q, O, scale, window, sinks, q_len, k_len, q_start)
+    if K.shape != V.shape or K.shape[0] != a.B or K.shape[3] != a.d_head or K.dtype != torch.bfloat16 or \
+            V.dtype != torch.bfloat16 or ((K.stride(3) != 1 or V.stride(3) != 1) and K.numel()):
+        raise TypeError("K and V are bfloat16 [B][H_kv][n_k][d_head], d_head contiguous")
+    a.H_kv, a.n_k = K.shape[1], K.shape[2]
+    a.K, a.k_stride_b, a.k_stride_h, a.k_stride_n = K.data_ptr(), K.stride(0), K.stride(1), K.stride(2)
+    a.V, a.v_stride_b, a.v_stride_h, a.v_stride_n = V.data_ptr(), V.stride(0), V.stride(1), V.stride(2)
+    ctx.check(lib().ficoco_window_attention(ctx._h, C.byref(a), ctx.stream()))
