@@ -98,6 +98,15 @@ __device__ __forceinline__ uint2 widen_e4m3(uint32_t q, float scale) {
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q, scale, true))};
 }
 
+// Between products and a branch behind which their results are read.  A result may be read a number of instructions after the product
+// at the earliest; the compiler keeps to that inside a block, but not everywhere across a branch (seen with ROCm 7.2: copies
+// of the last two registers of a 32 x 32 result in the block behind a branch, three instructions later, got what was there before).
+__device__ __forceinline__ void products_settle() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // How the keys of a call are cut: few workgroups otherwise leave compute units idle.
 struct AttendPlan {
   bool few;            // single tokens (cache_attn.hip), else tiles of 128 rows (tile_attn.hip)

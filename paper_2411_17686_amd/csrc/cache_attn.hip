@@ -156,6 +156,7 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendAr
         }
       }
     }
+    products_settle();
     const int last = key0 + kFewKeys - 1, lo = s.first, hi = s.first + s.queries - 1;
     const bool all_seen = there && last < s.keys && last <= lo && (a.window <= 0 || (int64_t)key0 > (int64_t)hi - a.window || last < a.sinks);
 #pragma unroll
@@ -215,6 +216,7 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendAr
         for (int ct = 0; ct < CT; ++ct) o[ct][4 * w + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, P[ct], o[ct][4 * w + i], 0, 0, 0);
       }
     }
+    products_settle();
   };
 
   FewRaw<D> r0, r1;

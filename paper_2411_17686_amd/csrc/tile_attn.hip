@@ -17,29 +17,35 @@ constexpr int kHole = 1 << 16;                // (beside two exponent bytes) a k
 typedef short i16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4_t* lds_i16x4_t;
 
-// Rows of keys and values in LDS, in bfloat16.  A key row is read 16 bytes a lane by 16 rows at once: 16 bytes of padding put
-// them on all 64 banks.  Of the values, groups of 16 lanes read four keys x 16 features: rows 64 bytes further on modulo 256.
-template <int D> constexpr int kKeyPitch = D + 8;
-template <int D> constexpr int kValuePitch = D + 32;
+// Rows of keys and values in LDS, in bfloat16, 16-byte chunks; chunk c of a row lies at c ^ swizzle.  A key row is read 16 bytes a lane
+// by 16 rows at once, a value row by groups of 16 lanes, two groups four keys x 32 features at once: these put either on all 64 banks.
+template <int D> __device__ __forceinline__ int key_swizzle(int row) { return D == 128 ? row & 15 : row >> 1 & 7; }
+template <int D> __device__ __forceinline__ int value_swizzle(int row) { return D == 128 ? (row & 3) << 2 : (row & 2) << 1; }
 
-template <int D, bool PAGED> struct TileRaw;       // one step's share of a thread
-template <int D> struct TileRaw<D, false> { uint4 k[D / 32], v[D / 32]; };
-template <int D> struct TileRaw<D, true> { uint4 k[D / 64], v[D / 64]; int exps[D / 64]; };
-
+// (fmaxf() would first bring either argument into canonical form, an instruction more for each)
+__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
 __device__ __forceinline__ float halves_max(float v) { return fmaxf(v, __shfl_xor(v, 32)); }
+
+enum TileSource {
+  kDenseDirect,      // 16-byte aligned rows: straight into LDS
+  kDense,            // any other: through registers
+  kPaged             // 8 bits: through registers, widened with their block's scale
+};
+template <int D, TileSource SRC> struct TileRaw { uint4 x[SRC == kPaged ? D / 64 : D / 32]; int e[D / 64]; };       // a thread's share of a step's keys or values
 
 // One pass with a running maximum and sum, 128 rows a workgroup, 32 a wavefront, 64 keys a step.  32 x 32 x 16 products:
 //   S^T[key][row] = K Q^T, the queries in registers; a lane holds 32 logits of one row
 //   O^T[feature][row] += V^T P^T, the contraction in the order in which the lanes hold the weights; V^T out of LDS by transposing reads
-// The next step's keys and values travel from memory to registers while one is computed (8 bits are widened, with their
-// block's scale, on the way into LDS) and are written to the other of two buffers.
-template <int D, bool PAGED>
+// A step's weights are formed beside the products of the next step's logits: exponentials and products of one wavefront otherwise take
+// turns.  So keys are in LDS a step ahead of the values; either in two buffers, what comes next on its way while a step is computed.
+template <int D, TileSource SRC>
 __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a) {
-  constexpr int KP = kKeyPitch<D>, VP = kValuePitch<D>, DT = D / 32, KS = D / 16;
-  constexpr int NL = PAGED ? D / 64 : D / 32;      // 16-byte loads of a thread, keys and values each
-  constexpr int CH = PAGED ? D / 16 : D / 8;       // of a row
-  __shared__ __align__(16) bf16_t sk[2][kTileKeys * KP];
-  __shared__ __align__(16) bf16_t sv[2][kTileKeys * VP];
+  constexpr bool PAGED = SRC == kPaged;
+  constexpr int DT = D / 32, KS = D / 16, CH = D / 8;
+  constexpr int NL = PAGED ? D / 64 : D / 32;      // 16-byte loads of a thread
+  constexpr int LC = PAGED ? D / 16 : D / 8;       // of a row
+  __shared__ __align__(16) bf16_t sk[2][kTileKeys * D];
+  __shared__ __align__(16) bf16_t sv[2][kTileKeys * D];
   __shared__ int hole[2];                          // 1 + the last step in this buffer some of whose keys have no page
   const int tid = threadIdx.x, lane = tid % kWave, wv = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int c32 = lane % 32, half = lane / 32;
@@ -71,97 +77,157 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
   for (int i = 0; i < DT; ++i) o[i] = f32x16_t{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
   float top = kNoLogit, sum = 0.0f;
 
-  // keys and values of a step: memory -> registers -> LDS
   const int32_t* table = PAGED ? a.table + (int64_t)slot * a.max_pages : nullptr;
   auto wanted = [&](int key) { return key < blocks.end && (key >= blocks.near_key || key < blocks.first_keys); };
-  auto page_at = [&](int step, int j) {
-    const int key = blocks.block(step) * kTileKeys + (tid + j * kTileThreads) / CH;
-    int p = -1;
-    if (step < end && wanted(key)) p = table[key >> a.page_shift];       // (keys lie inside the row: see sight_of)
-    return p < a.n_pages ? p : -1;
-  };
-  int pages[NL];
-  auto load = [&](TileRaw<D, PAGED>& raw, int step) {
+
+  // ---- straight into LDS: a wavefront's load fills 64 chunks in a row.  Rows that no query of the workgroup sees are
+  // replaced by one that is seen: their weights are zero, and zero times what memory happens to hold may be NaN.
+  const int d_row = 64 / CH * wv + lane / CH;                                   // rows of load j: d_row + RJ * j
+  constexpr int RJ = 64 * kTileWaves / CH;
+  auto direct = [&](const bf16_t* base, int64_t sn, bf16_t* to, int swizzle, int step) {
+    if (step >= end) return;
     const int key0 = blocks.block(step) * kTileKeys;
+    const char* from = (const char*)(base + (int64_t)key0 * sn);                // (uniform)
+    const uint32_t ch = (uint32_t)((lane % CH ^ swizzle) * 8), row_bytes = (uint32_t)sn * 2;      // (a step's keys lie within 2^31 bytes: launch_tile_rows)
+    const bool whole = key0 + kTileKeys <= blocks.end && (key0 >= blocks.near_key || key0 + kTileKeys <= blocks.first_keys);
+    auto one = [&](const char* x, int j) {
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)x,
+                                       (__attribute__((address_space(3))) void*)(to + (j * kTileWaves + wv) * 64 * 8), 16, 0, 0);
+    };
+    if (whole) {
+      const uint32_t off = (uint32_t)d_row * row_bytes + ch * 2;
 #pragma unroll
-    for (int j = 0; j < NL; ++j) {
-      const int at = tid + j * kTileThreads, key = key0 + at / CH, ch = at % CH;
-      raw.k[j] = raw.v[j] = uint4{0, 0, 0, 0};
-      if constexpr (PAGED) {
-        raw.exps[j] = pages[j] < 0 && wanted(key) ? kHole : 0;
-        if (pages[j] >= 0) {
-          const int64_t block = (int64_t)pages[j] * a.H_kv + h;
-          const int64_t from = ((block << a.page_shift) + (key & ((1 << a.page_shift) - 1))) * D + 16 * ch;
-          raw.k[j] = *(const uint4*)(a.k + from);
-          raw.v[j] = *(const uint4*)(a.v + from);
-          raw.exps[j] = a.k_exp[block] | a.v_exp[block] << 8;
-        }
-      } else if (wanted(key)) {
-        __builtin_memcpy(&raw.k[j], a.K + (int64_t)b * a.k_sb + (int64_t)h * a.k_sh + (int64_t)key * a.k_sn + 8 * ch, 16);
-        __builtin_memcpy(&raw.v[j], a.V + (int64_t)b * a.v_sb + (int64_t)h * a.v_sh + (int64_t)key * a.v_sn + 8 * ch, 16);
-      }
-    }
-    if constexpr (PAGED) {
+      for (int j = 0; j < NL; ++j) one(from + (int64_t)(RJ * j) * sn * 2 + off, j);
+    } else {
 #pragma unroll
-      for (int j = 0; j < NL; ++j) pages[j] = page_at(step + 1, j);
-    }
-  };
-  auto store = [&](const TileRaw<D, PAGED>& raw, int step, int buf) {
-#pragma unroll
-    for (int j = 0; j < NL; ++j) {
-      const int at = tid + j * kTileThreads, key = at / CH, ch = at % CH;
-      if constexpr (PAGED) {
-        if (raw.exps[j] & kHole) hole[buf] = step + 1;
-        const float ks = exp_scale(raw.exps[j] & 255), vs = exp_scale(raw.exps[j] >> 8 & 255);
-        const uint2 k0 = widen_e4m3(raw.k[j].x, ks), k1 = widen_e4m3(raw.k[j].y, ks), k2 = widen_e4m3(raw.k[j].z, ks), k3 = widen_e4m3(raw.k[j].w, ks);
-        const uint2 v0 = widen_e4m3(raw.v[j].x, vs), v1 = widen_e4m3(raw.v[j].y, vs), v2 = widen_e4m3(raw.v[j].z, vs), v3 = widen_e4m3(raw.v[j].w, vs);
-        uint4* k = (uint4*)&sk[buf][key * KP + 16 * ch];
-        uint4* v = (uint4*)&sv[buf][key * VP + 16 * ch];
-        k[0] = uint4{k0.x, k0.y, k1.x, k1.y};
-        k[1] = uint4{k2.x, k2.y, k3.x, k3.y};
-        v[0] = uint4{v0.x, v0.y, v1.x, v1.y};
-        v[1] = uint4{v2.x, v2.y, v3.x, v3.y};
-      } else {
-        *(uint4*)&sk[buf][key * KP + 8 * ch] = raw.k[j];
-        *(uint4*)&sv[buf][key * VP + 8 * ch] = raw.v[j];
+      for (int j = 0; j < NL; ++j) {
+        const int row = wanted(key0 + d_row + RJ * j) ? d_row + RJ * j : blocks.end - 1 - key0;
+        one(from + (int64_t)row * sn * 2 + ch * 2, j);
       }
     }
   };
 
-  auto compute = [&](int step, int buf) {
-    const int key0 = blocks.block(step) * kTileKeys, last = key0 + kTileKeys - 1;
-    if (key0 > hi || (a.window > 0 && (int64_t)last <= (int64_t)lo - a.window && key0 >= a.sinks)) return;      // nothing for this wavefront
-    f32x16_t S[2];
+  // ---- through registers
+  auto page_at = [&](int step, int j) {
+    const int key = blocks.block(step) * kTileKeys + (tid + j * kTileThreads) / LC;
+    int p = -1;
+    if (step < end && wanted(key)) p = table[key >> a.page_shift];       // (keys lie inside the row: see sight_of)
+    return p < a.n_pages ? p : -1;
+  };
+  int pages[NL], k_pages[NL];                      // of the next step's keys to be loaded, and of the keys loaded last
+  auto load_page = [&](TileRaw<D, SRC>& raw, const uint8_t* pool, const uint8_t* exps, const int (&page)[NL], int step) {
+    const int key0 = blocks.block(step) * kTileKeys;
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      const int at = tid + j * kTileThreads, key = key0 + at / LC;
+      raw.x[j] = uint4{0, 0, 0, 0};
+      raw.e[j] = 0;
+      if (page[j] >= 0) {
+        const int64_t block = (int64_t)page[j] * a.H_kv + h;
+        raw.x[j] = *(const uint4*)(pool + ((block << a.page_shift) + (key & ((1 << a.page_shift) - 1))) * D + 16 * (at % LC));
+        raw.e[j] = exps[block];
+      } else if (step < end && wanted(key)) {
+        raw.e[j] = kHole;
+      }
+    }
+  };
+  auto load_dense = [&](TileRaw<D, SRC>& raw, const bf16_t* base, int64_t sn, int step) {
+    const int key0 = blocks.block(step) * kTileKeys;
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      const int at = tid + j * kTileThreads, key = key0 + at / LC;
+      raw.x[j] = uint4{0, 0, 0, 0};
+      if (step < end && wanted(key)) __builtin_memcpy(&raw.x[j], base + (int64_t)key * sn + 8 * (at % LC), 16);
+    }
+  };
+  const bf16_t* Kb = a.K + (int64_t)b * a.k_sb + (int64_t)h * a.k_sh;
+  const bf16_t* Vb = a.V + (int64_t)b * a.v_sb + (int64_t)h * a.v_sh;
+  auto load_k = [&](TileRaw<D, SRC>& raw, int step) {
+    if constexpr (PAGED) {
+      load_page(raw, a.k, a.k_exp, pages, step);
+#pragma unroll
+      for (int j = 0; j < NL; ++j) {
+        k_pages[j] = pages[j];
+        pages[j] = page_at(step + 1, j);
+      }
+    } else if constexpr (SRC == kDense) {
+      load_dense(raw, Kb, a.k_sn, step);
+    } else {
+      direct(Kb, a.k_sn, sk[(step - begin) & 1], key_swizzle<D>(d_row), step);
+    }
+  };
+  auto load_v = [&](TileRaw<D, SRC>& raw, int step) {      // before load_k of the step behind it
+    if constexpr (PAGED) load_page(raw, a.v, a.v_exp, k_pages, step);
+    else if constexpr (SRC == kDense) load_dense(raw, Vb, a.v_sn, step);
+    else direct(Vb, a.v_sn, sv[(step - begin) & 1], value_swizzle<D>(d_row), step);
+  };
+  auto store = [&](const TileRaw<D, SRC>& raw, bool keys, int step) {
+    if constexpr (SRC != kDenseDirect) {
+      const int buf = (step - begin) & 1;
+      bf16_t* to = keys ? sk[buf] : sv[buf];
+#pragma unroll
+      for (int j = 0; j < NL; ++j) {
+        const int at = tid + j * kTileThreads, row = at / LC, ch = at % LC, swizzle = keys ? key_swizzle<D>(row) : value_swizzle<D>(row);
+        uint4* r = (uint4*)to + row * CH;
+        if constexpr (PAGED) {
+          if (keys && raw.e[j] & kHole) hole[buf] = step + 1;
+          const float scale = exp_scale(raw.e[j] & 255);
+          const uint2 y0 = widen_e4m3(raw.x[j].x, scale), y1 = widen_e4m3(raw.x[j].y, scale), y2 = widen_e4m3(raw.x[j].z, scale), y3 = widen_e4m3(raw.x[j].w, scale);
+          r[2 * ch ^ swizzle] = uint4{y0.x, y0.y, y1.x, y1.y};
+          r[2 * ch + 1 ^ swizzle] = uint4{y2.x, y2.y, y3.x, y3.y};
+        } else {
+          r[ch ^ swizzle] = raw.x[j];
+        }
+      }
+    }
+  };
+  auto arrived = [&]() {
+    if constexpr (SRC == kDenseDirect) __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0)
+    __syncthreads();
+  };
+
+  const int k_swizzle = key_swizzle<D>(c32);
+  auto logits = [&](f32x16_t (&S)[2], int step) {
+    const bf16_t* k0 = &sk[(step - begin) & 1][c32 * D];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        const bf16x8_t kf = *(const bf16x8_t*)&sk[buf][(kb * 32 + c32) * KP + 16 * k + 8 * half];
+        const bf16x8_t kf = *(const bf16x8_t*)(k0 + kb * 32 * D + (2 * k + half ^ k_swizzle) * 8);
         S[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[k], k == 0 ? f32x16_t{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0} : S[kb], 0, 0, 0);
       }
     }
-    bool all_seen = last < s.keys && last <= lo && (a.window <= 0 || (int64_t)key0 > (int64_t)hi - a.window || last < a.sinks);
-    if (PAGED) all_seen = all_seen && __builtin_amdgcn_readfirstlane(hole[buf]) != step + 1;
-    if (!all_seen) {
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = key0 + kb * 32 + i / 4 * 8 + 4 * half + i % 4;
-          bool seen = key_seen(a, key, pos, s.keys);
-          if (PAGED) {
-            const int at = key >> a.page_shift;
-            const int p = seen ? table[at] : -1;
-            seen = p >= 0 && p < a.n_pages;
-          }
-          S[kb][i] = seen ? S[kb][i] : -__builtin_huge_valf();
-        }
-      }
-    }
+  };
+  auto all_seen = [&](int step) {                  // every key of a step by every row of the wavefront
+    const int key0 = blocks.block(step) * kTileKeys, last = key0 + kTileKeys - 1;
+    const bool all = last < s.keys && last <= lo && (a.window <= 0 || (int64_t)key0 > (int64_t)hi - a.window || last < a.sinks);
+    return PAGED ? all && __builtin_amdgcn_readfirstlane(hole[(step - begin) & 1]) != step + 1 : all;
+  };
+  auto largest = [&](const f32x16_t (&S)[2]) {
     float m = fmaxf(S[0][0], S[1][0]);
 #pragma unroll
-    for (int i = 1; i < 16; ++i) m = fmaxf(m, fmaxf(S[0][i], S[1][i]));
-    m *= a.scale_log2e;
+    for (int i = 1; i < 16; ++i) m = max3(m, S[0][i], S[1][i]);
+    return m;
+  };
+  auto mask = [&](f32x16_t (&S)[2], int step) {    // what a row does not see: -infinity; a lane's largest logit
+    const int key0 = blocks.block(step) * kTileKeys;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = key0 + kb * 32 + i / 4 * 8 + 4 * half + i % 4;
+        bool seen = key_seen(a, key, pos, s.keys);
+        if (PAGED) {
+          const int p = seen ? table[key >> a.page_shift] : -1;
+          seen = p >= 0 && p < a.n_pages;
+        }
+        S[kb][i] = seen ? S[kb][i] : -__builtin_huge_valf();
+      }
+    }
+    return largest(S);
+  };
+  // the running maximum, moved where a logit (m: a lane's largest one) lies far above it
+  auto raise = [&](float m) {
     if (__any(m > top + kSlack)) {
       const float n = fmaxf(top, halves_max(m)), f = __builtin_amdgcn_exp2f(top - n);
       top = n;
@@ -169,47 +235,99 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
 #pragma unroll
       for (int i = 0; i < DT; ++i) o[i] *= f;
     }
+  };
+  const int v_row = 4 * half + lane % 16 / 4, v_swizzle = value_swizzle<D>(v_row);       // (of rows 8 and 16 further on too)
+  int k_at[KS], v_at[DT];                          // a lane's places in a row of keys, and of values
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+  for (int k = 0; k < KS; ++k) k_at[k] = c32 * D + (2 * k + half ^ k_swizzle) * 8;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        float p[8];
+  for (int i = 0; i < DT; ++i) v_at[i] = v_row * D + (4 * i + lane / 16 % 2 * 2 + lane % 4 / 2 ^ v_swizzle) * 8 + lane % 4 % 2 * 4;
+
+  TileRaw<D, SRC> raw;
+  auto advance = [&](f32x16_t (&S)[2], f32x16_t (&next)[2], int i) {
+    constexpr int NA = 2 * KS, NB = 4 * DT;        // products of either kind
+    constexpr int AHEAD = 4;                       // operands on their way out of LDS
+    constexpr int EA = 24;                         // weights formed beside the first kind; the other 8 beside the second
+    load_v(raw, i + 1);
+    if constexpr (SRC == kDenseDirect) load_k(raw, i + 2);
+    const bf16_t* k0 = sk[(i + 1 - begin) & 1];    // (behind the last step: whatever is there)
+    const bf16_t* v0 = sv[(i - begin) & 1];
+    bf16x8_t kf[AHEAD], vf[AHEAD], P[4];
+    float w[32];
+    auto read_k = [&](int g) { kf[g % AHEAD] = *(const bf16x8_t*)(k0 + g / KS * 32 * D + k_at[g % KS]); };
+    auto read_v = [&](int g) {
+      const bf16_t* v = v0 + 16 * (g / DT) * D + v_at[g % DT];
+      const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t)v));
+      const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t)(v + 8 * D)));
+      vf[g % AHEAD] = __builtin_bit_cast(bf16x8_t, uint4{x.x, x.y, y.x, y.y});
+    };
+    auto weight = [&](int e) {
+      w[e] = __builtin_amdgcn_exp2f(fmaf(S[e / 16][e % 16], a.scale_log2e, -top));
+      sum += w[e];
+      if (e % 8 == 7)
+        P[e / 8] = __builtin_bit_cast(bf16x8_t, uint4{pack_bf16(w[e - 7], w[e - 6]), pack_bf16(w[e - 5], w[e - 4]), pack_bf16(w[e - 3], w[e - 2]), pack_bf16(w[e - 1], w[e])});
+    };
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          p[i] = __builtin_amdgcn_exp2f(fmaf(S[kb][8 * u + i], a.scale_log2e, -top));
-          sum += p[i];
-        }
-        const bf16x8_t P = __builtin_bit_cast(bf16x8_t, uint4{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])});
-        const bf16_t* v = &sv[buf][(kb * 32 + 16 * u + 4 * half + lane % 16 / 4) * VP + lane / 16 % 2 * 16 + lane % 4 * 4];
+    for (int g = 0; g < AHEAD; ++g) read_k(g);
 #pragma unroll
-        for (int i = 0; i < DT; ++i) {
-          const i16x4_t v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t)(v + 32 * i));
-          const i16x4_t v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t)(v + 8 * VP + 32 * i));
-          const uint2 x = __builtin_bit_cast(uint2, v0), y = __builtin_bit_cast(uint2, v1);
-          o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, uint4{x.x, x.y, y.x, y.y}), P, o[i], 0, 0, 0);
-        }
+    for (int g = 0; g < NA; ++g) {
+      __builtin_amdgcn_sched_barrier(0);
+      next[g / KS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[g % AHEAD], qf[g % KS], g % KS == 0 ? f32x16_t{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0} : next[g / KS], 0, 0, 0);
+      if (g + AHEAD < NA) read_k(g + AHEAD);
+      else if constexpr (SRC == kDenseDirect) read_v(g + AHEAD - NA);
+#pragma unroll
+      for (int e = g * EA / NA; e < (g + 1) * EA / NA; ++e) weight(e);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (SRC != kDenseDirect) {
+      store(raw, false, i + 1);
+      load_k(raw, i + 2);
+#pragma unroll
+      for (int g = 0; g < AHEAD; ++g) read_v(g);
+    }
+    float m[2] = {next[0][0], next[0][1]};
+#pragma unroll
+    for (int g = 0; g < NB; ++g) {
+      __builtin_amdgcn_sched_barrier(0);
+      o[g % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[g % AHEAD], P[g / DT], o[g % DT], 0, 0, 0);
+      if (g + AHEAD < NB) read_v(g + AHEAD);
+#pragma unroll
+      for (int e = EA + g * 8 * 2 / NB; e < EA + (g + 1) * 8 * 2 / NB && e < 32; ++e) weight(e);
+      if (g >= NB / 2) {
+#pragma unroll
+        for (int e = (g - NB / 2) * 32 / NB; e < (g + 1 - NB / 2) * 32 / NB; ++e) m[e % 2] = max3(m[e % 2], next[e / 8][e % 8 * 2], next[e / 8][e % 8 * 2 + 1]);
       }
     }
+    products_settle();
+    if (i + 1 < end) raise((all_seen(i + 1) ? fmaxf(m[0], m[1]) : mask(next, i + 1)) * a.scale_log2e);
+    store(raw, true, i + 2);
+    arrived();
   };
-
-  TileRaw<D, PAGED> raw;
+  if (tid < 2) hole[tid] = 0;
+  __syncthreads();
+  f32x16_t S0[2], S1[2];
   if (begin < end) {
     if constexpr (PAGED) {
 #pragma unroll
       for (int j = 0; j < NL; ++j) pages[j] = page_at(begin, j);
     }
-    load(raw, begin);
+    load_k(raw, begin);
+    store(raw, true, begin);
+    load_v(raw, begin);
+    store(raw, false, begin);
+    load_k(raw, begin + 1);
+    store(raw, true, begin + 1);
   }
-  if (tid < 2) hole[tid] = 0;
-  __syncthreads();
-  if (begin < end) store(raw, begin, 0);
-  __syncthreads();
-  for (int i = begin; i < end; ++i) {
-    const int buf = (i - begin) & 1;
-    if (i + 1 < end) load(raw, i + 1);
-    compute(i, buf);
-    if (i + 1 < end) store(raw, i + 1, buf ^ 1);
-    __syncthreads();
+  arrived();
+  if (begin < end) {
+    logits(S0, begin);
+    products_settle();
+    raise((all_seen(begin) ? largest(S0) : mask(S0, begin)) * a.scale_log2e);
+  }
+  __syncthreads();                                 // (the first keys are read before their buffer is filled again)
+  for (int i = begin; i < end; i += 2) {
+    advance(S0, S1, i);
+    if (i + 1 < end) advance(S1, S0, i + 1);
   }
 
   sum += __shfl_xor(sum, 32);
@@ -262,12 +380,17 @@ AttendPlan attend_plan(const ficoco_attention& a, int heads, int64_t max_keys, b
 
 void launch_tile_rows(const AttendArgs& a, int d_head, bool paged, hipStream_t s) {
   const dim3 grid((unsigned)xcd_padded_total(a.B * a.H_kv * a.row_tiles * a.splits)), threads(kTileThreads);
-  if (paged) {
-    if (d_head == 128) hipLaunchKernelGGL((tile_rows_kernel<128, true>), grid, threads, 0, s, a);
-    else hipLaunchKernelGGL((tile_rows_kernel<64, true>), grid, threads, 0, s, a);
+  const bool aligned = (((uintptr_t)a.K | (uintptr_t)a.V) & 15) == 0 && ((a.k_sb | a.k_sh | a.k_sn | a.v_sb | a.v_sh | a.v_sn) & 7) == 0 &&
+                       a.k_sn < (1 << 24) && a.v_sn < (1 << 24);
+  const TileSource src = paged ? kPaged : aligned ? kDenseDirect : kDense;
+  if (d_head == 128) {
+    if (src == kPaged) hipLaunchKernelGGL((tile_rows_kernel<128, kPaged>), grid, threads, 0, s, a);
+    else if (src == kDense) hipLaunchKernelGGL((tile_rows_kernel<128, kDense>), grid, threads, 0, s, a);
+    else hipLaunchKernelGGL((tile_rows_kernel<128, kDenseDirect>), grid, threads, 0, s, a);
   } else {
-    if (d_head == 128) hipLaunchKernelGGL((tile_rows_kernel<128, false>), grid, threads, 0, s, a);
-    else hipLaunchKernelGGL((tile_rows_kernel<64, false>), grid, threads, 0, s, a);
+    if (src == kPaged) hipLaunchKernelGGL((tile_rows_kernel<64, kPaged>), grid, threads, 0, s, a);
+    else if (src == kDense) hipLaunchKernelGGL((tile_rows_kernel<64, kDense>), grid, threads, 0, s, a);
+    else hipLaunchKernelGGL((tile_rows_kernel<64, kDenseDirect>), grid, threads, 0, s, a);
   }
 }
 

@@ -218,12 +218,14 @@ WINDOW = [  # B, H_kv, group, d, n_q, n_k, window, sinks, q_len, k_len
 ]
 
 
+@pytest.mark.parametrize("aligned", [True, False])      # rows of 16-byte chunks go straight into LDS, others through registers
 @pytest.mark.parametrize("case", WINDOW, ids=str)
-def test_window_attention(ctx, case):
+def test_window_attention(ctx, case, aligned):
     B, heads, group, d, n_q, n_k, window, sinks, q_len, k_len = case
     g = torch.Generator(device="cuda").manual_seed(n_q)
     H = heads * group
-    qkv = torch.randn(B, max(n_q, n_k), H + 2 * heads, d + 3, generator=g, device="cuda").to(torch.bfloat16)[..., 1:d + 1]
+    qkv = torch.randn(B, max(n_q, n_k), H + 2 * heads, d + 8 if aligned else d + 3, generator=g, device="cuda").to(torch.bfloat16)
+    qkv = qkv[..., 8:d + 8] if aligned else qkv[..., 1:d + 1]
     Q = qkv[:, :n_q, :H].transpose(1, 2)
     K, V = qkv[:, :n_k, H:H + heads].transpose(1, 2), qkv[:, :n_k, H + heads:].transpose(1, 2)
     O = torch.full((B, n_q, H, d), 5.0, dtype=torch.bfloat16, device="cuda").transpose(1, 2)
