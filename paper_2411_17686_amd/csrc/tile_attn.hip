@@ -44,8 +44,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
   constexpr int DT = D / 32, KS = D / 16, CH = D / 8;
   constexpr int NL = PAGED ? D / 64 : D / 32;      // 16-byte loads of a thread
   constexpr int LC = PAGED ? D / 16 : D / 8;       // of a row
-  __shared__ __align__(16) bf16_t sk[2][kTileKeys * D];
-  __shared__ __align__(16) bf16_t sv[2][kTileKeys * D];
+  // (four arrays, chosen at compile time: the compiler then knows that loads into one do not concern reads of another)
+  __shared__ __align__(16) bf16_t sk0[kTileKeys * D], sk1[kTileKeys * D], sv0[kTileKeys * D], sv1[kTileKeys * D];
   __shared__ int hole[2];                          // 1 + the last step in this buffer some of whose keys have no page
   const int tid = threadIdx.x, lane = tid % kWave, wv = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int c32 = lane % 32, half = lane / 32;
@@ -80,30 +80,28 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
   const int32_t* table = PAGED ? a.table + (int64_t)slot * a.max_pages : nullptr;
   auto wanted = [&](int key) { return key < blocks.end && (key >= blocks.near_key || key < blocks.first_keys); };
 
-  // ---- straight into LDS: a wavefront's load fills 64 chunks in a row.  Rows that no query of the workgroup sees are
-  // replaced by one that is seen: their weights are zero, and zero times what memory happens to hold may be NaN.
+  // ---- straight into LDS: a wavefront's load fills 64 chunks in a row.  Rows that no query of the workgroup sees are replaced by one
+  // of the block that is seen: their weights are zero, and zero times what memory happens to hold may be NaN.
+  // (Buffer loads: behind a global load into LDS the compiler waits for all reads of LDS at once.)
   const int d_row = 64 / CH * wv + lane / CH;                                   // rows of load j: d_row + RJ * j
   constexpr int RJ = 64 * kTileWaves / CH;
   auto direct = [&](const bf16_t* base, int64_t sn, bf16_t* to, int swizzle, int step) {
     if (step >= end) return;
-    const int key0 = blocks.block(step) * kTileKeys;
-    const char* from = (const char*)(base + (int64_t)key0 * sn);                // (uniform)
-    const uint32_t ch = (uint32_t)((lane % CH ^ swizzle) * 8), row_bytes = (uint32_t)sn * 2;      // (a step's keys lie within 2^31 bytes: launch_tile_rows)
+    const int key0 = blocks.block(step) * kTileKeys, row_bytes = (int)sn * 2;    // (64 rows lie within 2^30 bytes: launch_tile_rows)
+    const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)(base + (int64_t)key0 * sn), 0, 0x7fffffff, 0x00027000);
+    const int ch = (lane % CH ^ swizzle) * 16;
     const bool whole = key0 + kTileKeys <= blocks.end && (key0 >= blocks.near_key || key0 + kTileKeys <= blocks.first_keys);
-    auto one = [&](const char* x, int j) {
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)x,
-                                       (__attribute__((address_space(3))) void*)(to + (j * kTileWaves + wv) * 64 * 8), 16, 0, 0);
+    auto one = [&](int j, int at, int add) {
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + (j * kTileWaves + wv) * 64 * 8), 16, at, add, 0, 0);
     };
     if (whole) {
-      const uint32_t off = (uint32_t)d_row * row_bytes + ch * 2;
 #pragma unroll
-      for (int j = 0; j < NL; ++j) one(from + (int64_t)(RJ * j) * sn * 2 + off, j);
+      for (int j = 0; j < NL; ++j) one(j, d_row * row_bytes + ch, RJ * j * row_bytes);
     } else {
+      const int behind = step < blocks.head ? blocks.first_keys : blocks.end;
+      const int seen = (behind < key0 + kTileKeys ? behind - key0 : kTileKeys) - 1;
 #pragma unroll
-      for (int j = 0; j < NL; ++j) {
-        const int row = wanted(key0 + d_row + RJ * j) ? d_row + RJ * j : blocks.end - 1 - key0;
-        one(from + (int64_t)row * sn * 2 + ch * 2, j);
-      }
+      for (int j = 0; j < NL; ++j) one(j, (wanted(key0 + d_row + RJ * j) ? d_row + RJ * j : seen) * row_bytes + ch, 0);
     }
   };
 
@@ -142,7 +140,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
   };
   const bf16_t* Kb = a.K + (int64_t)b * a.k_sb + (int64_t)h * a.k_sh;
   const bf16_t* Vb = a.V + (int64_t)b * a.v_sb + (int64_t)h * a.v_sh;
-  auto load_k = [&](TileRaw<D, SRC>& raw, int step) {
+  auto load_k = [&](TileRaw<D, SRC>& raw, bf16_t* to, int step) {
     if constexpr (PAGED) {
       load_page(raw, a.k, a.k_exp, pages, step);
 #pragma unroll
@@ -153,24 +151,22 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
     } else if constexpr (SRC == kDense) {
       load_dense(raw, Kb, a.k_sn, step);
     } else {
-      direct(Kb, a.k_sn, sk[(step - begin) & 1], key_swizzle<D>(d_row), step);
+      direct(Kb, a.k_sn, to, key_swizzle<D>(d_row), step);
     }
   };
-  auto load_v = [&](TileRaw<D, SRC>& raw, int step) {      // before load_k of the step behind it
+  auto load_v = [&](TileRaw<D, SRC>& raw, bf16_t* to, int step) {      // before load_k of the step behind it
     if constexpr (PAGED) load_page(raw, a.v, a.v_exp, k_pages, step);
     else if constexpr (SRC == kDense) load_dense(raw, Vb, a.v_sn, step);
-    else direct(Vb, a.v_sn, sv[(step - begin) & 1], value_swizzle<D>(d_row), step);
+    else direct(Vb, a.v_sn, to, value_swizzle<D>(d_row), step);
   };
-  auto store = [&](const TileRaw<D, SRC>& raw, bool keys, int step) {
+  auto store = [&](const TileRaw<D, SRC>& raw, bf16_t* to, bool keys, int step) {
     if constexpr (SRC != kDenseDirect) {
-      const int buf = (step - begin) & 1;
-      bf16_t* to = keys ? sk[buf] : sv[buf];
 #pragma unroll
       for (int j = 0; j < NL; ++j) {
         const int at = tid + j * kTileThreads, row = at / LC, ch = at % LC, swizzle = keys ? key_swizzle<D>(row) : value_swizzle<D>(row);
         uint4* r = (uint4*)to + row * CH;
         if constexpr (PAGED) {
-          if (keys && raw.e[j] & kHole) hole[buf] = step + 1;
+          if (keys && raw.e[j] & kHole) hole[(step - begin) & 1] = step + 1;
           const float scale = exp_scale(raw.e[j] & 255);
           const uint2 y0 = widen_e4m3(raw.x[j].x, scale), y1 = widen_e4m3(raw.x[j].y, scale), y2 = widen_e4m3(raw.x[j].z, scale), y3 = widen_e4m3(raw.x[j].w, scale);
           r[2 * ch ^ swizzle] = uint4{y0.x, y0.y, y1.x, y1.y};
@@ -187,8 +183,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
   };
 
   const int k_swizzle = key_swizzle<D>(c32);
-  auto logits = [&](f32x16_t (&S)[2], int step) {
-    const bf16_t* k0 = &sk[(step - begin) & 1][c32 * D];
+  auto logits = [&](f32x16_t (&S)[2]) {            // of the first step
+    const bf16_t* k0 = &sk0[c32 * D];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
@@ -244,19 +240,18 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
   for (int i = 0; i < DT; ++i) v_at[i] = v_row * D + (4 * i + lane / 16 % 2 * 2 + lane % 4 / 2 ^ v_swizzle) * 8 + lane % 4 % 2 * 4;
 
   TileRaw<D, SRC> raw;
-  auto advance = [&](f32x16_t (&S)[2], f32x16_t (&next)[2], int i) {
+  // (ka, va: of this step;  kb, vb: of the next one)
+  auto advance = [&](f32x16_t (&S)[2], f32x16_t (&next)[2], bf16_t* ka, bf16_t* kb, bf16_t* va, bf16_t* vb, int i) {
     constexpr int NA = 2 * KS, NB = 4 * DT;        // products of either kind
     constexpr int AHEAD = 4;                       // operands on their way out of LDS
     constexpr int EA = 24;                         // weights formed beside the first kind; the other 8 beside the second
-    load_v(raw, i + 1);
-    if constexpr (SRC == kDenseDirect) load_k(raw, i + 2);
-    const bf16_t* k0 = sk[(i + 1 - begin) & 1];    // (behind the last step: whatever is there)
-    const bf16_t* v0 = sv[(i - begin) & 1];
+    load_v(raw, vb, i + 1);
+    if constexpr (SRC == kDenseDirect) load_k(raw, ka, i + 2);
     bf16x8_t kf[AHEAD], vf[AHEAD], P[4];
     float w[32];
-    auto read_k = [&](int g) { kf[g % AHEAD] = *(const bf16x8_t*)(k0 + g / KS * 32 * D + k_at[g % KS]); };
+    auto read_k = [&](int g) { kf[g % AHEAD] = *(const bf16x8_t*)(kb + g / KS * 32 * D + k_at[g % KS]); };
     auto read_v = [&](int g) {
-      const bf16_t* v = v0 + 16 * (g / DT) * D + v_at[g % DT];
+      const bf16_t* v = va + 16 * (g / DT) * D + v_at[g % DT];
       const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t)v));
       const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t)(v + 8 * D)));
       vf[g % AHEAD] = __builtin_bit_cast(bf16x8_t, uint4{x.x, x.y, y.x, y.y});
@@ -280,8 +275,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
     }
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (SRC != kDenseDirect) {
-      store(raw, false, i + 1);
-      load_k(raw, i + 2);
+      store(raw, vb, false, i + 1);
+      load_k(raw, ka, i + 2);
 #pragma unroll
       for (int g = 0; g < AHEAD; ++g) read_v(g);
     }
@@ -300,7 +295,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
     }
     products_settle();
     if (i + 1 < end) raise((all_seen(i + 1) ? fmaxf(m[0], m[1]) : mask(next, i + 1)) * a.scale_log2e);
-    store(raw, true, i + 2);
+    store(raw, ka, true, i + 2);
     arrived();
   };
   if (tid < 2) hole[tid] = 0;
@@ -311,23 +306,23 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
 #pragma unroll
       for (int j = 0; j < NL; ++j) pages[j] = page_at(begin, j);
     }
-    load_k(raw, begin);
-    store(raw, true, begin);
-    load_v(raw, begin);
-    store(raw, false, begin);
-    load_k(raw, begin + 1);
-    store(raw, true, begin + 1);
+    load_k(raw, sk0, begin);
+    store(raw, sk0, true, begin);
+    load_v(raw, sv0, begin);
+    store(raw, sv0, false, begin);
+    load_k(raw, sk1, begin + 1);
+    store(raw, sk1, true, begin + 1);
   }
   arrived();
   if (begin < end) {
-    logits(S0, begin);
+    logits(S0);
     products_settle();
     raise((all_seen(begin) ? largest(S0) : mask(S0, begin)) * a.scale_log2e);
   }
   __syncthreads();                                 // (the first keys are read before their buffer is filled again)
   for (int i = begin; i < end; i += 2) {
-    advance(S0, S1, i);
-    if (i + 1 < end) advance(S1, S0, i + 1);
+    advance(S0, S1, sk0, sk1, sv0, sv1, i);
+    if (i + 1 < end) advance(S1, S0, sk1, sk0, sv1, sv0, i + 1);
   }
 
   sum += __shfl_xor(sum, 32);
@@ -381,7 +376,7 @@ AttendPlan attend_plan(const ficoco_attention& a, int heads, int64_t max_keys, b
 void launch_tile_rows(const AttendArgs& a, int d_head, bool paged, hipStream_t s) {
   const dim3 grid((unsigned)xcd_padded_total(a.B * a.H_kv * a.row_tiles * a.splits)), threads(kTileThreads);
   const bool aligned = (((uintptr_t)a.K | (uintptr_t)a.V) & 15) == 0 && ((a.k_sb | a.k_sh | a.k_sn | a.v_sb | a.v_sh | a.v_sn) & 7) == 0 &&
-                       a.k_sn < (1 << 24) && a.v_sn < (1 << 24);
+                       a.k_sn < (1 << 23) && a.v_sn < (1 << 23);
   const TileSource src = paged ? kPaged : aligned ? kDenseDirect : kDense;
   if (d_head == 128) {
     if (src == kPaged) hipLaunchKernelGGL((tile_rows_kernel<128, kPaged>), grid, threads, 0, s, a);
