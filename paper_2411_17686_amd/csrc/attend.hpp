@@ -85,9 +85,24 @@ struct Blocks {
   __device__ __forceinline__ int block(int i) const { return i < head ? i : near + (i - head); }
 };
 
-__device__ __forceinline__ bool key_seen(const AttendArgs& a, int key, int pos, int keys) {
-  return key < keys && key <= pos && (a.window <= 0 || (int64_t)key > (int64_t)pos - a.window || key < a.sinks);
-}
+// The keys that one row sees: [lo, lo + span], and those below `first`.
+struct RowSight {
+  int lo, first;
+  uint32_t span;
+  RowSight() = default;
+  __device__ __forceinline__ RowSight(const AttendArgs& a, int pos, int keys) {
+    const int hi = pos < keys ? pos : keys - 1;
+    const int64_t from = a.window > 0 ? (int64_t)pos - a.window + 1 : 0;
+    lo = from > 0 ? (int)from : 0;
+    first = a.window > 0 ? (a.sinks < hi + 1 ? a.sinks : hi + 1) : 0;
+    span = (uint32_t)(hi - lo);
+    if (hi < lo) {                       // nothing but first keys: a range that holds no key there can be
+      lo = 0x7fffffff;
+      span = 0;
+    }
+  }
+  __device__ __forceinline__ bool sees(int key) const { return (uint32_t)(key - lo) <= span; }
+};
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, bf16x2_t{(__bf16)a, (__bf16)b});

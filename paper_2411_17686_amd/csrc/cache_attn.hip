@@ -64,13 +64,13 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendAr
 
   // queries: row CT * 16 + c16, features 64 l + 16 q4 + 8 u .. + 8
   bf16x8_t qf[CT][L][2];
-  int pos[CT];
+  RowSight sight[CT];
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
     int r = ct * 16 + c16;
     r = r < rows ? r : rows - 1;
     const int t = r / a.group, g = r % a.group;
-    pos[ct] = s.first + t;
+    sight[ct] = RowSight(a, s.first + t, s.keys);
     const bf16_t* q = a.Q + (int64_t)b * a.q_sb + (int64_t)(h * a.group + g) * a.q_sh + (int64_t)t * a.q_sn;
 #pragma unroll
     for (int l = 0; l < L; ++l) {
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendAr
         for (int i = 0; i < 4; ++i) {
           const int key = key0 + 16 * u + 4 * q4 + i;
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct) S[ct][u][i] = have[u] && key_seen(a, key, pos[ct], s.keys) ? S[ct][u][i] : -__builtin_huge_valf();
+          for (int ct = 0; ct < CT; ++ct) S[ct][u][i] = have[u] && (sight[ct].sees(key) || key < sight[ct].first) ? S[ct][u][i] : -__builtin_huge_valf();
           // what no row sees may hold anything, and 0 * NaN is NaN
           if (!have[u] || key >= blocks.end || (key < blocks.near_key && key >= blocks.first_keys)) {
 #pragma unroll

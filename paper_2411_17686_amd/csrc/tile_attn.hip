@@ -205,19 +205,23 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
     for (int i = 1; i < 16; ++i) m = max3(m, S[0][i], S[1][i]);
     return m;
   };
+  const RowSight sight(a, pos, s.keys);
   auto mask = [&](f32x16_t (&S)[2], int step) {    // what a row does not see: -infinity; a lane's largest logit
-    const int key0 = blocks.block(step) * kTileKeys;
+    const int key0 = blocks.block(step) * kTileKeys + 4 * half;
+    const bool firsts = a.window > 0 && blocks.block(step) * kTileKeys < a.sinks, holes = PAGED && hole[(step - begin) & 1] == step + 1;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int key = key0 + kb * 32 + i / 4 * 8 + 4 * half + i % 4;
-        bool seen = key_seen(a, key, pos, s.keys);
-        if (PAGED) {
-          const int p = seen ? table[key >> a.page_shift] : -1;
-          seen = p >= 0 && p < a.n_pages;
+      for (int i = 0; i < 16; ++i) S[kb][i] = sight.sees(key0 + kb * 32 + i / 4 * 8 + i % 4) || (firsts && key0 + kb * 32 + i / 4 * 8 + i % 4 < sight.first) ? S[kb][i] : -__builtin_huge_valf();
+    }
+    if (holes) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = key0 + kb * 32 + i / 4 * 8 + i % 4, p = key < s.keys ? table[key >> a.page_shift] : -1;
+          S[kb][i] = p >= 0 && p < a.n_pages ? S[kb][i] : -__builtin_huge_valf();
         }
-        S[kb][i] = seen ? S[kb][i] : -__builtin_huge_valf();
       }
     }
     return largest(S);
