@@ -1,4 +1,4 @@
-// What the two attention kernels share: the rows of a workgroup, which keys they see, and the parts of a result whose
+// What the attention kernels share: the rows of a workgroup, which keys they see, and the parts of a result whose
 // keys are cut over several workgroups.
 #pragma once
 #include "cache.hpp"
@@ -113,6 +113,15 @@ __device__ __forceinline__ uint2 widen_e4m3(uint32_t q, float scale) {
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q, scale, true))};
 }
 
+constexpr int kTileWaves = 4, kTileThreads = kTileWaves * kWave;
+constexpr int kTileRows = 32 * kTileWaves;   // rows of a workgroup where there are many
+constexpr int kTileKeys = 64;                // keys of its step
+constexpr float kSlack = 8.0f;               // (units of log2) growth of a row's maximum that is put up with
+
+// (fmaxf() would first bring either argument into canonical form, an instruction more for each)
+__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
+__device__ __forceinline__ float halves_max(float v) { return fmaxf(v, __shfl_xor(v, 32)); }
+
 // Between products and a branch behind which their results are read.  A result may be read a number of instructions after the product
 // at the earliest; the compiler keeps to that inside a block, but not everywhere across a branch (seen with ROCm 7.2: copies
 // of the last two registers of a 32 x 32 result in the block behind a branch, three instructions later, got what was there before).
@@ -124,7 +133,7 @@ __device__ __forceinline__ void products_settle() {
 
 // How the keys of a call are cut: few workgroups otherwise leave compute units idle.
 struct AttendPlan {
-  bool few;            // single tokens (cache_attn.hip), else tiles of 128 rows (tile_attn.hip)
+  bool few;            // single tokens (cache_attn.hip), else tiles of 128 rows (page_attn.hip; dense: tile_attn.hip)
   int rows;            // rows of a workgroup
   int row_tiles, splits;
   size_t part_ms, part_o, total;
@@ -132,7 +141,8 @@ struct AttendPlan {
 AttendPlan attend_plan(const ficoco_attention& a, int heads, int64_t max_keys, bool paged);
 
 void launch_few_rows(const AttendArgs& a, const AttendPlan& pl, int d_head, hipStream_t s);
-void launch_tile_rows(const AttendArgs& a, int d_head, bool paged, hipStream_t s);
+void launch_page_rows(const AttendArgs& a, int d_head, hipStream_t s);
+void launch_dense_rows(const AttendArgs& a, int d_head, hipStream_t s);
 void launch_join_rows(const AttendArgs& a, int d_head, hipStream_t s);
 
 }  // namespace ficoco

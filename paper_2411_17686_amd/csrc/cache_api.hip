@@ -249,7 +249,7 @@ int ficoco_cache_attention(ficoco_ctx* ctx, const ficoco_cache* c, int32_t layer
   x.n_pages = c->n_pages; x.n_seqs = c->n_seqs; x.max_pages = c->max_pages;
   x.page_shift = __builtin_ctz((unsigned)c->page_size);
   if (pl.few) launch_few_rows(x, pl, a->d_head, (hipStream_t)stream);
-  else launch_tile_rows(x, a->d_head, true, (hipStream_t)stream);
+  else launch_page_rows(x, a->d_head, (hipStream_t)stream);
   if (pl.splits > 1) launch_join_rows(x, a->d_head, (hipStream_t)stream);
   return finish(ctx, fn);
 }
@@ -265,7 +265,7 @@ int ficoco_window_attention(ficoco_ctx* ctx, const ficoco_attention* a, void* st
   if (a->B == 0 || a->n_q == 0) return FICOCO_OK;
   const AttendPlan pl = attend_plan(*a, a->H_kv, a->n_k, false);
   if ((int64_t)a->B * a->H_kv * (pl.row_tiles + kXcds) > kMaxGridX) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "too many rows in one call");
-  launch_tile_rows(arguments(*a, a->H_kv, pl, nullptr), a->d_head, false, (hipStream_t)stream);
+  launch_dense_rows(arguments(*a, a->H_kv, pl, nullptr), a->d_head, (hipStream_t)stream);
   return finish(ctx, fn);
 }
 

@@ -1,5 +1,7 @@
 // Attention over pages of 8 bits for few rows: single tokens of a decoder (and the few of a draft), all query heads
 // of a key / value head together.
+#include <algorithm>
+
 #include "attend.hpp"
 
 namespace ficoco {
@@ -7,7 +9,6 @@ namespace {
 
 constexpr int kFewWaves = 4;
 constexpr int kFewKeys = 32;                 // keys of a step
-constexpr float kSlack = 8.0f;               // (units of log2) growth of a row's maximum that is put up with
 
 // One step's keys and values of a lane as they come out of memory.
 template <int D> struct FewRaw {
@@ -309,6 +310,27 @@ __global__ __launch_bounds__(4 * kWave) void join_rows_kernel(AttendArgs a) {
 }
 
 }  // namespace
+
+AttendPlan attend_plan(const ficoco_attention& a, int heads, int64_t max_keys, bool paged) {
+  AttendPlan pl{};
+  const int64_t rows = (int64_t)a.n_q * (a.H / heads), bh = (int64_t)a.B * heads;
+  pl.few = paged && rows <= 16;
+  pl.rows = pl.few ? 16 : kTileRows;
+  pl.row_tiles = (int)std::max<int64_t>(1, (rows + pl.rows - 1) / pl.rows);
+  pl.splits = 1;
+  if (paged && bh > 0) {
+    int64_t seen = max_keys;
+    if (a.window > 0) seen = std::min(seen, (int64_t)a.window + a.sinks + a.n_q);
+    // about two workgroups a compute unit, but at least two steps a wavefront, and four of a tile
+    const int64_t want = (512 + bh * pl.row_tiles - 1) / (bh * pl.row_tiles);
+    pl.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, seen / 256), 256));
+  }
+  const size_t parts = pl.splits > 1 ? (size_t)bh * pl.splits * pl.row_tiles * pl.rows : 0;
+  pl.part_ms = 0;
+  pl.part_o = (parts * sizeof(float2) + 255) / 256 * 256;
+  pl.total = std::max<size_t>(256, pl.part_o + (parts * a.d_head * sizeof(float) + 255) / 256 * 256);
+  return pl;
+}
 
 void launch_few_rows(const AttendArgs& a, const AttendPlan& pl, int d_head, hipStream_t s) {
   const dim3 grid((unsigned)((int64_t)a.B * a.H_kv * a.splits)), threads(kFewWaves * kWave);

@@ -1,18 +1,10 @@
-// Attention for many rows: dense prompts with a window, and questions of many tokens over pages of 8 bits.
+// Attention of dense prompts, with or without a window.
 #include <algorithm>
 
 #include "attend.hpp"
 
 namespace ficoco {
 namespace {
-
-constexpr int kTileWaves = 4;
-constexpr int kTileThreads = kTileWaves * kWave;
-constexpr int kTileRows = 32 * kTileWaves;   // rows of a workgroup
-constexpr int kTileKeys = 64;                // keys of a step
-constexpr float kSlack = 8.0f;               // (units of log2) growth of a row's maximum that is put up with
-
-constexpr int kHole = 1 << 16;                // (beside two exponent bytes) a key that would be seen has no page
 
 typedef short i16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4_t* lds_i16x4_t;
@@ -22,16 +14,11 @@ typedef __attribute__((address_space(3))) i16x4_t* lds_i16x4_t;
 template <int D> __device__ __forceinline__ int key_swizzle(int row) { return D == 128 ? row & 15 : row >> 1 & 7; }
 template <int D> __device__ __forceinline__ int value_swizzle(int row) { return D == 128 ? (row & 3) << 2 : (row & 2) << 1; }
 
-// (fmaxf() would first bring either argument into canonical form, an instruction more for each)
-__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
-__device__ __forceinline__ float halves_max(float v) { return fmaxf(v, __shfl_xor(v, 32)); }
-
 enum TileSource {
   kDenseDirect,      // 16-byte aligned rows: straight into LDS
-  kDense,            // any other: through registers
-  kPaged             // 8 bits: through registers, widened with their block's scale
+  kDense             // any other: through registers
 };
-template <int D, TileSource SRC> struct TileRaw { uint4 x[SRC == kPaged ? D / 64 : D / 32]; int e[D / 64]; };       // a thread's share of a step's keys or values
+template <int D> struct TileRaw { uint4 x[D / 32]; };       // a thread's share of a step's keys or values
 
 // One pass with a running maximum and sum, 128 rows a workgroup, 32 a wavefront, 64 keys a step.  32 x 32 x 16 products:
 //   S^T[key][row] = K Q^T, the queries in registers; a lane holds 32 logits of one row
@@ -40,13 +27,10 @@ template <int D, TileSource SRC> struct TileRaw { uint4 x[SRC == kPaged ? D / 64
 // turns.  So keys are in LDS a step ahead of the values; either in two buffers, what comes next on its way while a step is computed.
 template <int D, TileSource SRC>
 __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a) {
-  constexpr bool PAGED = SRC == kPaged;
   constexpr int DT = D / 32, KS = D / 16, CH = D / 8;
-  constexpr int NL = PAGED ? D / 64 : D / 32;      // 16-byte loads of a thread
-  constexpr int LC = PAGED ? D / 16 : D / 8;       // of a row
+  constexpr int NL = D / 32;                       // 16-byte loads of a thread
   // (four arrays, chosen at compile time: the compiler then knows that loads into one do not concern reads of another)
   __shared__ __align__(16) bf16_t sk0[kTileKeys * D], sk1[kTileKeys * D], sv0[kTileKeys * D], sv1[kTileKeys * D];
-  __shared__ int hole[2];                          // 1 + the last step in this buffer some of whose keys have no page
   const int tid = threadIdx.x, lane = tid % kWave, wv = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int c32 = lane % 32, half = lane / 32;
   const int per_head = a.row_tiles * a.splits, total = a.B * a.H_kv * per_head;
@@ -55,7 +39,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
   const int bh = id / per_head, in_head = id % per_head, h = bh % a.H_kv, b = bh / a.H_kv;
   const int split = in_head % a.splits, tile = a.row_tiles - 1 - in_head / a.splits;    // (the last rows see most keys)
   int slot;
-  const Sight s = sight_of<PAGED>(a, b, slot);
+  const Sight s = sight_of<false>(a, b, slot);
   const int rows = s.queries * a.group, row0 = tile * kTileRows;
   if (s.queries <= 0 || row0 >= rows) return;
   auto pos_of = [&](int r) { return s.first + (r < rows ? r : rows - 1) / a.group; };
@@ -77,7 +61,6 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
   for (int i = 0; i < DT; ++i) o[i] = f32x16_t{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
   float top = kNoLogit, sum = 0.0f;
 
-  const int32_t* table = PAGED ? a.table + (int64_t)slot * a.max_pages : nullptr;
   auto wanted = [&](int key) { return key < blocks.end && (key >= blocks.near_key || key < blocks.first_keys); };
 
   // ---- straight into LDS: a wavefront's load fills 64 chunks in a row.  Rows that no query of the workgroup sees are replaced by one
@@ -87,7 +70,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
   constexpr int RJ = 64 * kTileWaves / CH;
   auto direct = [&](const bf16_t* base, int64_t sn, bf16_t* to, int swizzle, int step) {
     if (step >= end) return;
-    const int key0 = blocks.block(step) * kTileKeys, row_bytes = (int)sn * 2;    // (64 rows lie within 2^30 bytes: launch_tile_rows)
+    const int key0 = blocks.block(step) * kTileKeys, row_bytes = (int)sn * 2;    // (64 rows lie within 2^30 bytes: launch_dense_rows)
     const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)(base + (int64_t)key0 * sn), 0, 0x7fffffff, 0x00027000);
     const int ch = (lane % CH ^ swizzle) * 16;
     const bool whole = key0 + kTileKeys <= blocks.end && (key0 >= blocks.near_key || key0 + kTileKeys <= blocks.first_keys);
@@ -106,74 +89,35 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
   };
 
   // ---- through registers
-  auto page_at = [&](int step, int j) {
-    const int key = blocks.block(step) * kTileKeys + (tid + j * kTileThreads) / LC;
-    int p = -1;
-    if (step < end && wanted(key)) p = table[key >> a.page_shift];       // (keys lie inside the row: see sight_of)
-    return p < a.n_pages ? p : -1;
-  };
-  int pages[NL], k_pages[NL];                      // of the next step's keys to be loaded, and of the keys loaded last
-  auto load_page = [&](TileRaw<D, SRC>& raw, const uint8_t* pool, const uint8_t* exps, const int (&page)[NL], int step) {
+  auto load_dense = [&](TileRaw<D>& raw, const bf16_t* base, int64_t sn, int step) {
     const int key0 = blocks.block(step) * kTileKeys;
 #pragma unroll
     for (int j = 0; j < NL; ++j) {
-      const int at = tid + j * kTileThreads, key = key0 + at / LC;
+      const int at = tid + j * kTileThreads, key = key0 + at / CH;
       raw.x[j] = uint4{0, 0, 0, 0};
-      raw.e[j] = 0;
-      if (page[j] >= 0) {
-        const int64_t block = (int64_t)page[j] * a.H_kv + h;
-        raw.x[j] = *(const uint4*)(pool + ((block << a.page_shift) + (key & ((1 << a.page_shift) - 1))) * D + 16 * (at % LC));
-        raw.e[j] = exps[block];
-      } else if (step < end && wanted(key)) {
-        raw.e[j] = kHole;
-      }
-    }
-  };
-  auto load_dense = [&](TileRaw<D, SRC>& raw, const bf16_t* base, int64_t sn, int step) {
-    const int key0 = blocks.block(step) * kTileKeys;
-#pragma unroll
-    for (int j = 0; j < NL; ++j) {
-      const int at = tid + j * kTileThreads, key = key0 + at / LC;
-      raw.x[j] = uint4{0, 0, 0, 0};
-      if (step < end && wanted(key)) __builtin_memcpy(&raw.x[j], base + (int64_t)key * sn + 8 * (at % LC), 16);
+      if (step < end && wanted(key)) __builtin_memcpy(&raw.x[j], base + (int64_t)key * sn + 8 * (at % CH), 16);
     }
   };
   const bf16_t* Kb = a.K + (int64_t)b * a.k_sb + (int64_t)h * a.k_sh;
   const bf16_t* Vb = a.V + (int64_t)b * a.v_sb + (int64_t)h * a.v_sh;
-  auto load_k = [&](TileRaw<D, SRC>& raw, bf16_t* to, int step) {
-    if constexpr (PAGED) {
-      load_page(raw, a.k, a.k_exp, pages, step);
-#pragma unroll
-      for (int j = 0; j < NL; ++j) {
-        k_pages[j] = pages[j];
-        pages[j] = page_at(step + 1, j);
-      }
-    } else if constexpr (SRC == kDense) {
+  auto load_k = [&](TileRaw<D>& raw, bf16_t* to, int step) {
+    if constexpr (SRC == kDense) {
       load_dense(raw, Kb, a.k_sn, step);
     } else {
       direct(Kb, a.k_sn, to, key_swizzle<D>(d_row), step);
     }
   };
-  auto load_v = [&](TileRaw<D, SRC>& raw, bf16_t* to, int step) {      // before load_k of the step behind it
-    if constexpr (PAGED) load_page(raw, a.v, a.v_exp, k_pages, step);
-    else if constexpr (SRC == kDense) load_dense(raw, Vb, a.v_sn, step);
+  auto load_v = [&](TileRaw<D>& raw, bf16_t* to, int step) {
+    if constexpr (SRC == kDense) load_dense(raw, Vb, a.v_sn, step);
     else direct(Vb, a.v_sn, to, value_swizzle<D>(d_row), step);
   };
-  auto store = [&](const TileRaw<D, SRC>& raw, bf16_t* to, bool keys, int step) {
+  auto store = [&](const TileRaw<D>& raw, bf16_t* to, bool keys) {
     if constexpr (SRC != kDenseDirect) {
 #pragma unroll
       for (int j = 0; j < NL; ++j) {
-        const int at = tid + j * kTileThreads, row = at / LC, ch = at % LC, swizzle = keys ? key_swizzle<D>(row) : value_swizzle<D>(row);
+        const int at = tid + j * kTileThreads, row = at / CH, ch = at % CH, swizzle = keys ? key_swizzle<D>(row) : value_swizzle<D>(row);
         uint4* r = (uint4*)to + row * CH;
-        if constexpr (PAGED) {
-          if (keys && raw.e[j] & kHole) hole[(step - begin) & 1] = step + 1;
-          const float scale = exp_scale(raw.e[j] & 255);
-          const uint2 y0 = widen_e4m3(raw.x[j].x, scale), y1 = widen_e4m3(raw.x[j].y, scale), y2 = widen_e4m3(raw.x[j].z, scale), y3 = widen_e4m3(raw.x[j].w, scale);
-          r[2 * ch ^ swizzle] = uint4{y0.x, y0.y, y1.x, y1.y};
-          r[2 * ch + 1 ^ swizzle] = uint4{y2.x, y2.y, y3.x, y3.y};
-        } else {
-          r[ch ^ swizzle] = raw.x[j];
-        }
+        r[ch ^ swizzle] = raw.x[j];
       }
     }
   };
@@ -196,8 +140,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
   };
   auto all_seen = [&](int step) {                  // every key of a step by every row of the wavefront
     const int key0 = blocks.block(step) * kTileKeys, last = key0 + kTileKeys - 1;
-    const bool all = last < s.keys && last <= lo && (a.window <= 0 || (int64_t)key0 > (int64_t)hi - a.window || last < a.sinks);
-    return PAGED ? all && __builtin_amdgcn_readfirstlane(hole[(step - begin) & 1]) != step + 1 : all;
+    return last < s.keys && last <= lo && (a.window <= 0 || (int64_t)key0 > (int64_t)hi - a.window || last < a.sinks);
   };
   auto largest = [&](const f32x16_t (&S)[2]) {
     float m = fmaxf(S[0][0], S[1][0]);
@@ -206,23 +149,13 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
     return m;
   };
   const RowSight sight(a, pos, s.keys);
-  auto mask = [&](f32x16_t (&S)[2], int step) {    // what a row does not see: -infinity; a lane's largest logit
+  auto mask = [&](f32x16_t (&S)[2], int step) __attribute__((always_inline)) {    // what a row does not see: -infinity; a lane's largest logit
     const int key0 = blocks.block(step) * kTileKeys + 4 * half;
-    const bool firsts = a.window > 0 && blocks.block(step) * kTileKeys < a.sinks, holes = PAGED && hole[(step - begin) & 1] == step + 1;
+    const bool firsts = a.window > 0 && blocks.block(step) * kTileKeys < a.sinks;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) S[kb][i] = sight.sees(key0 + kb * 32 + i / 4 * 8 + i % 4) || (firsts && key0 + kb * 32 + i / 4 * 8 + i % 4 < sight.first) ? S[kb][i] : -__builtin_huge_valf();
-    }
-    if (holes) {
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = key0 + kb * 32 + i / 4 * 8 + i % 4, p = key < s.keys ? table[key >> a.page_shift] : -1;
-          S[kb][i] = p >= 0 && p < a.n_pages ? S[kb][i] : -__builtin_huge_valf();
-        }
-      }
     }
     return largest(S);
   };
@@ -243,9 +176,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
 #pragma unroll
   for (int i = 0; i < DT; ++i) v_at[i] = v_row * D + (4 * i + lane / 16 % 2 * 2 + lane % 4 / 2 ^ v_swizzle) * 8 + lane % 4 % 2 * 4;
 
-  TileRaw<D, SRC> raw;
+  TileRaw<D> raw;
   // (ka, va: of this step;  kb, vb: of the next one)
-  auto advance = [&](f32x16_t (&S)[2], f32x16_t (&next)[2], bf16_t* ka, bf16_t* kb, bf16_t* va, bf16_t* vb, int i) {
+  auto advance = [&](f32x16_t (&S)[2], f32x16_t (&next)[2], bf16_t* ka, bf16_t* kb, bf16_t* va, bf16_t* vb, int i) __attribute__((always_inline)) {
     constexpr int NA = 2 * KS, NB = 4 * DT;        // products of either kind
     constexpr int AHEAD = 4;                       // operands on their way out of LDS
     constexpr int EA = 24;                         // weights formed beside the first kind; the other 8 beside the second
@@ -279,7 +212,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
     }
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (SRC != kDenseDirect) {
-      store(raw, vb, false, i + 1);
+      store(raw, vb, false);
       load_k(raw, ka, i + 2);
 #pragma unroll
       for (int g = 0; g < AHEAD; ++g) read_v(g);
@@ -299,23 +232,17 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
     }
     products_settle();
     if (i + 1 < end) raise((all_seen(i + 1) ? fmaxf(m[0], m[1]) : mask(next, i + 1)) * a.scale_log2e);
-    store(raw, ka, true, i + 2);
+    store(raw, ka, true);
     arrived();
   };
-  if (tid < 2) hole[tid] = 0;
-  __syncthreads();
   f32x16_t S0[2], S1[2];
   if (begin < end) {
-    if constexpr (PAGED) {
-#pragma unroll
-      for (int j = 0; j < NL; ++j) pages[j] = page_at(begin, j);
-    }
     load_k(raw, sk0, begin);
-    store(raw, sk0, true, begin);
+    store(raw, sk0, true);
     load_v(raw, sv0, begin);
-    store(raw, sv0, false, begin);
+    store(raw, sv0, false);
     load_k(raw, sk1, begin + 1);
-    store(raw, sk1, true, begin + 1);
+    store(raw, sk1, true);
   }
   arrived();
   if (begin < end) {
@@ -356,40 +283,16 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
 
 }  // namespace
 
-AttendPlan attend_plan(const ficoco_attention& a, int heads, int64_t max_keys, bool paged) {
-  AttendPlan pl{};
-  const int64_t rows = (int64_t)a.n_q * (a.H / heads), bh = (int64_t)a.B * heads;
-  pl.few = paged && rows <= 16;
-  pl.rows = pl.few ? 16 : kTileRows;
-  pl.row_tiles = (int)std::max<int64_t>(1, (rows + pl.rows - 1) / pl.rows);
-  pl.splits = 1;
-  if (paged && bh > 0) {
-    int64_t seen = max_keys;
-    if (a.window > 0) seen = std::min(seen, (int64_t)a.window + a.sinks + a.n_q);
-    // about two workgroups a compute unit, but at least two steps a wavefront, and four of a tile
-    const int64_t least = pl.few ? 256 : 256, want = (512 + bh * pl.row_tiles - 1) / (bh * pl.row_tiles);
-    pl.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, seen / least), 256));
-  }
-  const size_t parts = pl.splits > 1 ? (size_t)bh * pl.splits * pl.row_tiles * pl.rows : 0;
-  pl.part_ms = 0;
-  pl.part_o = (parts * sizeof(float2) + 255) / 256 * 256;
-  pl.total = std::max<size_t>(256, pl.part_o + (parts * a.d_head * sizeof(float) + 255) / 256 * 256);
-  return pl;
-}
-
-void launch_tile_rows(const AttendArgs& a, int d_head, bool paged, hipStream_t s) {
-  const dim3 grid((unsigned)xcd_padded_total(a.B * a.H_kv * a.row_tiles * a.splits)), threads(kTileThreads);
-  const bool aligned = (((uintptr_t)a.K | (uintptr_t)a.V) & 15) == 0 && ((a.k_sb | a.k_sh | a.k_sn | a.v_sb | a.v_sh | a.v_sn) & 7) == 0 &&
-                       a.k_sn < (1 << 23) && a.v_sn < (1 << 23);
-  const TileSource src = paged ? kPaged : aligned ? kDenseDirect : kDense;
+void launch_dense_rows(const AttendArgs& a, int d_head, hipStream_t s) {
+  const dim3 grid((unsigned)xcd_padded_total(a.B * a.H_kv * a.row_tiles)), threads(kTileThreads);
+  const bool direct = (((uintptr_t)a.K | (uintptr_t)a.V) & 15) == 0 && ((a.k_sb | a.k_sh | a.k_sn | a.v_sb | a.v_sh | a.v_sn) & 7) == 0 &&
+                      a.k_sn < (1 << 23) && a.v_sn < (1 << 23);
   if (d_head == 128) {
-    if (src == kPaged) hipLaunchKernelGGL((tile_rows_kernel<128, kPaged>), grid, threads, 0, s, a);
-    else if (src == kDense) hipLaunchKernelGGL((tile_rows_kernel<128, kDense>), grid, threads, 0, s, a);
-    else hipLaunchKernelGGL((tile_rows_kernel<128, kDenseDirect>), grid, threads, 0, s, a);
+    if (direct) hipLaunchKernelGGL((tile_rows_kernel<128, kDenseDirect>), grid, threads, 0, s, a);
+    else hipLaunchKernelGGL((tile_rows_kernel<128, kDense>), grid, threads, 0, s, a);
   } else {
-    if (src == kPaged) hipLaunchKernelGGL((tile_rows_kernel<64, kPaged>), grid, threads, 0, s, a);
-    else if (src == kDense) hipLaunchKernelGGL((tile_rows_kernel<64, kDense>), grid, threads, 0, s, a);
-    else hipLaunchKernelGGL((tile_rows_kernel<64, kDenseDirect>), grid, threads, 0, s, a);
+    if (direct) hipLaunchKernelGGL((tile_rows_kernel<64, kDenseDirect>), grid, threads, 0, s, a);
+    else hipLaunchKernelGGL((tile_rows_kernel<64, kDense>), grid, threads, 0, s, a);
   }
 }
 
