@@ -390,65 +390,114 @@ __global__ __launch_bounds__(kPlanThreads) void cache_compact_plan_kernel(ficoco
   }
 }
 
-// The new pages of one sequence, layer, head and K / V, a workgroup each in turn: rows gathered from the pages before,
-// with their exponents, the block's own exponent, and back to 8 bits.  The pages read are not among those written: they are
-// held until the plan of a later call.
-template <int GPT>
-__global__ __launch_bounds__(kMoveThreads) void cache_compact_kernel(ficoco_cache c, int layer_begin, int vis_begin, int N, int n_keep,
+// The largest magnitude of 16 E4M3 numbers that is not NaN, in units of their scale.  Bytes without their sign ascend with the magnitude;
+// one added, NaN (127) becomes 0 and the others 1 .. 127.
+__device__ __forceinline__ float largest_e4m3(const uint4& q) {
+  typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+  u16x2_t m = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t y = (w[i] & 0x7f7f7f7fu) + 0x01010101u;
+    m = __builtin_elementwise_max(m, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, y & 0x007f007fu), __builtin_bit_cast(u16x2_t, y >> 8 & 0x007f007fu)));
+  }
+  const int top = m.x > m.y ? m.x : m.y;
+  return top > 0 ? __builtin_amdgcn_cvt_f32_fp8(top - 1, 0) : 0.0f;
+}
+// 16 numbers from one scale to another, as to_e4m3() has them.
+__device__ __forceinline__ uint4 rescale_e4m3(const uint4& q, int from, int to) {
+  const int d = from - to + kExpBias;
+  const float f = exp_scale(d < 1 ? 1 : d < 254 ? d : 254);      // (beyond: nothing is left, or there is nothing but zeros)
+  float x[8];
+  from_e4m3(uint2{q.x, q.y}, f, x);
+  const uint2 a = to_e4m3(x, 1.0f);
+  from_e4m3(uint2{q.z, q.w}, f, x);
+  const uint2 b = to_e4m3(x, 1.0f);
+  return uint4{a.x, a.y, b.x, b.y};
+}
+
+// The new pages of one sequence: where a page's tokens come from is found once, in LDS, and holds for every layer, head, K and V;
+// then a wavefront takes a block (one page of one head, K or V) at a time, its 16-byte pieces in registers, the next block's on their way.
+// Blocks whose exponent stays keep their bytes.  The pages read are not among those written: they are held until the plan of a later call.
+//
+// Bound by memory (five crops, 4 sequences of 2979 tokens to 739, 16 layers of 8 heads: 194 MB).  A workgroup that took the blocks of one head, one
+// after the other, found every block's rows anew, four loads one behind the other: 103 us.
+template <int NG>
+__global__ __launch_bounds__(kMoveThreads) void cache_compact_kernel(ficoco_cache c, int layer_begin, int blocks, int per_wg, int vis_begin, int N, int n_keep,
                                                                      const int32_t* __restrict__ dst, const int32_t* __restrict__ keep_idx,
                                                                      const CompactMeta* __restrict__ meta, const int32_t* __restrict__ rows) {
-  __shared__ float scratch[kMoveThreads / kWave];
-  const int b = blockIdx.z >> 1;
+  __shared__ int from_page[128], from_slot[128];
+  const int b = blockIdx.z;
   const CompactMeta m = meta[b];
-  const int P = c.page_size, per_row = c.d_head / 8, block_bytes = P * c.d_head;
-  const int64_t layer = layer_begin + blockIdx.y / c.heads, h = blockIdx.y % c.heads;
-  uint8_t* pool = (uint8_t*)(blockIdx.z & 1 ? c.v : c.k);
-  uint8_t* exps = blockIdx.z & 1 ? c.v_exp : c.k_exp;
+  const int shift = __builtin_ctz(c.page_size), P = 1 << shift, per_row = c.d_head / 16, block_bytes = P * c.d_head;
+  const int lane = threadIdx.x % kWave, wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int first = blockIdx.y * per_wg + wv, end = min(blocks, (int)blockIdx.y * per_wg + per_wg);
   for (int page_at = m.first + blockIdx.x; page_at < m.pages; page_at += gridDim.x) {
     const int page = c.table[(int64_t)dst[b] * c.max_pages + page_at];
-    if (!page_ok(c, page)) continue;                       // (uniform)
-    uint2 q[GPT];
-    int e_old[GPT];
-#pragma unroll
-    for (int j = 0; j < GPT; ++j) {
-      const int g = threadIdx.x + j * kMoveThreads, row = g / per_row;
-      const int64_t r = (int64_t)page_at * P + row;
-      q[j] = uint2{0, 0};
-      e_old[j] = kExpMin;
-      if (row < P && r < m.tokens) {
-        int64_t t = r;
+    if ((int)threadIdx.x < P) {
+      const int64_t r = ((int64_t)page_at << shift) + threadIdx.x;
+      int p = -1;
+      int64_t t = r;
+      if (r < m.tokens) {
         if (r >= vis_begin + n_keep) {
           t = r + (N - n_keep);
         } else if (r >= vis_begin) {
           const int k = keep_idx[(int64_t)b * n_keep + (r - vis_begin)];
           t = vis_begin + (k < 0 ? 0 : k < N ? k : N - 1);
         }
-        const int old = rows[(int64_t)b * c.max_pages + t / P];
-        if (page_ok(c, old)) {
-          const int64_t block = (layer * c.n_pages + old) * c.heads + h;
-          __builtin_memcpy(&q[j], pool + block * block_bytes + t % P * c.d_head + g % per_row * 8, 8);
-          e_old[j] = exps[block];
+        p = rows[(int64_t)b * c.max_pages + (t >> shift)];
+        if (!page_ok(c, p)) p = -1;
+      }
+      from_page[threadIdx.x] = r < m.tokens ? p : -2;       // -1: zeros, -2: behind the last token, left as it is
+      from_slot[threadIdx.x] = (int)(t & (P - 1));
+    }
+    __syncthreads();
+    if (page_ok(c, page)) {                                  // (uniform)
+      struct Piece { uint4 q[NG]; int e[NG]; };
+      // block i: V behind K, heads behind layers
+      auto block_of = [&](int i, int p) { return ((int64_t)(layer_begin + i / 2 / c.heads) * c.n_pages + p) * c.heads + i / 2 % c.heads; };
+      auto load = [&](Piece& x, int i) {
+        const uint8_t* pool = (const uint8_t*)(i & 1 ? c.v : c.k);
+        const uint8_t* exps = i & 1 ? c.v_exp : c.k_exp;
+#pragma unroll
+        for (int j = 0; j < NG; ++j) {
+          const int g = lane + j * kWave, row = g / per_row, p = from_page[row];
+          x.q[j] = uint4{0, 0, 0, 0};
+          x.e[j] = kExpMin;
+          if (p >= 0) {
+            const int64_t block = block_of(i, p);
+            x.q[j] = *(const uint4*)(pool + block * block_bytes + from_slot[row] * c.d_head + g % per_row * 16);
+            x.e[j] = exps[block];
+          }
         }
+      };
+      auto put = [&](const Piece& x, int i) {
+        float top = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NG; ++j) top = fmaxf(top, largest_e4m3(x.q[j]) * exp_scale(x.e[j]));
+        const int e = block_exponent(wave_reduce(top, [](float u, float v) { return fmaxf(u, v); }));
+        const int64_t block = block_of(i, page);
+        uint8_t* pool = (uint8_t*)(i & 1 ? c.v : c.k) + block * block_bytes;
+#pragma unroll
+        for (int j = 0; j < NG; ++j) {
+          const int g = lane + j * kWave;
+          if (from_page[g / per_row] == -2) continue;
+          *(uint4*)(pool + (int64_t)g * 16) = x.e[j] == e ? x.q[j] : rescale_e4m3(x.q[j], x.e[j], e);
+        }
+        if (lane == 0) (i & 1 ? c.v_exp : c.k_exp)[block] = (uint8_t)e;
+      };
+      Piece x0, x1;
+      if (first < end) load(x0, first);
+      for (int i = first; i < end; i += 2 * (kMoveThreads / kWave)) {
+        const int next = i + kMoveThreads / kWave;
+        if (next < end) load(x1, next);
+        put(x0, i);
+        if (next >= end) break;
+        if (next + kMoveThreads / kWave < end) load(x0, next + kMoveThreads / kWave);
+        put(x1, next);
       }
     }
-    float v[GPT][8];
-    float top = 0.0f;
-#pragma unroll
-    for (int j = 0; j < GPT; ++j) {
-      from_e4m3(q[j], exp_scale(e_old[j]), v[j]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_magnitude(v[j][i]));
-    }
-    const int e = block_exponent(block_max(top, scratch));
-    const int64_t block = (layer * c.n_pages + page) * c.heads + h;
-#pragma unroll
-    for (int j = 0; j < GPT; ++j) {
-      const int g = threadIdx.x + j * kMoveThreads, row = g / per_row;
-      if (row >= P || (int64_t)page_at * P + row >= m.tokens) continue;
-      const uint2 w = to_e4m3(v[j], exp_inverse(e));
-      __builtin_memcpy(pool + block * block_bytes + (int64_t)g * 8, &w, 8);
-    }
-    if (threadIdx.x == 0) exps[block] = (uint8_t)e;
+    __syncthreads();
   }
 }
 
@@ -476,6 +525,12 @@ TokenSide side_of(const ficoco_cache& c, const ficoco_tokens& t, int layer, bool
 int page_walkers(const ficoco_cache& c, int64_t others) {
   const int64_t want = (8192 + others - 1) / others;
   return (int)(want < 1 ? 1 : want < c.max_pages ? want : c.max_pages);
+}
+
+template <int NG>
+void launch_compact_pages(const ficoco_cache& c, dim3 grid, int layer_begin, int blocks, int per_wg, int vis_begin, int N, int n_keep, const int32_t* dst,
+                          const int32_t* keep_idx, const CompactMeta* meta, const int32_t* rows, hipStream_t s) {
+  hipLaunchKernelGGL((cache_compact_kernel<NG>), grid, dim3(kMoveThreads), 0, s, c, layer_begin, blocks, per_wg, vis_begin, N, n_keep, dst, keep_idx, meta, rows);
 }
 
 template <typename T>
@@ -522,12 +577,18 @@ void launch_cache_compact(const ficoco_cache& c, int layer_begin, int n_layers, 
   int32_t* rows = (int32_t*)(ws + (size_t)n * sizeof(CompactMeta));
   hipLaunchKernelGGL(cache_compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, c, n, src, dst, vis_begin, N, n_keep, keep_idx, done, meta, rows);
   if (n_layers == 0) return;
-  const dim3 grid(page_walkers(c, (int64_t)n_layers * c.heads * n * 2), n_layers * c.heads, 2 * n);
-  const int groups = c.page_size * c.d_head / 8;
-  if (groups <= 256) hipLaunchKernelGGL((cache_compact_kernel<1>), grid, dim3(kMoveThreads), 0, s, c, layer_begin, vis_begin, N, n_keep, dst, keep_idx, meta, rows);
-  else if (groups <= 512) hipLaunchKernelGGL((cache_compact_kernel<2>), grid, dim3(kMoveThreads), 0, s, c, layer_begin, vis_begin, N, n_keep, dst, keep_idx, meta, rows);
-  else if (groups <= 1024) hipLaunchKernelGGL((cache_compact_kernel<4>), grid, dim3(kMoveThreads), 0, s, c, layer_begin, vis_begin, N, n_keep, dst, keep_idx, meta, rows);
-  else hipLaunchKernelGGL((cache_compact_kernel<8>), grid, dim3(kMoveThreads), 0, s, c, layer_begin, vis_begin, N, n_keep, dst, keep_idx, meta, rows);
+  // A wavefront takes up to eight blocks, fewer where the chip would not be filled (1024 workgroups; a sequence's pages count as eight).
+  const int blocks = 2 * n_layers * c.heads, waves = kMoveThreads / kWave;
+  const int64_t want = (int64_t)blocks * n * 8 / 1024;
+  const int per_wg = (int)(want < waves ? waves : want < 8 * waves ? want / waves * waves : 8 * waves);
+  const dim3 grid(c.max_pages < 64 ? c.max_pages : 64, (blocks + per_wg - 1) / per_wg, n);
+  switch (c.page_size * c.d_head / 1024) {
+    case 1: launch_compact_pages<1>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, dst, keep_idx, meta, rows, s); break;
+    case 2: launch_compact_pages<2>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, dst, keep_idx, meta, rows, s); break;
+    case 4: launch_compact_pages<4>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, dst, keep_idx, meta, rows, s); break;
+    case 8: launch_compact_pages<8>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, dst, keep_idx, meta, rows, s); break;
+    default: launch_compact_pages<16>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, dst, keep_idx, meta, rows, s); break;
+  }
 }
 
 void launch_cache_free(const ficoco_cache& c, int n, const int32_t* seq, hipStream_t s) {
