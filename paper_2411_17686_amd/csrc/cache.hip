@@ -51,16 +51,18 @@ __device__ __forceinline__ int free_mask(const ficoco_cache& c, int i0) {
   return m;
 }
 
+// `first_mask`: free_mask() of this thread's pages among the first 8 * kPlanThreads, read ahead of the rest of the plan.
 // Every entry's thread (tid < n, others need = 0) asks for `need` pages; take(b, k, page) gets page k of entry b, the free pages
 // in ascending order.  Entries are served in order as long as the pages last.  Returns whether this thread's entry is.
 template <typename F>
-__device__ __forceinline__ bool hand_out(const ficoco_cache& c, PlanLds& l, int n, int need, F take) {
+__device__ __forceinline__ bool hand_out(const ficoco_cache& c, PlanLds& l, int n, int need, int first_mask, F take) {
   int total;
   const int end = block_scan_inclusive(need, l.scratch, &total);
   if ((int)threadIdx.x < n) l.end[threadIdx.x] = end;
   if (total == 0) return true;                            // (uniform)
-  int n_free = 0;
-  for (int base = 0; base < c.n_pages && n_free < total; base += 8 * kPlanThreads) {
+  int n_free;
+  const int first_rank = block_scan_inclusive(__popc(first_mask), l.scratch, &n_free) - __popc(first_mask), first_free = n_free;
+  for (int base = 8 * kPlanThreads; base < c.n_pages && n_free < total; base += 8 * kPlanThreads) {
     int t;
     (void)block_scan_inclusive(__popc(free_mask(c, base + 8 * (int)threadIdx.x)), l.scratch, &t);
     n_free += t;
@@ -71,9 +73,9 @@ __device__ __forceinline__ bool hand_out(const ficoco_cache& c, PlanLds& l, int 
   const int give = l.served;
   int given = 0;
   for (int base = 0; base < c.n_pages && given < give; base += 8 * kPlanThreads) {
-    const int i0 = base + 8 * (int)threadIdx.x, m = free_mask(c, i0);
-    int t;
-    int r = given + block_scan_inclusive(__popc(m), l.scratch, &t) - __popc(m);
+    const int i0 = base + 8 * (int)threadIdx.x, m = base == 0 ? first_mask : free_mask(c, i0);
+    int t = first_free, r = first_rank;
+    if (base > 0) r = given + block_scan_inclusive(__popc(m), l.scratch, &t) - __popc(m);
     for (int j = 0; j < 8; ++j) {
       if (!(m >> j & 1)) continue;
       if (r < give) {
@@ -95,7 +97,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_reserve_kernel(ficoco_cach
                                                                      const int32_t* __restrict__ n_new, int n_each, int32_t* __restrict__ start) {
   __shared__ PlanLds l;
   __shared__ int slot[kMaxCall], have[kMaxCall];
-  const int b = threadIdx.x;
+  const int b = threadIdx.x, first_mask = free_mask(c, 8 * (int)threadIdx.x);
   auto slot_of = [&](int i) { return seq ? seq[i] : i; };
   find_owners(c, l, n, slot_of);
   int need = 0, len = 0, add = 0;
@@ -115,7 +117,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_reserve_kernel(ficoco_cach
     slot[b] = s;
   }
   __syncthreads();
-  const bool served = hand_out(c, l, n, need, [&](int e, int k, int page) {
+  const bool served = hand_out(c, l, n, need, first_mask, [&](int e, int k, int page) {
     c.table[(int64_t)slot[e] * c.max_pages + have[e] + k] = page;
     c.refs[page] = 1;
   });
@@ -162,55 +164,61 @@ __device__ __forceinline__ float block_max(float v, float* scratch) {
   return v;
 }
 
-// One workgroup per touched page, head, sequence and K / V.  GPT: groups of eight values a thread.
+// What a call writes to one sequence: positions [first, stop) of slot `slot`, none where first < 0.
+struct Span { int slot, first; int64_t stop; };
+__device__ __forceinline__ Span span_of(const ficoco_cache& c, int b, int n_max, const int32_t* seq, const int32_t* start, const int32_t* n_new) {
+  const int s = seq ? seq[b] : b, first = start[b];
+  int n = n_new ? n_new[b] : n_max;
+  n = n < n_max ? n : n_max;
+  return slot_ok(c, s) && first >= 0 && n > 0 ? Span{s, first, (int64_t)first + n} : Span{0, -1, -1};
+}
+
+// One workgroup per touched page, head, sequence and K / V: the new tokens' largest magnitude, then all of them.  GPT: groups of
+// eight values a thread.  The tokens are on their way before the page is looked up.
+//
+// Bound by memory (8 prompts of up to 2979 tokens, 8 heads of 128, bfloat16: 107 MB).
 template <typename T, int GPT>
 __global__ __launch_bounds__(kMoveThreads) void cache_append_kernel(ficoco_cache c, int64_t layer_pages, TokenSide ks, TokenSide vs, int n_max,
                                                                     const int32_t* __restrict__ seq, const int32_t* __restrict__ start,
                                                                     const int32_t* __restrict__ n_new) {
   __shared__ float scratch[kMoveThreads / kWave];
-  const int b = blockIdx.z >> 1, h = blockIdx.y, P = c.page_size, per_row = c.d_head / 8;
+  const int b = blockIdx.z >> 1, h = blockIdx.y, shift = __builtin_ctz(c.page_size), P = 1 << shift, row_shift = __builtin_ctz(c.d_head / 8);
   const TokenSide& side = blockIdx.z & 1 ? vs : ks;
-  const int s = seq ? seq[b] : b, first = start[b];
-  int n = n_new ? n_new[b] : n_max;
-  n = n < n_max ? n : n_max;
-  if (!slot_ok(c, s) || first < 0 || n <= 0) return;
-  const int64_t stop = (int64_t)first + n;
-  const int64_t at = first / P + (int64_t)blockIdx.x;
-  if (at * P >= stop || at >= c.max_pages) return;
-  const int page = c.table[(int64_t)s * c.max_pages + at];
+  const Span sp = span_of(c, b, n_max, seq, start, n_new);
+  const int64_t at = (sp.first >> shift) + (int64_t)blockIdx.x, pos0 = at << shift;
+  if (sp.first < 0 || pos0 >= sp.stop || at >= c.max_pages) return;
+  const T* x = (const T*)side.x + (int64_t)b * side.sb + (int64_t)h * side.sh;
+  float v[GPT][8];
+#pragma unroll
+  for (int j = 0; j < GPT; ++j) {
+    const int g = threadIdx.x + j * kMoveThreads, row = g >> row_shift;
+    const int64_t pos = pos0 + row;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[j][i] = 0.0f;
+    if (row < P && pos >= sp.first && pos < sp.stop) load8f(x + (pos - sp.first) * side.sn + (g & ((1 << row_shift) - 1)) * 8, v[j]);
+  }
+  const int page = c.table[(int64_t)sp.slot * c.max_pages + at];
   if (!page_ok(c, page)) return;
   const int64_t block = (layer_pages + page) * c.heads + h;
   uint8_t* pool = side.pool + block * P * c.d_head;
-  const T* x = (const T*)side.x + (int64_t)b * side.sb + (int64_t)h * side.sh;
-
-  float v[GPT][8];
+  const int old = pos0 < sp.first ? side.exps[block] : 0;
   float top = 0.0f;
-#pragma unroll
-  for (int j = 0; j < GPT; ++j) {
-    const int g = threadIdx.x + j * kMoveThreads, row = g / per_row;
-    const int64_t pos = at * P + row;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[j][i] = 0.0f;
-    if (row < P && pos >= first && pos < stop) load8f(x + (pos - first) * side.sn + g % per_row * 8, v[j]);
-  }
 #pragma unroll
   for (int j = 0; j < GPT; ++j) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_magnitude(v[j][i]));
   }
   int e = block_exponent(block_max(top, scratch));
-  const bool begun = at * P < first;
-  const int old = begun ? side.exps[block] : 0;
   e = e > old ? e : old;
   const float inv = exp_inverse(e);
   __syncthreads();                                         // the byte is read before it is written
 #pragma unroll
   for (int j = 0; j < GPT; ++j) {
-    const int g = threadIdx.x + j * kMoveThreads, row = g / per_row;
-    const int64_t pos = at * P + row;
-    if (row >= P || pos >= stop) continue;
+    const int g = threadIdx.x + j * kMoveThreads, row = g >> row_shift;
+    const int64_t pos = pos0 + row;
+    if (row >= P || pos >= sp.stop) continue;
     uint8_t* to = pool + (int64_t)g * 8;
-    if (pos < first) {
+    if (pos < sp.first) {
       if (e == old) continue;
       uint2 q;
       __builtin_memcpy(&q, to, 8);
@@ -222,11 +230,53 @@ __global__ __launch_bounds__(kMoveThreads) void cache_append_kernel(ficoco_cache
   if (threadIdx.x == 0) side.exps[block] = (uint8_t)e;
 }
 
+// One token a sequence (a decoder's step): eight values a lane, so a row of 16 lanes (heads of 64: half of one) holds the token of one head, K or V.
+// Older tokens of the page are touched only where the new one raises the exponent.
+template <typename T, int D>
+__global__ __launch_bounds__(kMoveThreads) void cache_append_token_kernel(ficoco_cache c, int64_t layer_pages, TokenSide ks, TokenSide vs, int items,
+                                                                          const int32_t* __restrict__ seq, const int32_t* __restrict__ start,
+                                                                          const int32_t* __restrict__ n_new) {
+  constexpr int L = D / 8;
+  const int item = (blockIdx.x * kMoveThreads + threadIdx.x) / L, g = threadIdx.x % L;      // V behind K, heads behind sequences
+  const bool there = item < items;
+  const int i = there ? item : items - 1, b = i / (2 * c.heads), h = i / 2 % c.heads;
+  const TokenSide& side = i & 1 ? vs : ks;
+  const Span sp = span_of(c, b, 1, seq, start, n_new);
+  const int shift = __builtin_ctz(c.page_size), slot = sp.first & ((1 << shift) - 1), at = sp.first >> shift;
+  float v[8] = {};
+  if (sp.first >= 0) load8f((const T*)side.x + (int64_t)b * side.sb + (int64_t)h * side.sh + 8 * g, v);
+  const int page = sp.first >= 0 && at < c.max_pages ? c.table[(int64_t)sp.slot * c.max_pages + at] : -1;
+  const bool ok = there && page_ok(c, page);
+  const int64_t block = ok ? (layer_pages + page) * c.heads + h : 0;
+  const int old = ok && slot > 0 ? side.exps[block] : 0;
+  float top = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = fmaxf(top, finite_magnitude(v[j]));
+  top = fmaxf(top, dpp_move<0xB1>(top));
+  top = fmaxf(top, dpp_move<0x4E>(top));
+  top = fmaxf(top, dpp_move<0x141>(top));
+  if constexpr (L == 16) top = fmaxf(top, dpp_move<0x140>(top));
+  if (!ok) return;
+  int e = block_exponent(top);
+  e = e > old ? e : old;
+  uint8_t* pool = side.pool + (block << shift) * D + 8 * g;
+  const uint2 q = to_e4m3(v, exp_inverse(e));
+  *(uint2*)(pool + slot * D) = q;
+  if (e != old && slot > 0) {
+    for (int r = 0; r < slot; ++r) {
+      float x[8];
+      from_e4m3(*(const uint2*)(pool + r * D), exp_scale(old), x);
+      *(uint2*)(pool + r * D) = to_e4m3(x, exp_inverse(e));
+    }
+  }
+  if (e != old && g == 0) side.exps[block] = (uint8_t)e;   // (the rows of a wavefront read the byte in one instruction, before)
+}
+
 template <typename T>
 __global__ __launch_bounds__(kMoveThreads) void cache_read_kernel(ficoco_cache c, int64_t layer_pages, TokenSide ks, TokenSide vs, int n_max,
                                                                   const int32_t* __restrict__ seq, const int32_t* __restrict__ start,
                                                                   const int32_t* __restrict__ n_new) {
-  const int b = blockIdx.z >> 1, h = blockIdx.y, P = c.page_size, per_row = c.d_head / 8;
+  const int b = blockIdx.z >> 1, h = blockIdx.y, shift = __builtin_ctz(c.page_size), per_row = c.d_head / 8;
   const TokenSide& side = blockIdx.z & 1 ? vs : ks;
   if (!side.x) return;
   const int s = seq ? seq[b] : b, first = start ? start[b] : 0;
@@ -236,13 +286,13 @@ __global__ __launch_bounds__(kMoveThreads) void cache_read_kernel(ficoco_cache c
   const int g = threadIdx.x % per_row;
   const int t = (int)(blockIdx.x * (kMoveThreads / per_row) + threadIdx.x / per_row);
   if (t >= n) return;
-  const int64_t pos = (int64_t)first + t, at = pos / P;
+  const int64_t pos = (int64_t)first + t, at = pos >> shift;
   float v[8] = {};
   const int page = slot_ok(c, s) && at < c.max_pages ? c.table[(int64_t)s * c.max_pages + at] : -1;
   if (page_ok(c, page)) {
     const int64_t block = (layer_pages + page) * c.heads + h;
     uint2 q;
-    __builtin_memcpy(&q, side.pool + (block * P + pos % P) * c.d_head + g * 8, 8);
+    __builtin_memcpy(&q, side.pool + ((block << shift) + (pos & (c.page_size - 1))) * c.d_head + g * 8, 8);
     from_e4m3(q, exp_scale(side.exps[block]), v);
   }
   store8f((T*)const_cast<void*>(side.x) + (int64_t)b * side.sb + (int64_t)h * side.sh + (int64_t)t * side.sn + g * 8, v);
@@ -253,7 +303,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_fork_kernel(ficoco_cache c
                                                                   int whole, int32_t* __restrict__ done) {
   __shared__ PlanLds l;
   __shared__ int from[kMaxCall], to[kMaxCall], shared[kMaxCall];
-  const int b = threadIdx.x;
+  const int b = threadIdx.x, first_mask = free_mask(c, 8 * (int)threadIdx.x);
   find_owners(c, l, n, [&](int i) { return dst[i]; });
   int need = 0, len = 0;
   bool ok = false;
@@ -270,7 +320,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_fork_kernel(ficoco_cache c
     need = ok ? pages_of(c, len) - shared[b] : 0;
   }
   __syncthreads();
-  const bool served = ok & hand_out(c, l, n, need, [&](int e, int k, int page) {
+  const bool served = ok & hand_out(c, l, n, need, first_mask, [&](int e, int k, int page) {
     c.table[(int64_t)to[e] * c.max_pages + shared[e] + k] = page;
     c.refs[page] = 1;
   });
@@ -318,7 +368,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_compact_plan_kernel(ficoco
                                                                           int32_t* __restrict__ done, CompactMeta* __restrict__ meta, int32_t* __restrict__ rows) {
   __shared__ PlanLds l;
   __shared__ int from[kMaxCall], to[kMaxCall], moved[kMaxCall], first[kMaxCall], had[kMaxCall], now[kMaxCall];
-  const int b = threadIdx.x, lane = threadIdx.x % kWave;
+  const int b = threadIdx.x, lane = threadIdx.x % kWave, first_mask = free_mask(c, 8 * (int)threadIdx.x);
   find_owners(c, l, n, [&](int i) { return dst[i]; });
   // the first preserved token that moves: its rank among the preserved ones
   for (int e = threadIdx.x / kWave; e < n; e += kPlanThreads / kWave) {
@@ -361,7 +411,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_compact_plan_kernel(ficoco
   for (int e = threadIdx.x / kWave; e < n; e += kPlanThreads / kWave)
     for (int i = lane; i < had[e]; i += kWave) rows[(int64_t)e * c.max_pages + i] = c.table[(int64_t)from[e] * c.max_pages + i];
   __syncthreads();                                         // the rows are saved before new pages go into them
-  const bool served = ok & hand_out(c, l, n, need, [&](int e, int k, int page) {
+  const bool served = ok & hand_out(c, l, n, need, first_mask, [&](int e, int k, int page) {
     c.table[(int64_t)to[e] * c.max_pages + first[e] + k] = page;
     c.refs[page] = 1;
   });
@@ -515,8 +565,7 @@ __global__ __launch_bounds__(kMoveThreads) void cache_free_kernel(ficoco_cache c
   if (threadIdx.x == 0) c.len[s] = 0;
 }
 
-TokenSide side_of(const ficoco_cache& c, const ficoco_tokens& t, int layer, bool v) {
-  (void)layer;
+TokenSide side_of(const ficoco_tokens& t, const ficoco_cache& c, bool v) {
   return v ? TokenSide{t.V, t.v_stride_b, t.v_stride_h, t.v_stride_n, (uint8_t*)c.v, c.v_exp}
            : TokenSide{t.K, t.k_stride_b, t.k_stride_h, t.k_stride_n, (uint8_t*)c.k, c.k_exp};
 }
@@ -535,10 +584,17 @@ void launch_compact_pages(const ficoco_cache& c, dim3 grid, int layer_begin, int
 
 template <typename T>
 void append_groups(const ficoco_cache& c, int layer, const ficoco_tokens& t, hipStream_t s) {
+  const TokenSide k = side_of(t, c, false), v = side_of(t, c, true);
+  const int64_t lp = (int64_t)layer * c.n_pages;
+  const int64_t items = (int64_t)2 * t.n * c.heads;
+  if (t.n_max == 1 && items <= 0x7fffffff / 16) {
+    const dim3 grid((unsigned)((items * (c.d_head / 8) + kMoveThreads - 1) / kMoveThreads));
+    if (c.d_head == 128) hipLaunchKernelGGL((cache_append_token_kernel<T, 128>), grid, dim3(kMoveThreads), 0, s, c, lp, k, v, (int)items, t.seq, t.start, t.n_new);
+    else hipLaunchKernelGGL((cache_append_token_kernel<T, 64>), grid, dim3(kMoveThreads), 0, s, c, lp, k, v, (int)items, t.seq, t.start, t.n_new);
+    return;
+  }
   const int touched = (t.n_max + c.page_size - 2) / c.page_size + 1;
   const dim3 grid(touched, c.heads, 2 * t.n);
-  const TokenSide k = side_of(c, t, layer, false), v = side_of(c, t, layer, true);
-  const int64_t lp = (int64_t)layer * c.n_pages;
   const int groups = c.page_size * c.d_head / 8;
   if (groups <= 256) hipLaunchKernelGGL((cache_append_kernel<T, 1>), grid, dim3(kMoveThreads), 0, s, c, lp, k, v, t.n_max, t.seq, t.start, t.n_new);
   else if (groups <= 512) hipLaunchKernelGGL((cache_append_kernel<T, 2>), grid, dim3(kMoveThreads), 0, s, c, lp, k, v, t.n_max, t.seq, t.start, t.n_new);
@@ -559,7 +615,7 @@ void launch_cache_append(const ficoco_cache& c, int layer, const ficoco_tokens& 
 void launch_cache_read(const ficoco_cache& c, int layer, const ficoco_tokens& t, hipStream_t s) {
   const int rows = kMoveThreads / (c.d_head / 8);
   const dim3 grid((t.n_max + rows - 1) / rows, c.heads, 2 * t.n);
-  const TokenSide k = side_of(c, t, layer, false), v = side_of(c, t, layer, true);
+  const TokenSide k = side_of(t, c, false), v = side_of(t, c, true);
   const int64_t lp = (int64_t)layer * c.n_pages;
   if (t.dtype == FICOCO_BF16) hipLaunchKernelGGL(cache_read_kernel<bf16_t>, grid, dim3(kMoveThreads), 0, s, c, lp, k, v, t.n_max, t.seq, t.start, t.n_new);
   else hipLaunchKernelGGL(cache_read_kernel<float>, grid, dim3(kMoveThreads), 0, s, c, lp, k, v, t.n_max, t.seq, t.start, t.n_new);
