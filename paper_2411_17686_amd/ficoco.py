@@ -6,6 +6,7 @@ no fallback: if the shared library has not been built, `lib()` raises.
 """
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -132,7 +133,7 @@ def lib():
         L.ficoco_v_step_static.argtypes = step[:2] + step[4:]
         L.ficoco_gather_tokens.argtypes = [vp, pp, i32p, vp, C.c_int64, C.c_int64, C.c_int32, vp, vp]
         L.ficoco_schedule.argtypes = [C.POINTER(ScheduleProblem), C.POINTER(C.c_int32), C.POINTER(C.c_double)]
-        cp, tp, ap, i32 = C.POINTER(CacheProblem), C.POINTER(TokensProblem), C.POINTER(AttentionProblem), C.c_int32
+        cp, tp, ap, i32 = C.POINTER(CacheProblem), vp, vp, C.c_int32       # (tokens and attention: packed bytes, see _TOKENS)
         L.ficoco_cache_reserve.argtypes = [vp, cp, i32, i32p, i32p, i32, i32p, vp]
         L.ficoco_cache_append.argtypes = [vp, cp, i32, tp, vp]
         L.ficoco_cache_read.argtypes = [vp, cp, i32, tp, vp]
@@ -198,6 +199,10 @@ class Context:
 
     def stream(self):
         return C.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
+
+    def raw_stream(self):
+        """The same as a number: a decoding step's calls take microseconds, and so does the stream object."""
+        return torch._C._cuda_getCurrentRawStream(self.device.index)
 
 
 def make_problem(X, *, variant, vis_begin, N, n_keep, A=None, a_q_begin=0, a_k_begin=0,
@@ -387,6 +392,12 @@ def ficoco_schedule(variant, layers, start_layer, N, M, D, F, min_keep, budget_f
 
 
 # ---- the decoder's key / value cache -----------------------------------------------------------
+# `ficoco_tokens` and `ficoco_attention` as packed bytes: filling a ctypes structure field by field takes longer than a
+# decoding step's kernels.
+_TOKENS = struct.Struct("@3i5P6q")
+_ATTENTION = struct.Struct("@6iP3q2P6qP3q4Pf3i")
+
+
 class Cache:
     """Tensors of a `ficoco_cache` (shapes as in include/ficoco.h) and its description, filled once."""
 
@@ -401,8 +412,10 @@ class Cache:
                 raise TypeError("the tensors of a cache are contiguous, on one device, of the types and shapes in ficoco.h")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self.table, self.len, self.refs = table, length, refs
+        self.device = k.device
         self.c = CacheProblem(layers, n_pages, page_size, heads, d_head, n_seqs, max_pages, k.data_ptr(), v.data_ptr(),
                               k_exp.data_ptr(), v_exp.data_ptr(), table.data_ptr(), length.data_ptr(), refs.data_ptr())
+        self._p = C.byref(self.c)
 
     @classmethod
     def empty(cls, layers, n_pages, page_size, heads, d_head, n_seqs, max_pages, device="cuda"):
@@ -418,129 +431,159 @@ class Workspace:
     """Device memory for one call at a time, 256-byte aligned."""
 
     def __init__(self, n, device):
-        self.bytes = n
+        self.bytes, self.device = n, torch.device(device)
         self.t = torch.empty(n + 256, dtype=torch.uint8, device=device)
         self.ptr = self.t.data_ptr() + (-self.t.data_ptr()) % 256
 
 
-def _i32(t, n, name):
+def _i32(t, n, name, device):
+    """Address of n int32 values on `device`, 0 for None."""
     if t is None:
-        return None
-    if t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != n:
-        raise TypeError("%s must be %d contiguous int32 values" % (name, n))
-    return C.c_void_p(t.data_ptr())
+        return 0
+    if t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous() or t.device != device:
+        raise TypeError("%s must be %d contiguous int32 values on %s" % (name, n, device))
+    return t.data_ptr()
+
+
+def _same_device(ctx, *devices):
+    for d in devices:
+        if d != ctx.device:
+            raise TypeError("a tensor is on %s, the context on %s" % (d, ctx.device))
 
 
 def cache_workspace(cache, n):
     """Workspace of ficoco_cache_compact for n sequences."""
     out = C.c_size_t()
-    rc = lib().ficoco_cache_workspace_bytes(C.byref(cache.c), n, C.byref(out))
+    rc = lib().ficoco_cache_workspace_bytes(cache._p, n, C.byref(out))
     if rc != OK:
         raise FicocoError(rc, "ficoco_cache_workspace_bytes rejected the arguments")
-    return Workspace(out.value, cache.k.device)
+    return Workspace(out.value, cache.device)
 
 
 def ficoco_cache_reserve(ctx, cache, start, n_new, seq=None):
     """n_new: tokens of every sequence (int32 tensor), or one number for all."""
-    n = start.numel()
+    n, d = start.numel(), cache.device
+    _same_device(ctx, d)
     each = isinstance(n_new, int)
-    ctx.check(lib().ficoco_cache_reserve(ctx._h, C.byref(cache.c), n, _i32(seq, n, "seq"),
-                                         None if each else _i32(n_new, n, "n_new"), n_new if each else 0,
-                                         _i32(start, n, "start"), ctx.stream()))
+    rc = lib().ficoco_cache_reserve(ctx._h, cache._p, n, _i32(seq, n, "seq", d), 0 if each else _i32(n_new, n, "n_new", d),
+                                    n_new if each else 0, _i32(start, n, "start", d), ctx.raw_stream())
+    if rc:
+        ctx.check(rc)
 
 
-def _tokens(cache, K, V, start, n_new, seq):
+def _tokens(ctx, cache, K, V, start, n_new, seq):
     some = K if K is not None else V
     if some is None:
         raise TypeError("K and V are both None")
     n, heads, n_max, d = some.shape
+    dev = cache.device
     if heads != cache.c.heads or d != cache.c.d_head:
         raise TypeError("tokens are [n][heads][n_max][d_head] of the cache")
+    _same_device(ctx, dev, some.device)
+    at, strides = [], []
     for t in (K, V):
-        if t is not None and (t.shape != some.shape or t.dtype != some.dtype or (t.stride(3) != 1 and t.numel())):
+        if t is None:
+            at.append(0)
+            strides += (0, 0, 0)
+            continue
+        st = t.stride()
+        if t is not some and (t.shape != some.shape or t.dtype != some.dtype or t.device != dev) or st[3] != 1:
             raise TypeError("K and V are of one shape and type, d_head contiguous")
-    p = TokensProblem(n=n, n_max=n_max, dtype=_dtype_code(some))
-    p.seq, p.start, p.n_new = _i32(seq, n, "seq"), _i32(start, n, "start"), _i32(n_new, n, "n_new")
-    if K is not None:
-        p.K, p.k_stride_b, p.k_stride_h, p.k_stride_n = K.data_ptr(), K.stride(0), K.stride(1), K.stride(2)
-    if V is not None:
-        p.V, p.v_stride_b, p.v_stride_h, p.v_stride_n = V.data_ptr(), V.stride(0), V.stride(1), V.stride(2)
-    return p
+        at.append(t.data_ptr())
+        strides += st[:3]
+    return _TOKENS.pack(n, n_max, _dtype_code(some), _i32(seq, n, "seq", dev), _i32(start, n, "start", dev),
+                        _i32(n_new, n, "n_new", dev), *at, *strides)
 
 
 def ficoco_cache_append(ctx, cache, layer, K, V, start, n_new=None, seq=None):
-    t = _tokens(cache, K, V, start, n_new, seq)
-    ctx.check(lib().ficoco_cache_append(ctx._h, C.byref(cache.c), layer, C.byref(t), ctx.stream()))
+    rc = lib().ficoco_cache_append(ctx._h, cache._p, layer, _tokens(ctx, cache, K, V, start, n_new, seq), ctx.raw_stream())
+    if rc:
+        ctx.check(rc)
 
 
 def ficoco_cache_read(ctx, cache, layer, K, V, start=None, n_new=None, seq=None):
     """Into K and V (either may be None)."""
-    t = _tokens(cache, K, V, start, n_new, seq)
-    ctx.check(lib().ficoco_cache_read(ctx._h, C.byref(cache.c), layer, C.byref(t), ctx.stream()))
+    rc = lib().ficoco_cache_read(ctx._h, cache._p, layer, _tokens(ctx, cache, K, V, start, n_new, seq), ctx.raw_stream())
+    if rc:
+        ctx.check(rc)
 
 
 def ficoco_cache_fork(ctx, cache, src, dst, done, whole=False):
-    n = done.numel()
-    ctx.check(lib().ficoco_cache_fork(ctx._h, C.byref(cache.c), n, _i32(src, n, "src"), _i32(dst, n, "dst"), int(whole),
-                                      _i32(done, n, "done"), ctx.stream()))
+    n, d = done.numel(), cache.device
+    _same_device(ctx, d)
+    rc = lib().ficoco_cache_fork(ctx._h, cache._p, n, _i32(src, n, "src", d), _i32(dst, n, "dst", d), int(whole),
+                                 _i32(done, n, "done", d), ctx.raw_stream())
+    if rc:
+        ctx.check(rc)
 
 
 def ficoco_cache_compact(ctx, cache, layer_begin, n_layers, src, dst, vis_begin, N, keep_idx, done, ws):
     """keep_idx [n][n_keep] int32, as the filter of a step leaves it."""
-    n = done.numel()
+    n, d = done.numel(), cache.device
     if keep_idx.dim() != 2 or keep_idx.shape[0] != n:
         raise TypeError("keep_idx must be [n][n_keep]")
-    ctx.check(lib().ficoco_cache_compact(ctx._h, C.byref(cache.c), layer_begin, n_layers, n, _i32(src, n, "src"),
-                                         _i32(dst, n, "dst"), vis_begin, N, keep_idx.shape[1],
-                                         _i32(keep_idx, keep_idx.numel(), "keep_idx"), _i32(done, n, "done"),
-                                         C.c_void_p(ws.ptr), ws.bytes, ctx.stream()))
+    _same_device(ctx, d, ws.device)
+    rc = lib().ficoco_cache_compact(ctx._h, cache._p, layer_begin, n_layers, n, _i32(src, n, "src", d), _i32(dst, n, "dst", d),
+                                    vis_begin, N, keep_idx.shape[1], _i32(keep_idx, keep_idx.numel(), "keep_idx", d),
+                                    _i32(done, n, "done", d), ws.ptr, ws.bytes, ctx.raw_stream())
+    if rc:
+        ctx.check(rc)
 
 
 def ficoco_cache_free(ctx, cache, seq):
     n = seq.numel()
-    ctx.check(lib().ficoco_cache_free(ctx._h, C.byref(cache.c), n, _i32(seq, n, "seq"), ctx.stream()))
+    _same_device(ctx, cache.device)
+    rc = lib().ficoco_cache_free(ctx._h, cache._p, n, _i32(seq, n, "seq", cache.device), ctx.raw_stream())
+    if rc:
+        ctx.check(rc)
 
 
-def _attention(Q, O, scale, window, sinks, q_len, k_len, q_start):
-    B, H, n_q, d = Q.shape
-    if O.shape != Q.shape or Q.dtype != torch.bfloat16 or O.dtype != torch.bfloat16 or \
-            ((Q.stride(3) != 1 or O.stride(3) != 1) and Q.numel()):
-        raise TypeError("Q and O are bfloat16 [B][H][n_q][d_head], d_head contiguous")
-    a = AttentionProblem(B=B, H=H, n_q=n_q, d_head=d, window=window, sinks=sinks)
-    a.Q, a.q_stride_b, a.q_stride_h, a.q_stride_n = Q.data_ptr(), Q.stride(0), Q.stride(1), Q.stride(2)
-    a.O, a.o_stride_b, a.o_stride_h, a.o_stride_n = O.data_ptr(), O.stride(0), O.stride(1), O.stride(2)
-    a.scale = float(d) ** -0.5 if scale is None else scale
-    a.q_len, a.k_len, a.q_start = _i32(q_len, B, "q_len"), _i32(k_len, B, "k_len"), _i32(q_start, B, "q_start")
-    return a
+def _attention(Q, O, K, V, scale, window, sinks, q_len, k_len, q_start, seq, max_len):
+    shape, dev = Q.shape, Q.device
+    B, H, n_q, d = shape
+    q, o = Q.stride(), O.stride()
+    if O.shape != shape or Q.dtype != torch.bfloat16 or O.dtype != torch.bfloat16 or q[3] != 1 or o[3] != 1 or O.device != dev:
+        raise TypeError("Q and O are bfloat16 [B][H][n_q][d_head], d_head contiguous, on one device")
+    if K is None:
+        H_kv = n_k = k_at = v_at = 0
+        k = v = (0, 0, 0, 1)
+    else:
+        k, v = K.stride(), V.stride()
+        if K.shape != V.shape or K.shape[0] != B or K.shape[3] != d or K.dtype != torch.bfloat16 or V.dtype != torch.bfloat16 \
+                or k[3] != 1 or v[3] != 1 or K.device != dev or V.device != dev:
+            raise TypeError("K and V are bfloat16 [B][H_kv][n_k][d_head], d_head contiguous, on the device of Q")
+        H_kv, n_k, k_at, v_at = K.shape[1], K.shape[2], K.data_ptr(), V.data_ptr()
+    return _ATTENTION.pack(B, H, H_kv, n_q, n_k, d, Q.data_ptr(), q[0], q[1], q[2], k_at, v_at, k[0], k[1], k[2], v[0], v[1], v[2],
+                           O.data_ptr(), o[0], o[1], o[2], _i32(seq, B, "seq", dev), _i32(q_len, B, "q_len", dev),
+                           _i32(k_len, B, "k_len", dev), _i32(q_start, B, "q_start", dev),
+                           float(d) ** -0.5 if scale is None else scale, window, sinks, max_len)
 
 
 def attention_workspace(cache, Q, O, window=0, sinks=0, max_len=0):
     """Workspace of ficoco_cache_attention for calls of these shapes."""
-    a = _attention(Q, O, None, window, sinks, None, None, None)
-    a.max_len = max_len
     out = C.c_size_t()
-    rc = lib().ficoco_cache_attention_workspace_bytes(C.byref(cache.c), C.byref(a), C.byref(out))
+    rc = lib().ficoco_cache_attention_workspace_bytes(
+        cache._p, _attention(Q, O, None, None, None, window, sinks, None, None, None, None, max_len), C.byref(out))
     if rc != OK:
         raise FicocoError(rc, "ficoco_cache_attention_workspace_bytes rejected the arguments")
-    return Workspace(out.value, cache.k.device)
+    return Workspace(out.value, cache.device)
 
 
 def ficoco_cache_attention(ctx, cache, layer, Q, O, ws, scale=None, window=0, sinks=0, q_len=None, k_len=None,
                            q_start=None, seq=None, max_len=0):
     """Into O; scale None = d_head ** -0.5."""
-    a = _attention(Q, O, scale, window, sinks, q_len, k_len, q_start)
-    a.seq, a.max_len = _i32(seq, a.B, "seq"), max_len
-    ctx.check(lib().ficoco_cache_attention(ctx._h, C.byref(cache.c), layer, C.byref(a), C.c_void_p(ws.ptr), ws.bytes,
-                                           ctx.stream()))
+    _same_device(ctx, cache.device, Q.device, ws.device)
+    rc = lib().ficoco_cache_attention(ctx._h, cache._p, layer,
+                                      _attention(Q, O, None, None, scale, window, sinks, q_len, k_len, q_start, seq, max_len),
+                                      ws.ptr, ws.bytes, ctx.raw_stream())
+    if rc:
+        ctx.check(rc)
 
 
 def ficoco_window_attention(ctx, Q, K, V, O, scale=None, window=0, sinks=0, q_len=None, k_len=None, q_start=None):
     """Into O; scale None = d_head ** -0.5."""
-    a = _attention(Q, O, scale, window, sinks, q_len, k_len, q_start)
-    if K.shape != V.shape or K.shape[0] != a.B or K.shape[3] != a.d_head or K.dtype != torch.bfloat16 or \
-            V.dtype != torch.bfloat16 or ((K.stride(3) != 1 or V.stride(3) != 1) and K.numel()):
-        raise TypeError("K and V are bfloat16 [B][H_kv][n_k][d_head], d_head contiguous")
-    a.H_kv, a.n_k = K.shape[1], K.shape[2]
-    a.K, a.k_stride_b, a.k_stride_h, a.k_stride_n = K.data_ptr(), K.stride(0), K.stride(1), K.stride(2)
-    a.V, a.v_stride_b, a.v_stride_h, a.v_stride_n = V.data_ptr(), V.stride(0), V.stride(1), V.stride(2)
-    ctx.check(lib().ficoco_window_attention(ctx._h, C.byref(a), ctx.stream()))
+    _same_device(ctx, Q.device)
+    rc = lib().ficoco_window_attention(ctx._h, _attention(Q, O, K, V, scale, window, sinks, q_len, k_len, q_start, None, 0),
+                                       ctx.raw_stream())
+    if rc:
+        ctx.check(rc)

@@ -24,6 +24,10 @@ def test_struct_layouts_match_the_header(tmp_path, name, mirror):
     out = [int(x) for x in subprocess.check_output([str(exe)]).split()]
     assert out[0] == C.sizeof(mirror)
     assert out[1:] == [getattr(mirror, f).offset for f in fields]
+    packed = {"ficoco_tokens": fc._TOKENS, "ficoco_attention": fc._ATTENTION}.get(name)       # (what the binding passes)
+    if packed is not None:
+        values = [float(3 * i + 1) if t is C.c_float else 3 * i + 1 for i, (_, t) in enumerate(mirror._fields_)]
+        assert packed.size == out[0] and packed.pack(*values) == bytes(mirror(*values))
 
 
 def _cache(**kw):
