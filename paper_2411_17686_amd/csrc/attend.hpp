@@ -140,7 +140,7 @@ struct AttendPlan {
 };
 AttendPlan attend_plan(const ficoco_attention& a, int heads, int64_t max_keys, bool paged);
 
-void launch_few_rows(const AttendArgs& a, const AttendPlan& pl, int d_head, hipStream_t s);
+void launch_few_rows(const AttendArgs& a, int d_head, hipStream_t s);
 void launch_page_rows(const AttendArgs& a, int d_head, hipStream_t s);
 void launch_dense_rows(const AttendArgs& a, int d_head, hipStream_t s);
 void launch_join_rows(const AttendArgs& a, int d_head, hipStream_t s);

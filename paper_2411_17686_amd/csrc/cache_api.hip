@@ -248,7 +248,7 @@ int ficoco_cache_attention(ficoco_ctx* ctx, const ficoco_cache* c, int32_t layer
   x.table = c->table; x.len = c->len;
   x.n_pages = c->n_pages; x.n_seqs = c->n_seqs; x.max_pages = c->max_pages;
   x.page_shift = __builtin_ctz((unsigned)c->page_size);
-  if (pl.few) launch_few_rows(x, pl, a->d_head, (hipStream_t)stream);
+  if (pl.few) launch_few_rows(x, a->d_head, (hipStream_t)stream);
   else launch_page_rows(x, a->d_head, (hipStream_t)stream);
   if (pl.splits > 1) launch_join_rows(x, a->d_head, (hipStream_t)stream);
   return finish(ctx, fn);

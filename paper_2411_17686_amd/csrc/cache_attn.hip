@@ -7,14 +7,12 @@
 namespace ficoco {
 namespace {
 
-constexpr int kFewWaves = 4;
+constexpr int kFewWaves = 4, kFewRows = 16;
 constexpr int kFewKeys = 32;                 // keys of a step
 
-// One step's keys and values of a lane as they come out of memory.
-template <int D> struct FewRaw {
-  uint4 k[2][D / 64];
-  uint32_t v[2][4][D / 64];
-};
+// One step's keys, and values, of a lane as they come out of memory.
+template <int D> struct FewKeys { uint4 x[2][D / 64]; };
+template <int D> struct FewValues { uint32_t x[2][4][D / 64]; };
 
 // Four dwords of four keys, each four features, as four dwords of four features, each four keys.
 __device__ __forceinline__ void transpose4(const uint32_t (&a)[4], uint32_t (&t)[4]) {
@@ -35,7 +33,7 @@ __device__ __forceinline__ float quarters_sum(float v) {
   return v + __shfl_xor(v, 32);
 }
 
-// o = sum_j softmax_j(scale q . k_j) v_j for 16 * CT rows, in one pass with a running maximum and sum.  Every wavefront takes steps of
+// o = sum_j softmax_j(scale q . k_j) v_j for 16 rows, in one pass with a running maximum and sum.  Every wavefront takes steps of
 // 32 keys of its own, straight from memory into registers, the next step's loads in flight while one is computed:
 //   S^T[key][row] = K Q^T      operand A a lane's 32 bytes of key lane % 16 (the features of a lane are not in order: Q has them alike)
 //   O^T[feature][row] += V^T P^T   contraction over 32 keys in the order in which a lane holds its logits, so that the weights
@@ -44,13 +42,12 @@ __device__ __forceinline__ float quarters_sum(float v) {
 // exponentials as long as no logit lies more than 2^8 above it.
 //
 // Bound by memory: 2 d_head bytes a token and head.
-template <int D, int CT>
+template <int D>
 __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendArgs a) {
   constexpr int L = D / 64;                  // 16-byte loads of a key
   constexpr int M = D / 16;                  // blocks of 16 features; features of a lane's value load
-  constexpr int R = 16 * CT;
-  __shared__ float so[kFewWaves][R][D + 4];
-  __shared__ float sm[kFewWaves][R], ss[kFewWaves][R];
+  __shared__ float so[kFewWaves][kFewRows][D + 4];
+  __shared__ float sm[kFewWaves][kFewRows], ss[kFewWaves][kFewRows];
   const int lane = threadIdx.x % kWave, wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int c16 = lane % 16, q4 = lane / 16;
   const int split = blockIdx.x % a.splits, bh = blockIdx.x / a.splits, h = bh % a.H_kv, b = bh / a.H_kv;
@@ -63,31 +60,22 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendAr
   per = (per + kFewWaves - 1) / kFewWaves * kFewWaves;
   const int begin = split * per, end = begin + per < blocks.count ? begin + per : blocks.count;
 
-  // queries: row CT * 16 + c16, features 64 l + 16 q4 + 8 u .. + 8
-  bf16x8_t qf[CT][L][2];
-  RowSight sight[CT];
-#pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    int r = ct * 16 + c16;
-    r = r < rows ? r : rows - 1;
-    const int t = r / a.group, g = r % a.group;
-    sight[ct] = RowSight(a, s.first + t, s.keys);
-    const bf16_t* q = a.Q + (int64_t)b * a.q_sb + (int64_t)(h * a.group + g) * a.q_sh + (int64_t)t * a.q_sn;
+  // queries: row c16, features 64 l + 16 q4 + 8 u .. + 8
+  bf16x8_t qf[L][2];
+  const int my_r = c16 < rows ? c16 : rows - 1;
+  const RowSight sight(a, s.first + my_r / a.group, s.keys);
+  {
+    const bf16_t* q = a.Q + (int64_t)b * a.q_sb + (int64_t)(h * a.group + my_r % a.group) * a.q_sh + (int64_t)(my_r / a.group) * a.q_sn;
 #pragma unroll
     for (int l = 0; l < L; ++l) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) __builtin_memcpy(&qf[ct][l][u], q + 64 * l + 16 * q4 + 8 * u, 16);
+      for (int u = 0; u < 2; ++u) __builtin_memcpy(&qf[l][u], q + 64 * l + 16 * q4 + 8 * u, 16);
     }
   }
-  f32x4_t o[CT][M];
-  float top[CT], sum[CT];
+  f32x4_t o[M];
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    top[ct] = kNoLogit;
-    sum[ct] = 0.0f;
-#pragma unroll
-    for (int m = 0; m < M; ++m) o[ct][m] = f32x4_t{0, 0, 0, 0};
-  }
+  for (int m = 0; m < M; ++m) o[m] = f32x4_t{0, 0, 0, 0};
+  float top = kNoLogit, sum = 0.0f;
 
   // Pages and exponents of 32 steps (64 half steps of 16 keys, one a lane): the page or -1, and both bytes.
   struct Meta { int page, exps; };
@@ -107,29 +95,35 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendAr
   const int steps = begin + wv < end ? (end - begin - wv + kFewWaves - 1) / kFewWaves : 0;
   Meta now = meta_of(0), next = steps > 32 ? meta_of(1) : Meta{-1, 0};
   const int page_bytes = D << a.page_shift;
-  auto load = [&](FewRaw<D>& raw, int step, const Meta& m) {
-    const int key0 = blocks.block(begin + wv + step * kFewWaves) * kFewKeys;
+  auto block_at = [&](int step, const Meta& m, int u) {           // bytes to half step u's first key
+    const int key = blocks.block(begin + wv + step * kFewWaves) * kFewKeys + 16 * u, p = __builtin_amdgcn_readlane(m.page, (step & 31) * 2 + u);
+    return ((int64_t)(p < 0 ? 0 : p) * a.H_kv + h) * page_bytes + (key & ((1 << a.page_shift) - 1)) * D;
+  };
+  auto load_keys = [&](FewKeys<D>& raw, int step, const Meta& m) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int p = __builtin_amdgcn_readlane(m.page, (step & 31) * 2 + u);
-      const int64_t at = ((int64_t)(p < 0 ? 0 : p) * a.H_kv + h) * page_bytes + ((key0 + 16 * u) & ((1 << a.page_shift) - 1)) * D;
-      const uint8_t* k = a.k + at;
-      const uint8_t* v = a.v + at;
+      const uint8_t* k = a.k + block_at(step, m, u);
 #pragma unroll
-      for (int l = 0; l < L; ++l) raw.k[u][l] = *(const uint4*)(k + (c16 * D + 16 * q4) + 64 * l);
+      for (int l = 0; l < L; ++l) raw.x[u][l] = *(const uint4*)(k + (c16 * D + 16 * q4) + 64 * l);
+    }
+  };
+  auto load_values = [&](FewValues<D>& raw, int step, const Meta& m) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint8_t* v = a.v + block_at(step, m, u);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if constexpr (L == 2) {
           const uint2 x = *(const uint2*)(v + (4 * q4 * D + c16 * M) + i * D);
-          raw.v[u][i][0] = x.x;
-          raw.v[u][i][1] = x.y;
+          raw.x[u][i][0] = x.x;
+          raw.x[u][i][1] = x.y;
         } else {
-          raw.v[u][i][0] = *(const uint32_t*)(v + (4 * q4 * D + c16 * M) + i * D);
+          raw.x[u][i][0] = *(const uint32_t*)(v + (4 * q4 * D + c16 * M) + i * D);
         }
       }
     }
   };
-  auto compute = [&](FewRaw<D>& raw, int step, const Meta& m) {
+  auto compute = [&](const FewKeys<D>& keys, FewValues<D>& values, int step, const Meta& m) {
     const int key0 = blocks.block(begin + wv + step * kFewWaves) * kFewKeys;
     float ks[2], vs[2];
     bool there = true, have[2];
@@ -141,95 +135,87 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendAr
       ks[u] = exp_scale(e & 255);
       vs[u] = exp_scale(e >> 8);
     }
-    f32x4_t S[CT][2];
+    f32x4_t S[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
 #pragma unroll
       for (int l = 0; l < L; ++l) {
-        const uint32_t w[4] = {raw.k[u][l].x, raw.k[u][l].y, raw.k[u][l].z, raw.k[u][l].w};
+        const uint32_t w[4] = {keys.x[u][l].x, keys.x[u][l].y, keys.x[u][l].z, keys.x[u][l].w};
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           const uint2 x = widen_e4m3(w[2 * half], ks[u]), y = widen_e4m3(w[2 * half + 1], ks[u]);
-          const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, uint4{x.x, x.y, y.x, y.y});
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct)
-            S[ct][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[ct][l][half], l + half == 0 ? f32x4_t{0, 0, 0, 0} : S[ct][u], 0, 0, 0);
+          S[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, uint4{x.x, x.y, y.x, y.y}), qf[l][half], l + half == 0 ? f32x4_t{0, 0, 0, 0} : S[u], 0, 0, 0);
         }
       }
+      __builtin_amdgcn_sched_barrier(0);                  // (here and below: or the compiler runs ahead, and out of registers)
     }
     products_settle();
     const int last = key0 + kFewKeys - 1, lo = s.first, hi = s.first + s.queries - 1;
     const bool all_seen = there && last < s.keys && last <= lo && (a.window <= 0 || (int64_t)key0 > (int64_t)hi - a.window || last < a.sinks);
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u) S[ct][u] *= a.scale_log2e;
-    }
+    S[0] *= a.scale_log2e;
+    S[1] *= a.scale_log2e;
     if (!all_seen) {                                      // (uniform)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int key = key0 + 16 * u + 4 * q4 + i;
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct) S[ct][u][i] = have[u] && (sight[ct].sees(key) || key < sight[ct].first) ? S[ct][u][i] : -__builtin_huge_valf();
+          const bool seen = have[u] & (sight.sees(key) | (key < sight.first));
+          S[u][i] = seen ? S[u][i] : -__builtin_huge_valf();
           // what no row sees may hold anything, and 0 * NaN is NaN
-          if (!have[u] || key >= blocks.end || (key < blocks.near_key && key >= blocks.first_keys)) {
+          const bool some = have[u] & (key < blocks.end) & ((key >= blocks.near_key) | (key < blocks.first_keys));
 #pragma unroll
-            for (int l = 0; l < L; ++l) raw.v[u][i][l] = 0;
-          }
+          for (int l = 0; l < L; ++l) values.x[u][i][l] = some ? values.x[u][i][l] : 0u;
         }
       }
     }
-    bf16x8_t P[CT];
+    const float t = fmaxf(max3(S[0][0], S[0][1], S[0][2]), max3(S[0][3], max3(S[1][0], S[1][1], S[1][2]), S[1][3]));
+    if (__any(t > top + kSlack)) {
+      const float m = fmaxf(top, quarters_max(t)), f = __builtin_amdgcn_exp2f(top - m);
+      top = m;
+      sum *= f;
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-      float t = fmaxf(fmaxf(S[ct][0][0], S[ct][0][1]), fmaxf(S[ct][0][2], S[ct][0][3]));
-      t = fmaxf(t, fmaxf(fmaxf(S[ct][1][0], S[ct][1][1]), fmaxf(S[ct][1][2], S[ct][1][3])));
-      if (__any(t > top[ct] + kSlack)) {
-        const float m = fmaxf(top[ct], quarters_max(t)), f = __builtin_amdgcn_exp2f(top[ct] - m);
-        top[ct] = m;
-        sum[ct] *= f;
-#pragma unroll
-        for (int i = 0; i < M; ++i) o[ct][i] *= f;
-      }
-      float p[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(S[ct][i / 4][i % 4] - top[ct]);
-        sum[ct] += p[i];
-      }
-      P[ct] = __builtin_bit_cast(bf16x8_t, uint4{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])});
+      for (int i = 0; i < M; ++i) o[i] *= f;
     }
+    float p[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(S[i / 4][i % 4] - top);
+      sum += p[i];
+    }
+    const bf16x8_t P = __builtin_bit_cast(bf16x8_t, uint4{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])});
 #pragma unroll
     for (int w = 0; w < M / 4; ++w) {                     // four features of the lane at a time
       uint32_t t[2][4];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const uint32_t x[4] = {raw.v[u][0][w], raw.v[u][1][w], raw.v[u][2][w], raw.v[u][3][w]};
+        const uint32_t x[4] = {values.x[u][0][w], values.x[u][1][w], values.x[u][2][w], values.x[u][3][w]};
         transpose4(x, t[u]);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const uint2 x = widen_e4m3(t[0][i], vs[0]), y = widen_e4m3(t[1][i], vs[1]);
-        const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, uint4{x.x, x.y, y.x, y.y});
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) o[ct][4 * w + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, P[ct], o[ct][4 * w + i], 0, 0, 0);
+        o[4 * w + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, uint4{x.x, x.y, y.x, y.y}), P, o[4 * w + i], 0, 0, 0);
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
     products_settle();
   };
 
-  FewRaw<D> r0, r1;
-  if (steps > 0) load(r0, 0, now);
+  // A step's values and the next step's keys are on their way while its logits are formed, the next step's keys beyond that.
+  FewKeys<D> k0, k1;
+  FewValues<D> values;
+  if (steps > 0) load_keys(k0, 0, now);
   for (int i = 0; i < steps; i += 2) {
     // (a chunk is 32 steps: an even step and the next one are of the same chunk)
-    if (i + 1 < steps) load(r1, i + 1, now);
-    compute(r0, i, now);
+    load_values(values, i, now);
+    if (i + 1 < steps) load_keys(k1, i + 1, now);
+    compute(k0, values, i, now);
     if (i + 1 >= steps) break;
+    load_values(values, i + 1, now);
     const bool turn = ((i + 2) & 31) == 0;
-    if (i + 2 < steps) load(r0, i + 2, turn ? next : now);
-    compute(r1, i + 1, now);
+    if (i + 2 < steps) load_keys(k0, i + 2, turn ? next : now);
+    compute(k1, values, i + 1, now);
     if (turn) {
       now = next;
       if (i + 34 < steps) next = meta_of((i + 34) / 32);
@@ -237,22 +223,18 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendAr
   }
 
   // the wavefronts' parts
+  const float total_here = quarters_sum(sum);
+  if (q4 == 0) {
+    sm[wv][c16] = top;
+    ss[wv][c16] = total_here;
+  }
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    const int r = ct * 16 + c16;
-    const float total = quarters_sum(sum[ct]);
-    if (q4 == 0) {
-      sm[wv][r] = top[ct];
-      ss[wv][r] = total;
-    }
+  for (int m = 0; m < M; ++m) {
 #pragma unroll
-    for (int m = 0; m < M; ++m) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) so[wv][r][(4 * q4 + i) * M + m] = o[ct][m][i];
-    }
+    for (int i = 0; i < 4; ++i) so[wv][c16][(4 * q4 + i) * M + m] = o[m][i];
   }
   __syncthreads();
-  for (int j = threadIdx.x; j < R * D / 8; j += kFewWaves * kWave) {
+  for (int j = threadIdx.x; j < kFewRows * D / 8; j += kFewWaves * kWave) {
     const int r = j / (D / 8), d = j % (D / 8) * 8;
     if (r >= rows) continue;
     float m = sm[0][r];
@@ -314,8 +296,8 @@ __global__ __launch_bounds__(4 * kWave) void join_rows_kernel(AttendArgs a) {
 AttendPlan attend_plan(const ficoco_attention& a, int heads, int64_t max_keys, bool paged) {
   AttendPlan pl{};
   const int64_t rows = (int64_t)a.n_q * (a.H / heads), bh = (int64_t)a.B * heads;
-  pl.few = paged && rows <= 16;
-  pl.rows = pl.few ? 16 : kTileRows;
+  pl.few = paged && rows <= kFewRows;
+  pl.rows = pl.few ? kFewRows : kTileRows;
   pl.row_tiles = (int)std::max<int64_t>(1, (rows + pl.rows - 1) / pl.rows);
   pl.splits = 1;
   if (paged && bh > 0) {
@@ -332,15 +314,10 @@ AttendPlan attend_plan(const ficoco_attention& a, int heads, int64_t max_keys, b
   return pl;
 }
 
-void launch_few_rows(const AttendArgs& a, const AttendPlan& pl, int d_head, hipStream_t s) {
+void launch_few_rows(const AttendArgs& a, int d_head, hipStream_t s) {
   const dim3 grid((unsigned)((int64_t)a.B * a.H_kv * a.splits)), threads(kFewWaves * kWave);
-  if (d_head == 128) {
-    if (pl.rows <= 16) hipLaunchKernelGGL((few_rows_kernel<128, 1>), grid, threads, 0, s, a);
-    else hipLaunchKernelGGL((few_rows_kernel<128, 2>), grid, threads, 0, s, a);
-  } else {
-    if (pl.rows <= 16) hipLaunchKernelGGL((few_rows_kernel<64, 1>), grid, threads, 0, s, a);
-    else hipLaunchKernelGGL((few_rows_kernel<64, 2>), grid, threads, 0, s, a);
-  }
+  if (d_head == 128) hipLaunchKernelGGL(few_rows_kernel<128>, grid, threads, 0, s, a);
+  else hipLaunchKernelGGL(few_rows_kernel<64>, grid, threads, 0, s, a);
 }
 
 void launch_join_rows(const AttendArgs& a, int d_head, hipStream_t s) {

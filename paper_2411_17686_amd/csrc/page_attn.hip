@@ -154,7 +154,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void page_rows_kernel(AttendArgs a
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int key = key0 + kb * 32 + i / 4 * 8 + i % 4;
-        S[kb][i] = (sight.sees(key) || (firsts && key < sight.first)) && !(e[2 * kb + i / 8] & kHole) ? S[kb][i] : -__builtin_huge_valf();
+        const bool seen = (sight.sees(key) | (firsts & (key < sight.first))) & !(e[2 * kb + i / 8] & kHole);
+        S[kb][i] = seen ? S[kb][i] : -__builtin_huge_valf();
       }
     }
     return largest(S);

@@ -155,7 +155,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) S[kb][i] = sight.sees(key0 + kb * 32 + i / 4 * 8 + i % 4) || (firsts && key0 + kb * 32 + i / 4 * 8 + i % 4 < sight.first) ? S[kb][i] : -__builtin_huge_valf();
+      for (int i = 0; i < 16; ++i) S[kb][i] = sight.sees(key0 + kb * 32 + i / 4 * 8 + i % 4) | (firsts & (key0 + kb * 32 + i / 4 * 8 + i % 4 < sight.first)) ? S[kb][i] : -__builtin_huge_valf();
     }
     return largest(S);
   };
