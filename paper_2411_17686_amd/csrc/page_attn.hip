@@ -173,7 +173,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void page_rows_kernel(AttendArgs a
   auto advance = [&](f32x16_t (&S)[2], f32x16_t (&next)[2], const uint8_t* kn, const uint8_t* v, uint8_t* kl, uint8_t* vl, int i) __attribute__((always_inline)) {
     constexpr int NA = 2 * KS, NB = 4 * DT;        // products of either kind
     constexpr int AHEAD = 4;                       // value operands on their way out of LDS; keys: half as many, for two products each
-    constexpr int EA = 24;                         // weights formed beside the first kind; the other 8 beside the second
+    // Weights: logit, exponential and sum three places apart, so that none waits for the one before; `place` p takes logit p + 3, exponential p and sum
+    // p - 3.  The first places beside the first kind of product (three operands of the second kind are then there), the others beside the second.
+    constexpr int PLACES = 35, PA = 28;
     const bool turn = (i - begin) % kChunk == 0 && i + kChunk < end;
     int2 m2 = {-1, 0};
     if (turn) m2 = look_up((i - begin) / kChunk + 1);
@@ -183,15 +185,19 @@ __global__ __launch_bounds__(kTileThreads, 2) void page_rows_kernel(AttendArgs a
     uint4 kr[AHEAD / 2];
     uint2 vr[AHEAD];
     bf16x8_t P[4];
-    float w[32];
+    float x[32], w[32];
     auto read_k = [&](int p) { kr[p % (AHEAD / 2)] = *(const uint4*)(kn + p / DT * 32 * D + k_at[p % DT]); };
     auto read_v = [&](int n) { vr[n % AHEAD] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2_t)(v + 16 * (n / DT) * D + v_at[n % DT]))); };
-    auto weight = [&](int e) {
-      w[e] = __builtin_amdgcn_exp2f(fmaf(S[e / 16][e % 16], a.scale_log2e, -top));
-      sum += w[e];
-      if (e % 8 == 7)
+    auto place = [&](int p) {
+      if (p + 3 < 32) x[p + 3] = fmaf(S[(p + 3) / 16][(p + 3) % 16], a.scale_log2e, -top);
+      if (p < 32) w[p] = __builtin_amdgcn_exp2f(x[p]);
+      const int e = p - 3;
+      if (e >= 0) sum += w[e];
+      if (e >= 0 && e % 8 == 7)
         P[e / 8] = __builtin_bit_cast(bf16x8_t, uint4{pack_bf16(w[e - 7], w[e - 6]), pack_bf16(w[e - 5], w[e - 4]), pack_bf16(w[e - 3], w[e - 2]), pack_bf16(w[e - 1], w[e])});
     };
+#pragma unroll
+    for (int e = 0; e < 3; ++e) x[e] = fmaf(S[0][e], a.scale_log2e, -top);
 #pragma unroll
     for (int p = 0; p < AHEAD / 2; ++p) read_k(p);
     const float ks[2] = {key_scale(e_next, 0), key_scale(e_next, 1)};
@@ -203,7 +209,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void page_rows_kernel(AttendArgs a
       if (n % 2 == 1 && n / 2 + AHEAD / 2 < NA / 2) read_k(n / 2 + AHEAD / 2);
       if (n >= NA - AHEAD) read_v(n - (NA - AHEAD));
 #pragma unroll
-      for (int e = n * EA / NA; e < (n + 1) * EA / NA; ++e) weight(e);
+      for (int p = n * PA / NA; p < (n + 1) * PA / NA; ++p) place(p);
     }
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
@@ -213,7 +219,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void page_rows_kernel(AttendArgs a
       o[n % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, uint4{x.x, x.y, y.x, y.y}), P[n / DT], o[n % DT], 0, 0, 0);
       if (n + AHEAD < NB) read_v(n + AHEAD);
 #pragma unroll
-      for (int e = EA + n * 8 * 2 / NB; e < EA + (n + 1) * 8 * 2 / NB && e < 32; ++e) weight(e);
+      for (int p = PA + n * 16 / NB; p < PA + (n + 1) * 16 / NB && p < PLACES; ++p) place(p);
     }
     products_settle();
     if (i + 1 < end) raise((all_seen(e_next, i + 1) ? largest(next) : mask(next, e_next, i + 1)) * a.scale_log2e);

@@ -63,29 +63,28 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
 
   auto wanted = [&](int key) { return key < blocks.end && (key >= blocks.near_key || key < blocks.first_keys); };
 
-  // ---- straight into LDS: a wavefront's load fills 64 chunks in a row.  Rows that no query of the workgroup sees are replaced by one
-  // of the block that is seen: their weights are zero, and zero times what memory happens to hold may be NaN.
+  // ---- straight into LDS: a wavefront's load fills 64 chunks in a row.  Rows that no query of the workgroup sees become zeros (places
+  // behind the end of their buffer): their weights are zero, and zero times what memory happens to hold may be NaN.
   // (Buffer loads: behind a global load into LDS the compiler waits for all reads of LDS at once.)
   const int d_row = 64 / CH * wv + lane / CH;                                   // rows of load j: d_row + RJ * j
   constexpr int RJ = 64 * kTileWaves / CH;
-  auto direct = [&](const bf16_t* base, int64_t sn, bf16_t* to, int swizzle, int step) {
-    if (step >= end) return;
-    const int key0 = blocks.block(step) * kTileKeys, row_bytes = (int)sn * 2;    // (64 rows lie within 2^30 bytes: launch_dense_rows)
-    const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)(base + (int64_t)key0 * sn), 0, 0x7fffffff, 0x00027000);
-    const int ch = (lane % CH ^ swizzle) * 16;
-    const bool whole = key0 + kTileKeys <= blocks.end && (key0 >= blocks.near_key || key0 + kTileKeys <= blocks.first_keys);
-    auto one = [&](int j, int at, int add) {
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + (j * kTileWaves + wv) * 64 * 8), 16, at, add, 0, 0);
-    };
-    if (whole) {
+  auto rows_at = [&](const bf16_t* base, int64_t sn, int step) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)(base + (int64_t)blocks.block(step) * kTileKeys * sn), 0, step < end ? 0x7fffffff : 0, 0x00027000);
+  };
+  auto hidden_rows = [&](int step) {               // bit j: the row of load j is hidden
+    const int key0 = blocks.block(step) * kTileKeys;
+    int hidden = 0;
+    if (!(key0 + kTileKeys <= blocks.end && (key0 >= blocks.near_key || key0 + kTileKeys <= blocks.first_keys))) {
 #pragma unroll
-      for (int j = 0; j < NL; ++j) one(j, d_row * row_bytes + ch, RJ * j * row_bytes);
-    } else {
-      const int behind = step < blocks.head ? blocks.first_keys : blocks.end;
-      const int seen = (behind < key0 + kTileKeys ? behind - key0 : kTileKeys) - 1;
-#pragma unroll
-      for (int j = 0; j < NL; ++j) one(j, (wanted(key0 + d_row + RJ * j) ? d_row + RJ * j : seen) * row_bytes + ch, 0);
+      for (int j = 0; j < NL; ++j) hidden |= (wanted(key0 + d_row + RJ * j) ? 0 : 1) << j;
     }
+    return hidden;
+  };
+  const int k_bytes = (int)a.k_sn * 2, v_bytes = (int)a.v_sn * 2;               // (64 rows lie within 2^30 bytes: launch_dense_rows)
+  const int k_off = d_row * k_bytes + (lane % CH ^ key_swizzle<D>(d_row)) * 16, v_off = d_row * v_bytes + (lane % CH ^ value_swizzle<D>(d_row)) * 16;
+  auto direct = [&](__amdgpu_buffer_rsrc_t from, int hidden, bf16_t* to, int off, int row_bytes, int j) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + (j * kTileWaves + wv) * 64 * 8), 16,
+                                             off + (int)((uint32_t)hidden << (31 - j) & 0x80000000u), RJ * j * row_bytes, 0, 0);
   };
 
   // ---- through registers
@@ -104,12 +103,21 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
     if constexpr (SRC == kDense) {
       load_dense(raw, Kb, a.k_sn, step);
     } else {
-      direct(Kb, a.k_sn, to, key_swizzle<D>(d_row), step);
+      const __amdgpu_buffer_rsrc_t from = rows_at(Kb, a.k_sn, step);
+      const int hidden = hidden_rows(step);
+#pragma unroll
+      for (int j = 0; j < NL; ++j) direct(from, hidden, to, k_off, k_bytes, j);
     }
   };
   auto load_v = [&](TileRaw<D>& raw, bf16_t* to, int step) {
-    if constexpr (SRC == kDense) load_dense(raw, Vb, a.v_sn, step);
-    else direct(Vb, a.v_sn, to, value_swizzle<D>(d_row), step);
+    if constexpr (SRC == kDense) {
+      load_dense(raw, Vb, a.v_sn, step);
+    } else {
+      const __amdgpu_buffer_rsrc_t from = rows_at(Vb, a.v_sn, step);
+      const int hidden = hidden_rows(step);
+#pragma unroll
+      for (int j = 0; j < NL; ++j) direct(from, hidden, to, v_off, v_bytes, j);
+    }
   };
   auto store = [&](const TileRaw<D>& raw, bf16_t* to, bool keys) {
     if constexpr (SRC != kDenseDirect) {
@@ -138,9 +146,12 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
       }
     }
   };
-  auto all_seen = [&](int step) {                  // every key of a step by every row of the wavefront
+  // Every key of a step by every row of the wavefront: keys up to seen_to, from seen_from on or among the first ones.
+  const int seen_to = __builtin_amdgcn_readfirstlane(lo < s.keys ? lo : s.keys - 1);
+  const int seen_from = __builtin_amdgcn_readfirstlane(a.window > 0 && hi >= a.window ? hi - a.window + 1 : 0);
+  auto all_seen = [&](int step) {
     const int key0 = blocks.block(step) * kTileKeys, last = key0 + kTileKeys - 1;
-    return last < s.keys && last <= lo && (a.window <= 0 || (int64_t)key0 > (int64_t)hi - a.window || last < a.sinks);
+    return last <= seen_to && (key0 >= seen_from || last < a.sinks);
   };
   auto largest = [&](const f32x16_t (&S)[2]) {
     float m = fmaxf(S[0][0], S[1][0]);
@@ -170,35 +181,40 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
     }
   };
   const int v_row = 4 * half + lane % 16 / 4, v_swizzle = value_swizzle<D>(v_row);       // (of rows 8 and 16 further on too)
-  int k_at[KS], v_at[DT];                          // a lane's places in a row of keys, and of values
-#pragma unroll
-  for (int k = 0; k < KS; ++k) k_at[k] = c32 * D + (2 * k + half ^ k_swizzle) * 8;
-#pragma unroll
-  for (int i = 0; i < DT; ++i) v_at[i] = v_row * D + (4 * i + lane / 16 % 2 * 2 + lane % 4 / 2 ^ v_swizzle) * 8 + lane % 4 % 2 * 4;
+  // a lane's places: chunk 2 k + half of key c32, and the four features from 32 i on of its first key (the swizzle is an exclusive or too)
+  const int k_at = c32 * D + (half ^ k_swizzle) * 8, v_at = v_row * D + (lane / 16 % 2 * 2 + lane % 4 / 2 ^ v_swizzle) * 8 + lane % 4 % 2 * 4;
 
   TileRaw<D> raw;
   // (ka, va: of this step;  kb, vb: of the next one)
   auto advance = [&](f32x16_t (&S)[2], f32x16_t (&next)[2], bf16_t* ka, bf16_t* kb, bf16_t* va, bf16_t* vb, int i) __attribute__((always_inline)) {
     constexpr int NA = 2 * KS, NB = 4 * DT;        // products of either kind
     constexpr int AHEAD = 4;                       // operands on their way out of LDS
-    constexpr int EA = 24;                         // weights formed beside the first kind; the other 8 beside the second
-    load_v(raw, vb, i + 1);
-    if constexpr (SRC == kDenseDirect) load_k(raw, ka, i + 2);
+    // Weights: logit, exponential and sum three places apart, so that none waits for the one before; `place` p takes logit p + 3, exponential p and sum
+    // p - 3.  The first places beside the first kind of product (three operands of the second kind are then there), the others beside the second.
+    constexpr int PLACES = 35, PA = 28;
+    // Direct loads go one by one between the products: all at once they hold up the reads of LDS.
+    const __amdgpu_buffer_rsrc_t next_k = rows_at(Kb, a.k_sn, i + 2), next_v = rows_at(Vb, a.v_sn, i + 1);
+    const int hidden_k = hidden_rows(i + 2), hidden_v = hidden_rows(i + 1);
+    if constexpr (SRC == kDense) load_v(raw, vb, i + 1);
     bf16x8_t kf[AHEAD], vf[AHEAD], P[4];
-    float w[32];
-    auto read_k = [&](int g) { kf[g % AHEAD] = *(const bf16x8_t*)(kb + g / KS * 32 * D + k_at[g % KS]); };
+    float x[32], w[32];
+    auto read_k = [&](int g) { kf[g % AHEAD] = *(const bf16x8_t*)(kb + g / KS * 32 * D + (k_at ^ g % KS * 16)); };
     auto read_v = [&](int g) {
-      const bf16_t* v = va + 16 * (g / DT) * D + v_at[g % DT];
+      const bf16_t* v = va + 16 * (g / DT) * D + (v_at ^ g % DT * 32);
       const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t)v));
       const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t)(v + 8 * D)));
       vf[g % AHEAD] = __builtin_bit_cast(bf16x8_t, uint4{x.x, x.y, y.x, y.y});
     };
-    auto weight = [&](int e) {
-      w[e] = __builtin_amdgcn_exp2f(fmaf(S[e / 16][e % 16], a.scale_log2e, -top));
-      sum += w[e];
-      if (e % 8 == 7)
+    auto place = [&](int p) {
+      if (p + 3 < 32) x[p + 3] = fmaf(S[(p + 3) / 16][(p + 3) % 16], a.scale_log2e, -top);
+      if (p < 32) w[p] = __builtin_amdgcn_exp2f(x[p]);
+      const int e = p - 3;
+      if (e >= 0) sum += w[e];
+      if (e >= 0 && e % 8 == 7)
         P[e / 8] = __builtin_bit_cast(bf16x8_t, uint4{pack_bf16(w[e - 7], w[e - 6]), pack_bf16(w[e - 5], w[e - 4]), pack_bf16(w[e - 3], w[e - 2]), pack_bf16(w[e - 1], w[e])});
     };
+#pragma unroll
+    for (int e = 0; e < 3; ++e) x[e] = fmaf(S[0][e], a.scale_log2e, -top);
 #pragma unroll
     for (int g = 0; g < AHEAD; ++g) read_k(g);
 #pragma unroll
@@ -207,8 +223,12 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
       next[g / KS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[g % AHEAD], qf[g % KS], g % KS == 0 ? f32x16_t{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0} : next[g / KS], 0, 0, 0);
       if (g + AHEAD < NA) read_k(g + AHEAD);
       else if constexpr (SRC == kDenseDirect) read_v(g + AHEAD - NA);
+      if constexpr (SRC == kDenseDirect) {
+        if (g % 2 == 1 && g / 2 < NL) direct(next_k, hidden_k, ka, k_off, k_bytes, g / 2);
+        else if (g % 2 == 1) direct(next_v, hidden_v, vb, v_off, v_bytes, g / 2 - NL);
+      }
 #pragma unroll
-      for (int e = g * EA / NA; e < (g + 1) * EA / NA; ++e) weight(e);
+      for (int p = g * PA / NA; p < (g + 1) * PA / NA; ++p) place(p);
     }
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (SRC != kDenseDirect) {
@@ -224,7 +244,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
       o[g % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[g % AHEAD], P[g / DT], o[g % DT], 0, 0, 0);
       if (g + AHEAD < NB) read_v(g + AHEAD);
 #pragma unroll
-      for (int e = EA + g * 8 * 2 / NB; e < EA + (g + 1) * 8 * 2 / NB && e < 32; ++e) weight(e);
+      for (int p = PA + g * 16 / NB; p < PA + (g + 1) * 16 / NB && p < PLACES; ++p) place(p);
       if (g >= NB / 2) {
 #pragma unroll
         for (int e = (g - NB / 2) * 32 / NB; e < (g + 1 - NB / 2) * 32 / NB; ++e) m[e % 2] = max3(m[e % 2], next[e / 8][e % 8 * 2], next[e / 8][e % 8 * 2 + 1]);
