@@ -10,6 +10,21 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
+// n / d without a division: m = floor(2^(31 + l) / d) + 1 with 2^l >= d, and n m / 2^(31 + l) is above n / d by less than 1 / d for n < 2^31.
+struct Divisor {
+  uint32_t d, m, s;
+  Divisor() = default;
+  explicit Divisor(int64_t by) : d((uint32_t)by), m(0), s(0) {
+    int l = 0;
+    while ((int64_t)1 << l < by) ++l;
+    if (l > 0) {
+      m = (uint32_t)(((uint64_t)1 << (31 + l)) / (uint64_t)by + 1);
+      s = (uint32_t)(l - 1);
+    }
+  }
+  __device__ __forceinline__ int of(int n) const { return d == 1 ? n : (int)(__umulhi((uint32_t)n, m) >> s); }
+};
+
 // A key / value head serves `group` query heads; their rows are taken together, row r = query r / group of head
 // r % group, so that a block's keys are read once for all of them.
 struct AttendArgs {
@@ -19,6 +34,7 @@ struct AttendArgs {
   int64_t o_sb, o_sh, o_sn;
   const int32_t *seq, *q_len, *k_len, *q_start;
   int B, H_kv, group, n_q, n_k, splits, row_tiles;
+  Divisor by_heads, by_group, by_splits, by_tiles;     // H_kv, group, splits, row_tiles * splits
   float scale_log2e;
   int window, sinks;
   // pages of the layer
@@ -121,6 +137,51 @@ constexpr float kSlack = 8.0f;               // (units of log2) growth of a row'
 // (fmaxf() would first bring either argument into canonical form, an instruction more for each)
 __device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
 __device__ __forceinline__ float halves_max(float v) { return fmaxf(v, __shfl_xor(v, 32)); }
+
+// The 32 rows of a wavefront, out of the lanes that hold them (a row in two lanes, four features at a time) through 64 * D bytes of
+// LDS of its own, so that lanes next to each other store 16 bytes next to each other: with 8 bytes a lane and two lanes a row the
+// stores of a workgroup took 1.6 us.  to(row, piece): where piece (16 bytes) of row 0 .. 31 goes, null for nowhere.
+template <int D, typename F>
+__device__ __forceinline__ void rows_out(const f32x16_t (&o)[D / 32], float inv, uint8_t* lds, F to) {
+  constexpr int CH = D / 8;
+  const int lane = threadIdx.x % kWave, row = lane % 32, half = lane / 32;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *(uint2*)(lds + row * 2 * D + ((4 * i + j) ^ (row & (CH - 1))) * 16 + half * 8) =
+          uint2{pack_bf16(o[i][4 * j] * inv, o[i][4 * j + 1] * inv), pack_bf16(o[i][4 * j + 2] * inv, o[i][4 * j + 3] * inv)};
+  }
+#pragma unroll
+  for (int k = 0; k < CH / 2; ++k) {
+    const int r = (k * kWave + lane) / CH, c = lane % CH;
+    const uint4 x = *(const uint4*)(lds + r * 2 * D + (c ^ (r & (CH - 1))) * 16);
+    if (void* p = to(r, c)) __builtin_memcpy(p, &x, 16);
+  }
+}
+// The same in single precision, half of the features at a time; pieces 0 .. D / 4 - 1.
+template <int D, typename F>
+__device__ __forceinline__ void float_rows_out(const f32x16_t (&o)[D / 32], uint8_t* lds, F to) {
+  constexpr int CH = D / 8, DH = D / 64;
+  const int lane = threadIdx.x % kWave, row = lane % 32, half = lane / 32;
+#pragma unroll
+  for (int part = 0; part < 2; ++part) {
+#pragma unroll
+    for (int i = 0; i < DH; ++i) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x16_t& x = o[part * DH + i];
+        *(f32x4_t*)(lds + row * 2 * D + ((8 * i + 2 * j + half) ^ (row & (CH - 1))) * 16) = f32x4_t{x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]};
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < CH / 2; ++k) {
+      const int r = (k * kWave + lane) / CH, c = lane % CH;
+      const uint4 x = *(const uint4*)(lds + r * 2 * D + (c ^ (r & (CH - 1))) * 16);
+      if (void* p = to(r, part * CH + c)) __builtin_memcpy(p, &x, 16);
+    }
+  }
+}
 
 // Between products and a branch behind which their results are read.  A result may be read a number of instructions after the product
 // at the earliest; the compiler keeps to that inside a block, but not everywhere across a branch (seen with ROCm 7.2: copies

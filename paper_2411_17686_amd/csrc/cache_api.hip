@@ -119,6 +119,7 @@ AttendArgs arguments(const ficoco_attention& a, int heads, const AttendPlan& pl,
   x.o_sb = a.o_stride_b; x.o_sh = a.o_stride_h; x.o_sn = a.o_stride_n;
   x.seq = a.seq; x.q_len = a.q_len; x.k_len = a.k_len; x.q_start = a.q_start;
   x.B = a.B; x.H_kv = heads; x.group = a.H / heads; x.n_q = a.n_q; x.n_k = a.n_k;
+  x.by_heads = Divisor(heads); x.by_group = Divisor(a.H / heads); x.by_splits = Divisor(pl.splits); x.by_tiles = Divisor((int64_t)pl.row_tiles * pl.splits);
   x.splits = pl.splits; x.row_tiles = pl.row_tiles; x.part_rows = pl.row_tiles * pl.rows;
   x.scale_log2e = a.scale * 1.44269504088896340736f;
   x.window = a.window; x.sinks = a.sinks;

@@ -50,22 +50,23 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendAr
   __shared__ float sm[kFewWaves][kFewRows], ss[kFewWaves][kFewRows];
   const int lane = threadIdx.x % kWave, wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int c16 = lane % 16, q4 = lane / 16;
-  const int split = blockIdx.x % a.splits, bh = blockIdx.x / a.splits, h = bh % a.H_kv, b = bh / a.H_kv;
+  const int bh = a.by_splits.of(blockIdx.x), split = blockIdx.x - bh * a.splits, b = a.by_heads.of(bh), h = bh - b * a.H_kv;
   int slot;
   const Sight s = sight_of<true>(a, b, slot);
   if (s.queries <= 0) return;
   const int rows = s.queries * a.group;
   const Blocks<kFewKeys> blocks(a, s, s.first, s.first + s.queries - 1);
-  int per = (blocks.count + a.splits - 1) / a.splits;
+  int per = a.by_splits.of(blocks.count + a.splits - 1);
   per = (per + kFewWaves - 1) / kFewWaves * kFewWaves;
   const int begin = split * per, end = begin + per < blocks.count ? begin + per : blocks.count;
 
   // queries: row c16, features 64 l + 16 q4 + 8 u .. + 8
   bf16x8_t qf[L][2];
   const int my_r = c16 < rows ? c16 : rows - 1;
-  const RowSight sight(a, s.first + my_r / a.group, s.keys);
+  const int my_t = a.by_group.of(my_r);
+  const RowSight sight(a, s.first + my_t, s.keys);
   {
-    const bf16_t* q = a.Q + (int64_t)b * a.q_sb + (int64_t)(h * a.group + my_r % a.group) * a.q_sh + (int64_t)(my_r / a.group) * a.q_sn;
+    const bf16_t* q = a.Q + (int64_t)b * a.q_sb + (int64_t)(h * a.group + my_r - my_t * a.group) * a.q_sh + (int64_t)my_t * a.q_sn;
 #pragma unroll
     for (int l = 0; l < L; ++l) {
 #pragma unroll
@@ -256,7 +257,8 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendAr
       const float inv = total > 0.0f ? 1.0f / total : 0.0f;
       const uint4 w = {pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv), pack_bf16(x[4] * inv, x[5] * inv),
                        pack_bf16(x[6] * inv, x[7] * inv)};
-      __builtin_memcpy(a.O + (int64_t)b * a.o_sb + (int64_t)(h * a.group + r % a.group) * a.o_sh + (int64_t)(r / a.group) * a.o_sn + d, &w, 16);
+      const int t = a.by_group.of(r);
+      __builtin_memcpy(a.O + (int64_t)b * a.o_sb + (int64_t)(h * a.group + r - t * a.group) * a.o_sh + (int64_t)t * a.o_sn + d, &w, 16);
     }
   }
 }
@@ -269,8 +271,8 @@ __global__ __launch_bounds__(4 * kWave) void join_rows_kernel(AttendArgs a) {
   const int64_t rows = (int64_t)a.n_q * a.group;
   const int64_t at = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
   if (at >= rows * a.B * a.H_kv) return;
-  const int r = (int)(at % rows), bh = (int)(at / rows), h = bh % a.H_kv, b = bh / a.H_kv;
-  const int t = r / a.group;
+  const int r = (int)(at % rows), bh = (int)(at / rows), b = a.by_heads.of(bh), h = bh - b * a.H_kv;
+  const int t = a.by_group.of(r);
   if (a.q_len && t >= a.q_len[b]) return;
   const int64_t part = (int64_t)bh * a.splits * a.part_rows + r;
   float m = kNoLogit;
@@ -286,7 +288,7 @@ __global__ __launch_bounds__(4 * kWave) void join_rows_kernel(AttendArgs a) {
     for (int e = 0; e < E; ++e) x[e] += f * a.part_o[p * D + lane * E + e];
   }
   const float inv = total > 0.0f ? 1.0f / total : 0.0f;
-  bf16_t* o = a.O + (int64_t)b * a.o_sb + (int64_t)(h * a.group + r % a.group) * a.o_sh + (int64_t)t * a.o_sn + lane * E;
+  bf16_t* o = a.O + (int64_t)b * a.o_sb + (int64_t)(h * a.group + r - t * a.group) * a.o_sh + (int64_t)t * a.o_sn + lane * E;
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = (bf16_t)__builtin_bit_cast(uint16_t, (__bf16)(x[e] * inv));
 }

@@ -36,19 +36,19 @@ __global__ __launch_bounds__(kTileThreads, 2) void page_rows_kernel(AttendArgs a
   const int per_head = a.row_tiles * a.splits, total = a.B * a.H_kv * per_head;
   const int id = xcd_logical_id(blockIdx.x, total);
   if (id >= total) return;
-  const int bh = id / per_head, in_head = id % per_head, h = bh % a.H_kv, b = bh / a.H_kv;
-  const int split = in_head % a.splits, tile = a.row_tiles - 1 - in_head / a.splits;    // (the last rows see most keys)
+  const int bh = a.by_tiles.of(id), in_head = id - bh * per_head, b = a.by_heads.of(bh), h = bh - b * a.H_kv;
+  const int tile_back = a.by_splits.of(in_head), split = in_head - tile_back * a.splits, tile = a.row_tiles - 1 - tile_back;    // (the last rows see most keys)
   int slot;
   const Sight s = sight_of<true>(a, b, slot);
   const int rows = s.queries * a.group, row0 = tile * kTileRows;
   if (s.queries <= 0 || row0 >= rows) return;
-  auto pos_of = [&](int r) { return s.first + (r < rows ? r : rows - 1) / a.group; };
+  auto pos_of = [&](int r) { return s.first + a.by_group.of(r < rows ? r : rows - 1); };
   const Blocks<kTileKeys> blocks(a, s, pos_of(row0), pos_of(row0 + kTileRows - 1));
-  const int per = (blocks.count + a.splits - 1) / a.splits;
+  const int per = a.by_splits.of(blocks.count + a.splits - 1);
   const int begin = split * per, end = begin + per < blocks.count ? begin + per : blocks.count;
 
   const int r = row0 + 32 * wv + c32, my_r = r < rows ? r : rows - 1;
-  const int t = my_r / a.group, g = my_r % a.group, pos = s.first + t;
+  const int t = a.by_group.of(my_r), g = my_r - t * a.group, pos = s.first + t;
   const int lo = pos_of(row0 + 32 * wv), hi = pos_of(row0 + 32 * wv + 31);      // positions of the wavefront
   // a lane's 16 bytes of a key are features 32 l + 16 half .. + 16, for two products
   bf16x8_t qf[KS];
@@ -265,28 +265,19 @@ __global__ __launch_bounds__(kTileThreads, 2) void page_rows_kernel(AttendArgs a
   }
 
   sum += __shfl_xor(sum, 32);
-  if (r >= rows) return;
+  const int first_row = row0 + 32 * wv;
+  uint8_t* lds = wv < 2 ? wv == 0 ? k0 : k1 : wv == 2 ? k2 : k3;
   if (a.splits > 1) {
-    const int64_t at = ((int64_t)bh * a.splits + split) * a.part_rows + r;
-    if (half == 0) a.part_ms[at] = float2{top, sum};
-#pragma unroll
-    for (int i = 0; i < DT; ++i) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *(f32x4_t*)(a.part_o + at * D + 32 * i + 8 * j + 4 * half) = f32x4_t{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
-    }
+    const int64_t at = ((int64_t)bh * a.splits + split) * a.part_rows + first_row;
+    if (half == 0 && r < rows) a.part_ms[at + c32] = float2{top, sum};
+    float_rows_out<D>(o, lds, [&](int row, int piece) -> void* { return first_row + row < rows ? a.part_o + (at + row) * D + 4 * piece : nullptr; });
     return;
   }
   const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-  bf16_t* out = a.O + (int64_t)b * a.o_sb + (int64_t)(h * a.group + g) * a.o_sh + (int64_t)t * a.o_sn + 4 * half;
-#pragma unroll
-  for (int i = 0; i < DT; ++i) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint2 w = {pack_bf16(o[i][4 * j] * inv, o[i][4 * j + 1] * inv), pack_bf16(o[i][4 * j + 2] * inv, o[i][4 * j + 3] * inv)};
-      __builtin_memcpy(out + 32 * i + 8 * j, &w, 8);
-    }
-  }
+  rows_out<D>(o, inv, lds, [&](int row, int piece) -> void* {
+    const int r = first_row + row, t = a.by_group.of(r);
+    return r < rows ? a.O + (int64_t)b * a.o_sb + (int64_t)(h * a.group + r - t * a.group) * a.o_sh + (int64_t)t * a.o_sn + 8 * piece : nullptr;
+  });
 }
 
 }  // namespace

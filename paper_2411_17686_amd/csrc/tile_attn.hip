@@ -36,26 +36,21 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
   const int per_head = a.row_tiles * a.splits, total = a.B * a.H_kv * per_head;
   const int id = xcd_logical_id(blockIdx.x, total);
   if (id >= total) return;
-  const int bh = id / per_head, in_head = id % per_head, h = bh % a.H_kv, b = bh / a.H_kv;
-  const int split = in_head % a.splits, tile = a.row_tiles - 1 - in_head / a.splits;    // (the last rows see most keys)
+  const int bh = a.by_tiles.of(id), in_head = id - bh * per_head, b = a.by_heads.of(bh), h = bh - b * a.H_kv;
+  const int tile_back = a.by_splits.of(in_head), split = in_head - tile_back * a.splits, tile = a.row_tiles - 1 - tile_back;    // (the last rows see most keys)
   int slot;
   const Sight s = sight_of<false>(a, b, slot);
   const int rows = s.queries * a.group, row0 = tile * kTileRows;
   if (s.queries <= 0 || row0 >= rows) return;
-  auto pos_of = [&](int r) { return s.first + (r < rows ? r : rows - 1) / a.group; };
+  auto pos_of = [&](int r) { return s.first + a.by_group.of(r < rows ? r : rows - 1); };
   const Blocks<kTileKeys> blocks(a, s, pos_of(row0), pos_of(row0 + kTileRows - 1));
-  const int per = (blocks.count + a.splits - 1) / a.splits;
+  const int per = a.by_splits.of(blocks.count + a.splits - 1);
   const int begin = split * per, end = begin + per < blocks.count ? begin + per : blocks.count;
 
   const int r = row0 + 32 * wv + c32, my_r = r < rows ? r : rows - 1;
-  const int t = my_r / a.group, g = my_r % a.group, pos = s.first + t;
+  const int t = a.by_group.of(my_r), g = my_r - t * a.group, pos = s.first + t;
   const int lo = pos_of(row0 + 32 * wv), hi = pos_of(row0 + 32 * wv + 31);      // positions of the wavefront
   bf16x8_t qf[KS];
-  {
-    const bf16_t* q = a.Q + (int64_t)b * a.q_sb + (int64_t)(h * a.group + g) * a.q_sh + (int64_t)t * a.q_sn + 8 * half;
-#pragma unroll
-    for (int k = 0; k < KS; ++k) __builtin_memcpy(&qf[k], q + 16 * k, 16);
-  }
   f32x16_t o[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i) o[i] = f32x16_t{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
@@ -264,6 +259,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
     load_k(raw, sk1, begin + 1);
     store(raw, sk1, true);
   }
+  {                                                // (behind the keys, which more has to wait for)
+    const bf16_t* q = a.Q + (int64_t)b * a.q_sb + (int64_t)(h * a.group + g) * a.q_sh + (int64_t)t * a.q_sn + 8 * half;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) __builtin_memcpy(&qf[k], q + 16 * k, 16);
+  }
   arrived();
   if (begin < end) {
     logits(S0);
@@ -277,28 +277,12 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
   }
 
   sum += __shfl_xor(sum, 32);
-  if (r >= rows) return;
-  if (a.splits > 1) {
-    const int64_t at = ((int64_t)bh * a.splits + split) * a.part_rows + r;
-    if (half == 0) a.part_ms[at] = float2{top, sum};
-#pragma unroll
-    for (int i = 0; i < DT; ++i) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *(f32x4_t*)(a.part_o + at * D + 32 * i + 8 * j + 4 * half) = f32x4_t{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
-    }
-    return;
-  }
   const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-  bf16_t* out = a.O + (int64_t)b * a.o_sb + (int64_t)(h * a.group + g) * a.o_sh + (int64_t)t * a.o_sn + 4 * half;
-#pragma unroll
-  for (int i = 0; i < DT; ++i) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint2 w = {pack_bf16(o[i][4 * j] * inv, o[i][4 * j + 1] * inv), pack_bf16(o[i][4 * j + 2] * inv, o[i][4 * j + 3] * inv)};
-      __builtin_memcpy(out + 32 * i + 8 * j, &w, 8);
-    }
-  }
+  const int first_row = row0 + 32 * wv;
+  rows_out<D>(o, inv, (uint8_t*)(wv < 2 ? sk0 : sk1) + wv % 2 * 64 * D, [&](int row, int piece) -> void* {
+    const int r = first_row + row, t = a.by_group.of(r);
+    return r < rows ? a.O + (int64_t)b * a.o_sb + (int64_t)(h * a.group + r - t * a.group) * a.o_sh + (int64_t)t * a.o_sn + 8 * piece : nullptr;
+  });
 }
 
 }  // namespace
