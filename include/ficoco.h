@@ -396,7 +396,8 @@ int ficoco_v_step_static(ficoco_ctx *ctx, const ficoco_problem *p, void *X_out, 
  * Sequences are named by slots 0 .. n_seqs - 1 in arrays on the device, which no call can check on the host:
  * entries that are out of range, or that name a slot a second time where that has no meaning, are left out as each
  * function says; page numbers out of range are taken for -1.  Limits: page_size 16, 32, 64 or 128; d_head 64 or 128
- * (others FICOCO_EUNSUPPORTED); n_seqs <= 8192; at most 1024 sequences in a call of reserve, fork or compact.
+ * (others FICOCO_EUNSUPPORTED); n_seqs <= 8192; at most 2^30 tokens in a sequence or a call, at most 1024 sequences in a call of
+ * reserve, fork or compact.
  */
 typedef struct {
   int32_t layers, n_pages, page_size, heads, d_head, n_seqs, max_pages;
@@ -420,8 +421,10 @@ typedef struct {
  *   j < k_len[b],  j <= p,  and (window = 0 or j > p - window or j < sinks):
  * O[b][h][t] = sum_j softmax_j(scale * Q[b][h][t] . K[j]) V[j], zeros where no key is seen.  Rows t >= q_len[b] are left
  * as they are.  Query head h reads key / value head h / (H / H_kv).  NULL arrays: q_len = n_q, q_start = k_len - q_len
- * (the queries are the last tokens; a negative position sees nothing).  bfloat16; logits, exponentials and sums in single precision, the
- * weights are rounded to bfloat16 for the product with V.  Strides in elements, d_head contiguous, any element alignment. */
+ * (the queries are the last tokens; a negative position sees nothing; q_start + n_q stays below 2^31).  bfloat16; logits, exponentials and sums in single precision, the
+ * weights are rounded to bfloat16 for the product with V.  Keys that no query of a sequence sees may hold anything; an infinity or a NaN
+ * in V at a key that some query sees may reach the other queries of the call, as zero times it.  Strides in elements,
+ * d_head contiguous, any element alignment; rows of O must not overlap. */
 typedef struct {
   int32_t B, H, H_kv, n_q, n_k, d_head;
   const void *Q; /* [B][H][n_q][d_head] */
@@ -448,11 +451,12 @@ int ficoco_cache_reserve(ficoco_ctx *ctx, const ficoco_cache *c, int32_t n, cons
 
 /* Writes the tokens of one layer into their pages.  A page that is begun inside keeps what lies before: it takes the larger of
  * its exponent and that of the new tokens, the older ones rewritten to it (exactly, but for E4M3's denormals).  What lies behind
- * the new tokens in a page is void.  Sequences with start[b] < 0 are left out, and so are positions that have no page. */
+ * the new tokens in a page is void.  Sequences with start[b] < 0 are left out, and so are positions that have no page.  Two entries
+ * of a call must not write one page (the starts of ficoco_cache_reserve see to it). */
 int ficoco_cache_append(ficoco_ctx *ctx, const ficoco_cache *c, int32_t layer, const ficoco_tokens *t, void *stream);
 
 /* The values that a layer's pages hold, as bfloat16 (exact) or single precision; K or V may be NULL.  start NULL = 0.  Positions
- * that have no page give zeros, sequences with start[b] < 0 are left out.  (With K: the keys of ficoco_l_step's query/key form.) */
+ * that have no page give zeros, sequences with start[b] < 0 are left out; rows written must not overlap.  (With K: the keys of ficoco_l_step's query/key form.) */
 int ficoco_cache_read(ficoco_ctx *ctx, const ficoco_cache *c, int32_t layer, const ficoco_tokens *t, void *stream);
 
 /* Sequence dst[b] continues src[b]: it shares its whole pages and has a copy, in all layers, of the page that is not full, or of every

@@ -88,7 +88,7 @@ struct Blocks {
   int near_key, first_keys;       // keys below near_key are seen by no row unless they are below first_keys
   int end;                        // keys behind the last one seen
   __device__ __forceinline__ Blocks(const AttendArgs& a, const Sight& s, int lo, int hi) {
-    end = hi + 1 < s.keys ? hi + 1 : s.keys;
+    end = hi < s.keys ? hi + 1 : s.keys;
     end = end > 0 ? end : 0;
     near_key = a.window > 0 && lo >= a.window ? lo - a.window + 1 : 0;
     near_key = near_key < end ? near_key : end;

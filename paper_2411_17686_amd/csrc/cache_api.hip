@@ -1,6 +1,8 @@
 // C-ABI layer of the decoder's cache and its attention: argument checks and launches.  Host code only.
 #include <algorithm>
+#include <array>
 #include <cmath>
+#include <utility>
 
 #include "attend.hpp"
 #include "ctx.hpp"
@@ -10,6 +12,18 @@ using namespace ficoco;
 namespace {
 
 constexpr int64_t kMaxGridY = 65535, kMaxGridX = 0x7fffffff;
+constexpr int64_t kMaxTokens = 1 << 30;      // (a block behind the last token, too, is named by 32 bits)
+
+// Whether rows of d elements may share elements: none do where every stride steps over all that the smaller ones span.
+bool rows_collide(int64_t d, std::array<std::pair<int64_t, int64_t>, 3> dims) {      // (stride, extent)
+  std::sort(dims.begin(), dims.end());
+  for (const auto& [stride, extent] : dims) {
+    if (extent <= 1) continue;
+    if (stride < d) return true;
+    d += stride * (extent - 1);
+  }
+  return false;
+}
 
 // What is wrong with the description of a cache, or nullptr; *code its status.
 const char* cache_fault(const ficoco_cache& c, int* code) {
@@ -22,7 +36,7 @@ const char* cache_fault(const ficoco_cache& c, int* code) {
   if (c.page_size != 16 && c.page_size != 32 && c.page_size != 64 && c.page_size != 128) return "page_size must be 16, 32, 64 or 128";
   if (c.d_head != 64 && c.d_head != 128) return "d_head must be 64 or 128";
   if (c.n_seqs > kMaxSlots) return "more than 8192 slots";
-  if ((int64_t)c.max_pages * c.page_size > 0x7fffffff) return "a row of the table holds 2^31 tokens or more";
+  if ((int64_t)c.max_pages * c.page_size > kMaxTokens) return "a row of the table holds more than 2^30 tokens";
   if (c.heads > kMaxGridY) return "too many heads";
   *code = FICOCO_OK;
   return nullptr;
@@ -53,16 +67,14 @@ int check_tokens(ficoco_ctx* ctx, const ficoco_cache& c, int32_t layer, const fi
   if (write ? !t->K || !t->V || !t->start : !t->K && !t->V) return fail(ctx, FICOCO_EINVAL, fn, "a pointer is NULL");
   const uintptr_t align = t->dtype == FICOCO_BF16 ? 1 : 3;
   if (((uintptr_t)t->K | (uintptr_t)t->V) & align) return fail(ctx, FICOCO_EINVAL, fn, "K or V is not aligned to its elements");
+  if (t->n_max > kMaxTokens) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "more than 2^30 tokens of a sequence");
   if (2 * (int64_t)t->n > kMaxGridY) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "more than 32767 sequences in a call");
   if (t->k_stride_b < 0 || t->k_stride_h < 0 || t->k_stride_n < 0 || t->v_stride_b < 0 || t->v_stride_h < 0 || t->v_stride_n < 0)
     return fail(ctx, FICOCO_EINVAL, fn, "a stride is negative");
   if (!write) {
-    const int64_t st[2][3] = {{t->k_stride_b, t->k_stride_h, t->k_stride_n}, {t->v_stride_b, t->v_stride_h, t->v_stride_n}};
-    for (int i = 0; i < 2; ++i) {
-      if (!(i ? t->V : t->K)) continue;
-      if ((t->n > 1 && st[i][0] < c.d_head) || (c.heads > 1 && st[i][1] < c.d_head) || (t->n_max > 1 && st[i][2] < c.d_head))
-        return fail(ctx, FICOCO_EINVAL, fn, "rows that are written overlap");
-    }
+    if ((t->K && rows_collide(c.d_head, {{{t->k_stride_b, t->n}, {t->k_stride_h, c.heads}, {t->k_stride_n, t->n_max}}})) ||
+        (t->V && rows_collide(c.d_head, {{{t->v_stride_b, t->n}, {t->v_stride_h, c.heads}, {t->v_stride_n, t->n_max}}})) || t->K == t->V)
+      return fail(ctx, FICOCO_EINVAL, fn, "rows that are written overlap");
   }
   return FICOCO_OK;
 }
@@ -88,8 +100,6 @@ const char* attention_fault(const ficoco_attention& a, int heads, int d_head, bo
                             {a.k_stride_b, a.k_stride_h, a.k_stride_n}, {a.v_stride_b, a.v_stride_h, a.v_stride_n}};
   for (int i = 0; i < (paged ? 2 : 4); ++i)
     if (st[i][0] < 0 || st[i][1] < 0 || st[i][2] < 0) return "a stride is negative";
-  if ((a.B > 1 && a.o_stride_b < d_head) || (a.H > 1 && a.o_stride_h < d_head) || (a.n_q > 1 && a.o_stride_n < d_head))
-    return "rows of O overlap";
   if (a.B > 0 && a.n_q > 0) {
     if (!a.Q || !a.O || (!paged && a.n_k > 0 && (!a.K || !a.V))) return "a pointer is NULL";
     if (((uintptr_t)a.Q | (uintptr_t)a.O | (paged ? 0 : (uintptr_t)a.K | (uintptr_t)a.V)) & 1) return "a tensor is not aligned to its elements";
@@ -102,6 +112,9 @@ const char* attention_fault(const ficoco_attention& a, int heads, int d_head, bo
   *code = FICOCO_EUNSUPPORTED;
   if (d_head != 64 && d_head != 128) return "d_head must be 64 or 128";
   if ((int64_t)a.n_q * (a.H / heads) > 0x3fffffff) return "more than 2^30 rows of one key / value head";
+  if (!paged && a.n_k > kMaxTokens) return "more than 2^30 keys";
+  *code = FICOCO_EINVAL;
+  if (rows_collide(d_head, {{{a.o_stride_b, a.B}, {a.o_stride_h, a.H}, {a.o_stride_n, a.n_q}}})) return "rows of O overlap";
   *code = FICOCO_OK;
   return nullptr;
 }
