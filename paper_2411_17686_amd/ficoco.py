@@ -431,8 +431,8 @@ class Workspace:
     """Device memory for one call at a time, 256-byte aligned."""
 
     def __init__(self, n, device):
-        self.bytes, self.device = n, torch.device(device)
         self.t = torch.empty(n + 256, dtype=torch.uint8, device=device)
+        self.bytes, self.device = n, self.t.device
         self.ptr = self.t.data_ptr() + (-self.t.data_ptr()) % 256
 
 

@@ -1,0 +1,464 @@
+"""The cache and its attention as a decoder uses them: with the reduction step, in captured graphs, on other streams, in pools
+beyond 32 bits; and the calls they refuse."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2411_17686_amd import ficoco as fc
+from tests import cache_ref as R
+from tests.test_gpu_cache import append, i32, pair, reserve, same
+from tests.test_gpu_cache_attention import check
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = fc.Context(0)
+    yield c
+    c.close()
+
+
+def rows(seed, *shape):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(*shape, generator=g, device="cuda").to(torch.bfloat16)
+
+
+def held(h, layer, slot, n):
+    """Keys and values of the host's model, float64 [heads][n][d]."""
+    return [np.stack([h.values(x, layer, slot, t) for t in range(n)], axis=1) for x in "kv"]
+
+
+def test_a_prompt_reduced_shared_and_continued(ctx):
+    """Two prompts through a decoder of two layers: layer 0 over dense keys with a window, layer 1 over the pages; the step of layer 1 takes
+    its keys from the cache and its choice shortens the cache, which two continuations each then share and extend by three tokens."""
+    layers, B, n_sys, N, M, heads, d, P, n_keep = 2, 2, 21, 120, 19, 4, 64, 16, 37
+    n, dim = n_sys + N + M, heads * d
+    g, h = pair(layers, 60, P, heads, d, 6, 20)
+    Q, K, V = (rows(s, layers, B, heads, n, d) for s in (1, 2, 3))
+    X = rows(4, B, n, dim)
+    start, at = reserve(ctx, g, h, [0, 1], [n, n])
+    assert at == [0, 0]
+
+    # layer 0: the prompt's own keys, a window with the system tokens visible
+    append(ctx, g, h, 0, K[0].cpu(), V[0].cpu(), at, [n, n], [0, 1])
+    out = torch.zeros_like(Q[0])
+    fc.ficoco_window_attention(ctx, Q[0], K[0], V[0], out, window=64, sinks=n_sys)
+    check(out, Q[0], K[0].double().cpu().numpy(), V[0].double().cpu().numpy(), [n, n], d ** -0.5, [0, 0], [n, n], 64, n_sys, 1)
+
+    # layer 1: over the pages
+    append(ctx, g, h, 1, K[1].cpu(), V[1].cpu(), at, [n, n], [0, 1])
+    ws = fc.attention_workspace(g, Q[1], out)
+    fc.ficoco_cache_attention(ctx, g, 1, Q[1], out, ws, seq=i32([0, 1]))
+    k, v = (np.stack(t) for t in zip(*[held(h, 1, b, n) for b in range(B)]))
+    check(out, Q[1], k, v, [n, n], d ** -0.5, [0, 0], [n, n], 0, 0, 1)
+
+    # the step, with the keys as the cache has them, and its choice in the cache
+    keys = torch.empty(B, heads, n, d, dtype=torch.bfloat16, device="cuda")
+    fc.ficoco_cache_read(ctx, g, 1, keys, None)
+    assert np.array_equal(keys.double().cpu().numpy(), k)
+    p = fc.make_problem(X, variant=fc.VARIANT_L, vis_begin=n_sys, N=N, n_keep=n_keep, w_score=0.6, gamma=0.6, eps=0.998, red_src=fc.R_ATTN_RECV,
+                        sem_src=fc.G_TEXT_ATTN, corr_src=fc.C_ATTN, window=0, Q=Q[1], K=keys, qk_begin=0, M=M)
+    buf = fc.Buffers(p, "cuda", X.dtype)
+    fc.ficoco_l_step(ctx, p, buf)
+    done = i32([7, 7])
+    fc.ficoco_cache_compact(ctx, g, 0, layers, i32([0, 1]), i32([0, 1]), n_sys, N, buf.keep_idx, done, fc.cache_workspace(g, B))
+    keep = buf.keep_idx.cpu().numpy()
+    assert done.tolist() == h.compact(range(layers), [0, 1], [0, 1], n_sys, N, keep) == [1, 1]
+    left = n - N + n_keep
+    assert g.len.tolist()[:2] == [left, left] and buf.X_out.shape[1] == left
+    same(g, h)
+
+    # two continuations of each prompt
+    done = i32([7] * 4)
+    fc.ficoco_cache_fork(ctx, g, i32([0, 0, 1, 1]), i32([2, 3, 4, 5]), done)
+    assert done.tolist() == h.fork([0, 0, 1, 1], [2, 3, 4, 5], False) == [1] * 4
+    fc.ficoco_cache_free(ctx, g, i32([0, 1]))
+    h.free([0, 1])
+    same(g, h)
+    seq = [5, 2, 4, 3]
+    for step in range(3):
+        start, at = reserve(ctx, g, h, seq, [1] * 4)
+        assert at == [left + step] * 4
+        q1, k1, v1 = (rows(10 * step + s, layers, 4, heads, 1, d) for s in (5, 6, 7))
+        for layer in range(layers):
+            append(ctx, g, h, layer, k1[layer].cpu(), v1[layer].cpu(), at, [1] * 4, seq)
+            o1 = torch.zeros_like(q1[layer])
+            window = 40 if layer == 0 else 0
+            kw = dict(window=window, sinks=n_sys if window else 0, max_len=left + 3)
+            fc.ficoco_cache_attention(ctx, g, layer, q1[layer], o1, fc.attention_workspace(g, q1[layer], o1, **kw), seq=i32(seq), **kw)
+            k, v = (np.stack(t) for t in zip(*[held(h, layer, s, left + step + 1) for s in seq]))
+            check(o1, q1[layer], k, v, [left + step + 1] * 4, d ** -0.5, at, [1] * 4, window, n_sys if window else 0, 1)
+        same(g, h)
+    fc.ficoco_cache_free(ctx, g, i32(seq))
+    h.free(seq)
+    same(g, h)
+    assert not g.refs.any() and not g.len.any() and (g.table == -1).all()
+
+
+def _caches(n=2):
+    """Equal caches of two sequences with 90 and 41 tokens."""
+    made = []
+    for _ in range(n):
+        c = fc.Cache.empty(1, 40, 16, 2, 64, 5, 16)
+        c.refs[3] = c.refs[5] = 1                                # (pages that belong to nobody here)
+        made.append(c)
+    return made
+
+
+ARRAYS = ("k", "v", "k_exp", "v_exp", "table", "len", "refs")
+
+
+def test_replays_of_captured_decoding_equal_eager(ctx):
+    """One token for every sequence a replay: pages, tokens, attention (few rows, cut over workgroups, and many) and a window over them."""
+    g, e = _caches()
+    seq = i32([0, 1, 2])
+    K, V = rows(1, 3, 2, 90, 64), rows(2, 3, 2, 90, 64)
+    for c in (g, e):
+        start = i32([0] * 3)
+        fc.ficoco_cache_reserve(ctx, c, start, i32([90, 41, 0]), seq=seq)
+        fc.ficoco_cache_append(ctx, c, 0, K, V, start, n_new=i32([90, 41, 0]), seq=seq)
+    k1, v1, q1 = (rows(s, 3, 2 if s < 5 else 4, 1, 64) for s in (3, 4, 5))
+    q30 = rows(6, 3, 4, 30, 64)
+
+    def step(c, start, o1, o30, ow, w1, w30):
+        fc.ficoco_cache_reserve(ctx, c, start, 1, seq=seq)
+        fc.ficoco_cache_append(ctx, c, 0, k1, v1, start, seq=seq)
+        fc.ficoco_cache_attention(ctx, c, 0, q1, o1, w1, seq=seq)
+        fc.ficoco_cache_attention(ctx, c, 0, q30, o30, w30, seq=seq, window=20, sinks=2)
+        fc.ficoco_window_attention(ctx, q30, q30[:, ::2], q30[:, 1::2], ow, window=9, sinks=1)
+
+    def buffers(c):
+        o1, o30, ow = torch.zeros_like(q1), torch.zeros_like(q30), torch.zeros_like(q30)
+        return i32([0] * 3), o1, o30, ow, fc.attention_workspace(c, q1, o1), fc.attention_workspace(c, q30, o30, window=20, sinks=2)
+
+    bg, be = buffers(g), buffers(e)
+    warm = _caches(1)[0]
+    step(warm, *buffers(warm))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        step(g, *bg)
+    for i in range(20):                                          # (over the end of a page, and a raised exponent)
+        for t in (k1, v1, q1, q30):
+            t.copy_(rows(50 + i, *t.shape) * (4.0 if i % 5 == 4 else 1.0))
+        step(e, *be)
+        for t in bg[1:4]:
+            t.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(bg[:4], be[:4]):
+            assert torch.equal(a, b), i
+        for name in ARRAYS:
+            assert torch.equal(getattr(g, name), getattr(e, name)), (i, name)
+    assert g.len.tolist() == [110, 61, 20, 0, 0]
+
+
+def test_replays_of_captured_page_changes_equal_eager(ctx):
+    """A prompt in, shortened, forked, copied whole, and all but one of them given back, in one graph."""
+    g, e = _caches()
+    K, V = rows(1, 2, 2, 75, 64), rows(2, 2, 2, 75, 64)
+    keep = i32([[0, 3, 4, 9, 30], [0, 1, 2, 3, 4]])
+
+    def life(c, start, done, ws):
+        fc.ficoco_cache_free(ctx, c, i32_3)
+        fc.ficoco_cache_reserve(ctx, c, start, n_new, seq=i32_01)
+        fc.ficoco_cache_append(ctx, c, 0, K, V, start, n_new=n_new, seq=i32_01)
+        fc.ficoco_cache_compact(ctx, c, 0, 1, i32_01, i32_01, 18, 40, keep, done[:2], ws)
+        fc.ficoco_cache_fork(ctx, c, i32_01, i32_23, done[2:4])
+        fc.ficoco_cache_fork(ctx, c, i32_01[:1], i32_4, done[4:], whole=True)
+        fc.ficoco_cache_free(ctx, c, i32_0124)
+
+    i32_01, i32_23, i32_3, i32_4, i32_0124, n_new = i32([0, 1]), i32([2, 3]), i32([3]), i32([4]), i32([0, 1, 2, 4]), i32([75, 61])
+    bg, be = ((i32([0, 0]), i32([7] * 5), fc.cache_workspace(c, 2)) for c in (g, e))
+    warm = _caches(1)[0]
+    life(warm, *be)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        life(g, *bg)
+    for i in range(4):
+        K.copy_(rows(70 + i, *K.shape))
+        V.copy_(rows(80 + i, *V.shape))
+        keep[0, -1] = 30 + i
+        n_new[1] = 61 + i
+        life(e, *be)
+        bg[1].fill_(7)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert bg[1].tolist() == be[1].tolist() == [1] * 5 and torch.equal(bg[0], be[0])
+        for name in ARRAYS:
+            assert torch.equal(getattr(g, name), getattr(e, name)), (i, name)
+    assert g.len.tolist() == [0, 0, 0, 64 - 35, 0]
+
+
+def test_two_streams_at_once(ctx):
+    """A cache and a workspace each; what either computes is what it computes alone."""
+    c = fc.Cache.empty(1, 400, 32, 2, 128, 4, 100)
+    start = i32([0] * 4)
+    fc.ficoco_cache_reserve(ctx, c, start, 3000)
+    K, V = rows(1, 4, 2, 3000, 128), rows(2, 4, 2, 3000, 128)
+    fc.ficoco_cache_append(ctx, c, 0, K, V, start)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    Qs = [rows(10 + i, 4, 8, n_q, 128) for i, n_q in enumerate((1, 50, 3))]
+    want, got, spaces = [], [], []
+    for Q in Qs:
+        out = torch.zeros_like(Q)
+        fc.ficoco_cache_attention(ctx, c, 0, Q, out, fc.attention_workspace(c, Q, out))
+        want.append(out)
+        got.append(torch.zeros_like(Q))
+        spaces.append(fc.attention_workspace(c, Q, out))
+    others = [fc.Cache.empty(1, 400, 32, 2, 128, 4, 100) for _ in streams]
+    starts = [i32([0] * 4) for _ in streams]
+    torch.cuda.synchronize()
+    for turn in range(5):
+        for s, other, at, Q, out, ws in zip(streams, others, starts, Qs, got, spaces):
+            with torch.cuda.stream(s):
+                out.zero_()
+                fc.ficoco_cache_attention(ctx, c, 0, Q, out, ws)
+                if turn == 0:
+                    fc.ficoco_cache_reserve(ctx, other, at, 3000)
+                    fc.ficoco_cache_append(ctx, other, 0, K, V, at)
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    for other in others:
+        for name in ARRAYS:
+            assert torch.equal(getattr(other, name), getattr(c, name)), name
+
+
+def test_pages_beyond_32_bits(ctx):
+    """Pools of 5 GiB each; the pages that are free lie behind 2^32 bytes of them."""
+    heads, P, d = 8, 128, 128
+    n_pages = (5 << 30) // (heads * P * d)
+    c = fc.Cache(*(torch.empty(1, n_pages, heads, P, d, dtype=torch.uint8, device="cuda") for _ in range(2)),
+                 *(torch.empty(1, n_pages, heads, dtype=torch.uint8, device="cuda") for _ in range(2)),
+                 i32([[-1] * 8] * 3), i32([0] * 3), i32([0] * n_pages))
+    c.refs[:n_pages - 20] = 1
+    lens = [700, 130, 0]
+    start = i32([0] * 3)
+    fc.ficoco_cache_reserve(ctx, c, start, i32(lens))
+    assert start.tolist() == [0, 0, 0] and int(c.table.max()) == n_pages - 13
+    K, V = rows(1, 3, heads, 700, d), rows(2, 3, heads, 700, d)
+    fc.ficoco_cache_append(ctx, c, 0, K, V, start, n_new=i32(lens))
+    done = i32([0])
+    fc.ficoco_cache_compact(ctx, c, 0, 1, i32([0]), i32([0]), 100, 400, i32([list(range(0, 400, 2))]), done, fc.cache_workspace(c, 1))
+    fc.ficoco_cache_fork(ctx, c, i32([0]), i32([2]), done, whole=True)
+    assert done.tolist() == [1]
+    one = i32([0] * 3)
+    fc.ficoco_cache_reserve(ctx, c, one, 1)
+    k1, v1 = rows(3, 3, heads, 1, d), rows(4, 3, heads, 1, d)
+    fc.ficoco_cache_append(ctx, c, 0, k1, v1, one)
+    lens = [501, 131, 501]
+    assert c.len.tolist() == lens
+    kept = list(range(100)) + list(range(100, 500, 2)) + list(range(500, 700))
+    gone = [torch.zeros(3, heads, 501, d, device="cuda") for _ in range(2)]
+    fc.ficoco_cache_read(ctx, c, 0, *gone)
+    for got, x, x1 in zip(gone, (K, V), (k1, v1)):
+        for b, n in enumerate(lens):
+            whole = torch.cat([x[0, :, kept] if b != 1 else x[1, :, :130], x1[b]], 1).float()
+            err = (got[b, :, :n] - whole).abs()
+            # two roundings to E4M3, each 2^-4 of the value, and up to three that end in denormals, each half of the smallest (2^-10 of a scale
+            # of which 448 are less than twice the largest value)
+            assert (err <= 2.2 * 2.0 ** -4 * whole.abs() + 3 * 2.0 ** -10 * (2 * float(whole.abs().max()) / 448)).all(), b
+    k, v = (t.double().cpu().numpy() for t in gone)
+    for n_q in (1, 40):
+        Q = rows(5, 3, heads, n_q, d)
+        out = torch.zeros_like(Q)
+        fc.ficoco_cache_attention(ctx, c, 0, Q, out, fc.attention_workspace(c, Q, out))
+        check(out, Q, k, v, lens, d ** -0.5, [n - n_q for n in lens], [n_q] * 3, 0, 0, 1)
+
+
+@pytest.mark.parametrize("step", [(1 << 23) - 8, 1 << 24])       # straight into LDS, and rows too far apart for that
+def test_rows_far_apart(ctx, step):
+    """Queries, keys, values and results whose rows lie up to 4 GiB apart; tokens of the cache as far."""
+    n, d = 130, 64
+    space = torch.zeros(n * step + 4 * d, dtype=torch.bfloat16, device="cuda")
+    Q, K, V, out = (space[i * d:i * d + (n - 1) * step + d].as_strided((1, 1, n, d), (1, 1, step, 1)) for i in range(4))
+    for i, t in enumerate((Q, K, V)):
+        t.copy_(rows(i, 1, 1, n, d))
+    with pytest.raises(fc.FicocoError):
+        fc.ficoco_window_attention(ctx, Q, K, V, out)            # (its range holds the queries)
+    packed = torch.zeros(1, 1, n, d, dtype=torch.bfloat16, device="cuda")
+    fc.ficoco_window_attention(ctx, Q, K, V, packed, window=100, sinks=3)
+    k, v = (t.double().cpu().numpy() for t in (K, V))
+    check(packed, Q, k, v, [n], d ** -0.5, [0], [n], 100, 3, 1)
+    q = Q.contiguous()
+    far = torch.full((n * step,), 3.0, dtype=torch.bfloat16, device="cuda").as_strided((1, 1, n, d), (1, 1, step, 1))
+    fc.ficoco_window_attention(ctx, q, K.contiguous(), V.contiguous(), far, window=100, sinks=3)
+    assert torch.equal(far, packed)
+    c = fc.Cache.empty(1, 9, 16, 1, d, 1, 9)
+    start = i32([0])
+    fc.ficoco_cache_reserve(ctx, c, start, n)
+    fc.ficoco_cache_append(ctx, c, 0, K, V, start)
+    e = fc.Cache.empty(1, 9, 16, 1, d, 1, 9)
+    fc.ficoco_cache_reserve(ctx, e, start, n)
+    fc.ficoco_cache_append(ctx, e, 0, K.contiguous(), V.contiguous(), start)
+    for name in ARRAYS:
+        assert torch.equal(getattr(c, name), getattr(e, name)), name
+    near = torch.zeros_like(q)
+    fc.ficoco_cache_read(ctx, c, 0, near, None)
+    fc.ficoco_cache_read(ctx, c, 0, far, None)
+    assert torch.equal(far, near)
+    fc.ficoco_cache_attention(ctx, c, 0, Q, far, fc.attention_workspace(c, Q, far))
+    fc.ficoco_cache_attention(ctx, c, 0, q, near, fc.attention_workspace(c, q, near))
+    assert torch.equal(far, near)
+
+
+def test_many_sequences_of_one_token(ctx):
+    """700 sequences a call: tokens one at a time across a page, some of them louder than all before, slots out of order and out of range."""
+    n, heads, d, P = 700, 1, 64, 16
+    g, h = pair(1, 1500, P, heads, d, 720, 2)
+    order = np.random.RandomState(1).permutation(720)[:n].tolist()
+    order[5], order[9] = -1, 720
+    for step in range(20):
+        start, at = reserve(ctx, g, h, order, [1] * n)
+        assert at[5] == at[9] == -1
+        K, V = (torch.randn(n, heads, 1, d, generator=torch.Generator().manual_seed(2 * step + i)) * (1 + step * (step % 3 == 2) * 9) for i in (0, 1))
+        K, V = K.to(torch.bfloat16), V.to(torch.bfloat16)
+        append(ctx, g, h, 0, K, V, at, [1] * n, order)
+    same(g, h)
+    Q = rows(3, n, 2, 1, d)
+    out = torch.full_like(Q, 7.0)
+    fc.ficoco_cache_attention(ctx, g, 0, Q, out, fc.attention_workspace(g, Q, out), seq=i32(order))
+    some = list(range(0, n, 41)) + [5, 9]
+    k, v = (np.stack(t) for t in zip(*[held(h, 0, order[b] if at[b] >= 0 else 0, 20) for b in some]))
+    check(out[some], Q[some], k, v, [20 if at[b] >= 0 else 0 for b in some], d ** -0.5, [19] * len(some), [1] * len(some), 0, 0, 2)
+
+
+@pytest.mark.parametrize("n_q", [1, 40])
+def test_extreme_positions(ctx, n_q):
+    """Positions, windows and counts at the ends of 32 bits."""
+    c = fc.Cache.empty(1, 40, 16, 1, 64, 5, 8)
+    K, V = rows(1, 5, 1, 100, 64), rows(2, 5, 1, 100, 64)
+    start = i32([0] * 5)
+    fc.ficoco_cache_reserve(ctx, c, start, 100)
+    fc.ficoco_cache_append(ctx, c, 0, K, V, start)
+    k, v = (torch.zeros(5, 1, 100, 64, device="cuda") for _ in range(2))
+    fc.ficoco_cache_read(ctx, c, 0, k, v)
+    top, low = 2 ** 31 - 1 - n_q, -2 ** 31
+    starts = [top, low, 99, -n_q, 5]
+    k_len, q_len = [2 ** 31 - 1, 100, 2 ** 31 - 1, low, 7], [2 ** 31 - 1, n_q, n_q, n_q, low]
+    Q = rows(3, 5, 2, n_q, 64)
+    for window, sinks in ((0, 0), (2 ** 31 - 1, 2 ** 31 - 1), (1, 2 ** 31 - 1), (2 ** 31 - 1, 0), (2 ** 31 - 60, 1)):
+        for paged in (True, False):
+            out = torch.full_like(Q, 9.0)
+            kw = dict(window=window, sinks=sinks, q_start=i32(starts), k_len=i32(k_len), q_len=i32(q_len))
+            if paged:
+                fc.ficoco_cache_attention(ctx, c, 0, Q, out, fc.attention_workspace(c, Q, out, window=window, sinks=sinks), **kw)
+                k64, v64 = k.double().cpu().numpy(), v.double().cpu().numpy()
+            else:
+                fc.ficoco_window_attention(ctx, Q, K, V, out, **kw)
+                k64, v64 = K.double().cpu().numpy(), V.double().cpu().numpy()
+            check(out, Q, k64, v64, [100, 100, 100, 0, 7], 0.125, starts, [n_q] * 4 + [0], window, sinks, 2, before=9.0)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("n_q,aligned", [(4, True), (100, True), (100, False)])
+def test_a_key_that_is_no_number_concerns_those_who_see_it(ctx, bad, n_q, aligned):
+    """One NaN or infinity in the third key from the end: the queries before it are those of the formula, and NaN reaches those behind it (an infinity
+    in the cache is its largest number)."""
+    n, d, at = 150, 64, 147
+    K, V = rows(1, 1, 1, n, d), rows(2, 1, 1, n, d)
+    K[0, 0, at, 5] = bad
+    Q = rows(3, 1, 2, n_q, d)
+    Q[..., 5] = 1.0
+    if not aligned:
+        K, V = (torch.nn.functional.pad(t, (1, 2))[..., 1:-2] for t in (K, V))
+    c = fc.Cache.empty(1, 10, 16, 1, d, 1, 10)
+    start = i32([0])
+    fc.ficoco_cache_reserve(ctx, c, start, n)
+    fc.ficoco_cache_append(ctx, c, 0, K, V, start)
+    k, v = (torch.zeros(1, 1, n, d, device="cuda") for _ in range(2))
+    fc.ficoco_cache_read(ctx, c, 0, k, v)
+    before = n_q - (n - at)
+    for paged in (True, False):
+        out = torch.zeros_like(Q)
+        if paged:
+            fc.ficoco_cache_attention(ctx, c, 0, Q, out, fc.attention_workspace(c, Q, out))
+        else:
+            fc.ficoco_window_attention(ctx, Q, K, V, out)
+        k64, v64 = ((k, v) if paged else (K, V))
+        check(out[:, :, :before], Q[:, :, :before], k64.double().cpu().numpy(), v64.double().cpu().numpy(), [n], 0.125, [n - n_q], [before], 0, 0, 2)
+        if paged and bad == bad:
+            check(out, Q, k64.double().cpu().numpy(), v64.double().cpu().numpy(), [n], 0.125, [n - n_q], [n_q], 0, 0, 2)
+        elif bad != bad:
+            assert out[:, :, before:].isnan().all()
+
+
+def test_refusals(ctx):
+    c = fc.Cache.empty(2, 10, 16, 2, 64, 4, 4)
+    before = [getattr(c, name).clone() for name in ARRAYS]
+    K, V = rows(1, 2, 2, 8, 64), rows(2, 2, 2, 8, 64)
+    Q, out = rows(3, 2, 4, 1, 64), torch.full((2, 4, 1, 64), 5.0, dtype=torch.bfloat16, device="cuda")
+    two, keep = i32([0, 1]), i32([[0, 1]] * 2)
+    ws, cws = fc.attention_workspace(c, Q, out), fc.cache_workspace(c, 2)
+
+    def space(n=None, off=0, of=ws):
+        w = fc.Workspace(of.bytes if n is None else n, "cuda")
+        w.ptr += off
+        return w
+
+    flat = torch.zeros(4096, dtype=torch.bfloat16, device="cuda")
+    pages = c.k.view(torch.bfloat16).flatten()
+    crossed = flat.as_strided((2, 4, 2, 64), (512, 64, 64, 1))           # two rows of a head are rows of its neighbours
+    attend = lambda **kw: fc.ficoco_cache_attention(ctx, c, kw.pop("layer", 0), kw.pop("Q", Q), kw.pop("O", out), kw.pop("ws", ws), **kw)
+    window = lambda **kw: fc.ficoco_window_attention(ctx, kw.pop("Q", Q), kw.pop("K", K), kw.pop("V", V), kw.pop("O", out), **kw)
+    compact = lambda *a, src=two, dst=two, keep=keep, ws=cws: fc.ficoco_cache_compact(ctx, c, *a[:2], src, dst, *a[2:], keep, i32([0, 0]), ws)
+    refused = [
+        (fc.EUNSUPPORTED, lambda: fc.ficoco_cache_reserve(ctx, c, i32([0] * 1025), 1)),
+        (fc.EINVAL, lambda: fc.ficoco_cache_reserve(ctx, c, i32([0]), -1)),
+        (fc.EINVAL, lambda: fc.ficoco_cache_append(ctx, c, 2, K, V, two)),
+        (fc.EINVAL, lambda: fc.ficoco_cache_append(ctx, c, -1, K, V, two)),
+        (fc.EINVAL, lambda: fc.ficoco_cache_append(ctx, c, 0, K, None, two)),
+        (fc.EINVAL, lambda: fc.ficoco_cache_append(ctx, c, 0, K, V, None)),
+        (fc.EINVAL, lambda: fc.ficoco_cache_read(ctx, c, 2, K, V)),
+        (fc.EINVAL, lambda: fc.ficoco_cache_read(ctx, c, 0, K, K)),
+        (fc.EINVAL, lambda: fc.ficoco_cache_read(ctx, c, 0, K[:, :, :1].expand(2, 2, 8, 64), None)),
+        (fc.EINVAL, lambda: fc.ficoco_cache_read(ctx, c, 0, None, flat.as_strided((2, 2, 8, 64), (1024, 64, 64, 1)))),
+        (fc.EUNSUPPORTED, lambda: fc.ficoco_cache_read(ctx, c, 0, flat.as_strided((32768, 2, 1, 64), (0, 64, 64, 1)), None)),
+        (fc.EINVAL, lambda: fc.ficoco_cache_fork(ctx, c, None, two, i32([0, 0]))),
+        (fc.EINVAL, lambda: fc.ficoco_cache_fork(ctx, c, two, None, i32([0, 0]))),
+        (fc.EUNSUPPORTED, lambda: fc.ficoco_cache_fork(ctx, c, i32([0] * 1025), i32([1] * 1025), i32([0] * 1025))),
+        (fc.EINVAL, lambda: compact(0, 3, 0, 4)), (fc.EINVAL, lambda: compact(-1, 1, 0, 4)), (fc.EINVAL, lambda: compact(0, 2, -1, 4)),
+        (fc.EINVAL, lambda: compact(0, 2, 0, 1)), (fc.EINVAL, lambda: compact(0, 2, 2 ** 31 - 2, 4)), (fc.EINVAL, lambda: compact(0, 2, 0, 4, src=None)),
+        (fc.EINVAL, lambda: compact(0, 2, 0, 4, ws=space(of=cws, off=16))), (fc.ENOMEM, lambda: compact(0, 2, 0, 4, ws=space(32))),
+        (fc.EINVAL, lambda: attend(layer=2)), (fc.EINVAL, lambda: attend(layer=-1)), (fc.EINVAL, lambda: attend(ws=space(off=16))),
+        (fc.ENOMEM, lambda: attend(ws=space(8))), (fc.EINVAL, lambda: attend(scale=0.0)),
+        (fc.EINVAL, lambda: attend(scale=float("inf"))), (fc.EINVAL, lambda: attend(window=-1)), (fc.EINVAL, lambda: attend(sinks=-1)),
+        (fc.EINVAL, lambda: attend(max_len=-5)), (fc.EINVAL, lambda: attend(O=Q)), (fc.EINVAL, lambda: attend(O=pages[:512].view(2, 4, 1, 64))),
+        (fc.EINVAL, lambda: attend(O=out[:, :1].expand(2, 4, 1, 64))), (fc.EINVAL, lambda: attend(Q=Q[:, :3], O=out[:, :3])),
+        (fc.EINVAL, lambda: attend(Q=rows(1, 2, 4, 2, 64), O=crossed)), (fc.EINVAL, lambda: attend(Q=Q[..., :32], O=out[..., :32])),
+        (fc.EINVAL, lambda: window(O=Q)), (fc.EINVAL, lambda: window(scale=-1.0)),
+        (fc.EINVAL, lambda: window(Q=Q[:, :2], O=V[:, :, :1])), (fc.EINVAL, lambda: window(Q=rows(1, 2, 4, 2, 64), O=crossed)),
+        (fc.EUNSUPPORTED, lambda: window(Q=Q[..., :32], K=K[..., :32], V=V[..., :32], O=out[..., :32])),
+        (fc.EUNSUPPORTED, lambda: window(K=K[:, :, :1].expand(2, 2, (1 << 30) + 1, 64), V=V[:, :, :1].expand(2, 2, (1 << 30) + 1, 64))),
+    ]
+    for i, (code, call) in enumerate(refused):
+        with pytest.raises(fc.FicocoError) as err:
+            call()
+        assert err.value.code == code and str(err.value), i
+    for call in (lambda: fc.ficoco_cache_append(ctx, c, 0, K.cpu(), V.cpu(), two), lambda: fc.ficoco_cache_append(ctx, c, 0, K, V, two.cpu()),
+                 lambda: fc.ficoco_cache_append(ctx, c, 0, K.half(), V.half(), two), lambda: fc.ficoco_cache_append(ctx, c, 0, K, V.float(), two),
+                 lambda: fc.ficoco_cache_append(ctx, c, 0, K[..., ::2], V[..., ::2], two), lambda: fc.ficoco_cache_append(ctx, c, 0, K, V, two[:1]),
+                 lambda: fc.ficoco_cache_reserve(ctx, c, two.long(), 1), lambda: attend(Q=Q.cpu(), O=out.cpu()), lambda: attend(O=out.float()),
+                 lambda: attend(seq=two.cpu()), lambda: window(K=K[:1], V=V[:1]), lambda: window(V=V[:, :1]), lambda: compact(0, 2, 0, 4, keep=keep[0])):
+        with pytest.raises(TypeError):
+            call()
+    # nothing to do
+    fc.ficoco_cache_reserve(ctx, c, i32([]), 1)
+    fc.ficoco_cache_append(ctx, c, 0, K[:0], V[:0], i32([]))
+    fc.ficoco_cache_append(ctx, c, 0, K[:, :, :0], V[:, :, :0], two)
+    fc.ficoco_cache_fork(ctx, c, i32([]), i32([]), i32([]))
+    fc.ficoco_cache_free(ctx, c, i32([]))
+    attend(Q=Q[:0], O=out[:0])
+    window(Q=Q[:, :, :0], O=out[:, :, :0])
+    torch.cuda.synchronize()
+    for name, t in zip(ARRAYS, before):
+        assert torch.equal(getattr(c, name), t), name
+    assert (out == 5).all()
+    window(K=K[:, :, :0], V=V[:, :, :0])                         # no keys: zeros
+    attend()
+    assert not out.any()
