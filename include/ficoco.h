@@ -397,7 +397,7 @@ int ficoco_v_step_static(ficoco_ctx *ctx, const ficoco_problem *p, void *X_out, 
  * entries that are out of range, or that name a slot a second time where that has no meaning, are left out as each
  * function says; page numbers out of range are taken for -1.  Limits: page_size 16, 32, 64 or 128; d_head 64 or 128
  * (others FICOCO_EUNSUPPORTED); n_seqs <= 8192; at most 2^30 tokens in a sequence or a call, at most 1024 sequences in a call of
- * reserve, fork or compact.
+ * reserve, fork or compact, whose rows of the table have room for less than 2^31 pages together.
  */
 typedef struct {
   int32_t layers, n_pages, page_size, heads, d_head, n_seqs, max_pages;

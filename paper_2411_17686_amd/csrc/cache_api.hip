@@ -42,6 +42,9 @@ const char* cache_fault(const ficoco_cache& c, int* code) {
   return nullptr;
 }
 
+// The pages that a call can ask for are counted in 32 bits.
+bool too_many_pages(const ficoco_cache& c, int32_t n) { return (int64_t)n * c.max_pages > 0x7fffffff; }
+
 int begin(ficoco_ctx* ctx, const ficoco_cache* c, const char* fn) {
   if (!ctx) return FICOCO_EINVAL;
   if (!c) return fail(ctx, FICOCO_EINVAL, fn, "cache is NULL");
@@ -52,9 +55,10 @@ int begin(ficoco_ctx* ctx, const ficoco_cache* c, const char* fn) {
   return why ? fail(ctx, code, fn, why) : FICOCO_OK;
 }
 
-int check_count(ficoco_ctx* ctx, int32_t n, const char* fn) {
+int check_count(ficoco_ctx* ctx, const ficoco_cache& c, int32_t n, const char* fn) {
   if (n < 0) return fail(ctx, FICOCO_EINVAL, fn, "n is negative");
   if (n > kMaxCall) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "more than 1024 sequences in a call");
+  if (too_many_pages(c, n)) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "the rows of the table of a call have room for 2^31 pages or more");
   return FICOCO_OK;
 }
 
@@ -152,7 +156,7 @@ int ficoco_cache_reserve(ficoco_ctx* ctx, const ficoco_cache* c, int32_t n, cons
                          int32_t* start, void* stream) {
   const char* fn = "ficoco_cache_reserve";
   int rc = begin(ctx, c, fn);
-  if (rc == FICOCO_OK) rc = check_count(ctx, n, fn);
+  if (rc == FICOCO_OK) rc = check_count(ctx, *c, n, fn);
   if (rc != FICOCO_OK || n == 0) return rc;
   if (!start) return fail(ctx, FICOCO_EINVAL, fn, "start is NULL");
   if (!n_new && n_each < 0) return fail(ctx, FICOCO_EINVAL, fn, "n_each is negative");
@@ -182,7 +186,7 @@ int ficoco_cache_fork(ficoco_ctx* ctx, const ficoco_cache* c, int32_t n, const i
                       void* stream) {
   const char* fn = "ficoco_cache_fork";
   int rc = begin(ctx, c, fn);
-  if (rc == FICOCO_OK) rc = check_count(ctx, n, fn);
+  if (rc == FICOCO_OK) rc = check_count(ctx, *c, n, fn);
   if (rc != FICOCO_OK || n == 0) return rc;
   if (!src || !dst || !done) return fail(ctx, FICOCO_EINVAL, fn, "a pointer is NULL");
   if ((int64_t)c->layers * c->heads > kMaxGridY) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "more than 65535 heads in all layers");
@@ -194,6 +198,7 @@ int ficoco_cache_workspace_bytes(const ficoco_cache* c, int32_t n, size_t* out_b
   if (!c || !out_bytes || n < 0 || n > kMaxCall) return FICOCO_EINVAL;
   int code;
   if (cache_fault(*c, &code)) return code;
+  if (too_many_pages(*c, n)) return FICOCO_EUNSUPPORTED;
   *out_bytes = std::max<size_t>(256, compact_workspace(*c, n));
   return FICOCO_OK;
 }
@@ -203,7 +208,7 @@ int ficoco_cache_compact(ficoco_ctx* ctx, const ficoco_cache* c, int32_t layer_b
                          size_t ws_bytes, void* stream) {
   const char* fn = "ficoco_cache_compact";
   int rc = begin(ctx, c, fn);
-  if (rc == FICOCO_OK) rc = check_count(ctx, n, fn);
+  if (rc == FICOCO_OK) rc = check_count(ctx, *c, n, fn);
   if (rc != FICOCO_OK) return rc;
   if (layer_begin < 0 || n_layers < 0 || (int64_t)layer_begin + n_layers > c->layers) return fail(ctx, FICOCO_EINVAL, fn, "no such layers");
   if (vis_begin < 0 || N < 0 || n_keep < 0 || n_keep > N || (int64_t)vis_begin + N > 0x7fffffff)

@@ -21,8 +21,13 @@ template <int D> __device__ __forceinline__ int value_swizzle(int row) { return 
 
 // As tile_rows_kernel (tile_attn.hip): 128 rows a workgroup, 32 a wavefront, 64 keys a step, 32 x 32 x 16 products, a step's weights formed
 // beside the products of the next step's logits.  Pages go straight into LDS as bytes, three steps ahead, and become bfloat16 (exactly, with
-// their block's scale) in front of the products, in every wavefront: that costs 128 conversions of 2 cycles a step and saves the registers and
-// the second trip through LDS that a common conversion takes (question of 64 tokens behind 1251 .. 2400, 8 sequences, 32 heads on 8: 49 us so).
+// their block's scale) in front of the products, in every wavefront: that costs 128 conversions of 2 ns a step and saves the registers and
+// the second trip through LDS that a common conversion takes.
+//
+// Bound by the vector instructions beside the products: a step of a wavefront is 0.53 us of products and about as much of conversions, exponentials
+// and sums, and takes 1.05 us with two wavefronts a SIMD.  Questions of 64 tokens behind 1251 .. 2400, 8 sequences, 32 heads on 8: 34 us (a third of it
+// before the first step and after the last), 8 more for the join.  Sixty-four rows a wavefront, one wavefront a SIMD, halve the conversions,
+// but operands then pass through accumulation registers: 73 us instead of 40.
 template <int D>
 __global__ __launch_bounds__(kTileThreads, 2) void page_rows_kernel(AttendArgs a) {
   constexpr int DT = D / 32, KS = D / 16, CH = D / 16;

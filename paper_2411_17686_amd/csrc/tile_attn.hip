@@ -25,6 +25,10 @@ template <int D> struct TileRaw { uint4 x[D / 32]; };       // a thread's share 
 //   O^T[feature][row] += V^T P^T, the contraction in the order in which the lanes hold the weights; V^T out of LDS by transposing reads
 // A step's weights are formed beside the products of the next step's logits: exponentials and products of one wavefront otherwise take
 // turns.  So keys are in LDS a step ahead of the values; either in two buffers, what comes next on its way while a step is computed.
+//
+// Bound by the matrix cores at the clock that they leave (1.9 GHz): 16384 tokens, window of 4096, 32 heads of 128 on 8: 910 .. 940 us, 1.03 PFLOP/s of
+// products (a large library product reaches 1.2); without its loads it would take 714, without exponentials 843.  Two prompts of 675 tokens, 32 heads: 23 us, of
+// which 5 before the first step.
 template <int D, TileSource SRC>
 __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a) {
   constexpr int DT = D / 32, KS = D / 16, CH = D / 8;
@@ -289,6 +293,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
 
 void launch_dense_rows(const AttendArgs& a, int d_head, hipStream_t s) {
   const dim3 grid((unsigned)xcd_padded_total(a.B * a.H_kv * a.row_tiles)), threads(kTileThreads);
+  // (straight into LDS: no registers, and no waiting for them.  16384 tokens 940 us, through registers 1259; two prompts of 675 tokens 23.6, 30.5)
   const bool direct = (((uintptr_t)a.K | (uintptr_t)a.V) & 15) == 0 && ((a.k_sb | a.k_sh | a.k_sn | a.v_sb | a.v_sh | a.v_sn) & 7) == 0 &&
                       a.k_sn < (1 << 23) && a.v_sn < (1 << 23);
   if (d_head == 128) {

@@ -120,3 +120,10 @@ def test_binding_checks_types_and_shapes():
     with pytest.raises(fc.FicocoError) as e:
         fc.attention_workspace(c, Q, Q)
     assert e.value.code == fc.EINVAL
+
+
+def test_pages_of_a_call_are_counted_in_32_bits():
+    L = fc.lib()
+    large = dict(max_pages=1 << 21, page_size=16)
+    assert _bytes(L.ficoco_cache_workspace_bytes, C.byref(_cache(**large)), 1023)[0] == fc.OK
+    assert _bytes(L.ficoco_cache_workspace_bytes, C.byref(_cache(**large)), 1024)[0] == fc.EUNSUPPORTED

@@ -436,6 +436,11 @@ def test_refusals(ctx):
         (fc.EUNSUPPORTED, lambda: window(Q=Q[..., :32], K=K[..., :32], V=V[..., :32], O=out[..., :32])),
         (fc.EUNSUPPORTED, lambda: window(K=K[:, :, :1].expand(2, 2, (1 << 30) + 1, 64), V=V[:, :, :1].expand(2, 2, (1 << 30) + 1, 64))),
     ]
+    wide = fc.Cache.empty(1, 1, 16, 1, 64, 1, 1)                 # (described wider than it is: refused before anything is read)
+    wide.c.max_pages = 1 << 21
+    many = i32([0] * 1024)
+    refused += [(fc.EUNSUPPORTED, lambda: fc.ficoco_cache_reserve(ctx, wide, many, 1)),
+                (fc.EUNSUPPORTED, lambda: fc.ficoco_cache_fork(ctx, wide, many, many, many))]
     for i, (code, call) in enumerate(refused):
         with pytest.raises(fc.FicocoError) as err:
             call()
