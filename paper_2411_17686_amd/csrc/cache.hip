@@ -174,7 +174,7 @@ __device__ __forceinline__ Span span_of(const ficoco_cache& c, int b, int n_max,
 }
 
 // One workgroup per touched page, head, sequence and K / V: the new tokens' largest magnitude, then all of them.  GPT: groups of
-// eight values a thread.  The tokens are on their way before the page is looked up.
+// sixteen values a thread.  The tokens are on their way before the page is looked up.
 //
 // Bound by memory (8 prompts of up to 2979 tokens, 8 heads of 128, bfloat16, 107 MB: 31 us).
 template <typename T, int GPT>
@@ -182,20 +182,24 @@ __global__ __launch_bounds__(kMoveThreads) void cache_append_kernel(ficoco_cache
                                                                     const int32_t* __restrict__ seq, const int32_t* __restrict__ start,
                                                                     const int32_t* __restrict__ n_new) {
   __shared__ float scratch[kMoveThreads / kWave];
-  const int b = blockIdx.z >> 1, h = blockIdx.y, shift = __builtin_ctz(c.page_size), P = 1 << shift, row_shift = __builtin_ctz(c.d_head / 8);
+  const int b = blockIdx.z >> 1, h = blockIdx.y, shift = __builtin_ctz(c.page_size), P = 1 << shift, row_shift = __builtin_ctz(c.d_head / 16);
   const TokenSide& side = blockIdx.z & 1 ? vs : ks;
   const Span sp = span_of(c, b, n_max, seq, start, n_new);
   const int64_t at = (sp.first >> shift) + (int64_t)blockIdx.x, pos0 = at << shift;
   if (sp.first < 0 || pos0 >= sp.stop || at >= c.max_pages) return;
   const T* x = (const T*)side.x + (int64_t)b * side.sb + (int64_t)h * side.sh;
-  float v[GPT][8];
+  float v[GPT][2][8];
 #pragma unroll
   for (int j = 0; j < GPT; ++j) {
     const int g = threadIdx.x + j * kMoveThreads, row = g >> row_shift;
     const int64_t pos = pos0 + row;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[j][i] = 0.0f;
-    if (row < P && pos >= sp.first && pos < sp.stop) load8f(x + (pos - sp.first) * side.sn + (g & ((1 << row_shift) - 1)) * 8, v[j]);
+    for (int i = 0; i < 8; ++i) v[j][0][i] = v[j][1][i] = 0.0f;
+    if (row < P && pos >= sp.first && pos < sp.stop) {
+      const T* from = x + (pos - sp.first) * side.sn + (g & ((1 << row_shift) - 1)) * 16;
+      load8f(from, v[j][0]);
+      load8f(from + 8, v[j][1]);
+    }
   }
   const int page = c.table[(int64_t)sp.slot * c.max_pages + at];
   if (!page_ok(c, page)) return;
@@ -206,7 +210,7 @@ __global__ __launch_bounds__(kMoveThreads) void cache_append_kernel(ficoco_cache
 #pragma unroll
   for (int j = 0; j < GPT; ++j) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_magnitude(v[j][i]));
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, finite_magnitude(v[j][i / 8][i % 8]));
   }
   int e = block_exponent(block_max(top, scratch));
   e = e > old ? e : old;
@@ -217,15 +221,15 @@ __global__ __launch_bounds__(kMoveThreads) void cache_append_kernel(ficoco_cache
     const int g = threadIdx.x + j * kMoveThreads, row = g >> row_shift;
     const int64_t pos = pos0 + row;
     if (row >= P || pos >= sp.stop) continue;
-    uint8_t* to = pool + (int64_t)g * 8;
+    uint4* to = (uint4*)(pool + (int64_t)g * 16);
     if (pos < sp.first) {
       if (e == old) continue;
-      uint2 q;
-      __builtin_memcpy(&q, to, 8);
-      from_e4m3(q, exp_scale(old), v[j]);
+      const uint4 q = *to;
+      from_e4m3(uint2{q.x, q.y}, exp_scale(old), v[j][0]);
+      from_e4m3(uint2{q.z, q.w}, exp_scale(old), v[j][1]);
     }
-    const uint2 q = to_e4m3(v[j], inv);
-    __builtin_memcpy(to, &q, 8);
+    const uint2 q0 = to_e4m3(v[j][0], inv), q1 = to_e4m3(v[j][1], inv);
+    *to = uint4{q0.x, q0.y, q1.x, q1.y};
   }
   if (threadIdx.x == 0) side.exps[block] = (uint8_t)e;
 }
@@ -596,11 +600,10 @@ void append_groups(const ficoco_cache& c, int layer, const ficoco_tokens& t, hip
   }
   const int touched = (t.n_max + c.page_size - 2) / c.page_size + 1;
   const dim3 grid(touched, c.heads, 2 * t.n);
-  const int groups = c.page_size * c.d_head / 8;
+  const int groups = c.page_size * c.d_head / 16;
   if (groups <= 256) hipLaunchKernelGGL((cache_append_kernel<T, 1>), grid, dim3(kMoveThreads), 0, s, c, lp, k, v, t.n_max, t.seq, t.start, t.n_new);
   else if (groups <= 512) hipLaunchKernelGGL((cache_append_kernel<T, 2>), grid, dim3(kMoveThreads), 0, s, c, lp, k, v, t.n_max, t.seq, t.start, t.n_new);
-  else if (groups <= 1024) hipLaunchKernelGGL((cache_append_kernel<T, 4>), grid, dim3(kMoveThreads), 0, s, c, lp, k, v, t.n_max, t.seq, t.start, t.n_new);
-  else hipLaunchKernelGGL((cache_append_kernel<T, 8>), grid, dim3(kMoveThreads), 0, s, c, lp, k, v, t.n_max, t.seq, t.start, t.n_new);
+  else hipLaunchKernelGGL((cache_append_kernel<T, 4>), grid, dim3(kMoveThreads), 0, s, c, lp, k, v, t.n_max, t.seq, t.start, t.n_new);
 }
 
 }  // namespace
