@@ -9,14 +9,14 @@
 namespace ficoco {
 namespace {
 
-constexpr int kPlanThreads = kMaxCall;
+constexpr int kMaxPlanThreads = kMaxCall;
 constexpr int kNone = 0x7fffffff;
 constexpr int kMoveThreads = 256;
 
 struct PlanLds {
   int owner[kMaxSlots];      // the first entry of the call that names a slot
   int end[kMaxCall];         // pages needed by entries 0 .. b
-  int scratch[kPlanThreads / kWave];
+  int scratch[kMaxPlanThreads / kWave];
   int served;
 };
 
@@ -25,9 +25,9 @@ __device__ __forceinline__ bool page_ok(const ficoco_cache& c, int p) { return p
 __device__ __forceinline__ int pages_of(const ficoco_cache& c, int64_t tokens) { return (int)((tokens + c.page_size - 1) / c.page_size); }
 
 // owner[s] = the first entry b of the call with slot(b) == s
-template <typename F>
+template <int NT, typename F>
 __device__ __forceinline__ void find_owners(const ficoco_cache& c, PlanLds& l, int n, F slot) {
-  for (int i = threadIdx.x; i < c.n_seqs; i += kPlanThreads) l.owner[i] = kNone;
+  for (int i = threadIdx.x; i < c.n_seqs; i += NT) l.owner[i] = kNone;
   if (threadIdx.x == 0) l.served = 0;
   __syncthreads();
   if ((int)threadIdx.x < n) {
@@ -51,10 +51,10 @@ __device__ __forceinline__ int free_mask(const ficoco_cache& c, int i0) {
   return m;
 }
 
-// `first_mask`: free_mask() of this thread's pages among the first 8 * kPlanThreads, read ahead of the rest of the plan.
+// `first_mask`: free_mask() of this thread's pages among the first 8 * NT, read ahead of the rest of the plan.
 // Every entry's thread (tid < n, others need = 0) asks for `need` pages; take(b, k, page) gets page k of entry b, the free pages
 // in ascending order.  Entries are served in order as long as the pages last.  Returns whether this thread's entry is.
-template <typename F>
+template <int NT, typename F>
 __device__ __forceinline__ bool hand_out(const ficoco_cache& c, PlanLds& l, int n, int need, int first_mask, F take) {
   int total;
   const int end = block_scan_inclusive(need, l.scratch, &total);
@@ -62,7 +62,7 @@ __device__ __forceinline__ bool hand_out(const ficoco_cache& c, PlanLds& l, int 
   if (total == 0) return true;                            // (uniform)
   int n_free;
   const int first_rank = block_scan_inclusive(__popc(first_mask), l.scratch, &n_free) - __popc(first_mask), first_free = n_free;
-  for (int base = 8 * kPlanThreads; base < c.n_pages && n_free < total; base += 8 * kPlanThreads) {
+  for (int base = 8 * NT; base < c.n_pages && n_free < total; base += 8 * NT) {
     int t;
     (void)block_scan_inclusive(__popc(free_mask(c, base + 8 * (int)threadIdx.x)), l.scratch, &t);
     n_free += t;
@@ -72,7 +72,7 @@ __device__ __forceinline__ bool hand_out(const ficoco_cache& c, PlanLds& l, int 
   __syncthreads();
   const int give = l.served;
   int given = 0;
-  for (int base = 0; base < c.n_pages && given < give; base += 8 * kPlanThreads) {
+  for (int base = 0; base < c.n_pages && given < give; base += 8 * NT) {
     const int i0 = base + 8 * (int)threadIdx.x, m = base == 0 ? first_mask : free_mask(c, i0);
     int t = first_free, r = first_rank;
     if (base > 0) r = given + block_scan_inclusive(__popc(m), l.scratch, &t) - __popc(m);
@@ -93,13 +93,14 @@ __device__ __forceinline__ bool hand_out(const ficoco_cache& c, PlanLds& l, int 
   return ok;
 }
 
-__global__ __launch_bounds__(kPlanThreads) void cache_reserve_kernel(ficoco_cache c, int n, const int32_t* __restrict__ seq,
+template <int NT>
+__global__ __launch_bounds__(NT) void cache_reserve_kernel(ficoco_cache c, int n, const int32_t* __restrict__ seq,
                                                                      const int32_t* __restrict__ n_new, int n_each, int32_t* __restrict__ start) {
   __shared__ PlanLds l;
   __shared__ int slot[kMaxCall], have[kMaxCall];
   const int b = threadIdx.x, first_mask = free_mask(c, 8 * (int)threadIdx.x);
   auto slot_of = [&](int i) { return seq ? seq[i] : i; };
-  find_owners(c, l, n, slot_of);
+  find_owners<NT>(c, l, n, slot_of);
   int need = 0, len = 0, add = 0;
   bool ok = false;
   if (b < n) {
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_reserve_kernel(ficoco_cach
     slot[b] = s;
   }
   __syncthreads();
-  const bool served = hand_out(c, l, n, need, first_mask, [&](int e, int k, int page) {
+  const bool served = hand_out<NT>(c, l, n, need, first_mask, [&](int e, int k, int page) {
     c.table[(int64_t)slot[e] * c.max_pages + have[e] + k] = page;
     c.refs[page] = 1;
   });
@@ -304,12 +305,13 @@ __global__ __launch_bounds__(kMoveThreads) void cache_read_kernel(ficoco_cache c
 }
 
 // ---- fork -------------------------------------------------------------------------------------------------------
-__global__ __launch_bounds__(kPlanThreads) void cache_fork_kernel(ficoco_cache c, int n, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
+template <int NT>
+__global__ __launch_bounds__(NT) void cache_fork_kernel(ficoco_cache c, int n, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
                                                                   int whole, int32_t* __restrict__ done) {
   __shared__ PlanLds l;
-  __shared__ int from[kMaxCall], to[kMaxCall], shared[kMaxCall];
+  __shared__ int to[kMaxCall], shared[kMaxCall];
   const int b = threadIdx.x, first_mask = free_mask(c, 8 * (int)threadIdx.x);
-  find_owners(c, l, n, [&](int i) { return dst[i]; });
+  find_owners<NT>(c, l, n, [&](int i) { return dst[i]; });
   int need = 0, len = 0;
   bool ok = false;
   if (b < n) {
@@ -319,37 +321,35 @@ __global__ __launch_bounds__(kPlanThreads) void cache_fork_kernel(ficoco_cache c
       len = c.len[s];
       ok = c.len[d] == 0 && len >= 0 && pages_of(c, len) <= c.max_pages;
     }
-    from[b] = s;
     to[b] = d;
     shared[b] = ok && !whole ? len / c.page_size : 0;
     need = ok ? pages_of(c, len) - shared[b] : 0;
   }
   __syncthreads();
-  const bool served = ok & hand_out(c, l, n, need, first_mask, [&](int e, int k, int page) {
+  const bool served = ok & hand_out<NT>(c, l, n, need, first_mask, [&](int e, int k, int page) {
     c.table[(int64_t)to[e] * c.max_pages + shared[e] + k] = page;
     c.refs[page] = 1;
   });
   if (b < n) {
     if (served) c.len[to[b]] = len;
     done[b] = served;
-    if (!served) shared[b] = 0;
-  }
-  __syncthreads();                                         // (also: the scans are over before refs change below)
-  for (int e = threadIdx.x / kWave; e < n; e += kPlanThreads / kWave) {
-    for (int i = threadIdx.x % kWave; i < shared[e]; i += kWave) {
-      const int page = c.table[(int64_t)from[e] * c.max_pages + i];
-      c.table[(int64_t)to[e] * c.max_pages + i] = page;
-      if (page_ok(c, page)) atomicAdd(&c.refs[page], 1);
-    }
   }
 }
 
-// Whole pages of all layers, as they are.  Workgroups of one sequence, layer, head and K / V walk its copied pages.
+// Whole pages of all layers, as they are.  Workgroups of one sequence, layer, head and K / V walk its copied pages; one of a sequence's has its
+// shared ones entered (by the plan's one workgroup: 128 sequences of ten pages 27 us instead of 22).
 __global__ __launch_bounds__(kMoveThreads) void cache_copy_kernel(ficoco_cache c, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
                                                                   int whole, const int32_t* __restrict__ done) {
   const int b = blockIdx.z >> 1;
   if (!done[b]) return;
   const int from = src[b], to = dst[b], len = c.len[to], pages = pages_of(c, len);
+  if (!whole && (blockIdx.x | blockIdx.y | blockIdx.z & 1) == 0) {
+    for (int i = threadIdx.x; i < len / c.page_size; i += kMoveThreads) {
+      const int page = c.table[(int64_t)from * c.max_pages + i];
+      c.table[(int64_t)to * c.max_pages + i] = page;
+      if (page_ok(c, page)) atomicAdd(&c.refs[page], 1);
+    }
+  }
   const int layer = blockIdx.y / c.heads, h = blockIdx.y % c.heads;
   uint8_t* pool = (uint8_t*)(blockIdx.z & 1 ? c.v : c.k);
   uint8_t* exps = blockIdx.z & 1 ? c.v_exp : c.k_exp;
@@ -366,17 +366,18 @@ __global__ __launch_bounds__(kMoveThreads) void cache_copy_kernel(ficoco_cache c
 }
 
 // ---- compact ------------------------------------------------------------------------------------------------------
-struct CompactMeta { int first, pages, tokens, pad; };
+struct CompactMeta { int first, pages, tokens, had; };      // pages kept, pages and tokens now, pages before (0: not served)
 
-__global__ __launch_bounds__(kPlanThreads) void cache_compact_plan_kernel(ficoco_cache c, int n, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
+template <int NT>
+__global__ __launch_bounds__(NT) void cache_compact_plan_kernel(ficoco_cache c, int n, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
                                                                           int vis_begin, int N, int n_keep, const int32_t* __restrict__ keep_idx,
                                                                           int32_t* __restrict__ done, CompactMeta* __restrict__ meta, int32_t* __restrict__ rows) {
   __shared__ PlanLds l;
-  __shared__ int from[kMaxCall], to[kMaxCall], moved[kMaxCall], first[kMaxCall], had[kMaxCall], now[kMaxCall];
+  __shared__ int from[kMaxCall], to[kMaxCall], moved[kMaxCall], first[kMaxCall], had[kMaxCall];
   const int b = threadIdx.x, lane = threadIdx.x % kWave, first_mask = free_mask(c, 8 * (int)threadIdx.x);
-  find_owners(c, l, n, [&](int i) { return dst[i]; });
+  find_owners<NT>(c, l, n, [&](int i) { return dst[i]; });
   // the first preserved token that moves: its rank among the preserved ones
-  for (int e = threadIdx.x / kWave; e < n; e += kPlanThreads / kWave) {
+  for (int e = threadIdx.x / kWave; e < n; e += NT / kWave) {
     const int32_t* k = keep_idx + (int64_t)e * n_keep;
     int at = n_keep;
     for (int i0 = 0; i0 < n_keep; i0 += kWave) {
@@ -390,7 +391,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_compact_plan_kernel(ficoco
     if (lane == 0) moved[e] = at;
   }
   __syncthreads();
-  int need = 0, new_len = 0;
+  int need = 0, new_len = 0, now = 0;
   bool ok = false;
   if (b < n) {
     const int s = src[b], d = dst[b];
@@ -409,39 +410,21 @@ __global__ __launch_bounds__(kPlanThreads) void cache_compact_plan_kernel(ficoco
     to[b] = d;
     first[b] = ok ? f : 0;
     had[b] = ok ? have : 0;
-    now[b] = ok ? pages : 0;
+    now = pages;
     need = ok ? pages - f : 0;
   }
   __syncthreads();
-  for (int e = threadIdx.x / kWave; e < n; e += kPlanThreads / kWave)
+  for (int e = threadIdx.x / kWave; e < n; e += NT / kWave)
     for (int i = lane; i < had[e]; i += kWave) rows[(int64_t)e * c.max_pages + i] = c.table[(int64_t)from[e] * c.max_pages + i];
   __syncthreads();                                         // the rows are saved before new pages go into them
-  const bool served = ok & hand_out(c, l, n, need, first_mask, [&](int e, int k, int page) {
+  const bool served = ok & hand_out<NT>(c, l, n, need, first_mask, [&](int e, int k, int page) {
     c.table[(int64_t)to[e] * c.max_pages + first[e] + k] = page;
     c.refs[page] = 1;
   });
   if (b < n) {
     if (served) c.len[to[b]] = new_len;
     done[b] = served;
-    meta[b] = CompactMeta{first[b], served ? now[b] : 0, new_len, 0};
-    if (!served) had[b] = 0;
-  }
-  __syncthreads();
-  for (int e = threadIdx.x / kWave; e < n; e += kPlanThreads / kWave) {
-    const int32_t* row = rows + (int64_t)e * c.max_pages;
-    const bool in_place = from[e] == to[e];
-    for (int i = lane; i < had[e]; i += kWave) {
-      const int page = row[i];
-      if (i < first[e]) {
-        if (!in_place) {
-          c.table[(int64_t)to[e] * c.max_pages + i] = page;
-          if (page_ok(c, page)) atomicAdd(&c.refs[page], 1);
-        }
-      } else if (in_place) {
-        if (page_ok(c, page)) atomicSub(&c.refs[page], 1);
-        if (i >= now[e]) c.table[(int64_t)to[e] * c.max_pages + i] = -1;
-      }
-    }
+    meta[b] = CompactMeta{first[b], served ? now : 0, new_len, served ? had[b] : 0};
   }
 }
 
@@ -479,7 +462,7 @@ __device__ __forceinline__ uint4 rescale_e4m3(const uint4& q, int from, int to) 
 // after the other, found every block's rows anew, four loads one behind the other: 103 us; so it takes 50 us, 3.9 TB/s.
 template <int NG>
 __global__ __launch_bounds__(kMoveThreads) void cache_compact_kernel(ficoco_cache c, int layer_begin, int blocks, int per_wg, int vis_begin, int N, int n_keep,
-                                                                     const int32_t* __restrict__ dst, const int32_t* __restrict__ keep_idx,
+                                                                     const int32_t* __restrict__ src, const int32_t* __restrict__ dst, const int32_t* __restrict__ keep_idx,
                                                                      const CompactMeta* __restrict__ meta, const int32_t* __restrict__ rows) {
   __shared__ int from_page[128], from_slot[128];
   const int b = blockIdx.z;
@@ -487,6 +470,22 @@ __global__ __launch_bounds__(kMoveThreads) void cache_compact_kernel(ficoco_cach
   const int shift = __builtin_ctz(c.page_size), P = 1 << shift, per_row = c.d_head / 16, block_bytes = P * c.d_head;
   const int lane = threadIdx.x % kWave, wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int first = blockIdx.y * per_wg + wv, end = min(blocks, (int)blockIdx.y * per_wg + per_wg);
+  if ((blockIdx.x | blockIdx.y) == 0) {                    // the pages kept (shared) and those of before (given back)
+    int32_t* row = c.table + (int64_t)dst[b] * c.max_pages;
+    const bool in_place = src[b] == dst[b];
+    for (int i = threadIdx.x; i < m.had; i += kMoveThreads) {
+      const int old = rows[(int64_t)b * c.max_pages + i];
+      if (i < m.first) {
+        if (!in_place) {
+          row[i] = old;
+          if (page_ok(c, old)) atomicAdd(&c.refs[old], 1);
+        }
+      } else if (in_place) {
+        if (page_ok(c, old)) atomicSub(&c.refs[old], 1);
+        if (i >= m.pages) row[i] = -1;
+      }
+    }
+  }
   for (int page_at = m.first + blockIdx.x; page_at < m.pages; page_at += gridDim.x) {
     const int page = c.table[(int64_t)dst[b] * c.max_pages + page_at];
     if ((int)threadIdx.x < P) {
@@ -575,6 +574,11 @@ TokenSide side_of(const ficoco_tokens& t, const ficoco_cache& c, bool v) {
            : TokenSide{t.K, t.k_stride_b, t.k_stride_h, t.k_stride_n, (uint8_t*)c.k, c.k_exp};
 }
 
+// Whether a plan is made by 256 threads instead of 1024: pages that these see at one look, and no more entries than `most`.  Four wavefronts wait less for
+// each other: one prompt shared by 8, 15.6 us instead of 16.6; by 128, 22.3 and 23.3.  Where a wavefront takes one entry after the other (compact), sixteen get
+// on faster: 4 sequences 15.3 and 16.6, 8 17.7 and 18.5, 16 22.2 and 21.9, 64 45 and 38.
+bool small_plan(const ficoco_cache& c, int n, int most = 256) { return n <= most && c.n_pages <= 8 * 256 && c.n_seqs <= 8 * 256; }
+
 // Workgroups that walk the pages of one sequence, layer, head and K / V.
 int page_walkers(const ficoco_cache& c, int64_t others) {
   const int64_t want = (8192 + others - 1) / others;
@@ -582,9 +586,9 @@ int page_walkers(const ficoco_cache& c, int64_t others) {
 }
 
 template <int NG>
-void launch_compact_pages(const ficoco_cache& c, dim3 grid, int layer_begin, int blocks, int per_wg, int vis_begin, int N, int n_keep, const int32_t* dst,
+void launch_compact_pages(const ficoco_cache& c, dim3 grid, int layer_begin, int blocks, int per_wg, int vis_begin, int N, int n_keep, const int32_t* src, const int32_t* dst,
                           const int32_t* keep_idx, const CompactMeta* meta, const int32_t* rows, hipStream_t s) {
-  hipLaunchKernelGGL((cache_compact_kernel<NG>), grid, dim3(kMoveThreads), 0, s, c, layer_begin, blocks, per_wg, vis_begin, N, n_keep, dst, keep_idx, meta, rows);
+  hipLaunchKernelGGL((cache_compact_kernel<NG>), grid, dim3(kMoveThreads), 0, s, c, layer_begin, blocks, per_wg, vis_begin, N, n_keep, src, dst, keep_idx, meta, rows);
 }
 
 template <typename T>
@@ -609,7 +613,8 @@ void append_groups(const ficoco_cache& c, int layer, const ficoco_tokens& t, hip
 }  // namespace
 
 void launch_cache_reserve(const ficoco_cache& c, int n, const int32_t* seq, const int32_t* n_new, int n_each, int32_t* start, hipStream_t s) {
-  hipLaunchKernelGGL(cache_reserve_kernel, dim3(1), dim3(kPlanThreads), 0, s, c, n, seq, n_new, n_each, start);
+  if (small_plan(c, n)) hipLaunchKernelGGL(cache_reserve_kernel<256>, dim3(1), dim3(256), 0, s, c, n, seq, n_new, n_each, start);
+  else hipLaunchKernelGGL(cache_reserve_kernel<kMaxPlanThreads>, dim3(1), dim3(kMaxPlanThreads), 0, s, c, n, seq, n_new, n_each, start);
 }
 
 void launch_cache_append(const ficoco_cache& c, int layer, const ficoco_tokens& t, hipStream_t s) {
@@ -626,7 +631,8 @@ void launch_cache_read(const ficoco_cache& c, int layer, const ficoco_tokens& t,
 }
 
 void launch_cache_fork(const ficoco_cache& c, int n, const int32_t* src, const int32_t* dst, bool whole, int32_t* done, hipStream_t s) {
-  hipLaunchKernelGGL(cache_fork_kernel, dim3(1), dim3(kPlanThreads), 0, s, c, n, src, dst, (int)whole, done);
+  if (small_plan(c, n)) hipLaunchKernelGGL(cache_fork_kernel<256>, dim3(1), dim3(256), 0, s, c, n, src, dst, (int)whole, done);
+  else hipLaunchKernelGGL(cache_fork_kernel<kMaxPlanThreads>, dim3(1), dim3(kMaxPlanThreads), 0, s, c, n, src, dst, (int)whole, done);
   const int walkers = whole ? page_walkers(c, (int64_t)c.layers * c.heads * n * 2) : 1;
   hipLaunchKernelGGL(cache_copy_kernel, dim3(walkers, c.layers * c.heads, 2 * n), dim3(kMoveThreads), 0, s, c, src, dst, (int)whole, done);
 }
@@ -635,20 +641,20 @@ void launch_cache_compact(const ficoco_cache& c, int layer_begin, int n_layers, 
                           int n_keep, const int32_t* keep_idx, int32_t* done, char* ws, hipStream_t s) {
   CompactMeta* meta = (CompactMeta*)ws;
   int32_t* rows = (int32_t*)(ws + (size_t)n * sizeof(CompactMeta));
-  hipLaunchKernelGGL(cache_compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, c, n, src, dst, vis_begin, N, n_keep, keep_idx, done, meta, rows);
-  if (n_layers == 0) return;
+  if (small_plan(c, n, 8)) hipLaunchKernelGGL(cache_compact_plan_kernel<256>, dim3(1), dim3(256), 0, s, c, n, src, dst, vis_begin, N, n_keep, keep_idx, done, meta, rows);
+  else hipLaunchKernelGGL(cache_compact_plan_kernel<kMaxPlanThreads>, dim3(1), dim3(kMaxPlanThreads), 0, s, c, n, src, dst, vis_begin, N, n_keep, keep_idx, done, meta, rows);
   // A wavefront takes up to eight blocks, fewer where the chip would not be filled (1024 workgroups; a sequence's pages count as eight).  One image of 675
   // tokens, 4 layers: one block a wavefront 18 us, eight 35; four sequences of 2979 tokens, 16 layers: 65.8 and 64.2, sixteen 87.
   const int blocks = 2 * n_layers * c.heads, waves = kMoveThreads / kWave;
   const int64_t want = (int64_t)blocks * n * 8 / 1024;
   const int per_wg = (int)(want < waves ? waves : want < 8 * waves ? want / waves * waves : 8 * waves);
-  const dim3 grid(c.max_pages < 64 ? c.max_pages : 64, (blocks + per_wg - 1) / per_wg, n);
+  const dim3 grid(c.max_pages < 64 ? c.max_pages : 64, n_layers == 0 ? 1 : (blocks + per_wg - 1) / per_wg, n);
   switch (c.page_size * c.d_head / 1024) {
-    case 1: launch_compact_pages<1>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, dst, keep_idx, meta, rows, s); break;
-    case 2: launch_compact_pages<2>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, dst, keep_idx, meta, rows, s); break;
-    case 4: launch_compact_pages<4>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, dst, keep_idx, meta, rows, s); break;
-    case 8: launch_compact_pages<8>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, dst, keep_idx, meta, rows, s); break;
-    default: launch_compact_pages<16>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, dst, keep_idx, meta, rows, s); break;
+    case 1: launch_compact_pages<1>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, src, dst, keep_idx, meta, rows, s); break;
+    case 2: launch_compact_pages<2>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, src, dst, keep_idx, meta, rows, s); break;
+    case 4: launch_compact_pages<4>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, src, dst, keep_idx, meta, rows, s); break;
+    case 8: launch_compact_pages<8>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, src, dst, keep_idx, meta, rows, s); break;
+    default: launch_compact_pages<16>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, src, dst, keep_idx, meta, rows, s); break;
   }
 }
 

@@ -467,3 +467,29 @@ def test_refusals(ctx):
     window(K=K[:, :, :0], V=V[:, :, :0])                         # no keys: zeros
     attend()
     assert not out.any()
+
+
+@pytest.mark.parametrize("n,n_pages,n_seqs", [(8, 2048, 40), (9, 2048, 40), (8, 2049, 40), (8, 2048, 2049), (300, 4000, 700)])
+def test_plans_of_either_size(ctx, n, n_pages, n_seqs):
+    """Calls on both sides of the sizes at which a plan is made by fewer threads: reserve, fork, compact in place and into empty slots."""
+    g, h = pair(1, n_pages, 16, 1, 64, n_seqs, 4)
+    order = np.random.RandomState(n).permutation(n_seqs)
+    seq, dst = order[:n].tolist(), order[n:2 * n].tolist()
+    n_new = [int(x) for x in np.random.RandomState(1).randint(20, 60, n)]
+    start, at = reserve(ctx, g, h, seq, n_new)
+    K, V = (torch.randn(n, 1, 60, 64, generator=torch.Generator().manual_seed(i)).to(torch.bfloat16) for i in (1, 2))
+    append(ctx, g, h, 0, K, V, at, n_new, seq)
+    done = i32([7] * n)
+    fc.ficoco_cache_fork(ctx, g, i32(seq), i32(dst), done)
+    assert done.tolist() == h.fork(seq, dst, False)
+    same(g, h)
+    keep = np.sort(np.stack([np.random.RandomState(b).permutation(18)[:7] for b in range(n)]), axis=1).astype(np.int32)
+    fc.ficoco_cache_free(ctx, g, i32(dst[::2]))
+    h.free(dst[::2])
+    into = [d if i % 2 == 0 else s for i, (s, d) in enumerate(zip(seq, dst))]
+    fc.ficoco_cache_compact(ctx, g, 0, 1, i32(seq), i32(into), 2, 18, torch.from_numpy(keep).cuda(), done, fc.cache_workspace(g, n))
+    assert done.tolist() == h.compact([0], seq, into, 2, 18, keep) == [1] * n
+    same(g, h)
+    fc.ficoco_cache_compact(ctx, g, 0, 0, i32(seq), i32(seq), 0, 5, torch.from_numpy(keep[:, :0]).cuda(), done, fc.cache_workspace(g, n))
+    assert done.tolist() == h.compact([], seq, seq, 0, 5, keep[:, :0])
+    same(g, h, content=False)
