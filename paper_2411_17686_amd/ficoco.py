@@ -176,7 +176,8 @@ class Context:
         rc = lib().ficoco_create(C.byref(self._h), int(device))
         if rc != OK:
             raise FicocoError(rc, "ficoco_create failed")
-        self.device = torch.device("cuda", int(device))
+        self.index = int(device)
+        self.device = torch.device("cuda", self.index)
 
     def close(self):
         if self._h:
@@ -202,7 +203,7 @@ class Context:
 
     def raw_stream(self):
         """The same as a number: a decoding step's calls take microseconds, and so does the stream object."""
-        return torch._C._cuda_getCurrentRawStream(self.device.index)
+        return torch._C._cuda_getCurrentRawStream(self.index)
 
 
 def make_problem(X, *, variant, vis_begin, N, n_keep, A=None, a_q_begin=0, a_k_begin=0,
@@ -412,7 +413,7 @@ class Cache:
                 raise TypeError("the tensors of a cache are contiguous, on one device, of the types and shapes in ficoco.h")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self.table, self.len, self.refs = table, length, refs
-        self.device = k.device
+        self.device, self.index, self.heads, self.d_head = k.device, k.get_device(), heads, d_head
         self.c = CacheProblem(layers, n_pages, page_size, heads, d_head, n_seqs, max_pages, k.data_ptr(), v.data_ptr(),
                               k_exp.data_ptr(), v_exp.data_ptr(), table.data_ptr(), length.data_ptr(), refs.data_ptr())
         self._p = C.byref(self.c)
@@ -432,23 +433,23 @@ class Workspace:
 
     def __init__(self, n, device):
         self.t = torch.empty(n + 256, dtype=torch.uint8, device=device)
-        self.bytes, self.device = n, self.t.device
+        self.bytes, self.index = n, self.t.get_device()
         self.ptr = self.t.data_ptr() + (-self.t.data_ptr()) % 256
 
 
-def _i32(t, n, name, device):
-    """Address of n int32 values on `device`, 0 for None."""
+def _i32(t, n, name, index):
+    """Address of n int32 values on device `index`, 0 for None."""
     if t is None:
         return 0
-    if t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous() or t.device != device:
-        raise TypeError("%s must be %d contiguous int32 values on %s" % (name, n, device))
+    if t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous() or t.get_device() != index:
+        raise TypeError("%s must be %d contiguous int32 values on device %d" % (name, n, index))
     return t.data_ptr()
 
 
-def _same_device(ctx, *devices):
-    for d in devices:
-        if d != ctx.device:
-            raise TypeError("a tensor is on %s, the context on %s" % (d, ctx.device))
+def _same_device(ctx, *indices):
+    for i in indices:
+        if i != ctx.index:
+            raise TypeError("a tensor is on device %d, the context on %d" % (i, ctx.index))
 
 
 def cache_workspace(cache, n):
@@ -462,7 +463,7 @@ def cache_workspace(cache, n):
 
 def ficoco_cache_reserve(ctx, cache, start, n_new, seq=None):
     """n_new: tokens of every sequence (int32 tensor), or one number for all."""
-    n, d = start.numel(), cache.device
+    n, d = start.numel(), cache.index
     _same_device(ctx, d)
     each = isinstance(n_new, int)
     rc = lib().ficoco_cache_reserve(ctx._h, cache._p, n, _i32(seq, n, "seq", d), 0 if each else _i32(n_new, n, "n_new", d),
@@ -472,27 +473,28 @@ def ficoco_cache_reserve(ctx, cache, start, n_new, seq=None):
 
 
 def _tokens(ctx, cache, K, V, start, n_new, seq):
-    some = K if K is not None else V
+    some = V if K is None else K
     if some is None:
         raise TypeError("K and V are both None")
-    n, heads, n_max, d = some.shape
-    dev = cache.device
-    if heads != cache.c.heads or d != cache.c.d_head:
+    shape, dtype, index = some.shape, some.dtype, cache.index
+    n, heads, n_max, d = shape
+    if heads != cache.heads or d != cache.d_head:
         raise TypeError("tokens are [n][heads][n_max][d_head] of the cache")
-    _same_device(ctx, dev, some.device)
-    at, strides = [], []
-    for t in (K, V):
-        if t is None:
-            at.append(0)
-            strides += (0, 0, 0)
-            continue
-        st = t.stride()
-        if t is not some and (t.shape != some.shape or t.dtype != some.dtype or t.device != dev) or st[3] != 1:
-            raise TypeError("K and V are of one shape and type, d_head contiguous")
-        at.append(t.data_ptr())
-        strides += st[:3]
-    return _TOKENS.pack(n, n_max, _dtype_code(some), _i32(seq, n, "seq", dev), _i32(start, n, "start", dev),
-                        _i32(n_new, n, "n_new", dev), *at, *strides)
+    _same_device(ctx, index, some.get_device())
+    k_at = kb = kh = kn = v_at = vb = vh = vn = 0
+    k1 = v1 = 1
+    if K is not None:
+        k_at = K.data_ptr()
+        kb, kh, kn, k1 = K.stride()
+    if V is not None:
+        v_at = V.data_ptr()
+        vb, vh, vn, v1 = V.stride()
+        if V is not some and (V.shape != shape or V.dtype != dtype or V.get_device() != index):
+            raise TypeError("K and V are of one shape and type")
+    if k1 != 1 or v1 != 1:
+        raise TypeError("d_head of K and V must be contiguous")
+    return _TOKENS.pack(n, n_max, _dtype_code(some), _i32(seq, n, "seq", index), _i32(start, n, "start", index),
+                        _i32(n_new, n, "n_new", index), k_at, v_at, kb, kh, kn, vb, vh, vn)
 
 
 def ficoco_cache_append(ctx, cache, layer, K, V, start, n_new=None, seq=None):
@@ -509,7 +511,7 @@ def ficoco_cache_read(ctx, cache, layer, K, V, start=None, n_new=None, seq=None)
 
 
 def ficoco_cache_fork(ctx, cache, src, dst, done, whole=False):
-    n, d = done.numel(), cache.device
+    n, d = done.numel(), cache.index
     _same_device(ctx, d)
     rc = lib().ficoco_cache_fork(ctx._h, cache._p, n, _i32(src, n, "src", d), _i32(dst, n, "dst", d), int(whole),
                                  _i32(done, n, "done", d), ctx.raw_stream())
@@ -519,10 +521,10 @@ def ficoco_cache_fork(ctx, cache, src, dst, done, whole=False):
 
 def ficoco_cache_compact(ctx, cache, layer_begin, n_layers, src, dst, vis_begin, N, keep_idx, done, ws):
     """keep_idx [n][n_keep] int32, as the filter of a step leaves it."""
-    n, d = done.numel(), cache.device
+    n, d = done.numel(), cache.index
     if keep_idx.dim() != 2 or keep_idx.shape[0] != n:
         raise TypeError("keep_idx must be [n][n_keep]")
-    _same_device(ctx, d, ws.device)
+    _same_device(ctx, d, ws.index)
     rc = lib().ficoco_cache_compact(ctx._h, cache._p, layer_begin, n_layers, n, _i32(src, n, "src", d), _i32(dst, n, "dst", d),
                                     vis_begin, N, keep_idx.shape[1], _i32(keep_idx, keep_idx.numel(), "keep_idx", d),
                                     _i32(done, n, "done", d), ws.ptr, ws.bytes, ctx.raw_stream())
@@ -532,17 +534,17 @@ def ficoco_cache_compact(ctx, cache, layer_begin, n_layers, src, dst, vis_begin,
 
 def ficoco_cache_free(ctx, cache, seq):
     n = seq.numel()
-    _same_device(ctx, cache.device)
-    rc = lib().ficoco_cache_free(ctx._h, cache._p, n, _i32(seq, n, "seq", cache.device), ctx.raw_stream())
+    _same_device(ctx, cache.index)
+    rc = lib().ficoco_cache_free(ctx._h, cache._p, n, _i32(seq, n, "seq", cache.index), ctx.raw_stream())
     if rc:
         ctx.check(rc)
 
 
 def _attention(Q, O, K, V, scale, window, sinks, q_len, k_len, q_start, seq, max_len):
-    shape, dev = Q.shape, Q.device
+    shape, dev = Q.shape, Q.get_device()
     B, H, n_q, d = shape
     q, o = Q.stride(), O.stride()
-    if O.shape != shape or Q.dtype != torch.bfloat16 or O.dtype != torch.bfloat16 or q[3] != 1 or o[3] != 1 or O.device != dev:
+    if O.shape != shape or Q.dtype != torch.bfloat16 or O.dtype != torch.bfloat16 or q[3] != 1 or o[3] != 1 or O.get_device() != dev:
         raise TypeError("Q and O are bfloat16 [B][H][n_q][d_head], d_head contiguous, on one device")
     if K is None:
         H_kv = n_k = k_at = v_at = 0
@@ -550,7 +552,7 @@ def _attention(Q, O, K, V, scale, window, sinks, q_len, k_len, q_start, seq, max
     else:
         k, v = K.stride(), V.stride()
         if K.shape != V.shape or K.shape[0] != B or K.shape[3] != d or K.dtype != torch.bfloat16 or V.dtype != torch.bfloat16 \
-                or k[3] != 1 or v[3] != 1 or K.device != dev or V.device != dev:
+                or k[3] != 1 or v[3] != 1 or K.get_device() != dev or V.get_device() != dev:
             raise TypeError("K and V are bfloat16 [B][H_kv][n_k][d_head], d_head contiguous, on the device of Q")
         H_kv, n_k, k_at, v_at = K.shape[1], K.shape[2], K.data_ptr(), V.data_ptr()
     return _ATTENTION.pack(B, H, H_kv, n_q, n_k, d, Q.data_ptr(), q[0], q[1], q[2], k_at, v_at, k[0], k[1], k[2], v[0], v[1], v[2],
@@ -572,7 +574,7 @@ def attention_workspace(cache, Q, O, window=0, sinks=0, max_len=0):
 def ficoco_cache_attention(ctx, cache, layer, Q, O, ws, scale=None, window=0, sinks=0, q_len=None, k_len=None,
                            q_start=None, seq=None, max_len=0):
     """Into O; scale None = d_head ** -0.5."""
-    _same_device(ctx, cache.device, Q.device, ws.device)
+    _same_device(ctx, cache.index, Q.get_device(), ws.index)
     rc = lib().ficoco_cache_attention(ctx._h, cache._p, layer,
                                       _attention(Q, O, None, None, scale, window, sinks, q_len, k_len, q_start, seq, max_len),
                                       ws.ptr, ws.bytes, ctx.raw_stream())
@@ -582,7 +584,7 @@ def ficoco_cache_attention(ctx, cache, layer, Q, O, ws, scale=None, window=0, si
 
 def ficoco_window_attention(ctx, Q, K, V, O, scale=None, window=0, sinks=0, q_len=None, k_len=None, q_start=None):
     """Into O; scale None = d_head ** -0.5."""
-    _same_device(ctx, Q.device)
+    _same_device(ctx, Q.get_device())
     rc = lib().ficoco_window_attention(ctx._h, _attention(Q, O, K, V, scale, window, sinks, q_len, k_len, q_start, None, 0),
                                        ctx.raw_stream())
     if rc:
