@@ -543,22 +543,24 @@ def ficoco_cache_free(ctx, cache, seq):
 def _attention(Q, O, K, V, scale, window, sinks, q_len, k_len, q_start, seq, max_len):
     shape, dev = Q.shape, Q.get_device()
     B, H, n_q, d = shape
-    q, o = Q.stride(), O.stride()
-    if O.shape != shape or Q.dtype != torch.bfloat16 or O.dtype != torch.bfloat16 or q[3] != 1 or o[3] != 1 or O.get_device() != dev:
+    qb, qh, qn, q1 = Q.stride()
+    ob, oh, on, o1 = O.stride()
+    if O.shape != shape or Q.dtype != torch.bfloat16 or O.dtype != torch.bfloat16 or q1 != 1 or o1 != 1 or O.get_device() != dev:
         raise TypeError("Q and O are bfloat16 [B][H][n_q][d_head], d_head contiguous, on one device")
-    if K is None:
-        H_kv = n_k = k_at = v_at = 0
-        k = v = (0, 0, 0, 1)
-    else:
-        k, v = K.stride(), V.stride()
-        if K.shape != V.shape or K.shape[0] != B or K.shape[3] != d or K.dtype != torch.bfloat16 or V.dtype != torch.bfloat16 \
-                or k[3] != 1 or v[3] != 1 or K.get_device() != dev or V.get_device() != dev:
+    H_kv = n_k = k_at = v_at = kb = kh = kn = vb = vh = vn = 0
+    if K is not None:
+        shape = K.shape
+        B_k, H_kv, n_k, d_k = shape
+        kb, kh, kn, k1 = K.stride()
+        vb, vh, vn, v1 = V.stride()
+        if V.shape != shape or B_k != B or d_k != d or K.dtype != torch.bfloat16 or V.dtype != torch.bfloat16 or k1 != 1 or v1 != 1 \
+                or K.get_device() != dev or V.get_device() != dev:
             raise TypeError("K and V are bfloat16 [B][H_kv][n_k][d_head], d_head contiguous, on the device of Q")
-        H_kv, n_k, k_at, v_at = K.shape[1], K.shape[2], K.data_ptr(), V.data_ptr()
-    return _ATTENTION.pack(B, H, H_kv, n_q, n_k, d, Q.data_ptr(), q[0], q[1], q[2], k_at, v_at, k[0], k[1], k[2], v[0], v[1], v[2],
-                           O.data_ptr(), o[0], o[1], o[2], _i32(seq, B, "seq", dev), _i32(q_len, B, "q_len", dev),
-                           _i32(k_len, B, "k_len", dev), _i32(q_start, B, "q_start", dev),
-                           float(d) ** -0.5 if scale is None else scale, window, sinks, max_len)
+        k_at, v_at = K.data_ptr(), V.data_ptr()
+    return _ATTENTION.pack(B, H, H_kv, n_q, n_k, d, Q.data_ptr(), qb, qh, qn, k_at, v_at, kb, kh, kn, vb, vh, vn, O.data_ptr(), ob, oh, on,
+                           0 if seq is None else _i32(seq, B, "seq", dev), 0 if q_len is None else _i32(q_len, B, "q_len", dev),
+                           0 if k_len is None else _i32(k_len, B, "k_len", dev), 0 if q_start is None else _i32(q_start, B, "q_start", dev),
+                           d ** -0.5 if scale is None else scale, window, sinks, max_len)
 
 
 def attention_workspace(cache, Q, O, window=0, sinks=0, max_len=0):
