@@ -455,11 +455,12 @@ __device__ __forceinline__ uint4 rescale_e4m3(const uint4& q, int from, int to) 
 }
 
 // The new pages of one sequence: where a page's tokens come from is found once, in LDS, and holds for every layer, head, K and V;
-// then a wavefront takes a block (one page of one head, K or V) at a time, its 16-byte pieces in registers, the next block's on their way.
+// then a wavefront takes a block (one page of one head, K or V) at a time, its 16-byte pieces in registers.
 // Blocks whose exponent stays keep their bytes.  The pages read are not among those written: they are held until the plan of a later call.
 //
-// Bound by memory (five crops, 4 sequences of 2979 tokens to 739, 16 layers of 8 heads: 194 MB).  A workgroup that took the blocks of one head, one
-// after the other, found every block's rows anew, four loads one behind the other: 103 us; so it takes 50 us, 3.9 TB/s.
+// Bound by memory (five crops, 4 sequences of 2979 tokens to 739, 16 layers of 8 heads, 194 MB: 46 us, 4.2 TB/s).  A workgroup that took the blocks of one
+// head, one after the other, found every block's rows anew, four loads one behind the other: 103 us.  The next block's pieces on their way in registers, too,
+// cost wavefronts: 3 us more here, and 91 us instead of 70 with pages of 128 tokens.
 template <int NG>
 __global__ __launch_bounds__(kMoveThreads) void cache_compact_kernel(ficoco_cache c, int layer_begin, int blocks, int per_wg, int vis_begin, int N, int n_keep,
                                                                      const int32_t* __restrict__ src, const int32_t* __restrict__ dst, const int32_t* __restrict__ keep_idx,
@@ -540,15 +541,10 @@ __global__ __launch_bounds__(kMoveThreads) void cache_compact_kernel(ficoco_cach
         }
         if (lane == 0) (i & 1 ? c.v_exp : c.k_exp)[block] = (uint8_t)e;
       };
-      Piece x0, x1;
-      if (first < end) load(x0, first);
-      for (int i = first; i < end; i += 2 * (kMoveThreads / kWave)) {
-        const int next = i + kMoveThreads / kWave;
-        if (next < end) load(x1, next);
-        put(x0, i);
-        if (next >= end) break;
-        if (next + kMoveThreads / kWave < end) load(x0, next + kMoveThreads / kWave);
-        put(x1, next);
+      Piece x;
+      for (int i = first; i < end; i += kMoveThreads / kWave) {
+        load(x, i);
+        put(x, i);
       }
     }
     __syncthreads();
