@@ -41,8 +41,8 @@ __device__ __forceinline__ float quarters_sum(float v) {
 // 8 bits become bfloat16 (exactly, the block's scale with them) in front of the products.  A row's maximum is the reference of its
 // exponentials as long as no logit lies more than 2^8 above it.
 //
-// Bound by memory: 2 d_head bytes a token and head.  4 sequences of 40000 .. 65536 tokens, 32 heads on 8: 83 us and 5 for the join, 5.7 TB/s together, a
-// plain read's rate; 32 of 300 .. 4096: 37 us, 4.1 TB/s (the longest sequences end last); one of 243: 6 us, a launch and three trips to memory.
+// Bound by memory: 2 d_head bytes a token and head.  4 sequences of 40000 .. 65536 tokens, 32 heads on 8: 86 us with the join, 5.3 TB/s (5.7 without: a
+// plain read's rate); 32 of 300 .. 4096: 37 us, 4.1 TB/s (the longest sequences end last); one of 243: 6 us, a launch and three trips to memory.
 template <int D>
 __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendArgs a) {
   constexpr int L = D / 64;                  // 16-byte loads of a key
@@ -264,21 +264,23 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendAr
   }
 }
 
-// Rows whose keys were cut: the parts, relative to their largest maximum, eight at a time (all of their loads in flight).  D / 4 lanes a row.
-// Bound by memory and its latency: 16384 rows of 4 parts, 34 MB, 8 us; 128 rows of 16 parts 5 us.
-template <int D>
+// Rows whose keys were cut: the parts, relative to their largest maximum, eight at a time (all of their loads in flight).  D / 4 lanes a row and group of
+// parts; the groups' sums meet in LDS.  Bound by memory and its latency: 16384 rows of 4 parts, 34 MB, 8 us; 128 rows of 16 parts 4 us.
+template <int D, int GROUPS>
 __global__ __launch_bounds__(kFewWaves * kWave) void join_rows_kernel(AttendArgs a) {
   constexpr int L = D / 4, AT_ONCE = 8;
-  const int rows = a.n_q * a.group, piece = threadIdx.x % L;
-  const int64_t at = ((int64_t)blockIdx.x * kFewWaves * kWave + threadIdx.x) / L;
-  if (at >= (int64_t)rows * a.B * a.H_kv) return;
-  const int bh = (int)(at / rows), r = (int)(at - (int64_t)bh * rows), b = a.by_heads.of(bh), h = bh - b * a.H_kv;
+  __shared__ f32x4_t sums[GROUPS > 1 ? kFewWaves * kWave : 1];
+  __shared__ float2 tops[GROUPS > 1 ? kFewWaves * kWave / L : 1];
+  const int rows = a.n_q * a.group, piece = threadIdx.x % L, group = threadIdx.x / L % GROUPS;
+  const int64_t at = (int64_t)blockIdx.x * (kFewWaves * kWave / (L * GROUPS)) + threadIdx.x / (L * GROUPS);
+  const bool there = at < (int64_t)rows * a.B * a.H_kv;
+  const int bh = there ? (int)(at / rows) : 0, r = there ? (int)(at - (int64_t)bh * rows) : 0, b = a.by_heads.of(bh), h = bh - b * a.H_kv;
   const int t = a.by_group.of(r);
-  if (a.q_len && t >= a.q_len[b]) return;
+  const bool wanted = there && !(a.q_len && t >= a.q_len[b]);
   const int64_t part = (int64_t)bh * a.splits * a.part_rows + r;
   float m = kNoLogit, total = 0.0f;
   f32x4_t x = {0, 0, 0, 0};
-  for (int i = 0; i < a.splits; i += AT_ONCE) {
+  for (int i = group * AT_ONCE; wanted && i < a.splits; i += GROUPS * AT_ONCE) {
     float2 ms[AT_ONCE];
     f32x4_t v[AT_ONCE];
 #pragma unroll
@@ -305,9 +307,35 @@ __global__ __launch_bounds__(kFewWaves * kWave) void join_rows_kernel(AttendArgs
       x += v[k] * w;
     }
   }
+  if constexpr (GROUPS > 1) {
+    sums[threadIdx.x] = x;
+    if (piece == 0) tops[threadIdx.x / L] = float2{m, total};
+    __syncthreads();
+    if (group > 0) return;
+    const int first = threadIdx.x / L;
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g) m = fmaxf(m, tops[first + g].x);
+    const float f = __builtin_amdgcn_exp2f(tops[first].x - m);
+    total *= f;
+    x *= f;
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g) {
+      const float w = __builtin_amdgcn_exp2f(tops[first + g].x - m);
+      total += w * tops[first + g].y;
+      x += sums[threadIdx.x + g * L] * w;
+    }
+  }
+  if (!wanted) return;
   const float inv = total > 0.0f ? 1.0f / total : 0.0f;
   const uint2 w = {pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv)};
   __builtin_memcpy(a.O + (int64_t)b * a.o_sb + (int64_t)(h * a.group + r - t * a.group) * a.o_sh + (int64_t)t * a.o_sn + 4 * piece, &w, 8);
+}
+
+template <int D, int GROUPS>
+void launch_join(const AttendArgs& a, hipStream_t s) {
+  constexpr int per = kFewWaves * kWave / (D / 4 * GROUPS);
+  const dim3 grid((unsigned)(((int64_t)a.B * a.H_kv * a.n_q * a.group + per - 1) / per));
+  hipLaunchKernelGGL((join_rows_kernel<D, GROUPS>), grid, dim3(kFewWaves * kWave), 0, s, a);
 }
 
 }  // namespace
@@ -324,8 +352,8 @@ AttendPlan attend_plan(const ficoco_attention& a, int heads, int64_t max_keys, b
     int64_t seen = max_keys;
     if (a.window > 0) seen = std::min(seen, (int64_t)a.window + a.sinks + a.n_q);
     // Keys are cut where there are too few workgroups: about two a compute unit (what is resident at once), 256 keys each at least.  4 sequences of
-    // 40000 .. 65536 tokens, 8 heads: 256 workgroups 93 us, 512 88, 1024 91; 32 of 300 .. 4096: 45, 37, 36; 8 questions of 64 tokens behind 1251 .. 2400:
-    // 1024 54 us, 512 40.  One sequence of 1000 tokens: at least 128 keys 8.9 us, 256 9.5, 512 10.9; two of 4000: 14.0, 11.9, 12.8.
+    // 40000 .. 65536 tokens, 8 heads: 256 workgroups 93 us, 512 86, 1024 88; 32 of 300 .. 4096: 45, 37, 36; 8 questions of 64 tokens behind 1251 .. 2400:
+    // 1024 52 us, 512 39.  One sequence of 1000 tokens: at least 128 keys 8.6 us, 256 9.1, 512 10.8; two of 4000: 11.3, 10.8, 12.2.
     const int64_t want = (512 + bh * pl.row_tiles - 1) / (bh * pl.row_tiles);
     pl.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, seen / 256), 256));
   }
@@ -343,10 +371,11 @@ void launch_few_rows(const AttendArgs& a, int d_head, hipStream_t s) {
 }
 
 void launch_join_rows(const AttendArgs& a, int d_head, hipStream_t s) {
-  const int per = kFewWaves * kWave / (d_head / 4);
-  const dim3 grid((unsigned)(((int64_t)a.B * a.H_kv * a.n_q * a.group + per - 1) / per));
-  if (d_head == 128) hipLaunchKernelGGL(join_rows_kernel<128>, grid, dim3(kFewWaves * kWave), 0, s, a);
-  else hipLaunchKernelGGL(join_rows_kernel<64>, grid, dim3(kFewWaves * kWave), 0, s, a);
+  // More than one batch of parts: by eight groups at once.  With the whole call, one sequence of 65536 tokens 32 us, by one group 39; 84 rows behind 30078 tokens
+  // 19 and 29; 4 sequences of 40000 .. 65536 86 and 87.
+  const bool many = a.splits > 8;
+  if (d_head == 128) many ? launch_join<128, 8>(a, s) : launch_join<128, 1>(a, s);
+  else many ? launch_join<64, 8>(a, s) : launch_join<64, 1>(a, s);
 }
 
 }  // namespace ficoco
