@@ -493,3 +493,46 @@ def test_plans_of_either_size(ctx, n, n_pages, n_seqs):
     fc.ficoco_cache_compact(ctx, g, 0, 0, i32(seq), i32(seq), 0, 5, torch.from_numpy(keep[:, :0]).cuda(), done, fc.cache_workspace(g, n))
     assert done.tolist() == h.compact([], seq, seq, 0, 5, keep[:, :0])
     same(g, h, content=False)
+
+
+def test_largest_calls(ctx):
+    """8192 slots, 1024 sequences a call, more wanted than there is; slots named twice in one call."""
+    g, h = pair(1, 6000, 16, 1, 64, 8192, 6, junk=False)
+    rng = np.random.RandomState(3)
+    seq = rng.permutation(8192)[:1024].tolist()
+    seq[100], seq[1023], seq[512] = seq[99], 8192, -1
+    for turn in range(3):
+        reserve(ctx, g, h, seq, rng.randint(0, 40, 1024).tolist())
+        same(g, h, content=False)
+    dst = rng.permutation(8192)[:1024].tolist()
+    dst[7] = dst[6]
+    done = i32([7] * 1024)
+    fc.ficoco_cache_fork(ctx, g, i32(seq), i32(dst), done)
+    assert done.tolist() == h.fork(seq, dst, False)
+    same(g, h, content=False)
+    keep = np.zeros((1024, 0), np.int32)
+    fc.ficoco_cache_compact(ctx, g, 0, 1, i32(seq), i32(seq), 3, 20, torch.from_numpy(keep).cuda(), done, fc.cache_workspace(g, 1024))
+    assert done.tolist() == h.compact([], seq, seq, 3, 20, keep)
+    same(g, h, content=False)
+    gone = seq + dst + list(range(0, 8192, 2))
+    fc.ficoco_cache_free(ctx, g, i32(gone))
+    h.free(gone)
+    same(g, h, content=False)
+
+
+@pytest.mark.parametrize("d,group", [(64, 1), (64, 3), (128, 5)])
+def test_long_sequences_cut_into_many_parts(ctx, d, group):
+    """One to three queries behind 40000 tokens (more than a hundred parts), sequences without tokens and without queries beside."""
+    lens, n_q = [40000, 0, 300, 40000], 3
+    c = fc.Cache.empty(1, 5100, 16, 1, d, 4, 2500)
+    start = i32([0] * 4)
+    fc.ficoco_cache_reserve(ctx, c, start, i32(lens))
+    K, V = rows(1, 4, 1, 40000, d), rows(2, 4, 1, 40000, d)
+    fc.ficoco_cache_append(ctx, c, 0, K, V, start, n_new=i32(lens))
+    k, v = (torch.zeros(4, 1, 40000, d, device="cuda") for _ in range(2))
+    fc.ficoco_cache_read(ctx, c, 0, k, v)
+    Q = rows(3, 4, group, n_q, d)
+    out = torch.full_like(Q, 9.0)
+    q_len = [3, 2, 1, 0]
+    fc.ficoco_cache_attention(ctx, c, 0, Q, out, fc.attention_workspace(c, Q, out), q_len=i32(q_len))
+    check(out, Q, k.double().cpu().numpy(), v.double().cpu().numpy(), lens, d ** -0.5, [n - q for n, q in zip(lens, q_len)], q_len, 0, 0, group, before=9.0)
