@@ -34,7 +34,7 @@ struct AttendArgs {
   int64_t o_sb, o_sh, o_sn;
   const int32_t *seq, *q_len, *k_len, *q_start;
   int B, H_kv, group, n_q, n_k, splits, row_tiles;
-  Divisor by_heads, by_group, by_splits, by_tiles;     // H_kv, group, splits, row_tiles * splits
+  Divisor by_heads, by_group, by_splits, by_all;       // H_kv, group, splits, B * H_kv
   float scale_log2e;
   int window, sinks;
   // pages of the layer

@@ -136,7 +136,7 @@ AttendArgs arguments(const ficoco_attention& a, int heads, const AttendPlan& pl,
   x.o_sb = a.o_stride_b; x.o_sh = a.o_stride_h; x.o_sn = a.o_stride_n;
   x.seq = a.seq; x.q_len = a.q_len; x.k_len = a.k_len; x.q_start = a.q_start;
   x.B = a.B; x.H_kv = heads; x.group = a.H / heads; x.n_q = a.n_q; x.n_k = a.n_k;
-  x.by_heads = Divisor(heads); x.by_group = Divisor(a.H / heads); x.by_splits = Divisor(pl.splits); x.by_tiles = Divisor((int64_t)pl.row_tiles * pl.splits);
+  x.by_heads = Divisor(heads); x.by_group = Divisor(a.H / heads); x.by_splits = Divisor(pl.splits); x.by_all = Divisor((int64_t)a.B * heads);
   x.splits = pl.splits; x.row_tiles = pl.row_tiles; x.part_rows = pl.row_tiles * pl.rows;
   x.scale_log2e = a.scale * 1.44269504088896340736f;
   x.window = a.window; x.sinks = a.sinks;
@@ -256,7 +256,7 @@ int ficoco_cache_attention(ficoco_ctx* ctx, const ficoco_cache* c, int32_t layer
   if (ranges_overlap(a->O, out, ws, pl.total)) return fail(ctx, FICOCO_EINVAL, fn, "O overlaps the workspace");
   if (ranges_overlap(a->O, out, c->k, pool_bytes(*c)) || ranges_overlap(a->O, out, c->v, pool_bytes(*c)))
     return fail(ctx, FICOCO_EINVAL, fn, "O overlaps the pages");
-  if ((int64_t)a->B * c->heads * std::max<int64_t>((int64_t)pl.row_tiles * pl.splits + kXcds, (int64_t)a->n_q * (a->H / c->heads)) > kMaxGridX)
+  if ((int64_t)a->B * c->heads * std::max<int64_t>((int64_t)pl.row_tiles * pl.splits, (int64_t)a->n_q * (a->H / c->heads)) > kMaxGridX)
     return fail(ctx, FICOCO_EUNSUPPORTED, fn, "too many rows in one call");
   AttendArgs x = arguments(*a, c->heads, pl, (char*)ws);
   const int64_t blocks = (int64_t)layer * c->n_pages * c->heads;
@@ -283,7 +283,7 @@ int ficoco_window_attention(ficoco_ctx* ctx, const ficoco_attention* a, void* st
   if (const char* why = attention_fault(*a, a->H_kv, a->d_head, false, &code)) return fail(ctx, code, fn, why);
   if (a->B == 0 || a->n_q == 0) return FICOCO_OK;
   const AttendPlan pl = attend_plan(*a, a->H_kv, a->n_k, false);
-  if ((int64_t)a->B * a->H_kv * (pl.row_tiles + kXcds) > kMaxGridX) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "too many rows in one call");
+  if ((int64_t)a->B * a->H_kv * pl.row_tiles > kMaxGridX) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "too many rows in one call");
   launch_dense_rows(arguments(*a, a->H_kv, pl, nullptr), a->d_head, (hipStream_t)stream);
   return finish(ctx, fn);
 }

@@ -39,11 +39,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void page_rows_kernel(AttendArgs a
   __shared__ int2 meta[2 * kChunk * kGroups];      // page (or -1) and exponents (keys, values << 8, kHole) of the groups
   const int tid = threadIdx.x, lane = tid % kWave, wv = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int c32 = lane % 32, half = lane / 32;
-  const int per_head = a.row_tiles * a.splits, total = a.B * a.H_kv * per_head;
-  const int id = xcd_logical_id(blockIdx.x, total);
-  if (id >= total) return;
-  const int bh = a.by_tiles.of(id), in_head = id - bh * per_head, b = a.by_heads.of(bh), h = bh - b * a.H_kv;
-  const int tile_back = a.by_splits.of(in_head), split = in_head - tile_back * a.splits, tile = a.row_tiles - 1 - tile_back;    // (the last rows see most keys)
+  // (the last rows of all heads first: see tile_rows_kernel; five prompts of up to 2400 tokens in pages, five heads of 64: 56.2 us in the other order, 48.5)
+  const int rest = a.by_all.of(blockIdx.x), bh = blockIdx.x - rest * a.B * a.H_kv, b = a.by_heads.of(bh), h = bh - b * a.H_kv;
+  const int back = a.by_splits.of(rest), split = rest - back * a.splits, tile = a.row_tiles - 1 - back;
   int slot;
   const Sight s = sight_of<true>(a, b, slot);
   const int rows = s.queries * a.group, row0 = tile * kTileRows;
@@ -289,7 +287,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void page_rows_kernel(AttendArgs a
 }  // namespace
 
 void launch_page_rows(const AttendArgs& a, int d_head, hipStream_t s) {
-  const dim3 grid((unsigned)xcd_padded_total(a.B * a.H_kv * a.row_tiles * a.splits)), threads(kTileThreads);
+  const dim3 grid((unsigned)(a.B * a.H_kv * a.row_tiles * a.splits)), threads(kTileThreads);
   if (d_head == 128) hipLaunchKernelGGL(page_rows_kernel<128>, grid, threads, 0, s, a);
   else hipLaunchKernelGGL(page_rows_kernel<64>, grid, threads, 0, s, a);
 }

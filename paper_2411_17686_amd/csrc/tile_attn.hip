@@ -27,7 +27,7 @@ template <int D> struct TileRaw { uint4 x[D / 32]; };       // a thread's share 
 // turns.  So keys are in LDS a step ahead of the values; either in two buffers, what comes next on its way while a step is computed.
 //
 // Bound by the matrix cores at the clock that they leave (1.9 GHz): 16384 tokens, window of 4096, 32 heads of 128 on 8: 910 .. 940 us, 1.03 PFLOP/s of
-// products (a large library product reaches 1.2); without its loads it would take 714, without exponentials 843.  Two prompts of 675 tokens, 32 heads: 23 us, of
+// products (a large library product reaches 1.2); without its loads it would take 714, without exponentials 843.  Two prompts of 675 tokens, 32 heads: 20 us, of
 // which 5 before the first step.
 template <int D, TileSource SRC>
 __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a) {
@@ -37,19 +37,17 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
   __shared__ __align__(16) bf16_t sk0[kTileKeys * D], sk1[kTileKeys * D], sv0[kTileKeys * D], sv1[kTileKeys * D];
   const int tid = threadIdx.x, lane = tid % kWave, wv = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int c32 = lane % 32, half = lane / 32;
-  const int per_head = a.row_tiles * a.splits, total = a.B * a.H_kv * per_head;
-  const int id = xcd_logical_id(blockIdx.x, total);
-  if (id >= total) return;
-  const int bh = a.by_tiles.of(id), in_head = id - bh * per_head, b = a.by_heads.of(bh), h = bh - b * a.H_kv;
-  const int tile_back = a.by_splits.of(in_head), split = in_head - tile_back * a.splits, tile = a.row_tiles - 1 - tile_back;    // (the last rows see most keys)
+  // The last rows of all heads first, as they see most keys; heads whose number is a multiple of 8 stay on their XCD.  (Head after head, an eighth of the
+  // workgroups to an XCD: two prompts of 675 tokens 23.4 us instead of 20.0, three of up to 7745 with 28 heads on 4 809 instead of 550, of 4096 with heads of 64
+  // 61 instead of 57, one of 16384 the same.)
+  const int back = a.by_all.of(blockIdx.x), bh = blockIdx.x - back * a.B * a.H_kv, b = a.by_heads.of(bh), h = bh - b * a.H_kv, tile = a.row_tiles - 1 - back;
   int slot;
   const Sight s = sight_of<false>(a, b, slot);
   const int rows = s.queries * a.group, row0 = tile * kTileRows;
   if (s.queries <= 0 || row0 >= rows) return;
   auto pos_of = [&](int r) { return s.first + a.by_group.of(r < rows ? r : rows - 1); };
   const Blocks<kTileKeys> blocks(a, s, pos_of(row0), pos_of(row0 + kTileRows - 1));
-  const int per = a.by_splits.of(blocks.count + a.splits - 1);
-  const int begin = split * per, end = begin + per < blocks.count ? begin + per : blocks.count;
+  const int begin = 0, end = blocks.count;
 
   const int r = row0 + 32 * wv + c32, my_r = r < rows ? r : rows - 1;
   const int t = a.by_group.of(my_r), g = my_r - t * a.group, pos = s.first + t;
@@ -292,8 +290,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
 }  // namespace
 
 void launch_dense_rows(const AttendArgs& a, int d_head, hipStream_t s) {
-  const dim3 grid((unsigned)xcd_padded_total(a.B * a.H_kv * a.row_tiles)), threads(kTileThreads);
-  // (straight into LDS: no registers, and no waiting for them.  16384 tokens 940 us, through registers 1259; two prompts of 675 tokens 23.6, 30.5)
+  const dim3 grid((unsigned)(a.B * a.H_kv * a.row_tiles)), threads(kTileThreads);
+  // (straight into LDS: no registers, and no waiting for them.  16384 tokens 922 us, through registers 1229; two prompts of 675 tokens 19.9, 27.1)
   const bool direct = (((uintptr_t)a.K | (uintptr_t)a.V) & 15) == 0 && ((a.k_sb | a.k_sh | a.k_sn | a.v_sb | a.v_sh | a.v_sn) & 7) == 0 &&
                       a.k_sn < (1 << 23) && a.v_sn < (1 << 23);
   if (d_head == 128) {
