@@ -351,10 +351,11 @@ AttendPlan attend_plan(const ficoco_attention& a, int heads, int64_t max_keys, b
   if (paged && bh > 0) {
     int64_t seen = max_keys;
     if (a.window > 0) seen = std::min(seen, (int64_t)a.window + a.sinks + a.n_q);
-    // Keys are cut where there are too few workgroups: about two a compute unit (what is resident at once), 256 keys each at least.  4 sequences of
+    // Keys are cut where there are too few workgroups: at most two a compute unit (what is resident at once; rounded up instead, the last few run alone: 20 questions of
+    // 325 tokens, 4 heads, 61 us and 44; 40 single tokens behind 2000 .. 3000, 8 heads, 52 and 48), 256 keys each at least.  4 sequences of
     // 40000 .. 65536 tokens, 8 heads: 256 workgroups 93 us, 512 86, 1024 88; 32 of 300 .. 4096: 45, 37, 36; 8 questions of 64 tokens behind 1251 .. 2400:
     // 1024 52 us, 512 39.  One sequence of 1000 tokens: at least 128 keys 8.6 us, 256 9.1, 512 10.8; two of 4000: 11.3, 10.8, 12.2.
-    const int64_t want = (512 + bh * pl.row_tiles - 1) / (bh * pl.row_tiles);
+    const int64_t want = 512 / (bh * pl.row_tiles);
     pl.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, seen / 256), 256));
   }
   const size_t parts = pl.splits > 1 ? (size_t)bh * pl.splits * pl.row_tiles * pl.rows : 0;
