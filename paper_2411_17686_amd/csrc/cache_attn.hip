@@ -1,5 +1,5 @@
-// Attention over pages of 8 bits for few rows: single tokens of a decoder (and the few of a draft), all query heads
-// of a key / value head together.
+// Attention over pages of 8 bits for few rows: single tokens of a decoder, the few of a draft and short questions, all query
+// heads of a key / value head together.
 #include <algorithm>
 
 #include "attend.hpp"
@@ -7,7 +7,7 @@
 namespace ficoco {
 namespace {
 
-constexpr int kFewWaves = 4, kFewRows = 16;
+constexpr int kFewWaves = 4, kFewRows = 16;         // rows of a workgroup
 constexpr int kFewKeys = 32;                 // keys of a step
 
 // One step's keys, and values, of a lane as they come out of memory.
@@ -33,7 +33,7 @@ __device__ __forceinline__ float quarters_sum(float v) {
   return v + __shfl_xor(v, 32);
 }
 
-// o = sum_j softmax_j(scale q . k_j) v_j for 16 rows, in one pass with a running maximum and sum.  Every wavefront takes steps of
+// o = sum_j softmax_j(scale q . k_j) v_j for 16 rows a workgroup, in one pass with a running maximum and sum.  Every wavefront takes steps of
 // 32 keys of its own, straight from memory into registers, the next step's loads in flight while one is computed:
 //   S^T[key][row] = K Q^T      operand A a lane's 32 bytes of key lane % 16 (the features of a lane are not in order: Q has them alike)
 //   O^T[feature][row] += V^T P^T   contraction over 32 keys in the order in which a lane holds its logits, so that the weights
@@ -51,19 +51,21 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendAr
   __shared__ float sm[kFewWaves][kFewRows], ss[kFewWaves][kFewRows];
   const int lane = threadIdx.x % kWave, wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int c16 = lane % 16, q4 = lane / 16;
-  const int bh = a.by_splits.of(blockIdx.x), split = blockIdx.x - bh * a.splits, b = a.by_heads.of(bh), h = bh - b * a.H_kv;
+  const int at = a.by_splits.of(blockIdx.x), split = blockIdx.x - at * a.splits, tile = a.by_all.of(at), bh = at - tile * a.B * a.H_kv;
+  const int b = a.by_heads.of(bh), h = bh - b * a.H_kv, row0 = tile * kFewRows;
   int slot;
   const Sight s = sight_of<true>(a, b, slot);
-  if (s.queries <= 0) return;
-  const int rows = s.queries * a.group;
-  const Blocks<kFewKeys> blocks(a, s, s.first, s.first + s.queries - 1);
+  const int all_rows = s.queries * a.group, rows = all_rows - row0 < kFewRows ? all_rows - row0 : kFewRows;      // (of this workgroup)
+  if (s.queries <= 0 || rows <= 0) return;
+  const int lo = s.first + a.by_group.of(row0), hi = s.first + a.by_group.of(row0 + rows - 1);
+  const Blocks<kFewKeys> blocks(a, s, lo, hi);
   int per = a.by_splits.of(blocks.count + a.splits - 1);
   per = (per + kFewWaves - 1) / kFewWaves * kFewWaves;
   const int begin = split * per, end = begin + per < blocks.count ? begin + per : blocks.count;
 
   // queries: row c16, features 64 l + 16 q4 + 8 u .. + 8
   bf16x8_t qf[L][2];
-  const int my_r = c16 < rows ? c16 : rows - 1;
+  const int my_r = row0 + (c16 < rows ? c16 : rows - 1);
   const int my_t = a.by_group.of(my_r);
   const RowSight sight(a, s.first + my_t, s.keys);
   {
@@ -152,7 +154,7 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendAr
       __builtin_amdgcn_sched_barrier(0);                  // (here and below: or the compiler runs ahead, and out of registers)
     }
     products_settle();
-    const int last = key0 + kFewKeys - 1, lo = s.first, hi = s.first + s.queries - 1;
+    const int last = key0 + kFewKeys - 1;
     const bool all_seen = there && last < s.keys && last <= lo && (a.window <= 0 || (int64_t)key0 > (int64_t)hi - a.window || last < a.sinks);
     S[0] *= a.scale_log2e;
     S[1] *= a.scale_log2e;
@@ -251,15 +253,15 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendAr
       for (int i = 0; i < 8; ++i) x[i] += f * so[w][r][d + i];
     }
     if (a.splits > 1) {
-      const int64_t at = ((int64_t)bh * a.splits + split) * a.part_rows + r;
+      const int64_t at = ((int64_t)bh * a.splits + split) * a.part_rows + row0 + r;
       if (d == 0) a.part_ms[at] = float2{m, total};
       __builtin_memcpy(a.part_o + at * D + d, x, 32);
     } else {
       const float inv = total > 0.0f ? 1.0f / total : 0.0f;
       const uint4 w = {pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv), pack_bf16(x[4] * inv, x[5] * inv),
                        pack_bf16(x[6] * inv, x[7] * inv)};
-      const int t = a.by_group.of(r);
-      __builtin_memcpy(a.O + (int64_t)b * a.o_sb + (int64_t)(h * a.group + r - t * a.group) * a.o_sh + (int64_t)t * a.o_sn + d, &w, 16);
+      const int t = a.by_group.of(row0 + r);
+      __builtin_memcpy(a.O + (int64_t)b * a.o_sb + (int64_t)(h * a.group + row0 + r - t * a.group) * a.o_sh + (int64_t)t * a.o_sn + d, &w, 16);
     }
   }
 }
@@ -343,8 +345,11 @@ void launch_join(const AttendArgs& a, hipStream_t s) {
 AttendPlan attend_plan(const ficoco_attention& a, int heads, int64_t max_keys, bool paged) {
   AttendPlan pl{};
   const int64_t rows = (int64_t)a.n_q * (a.H / heads), bh = (int64_t)a.B * heads;
-  // (up to 16 rows fit in one product: 4 rows of 243 tokens 6 us, in tiles of 128 rows 11; of 40000 .. 65536: 88 and 155; 16 rows of 2400: 16 and 24)
-  pl.few = paged && rows <= kFewRows;
+  // Workgroups of 16 rows that stream the keys, or of 128 that have them in LDS.  One of 16: 4 rows of 243 tokens 6 us, the other way 11; of 40000 .. 65536 86 and 155.
+  // Up to four of them, as long as there are few enough to have every key read and converted that often: 64 heads of 2400 tokens, 32 rows 17 and 25, 64 rows
+  // 23 and 27; 512 heads of 1000 .. 2000, 32 rows 71 and 75; 128 heads, 64 rows 28 and 33; but 1024 heads, 32 rows 150 and 133; 256 heads, 64 rows 56 and 51.
+  const int64_t tiles = (rows + kFewRows - 1) / kFewRows;
+  pl.few = paged && (tiles <= 1 || (tiles <= 4 && bh * tiles <= (tiles <= 3 ? 1024 : 512)));
   pl.rows = pl.few ? kFewRows : kTileRows;
   pl.row_tiles = (int)std::max<int64_t>(1, (rows + pl.rows - 1) / pl.rows);
   pl.splits = 1;
@@ -366,7 +371,7 @@ AttendPlan attend_plan(const ficoco_attention& a, int heads, int64_t max_keys, b
 }
 
 void launch_few_rows(const AttendArgs& a, int d_head, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)a.B * a.H_kv * a.splits)), threads(kFewWaves * kWave);
+  const dim3 grid((unsigned)((int64_t)a.B * a.H_kv * a.row_tiles * a.splits)), threads(kFewWaves * kWave);
   if (d_head == 128) hipLaunchKernelGGL(few_rows_kernel<128>, grid, threads, 0, s, a);
   else hipLaunchKernelGGL(few_rows_kernel<64>, grid, threads, 0, s, a);
 }

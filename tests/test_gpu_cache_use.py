@@ -536,3 +536,25 @@ def test_long_sequences_cut_into_many_parts(ctx, d, group):
     q_len = [3, 2, 1, 0]
     fc.ficoco_cache_attention(ctx, c, 0, Q, out, fc.attention_workspace(c, Q, out), q_len=i32(q_len))
     check(out, Q, k.double().cpu().numpy(), v.double().cpu().numpy(), lens, d ** -0.5, [n - q for n, q in zip(lens, q_len)], q_len, 0, 0, group, before=9.0)
+
+
+@pytest.mark.parametrize("n_q,group", [(5, 5), (20, 3), (64, 1), (16, 4)])
+@pytest.mark.parametrize("window,sinks,max_len", [(0, 0, 0), (500, 37, 0), (7, 0, 64)])
+def test_short_questions(ctx, n_q, group, window, sinks, max_len):
+    """17 to 64 rows of a head in workgroups of 16, cut over many and not; fewer queries than n_q, more than tokens, none."""
+    lens, d, heads = [9000, 40, 300, 9, 1000], 64, 2
+    c = fc.Cache.empty(1, 700, 16, heads, d, 5, 600)
+    start = i32([0] * 5)
+    fc.ficoco_cache_reserve(ctx, c, start, i32(lens))
+    c.k.fill_(127)
+    c.v.fill_(127)
+    fc.ficoco_cache_append(ctx, c, 0, rows(1, 5, heads, 9000, d), rows(2, 5, heads, 9000, d), start, n_new=i32(lens))
+    k, v = (torch.zeros(5, heads, 9000, d, device="cuda") for _ in range(2))
+    fc.ficoco_cache_read(ctx, c, 0, k, v, n_new=i32(lens))
+    Q = rows(3, 5, heads * group, n_q, d)
+    out = torch.full_like(Q, 9.0)
+    q_len = [n_q, n_q - 2, 0, n_q, 3]
+    kw = dict(window=window, sinks=sinks, max_len=max_len)
+    fc.ficoco_cache_attention(ctx, c, 0, Q, out, fc.attention_workspace(c, Q, out, **kw), q_len=i32(q_len), **kw)
+    check(out, Q, k.double().cpu().numpy(), v.double().cpu().numpy(), lens, d ** -0.5, [n - q for n, q in zip(lens, q_len)], q_len, window, sinks, group,
+          before=9.0)
