@@ -4,6 +4,8 @@
 // A call that hands out pages is two launches: one workgroup decides (a thread per sequence: what it needs, prefix sums
 // over the call, the free pages with the lowest numbers found by a scan of `refs`), then the chip moves the bytes.
 // Nothing is decided by the order in which workgroups run: every result is the same in every run.
+#include <algorithm>
+
 #include "cache.hpp"
 
 namespace ficoco {
@@ -455,22 +457,24 @@ __device__ __forceinline__ uint4 rescale_e4m3(const uint4& q, int from, int to) 
 }
 
 // The new pages of one sequence: where a page's tokens come from is found once, in LDS, and holds for every layer, head, K and V;
-// then a wavefront takes a block (one page of one head, K or V) at a time, its 16-byte pieces in registers.
+// then a wavefront, or a TEAM of them, takes a block (one page of one head, K or V) at a time, its 16-byte pieces in registers.
 // Blocks whose exponent stays keep their bytes.  The pages read are not among those written: they are held until the plan of a later call.
 //
-// Bound by memory (five crops, 4 sequences of 2979 tokens to 739, 16 layers of 8 heads, 194 MB: 44 us, 4.4 TB/s).  A workgroup that took the blocks of one
+// Bound by memory (five crops, 4 sequences of 2979 tokens to 739, 16 layers of 8 heads, 194 MB: 42 us, 4.6 TB/s).  A workgroup that took the blocks of one
 // head, one after the other, found every block's rows anew, four loads one behind the other: 103 us.  The next block's pieces on their way in registers, too,
-// cost wavefronts: 3 us more here, and 91 us instead of 70 with pages of 128 tokens.
-template <int NG>
+// cost wavefronts: 3 us more here.
+template <int NG, int TEAM>
 __global__ __launch_bounds__(kMoveThreads) void cache_compact_kernel(ficoco_cache c, int layer_begin, int blocks, int per_wg, int vis_begin, int N, int n_keep,
                                                                      const int32_t* __restrict__ src, const int32_t* __restrict__ dst, const int32_t* __restrict__ keep_idx,
                                                                      const CompactMeta* __restrict__ meta, const int32_t* __restrict__ rows) {
   __shared__ int from_page[128], from_slot[128];
+  __shared__ float tops[kMoveThreads / kWave];
+  constexpr int TEAMS = kMoveThreads / kWave / TEAM;
   const int b = blockIdx.z;
   const CompactMeta m = meta[b];
   const int shift = __builtin_ctz(c.page_size), P = 1 << shift, per_row = c.d_head / 16, block_bytes = P * c.d_head;
   const int lane = threadIdx.x % kWave, wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int first = blockIdx.y * per_wg + wv, end = min(blocks, (int)blockIdx.y * per_wg + per_wg);
+  const int end = min(blocks, (int)blockIdx.y * per_wg + per_wg);
   if ((blockIdx.x | blockIdx.y) == 0) {                    // the pages kept (shared) and those of before (given back)
     int32_t* row = c.table + (int64_t)dst[b] * c.max_pages;
     const bool in_place = src[b] == dst[b];
@@ -516,7 +520,7 @@ __global__ __launch_bounds__(kMoveThreads) void cache_compact_kernel(ficoco_cach
         const uint8_t* exps = i & 1 ? c.v_exp : c.k_exp;
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
-          const int g = lane + j * kWave, row = g / per_row, p = from_page[row];
+          const int g = lane + (wv % TEAM * NG + j) * kWave, row = g / per_row, p = from_page[row];
           x.q[j] = uint4{0, 0, 0, 0};
           x.e[j] = kExpMin;
           if (p >= 0) {
@@ -526,25 +530,35 @@ __global__ __launch_bounds__(kMoveThreads) void cache_compact_kernel(ficoco_cach
           }
         }
       };
-      auto put = [&](const Piece& x, int i) {
-        float top = 0.0f;
-#pragma unroll
-        for (int j = 0; j < NG; ++j) top = fmaxf(top, largest_e4m3(x.q[j]) * exp_scale(x.e[j]));
-        const int e = block_exponent(wave_reduce(top, [](float u, float v) { return fmaxf(u, v); }));
+      auto put = [&](const Piece& x, int i, int e) {
         const int64_t block = block_of(i, page);
         uint8_t* pool = (uint8_t*)(i & 1 ? c.v : c.k) + block * block_bytes;
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
-          const int g = lane + j * kWave;
+          const int g = lane + (wv % TEAM * NG + j) * kWave;
           if (from_page[g / per_row] == -2) continue;
           *(uint4*)(pool + (int64_t)g * 16) = x.e[j] == e ? x.q[j] : rescale_e4m3(x.q[j], x.e[j], e);
         }
-        if (lane == 0) (i & 1 ? c.v_exp : c.k_exp)[block] = (uint8_t)e;
+        if (lane == 0 && wv % TEAM == 0) (i & 1 ? c.v_exp : c.k_exp)[block] = (uint8_t)e;
       };
       Piece x;
-      for (int i = first; i < end; i += kMoveThreads / kWave) {
-        load(x, i);
-        put(x, i);
+      for (int i0 = blockIdx.y * per_wg; i0 < end; i0 += TEAMS) {
+        const int i = i0 + wv / TEAM;
+        float top = 0.0f;
+        if (i < end) {
+          load(x, i);
+#pragma unroll
+          for (int j = 0; j < NG; ++j) top = fmaxf(top, largest_e4m3(x.q[j]) * exp_scale(x.e[j]));
+          top = wave_reduce(top, [](float u, float v) { return fmaxf(u, v); });
+        }
+        if constexpr (TEAM > 1) {
+          __syncthreads();
+          if (lane == 0) tops[wv] = top;
+          __syncthreads();
+#pragma unroll
+          for (int w = 0; w < TEAM; ++w) top = fmaxf(top, tops[wv / TEAM * TEAM + w]);
+        }
+        if (i < end) put(x, i, block_exponent(top));
       }
     }
     __syncthreads();
@@ -581,10 +595,10 @@ int page_walkers(const ficoco_cache& c, int64_t others) {
   return (int)(want < 1 ? 1 : want < c.max_pages ? want : c.max_pages);
 }
 
-template <int NG>
+template <int NG, int TEAM>
 void launch_compact_pages(const ficoco_cache& c, dim3 grid, int layer_begin, int blocks, int per_wg, int vis_begin, int N, int n_keep, const int32_t* src, const int32_t* dst,
                           const int32_t* keep_idx, const CompactMeta* meta, const int32_t* rows, hipStream_t s) {
-  hipLaunchKernelGGL((cache_compact_kernel<NG>), grid, dim3(kMoveThreads), 0, s, c, layer_begin, blocks, per_wg, vis_begin, N, n_keep, src, dst, keep_idx, meta, rows);
+  hipLaunchKernelGGL((cache_compact_kernel<NG, TEAM>), grid, dim3(kMoveThreads), 0, s, c, layer_begin, blocks, per_wg, vis_begin, N, n_keep, src, dst, keep_idx, meta, rows);
 }
 
 template <typename T>
@@ -640,18 +654,19 @@ void launch_cache_compact(const ficoco_cache& c, int layer_begin, int n_layers, 
   int32_t* rows = (int32_t*)(ws + (size_t)n * sizeof(CompactMeta));
   if (small_plan(c, n, 8)) hipLaunchKernelGGL(cache_compact_plan_kernel<256>, dim3(1), dim3(256), 0, s, c, n, src, dst, vis_begin, N, n_keep, keep_idx, done, meta, rows);
   else hipLaunchKernelGGL(cache_compact_plan_kernel<kMaxPlanThreads>, dim3(1), dim3(kMaxPlanThreads), 0, s, c, n, src, dst, vis_begin, N, n_keep, keep_idx, done, meta, rows);
-  // A wavefront takes up to eight blocks, fewer where the chip would not be filled (1024 workgroups; a sequence's pages count as eight).  One image of 675
-  // tokens, 4 layers: one block a wavefront 18 us, eight 35; four sequences of 2979 tokens, 16 layers: 65.8 and 64.2, sixteen 87.
-  const int blocks = 2 * n_layers * c.heads, waves = kMoveThreads / kWave;
-  const int64_t want = (int64_t)blocks * n * 8 / 1024;
-  const int per_wg = (int)(want < waves ? waves : want < 8 * waves ? want / waves * waves : 8 * waves);
+  // A wavefront takes one block, four together where it has 16 KB (pages of 128 tokens, heads of 128; a wavefront each: 70 us instead of 60 for four
+  // sequences of 2979 tokens, 92 and 81 for three that keep 1200).  Blocks below 4 KB are less work than finding their rows: up to eight of them in turn, fewer where the chip
+  // would not be filled (1024 workgroups; a sequence's pages count as eight): pages of 16, heads of 64, 55 us by ones, 48 so.  Of 8 KB (five crops) two in turn 59.8, one 57.7.
+  const int blocks = 2 * n_layers * c.heads, block_bytes = c.page_size * c.d_head, teams = block_bytes == 16384 ? 1 : kMoveThreads / kWave;
+  const int64_t want = block_bytes >= 4096 ? 0 : (int64_t)blocks * n * 8 / 1024;
+  const int per_wg = std::max((int)(want < teams ? teams : want < 8 * teams ? want / teams * teams : 8 * teams), (blocks + 32767) / 32768);
   const dim3 grid(c.max_pages < 64 ? c.max_pages : 64, n_layers == 0 ? 1 : (blocks + per_wg - 1) / per_wg, n);
-  switch (c.page_size * c.d_head / 1024) {
-    case 1: launch_compact_pages<1>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, src, dst, keep_idx, meta, rows, s); break;
-    case 2: launch_compact_pages<2>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, src, dst, keep_idx, meta, rows, s); break;
-    case 4: launch_compact_pages<4>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, src, dst, keep_idx, meta, rows, s); break;
-    case 8: launch_compact_pages<8>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, src, dst, keep_idx, meta, rows, s); break;
-    default: launch_compact_pages<16>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, src, dst, keep_idx, meta, rows, s); break;
+  switch (block_bytes / 1024) {
+    case 1: launch_compact_pages<1, 1>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, src, dst, keep_idx, meta, rows, s); break;
+    case 2: launch_compact_pages<2, 1>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, src, dst, keep_idx, meta, rows, s); break;
+    case 4: launch_compact_pages<4, 1>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, src, dst, keep_idx, meta, rows, s); break;
+    case 8: launch_compact_pages<8, 1>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, src, dst, keep_idx, meta, rows, s); break;
+    default: launch_compact_pages<4, 4>(c, grid, layer_begin, blocks, per_wg, vis_begin, N, n_keep, src, dst, keep_idx, meta, rows, s); break;
   }
 }
 
