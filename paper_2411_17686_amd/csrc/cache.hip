@@ -179,7 +179,7 @@ __device__ __forceinline__ Span span_of(const ficoco_cache& c, int b, int n_max,
 // One workgroup per touched page, head, sequence and K / V: the new tokens' largest magnitude, then all of them.  GPT: groups of
 // sixteen values a thread.  The tokens are on their way before the page is looked up.
 //
-// Bound by memory (8 prompts of up to 2979 tokens, 8 heads of 128, bfloat16, 107 MB: 27 us, 4.0 TB/s).
+// Bound by memory (8 prompts of up to 2979 tokens, 8 heads of 128, bfloat16, 107 MB: 26 us, 4.1 TB/s).
 template <typename T, int GPT>
 __global__ __launch_bounds__(kMoveThreads) void cache_append_kernel(ficoco_cache c, int64_t layer_pages, TokenSide ks, TokenSide vs, int n_max,
                                                                     const int32_t* __restrict__ seq, const int32_t* __restrict__ start,
@@ -460,7 +460,7 @@ __device__ __forceinline__ uint4 rescale_e4m3(const uint4& q, int from, int to) 
 // then a wavefront, or a TEAM of them, takes a block (one page of one head, K or V) at a time, its 16-byte pieces in registers.
 // Blocks whose exponent stays keep their bytes.  The pages read are not among those written: they are held until the plan of a later call.
 //
-// Bound by memory (five crops, 4 sequences of 2979 tokens to 739, 16 layers of 8 heads, 194 MB: 42 us, 4.6 TB/s).  A workgroup that took the blocks of one
+// Bound by memory (five crops, 4 sequences of 2979 tokens to 739, 16 layers of 8 heads, 194 MB: 45 us, 4.4 TB/s).  A workgroup that took the blocks of one
 // head, one after the other, found every block's rows anew, four loads one behind the other: 103 us.  The next block's pieces on their way in registers, too,
 // cost wavefronts: 3 us more here.
 template <int NG, int TEAM>

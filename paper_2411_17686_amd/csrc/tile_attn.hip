@@ -26,7 +26,8 @@ template <int D> struct TileRaw { uint4 x[D / 32]; };       // a thread's share 
 // A step's weights are formed beside the products of the next step's logits: exponentials and products of one wavefront otherwise take
 // turns.  So keys are in LDS a step ahead of the values; either in two buffers, what comes next on its way while a step is computed.
 //
-// Bound by the matrix cores at the clock that they leave (1.9 GHz): 16384 tokens, window of 4096, 32 heads of 128 on 8: 910 .. 940 us, 1.03 PFLOP/s of
+// Bound by LDS, out of which four SIMDs at their full rate would take 128 bytes a cycle, all it gives, while the loads write to it, and by the matrix cores at the
+// clock that they leave (1.9 GHz): 16384 tokens, window of 4096, 32 heads of 128 on 8: 910 .. 940 us, 1.03 PFLOP/s of
 // products (a large library product reaches 1.2); without its loads it would take 714, without exponentials 843.  Two prompts of 675 tokens, 32 heads: 20 us, of
 // which 5 before the first step.
 template <int D, TileSource SRC>
