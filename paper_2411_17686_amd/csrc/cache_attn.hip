@@ -81,15 +81,17 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendAr
   for (int m = 0; m < M; ++m) o[m] = f32x4_t{0, 0, 0, 0};
   float top = kNoLogit, sum = 0.0f;
 
-  // Pages and exponents of 32 steps (64 half steps of 16 keys, one a lane): the page or -1, and both bytes.
+  // Pages and exponents of 32 steps (64 half steps of 16 keys, one a lane): the page or -1, and both bytes.  A half of which no row sees a key counts as one
+  // without a page: nobody need have written its exponents, and a byte of 255 would make NaN of the zeros that its values become.
   struct Meta { int page, exps; };
   const int32_t* row = a.table + (int64_t)slot * a.max_pages;
   auto meta_of = [&](int chunk) {
     Meta m{-1, 0};
     const int i = begin + wv + (chunk * 32 + lane / 2) * kFewWaves;
     if (i < end) {
-      const int at = (blocks.block(i) * kFewKeys + 16 * (lane & 1)) >> a.page_shift;
-      int p = at < a.max_pages ? row[at] : -1;
+      const int key = blocks.block(i) * kFewKeys + 16 * (lane & 1);
+      const bool some = key < blocks.end && (key + 16 > blocks.near_key || key < blocks.first_keys);       // (then key lies inside the row: see sight_of)
+      int p = some ? row[key >> a.page_shift] : -1;
       p = p < a.n_pages ? p : -1;
       if (p >= 0) m.exps = a.k_exp[(int64_t)p * a.H_kv + h] | a.v_exp[(int64_t)p * a.H_kv + h] << 8;
       m.page = p;
