@@ -420,8 +420,8 @@ typedef struct {
 /* Attention problem.  Query t < q_len[b] of sequence b stands at position p = q_start[b] + t and sees key j where
  *   j < k_len[b],  j <= p,  and (window = 0 or j > p - window or j < sinks):
  * O[b][h][t] = sum_j softmax_j(scale * Q[b][h][t] . K[j]) V[j], zeros where no key is seen.  Rows t >= q_len[b] are left
- * as they are.  Query head h reads key / value head h / (H / H_kv).  NULL arrays: q_len = n_q, q_start = k_len - q_len
- * (the queries are the last tokens; a negative position sees nothing; q_start + n_q stays below 2^31).  bfloat16; logits, exponentials and sums in single precision, the
+ * as they are, and a q_len[b] beyond n_q counts as n_q.  Query head h reads key / value head h / (H / H_kv).  NULL arrays: q_len = n_q,
+ * q_start = k_len - q_len (the queries are the last tokens; a negative position sees nothing; q_start + n_q stays below 2^31).  bfloat16; logits, exponentials and sums in single precision, the
  * weights are rounded to bfloat16 for the product with V.  Keys that no query of a sequence sees may hold anything; an infinity or a NaN
  * in V at a key that some query sees may reach the other queries of the call, as zero times it.  Strides in elements,
  * d_head contiguous, any element alignment; rows of O must not overlap. */

@@ -74,9 +74,8 @@ __device__ __forceinline__ Sight sight_of(const AttendArgs& a, int b, int& slot)
   }
   if (a.k_len) s.keys = a.k_len[b] < s.keys ? a.k_len[b] : s.keys;
   s.keys = s.keys > 0 ? s.keys : 0;
-  s.queries = a.q_len ? a.q_len[b] : a.n_q;
+  s.queries = a.q_len && a.q_len[b] < a.n_q ? a.q_len[b] : a.n_q;
   s.first = a.q_start ? a.q_start[b] : s.keys - s.queries;
-  s.queries = s.queries < a.n_q ? s.queries : a.n_q;
   return s;
 }
 
