@@ -391,7 +391,8 @@ int ficoco_v_step_static(ficoco_ctx *ctx, const ficoco_problem *p, void *X_out, 
  *
  * Values: a block's exponent byte e is the smallest with max|x| <= 448 * 2^(e - 127), at least 17 (2^-110, also the
  * byte of a block of zeros); x is stored as the E4M3 number nearest to x * 2^(127 - e), ties to even.  Infinities
- * are stored as the largest number and, like NaN, do not count for the maximum; NaN stays NaN (byte 127).
+ * are stored as the largest number, 448, and, like NaN, do not count for the maximum; NaN stays NaN (byte 127).  In a block with
+ * byte 247 (its largest value is beyond 1.75 * 2^127) numbers from 256 on mean infinity: there finite values are stored as 240 at most.
  *
  * Sequences are named by slots 0 .. n_seqs - 1 in arrays on the device, which no call can check on the host:
  * entries that are out of range, or that name a slot a second time where that has no meaning, are left out as each

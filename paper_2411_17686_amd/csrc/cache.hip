@@ -218,6 +218,13 @@ __global__ __launch_bounds__(kMoveThreads) void cache_append_kernel(ficoco_cache
   int e = block_exponent(block_max(top, scratch));
   e = e > old ? e : old;
   const float inv = exp_inverse(e);
+  if (e == kExpTop) {                                       // (uniform)
+#pragma unroll
+    for (int j = 0; j < GPT; ++j) {
+      keep_finite(v[j][0]);
+      keep_finite(v[j][1]);
+    }
+  }
   __syncthreads();                                         // the byte is read before it is written
 #pragma unroll
   for (int j = 0; j < GPT; ++j) {
@@ -268,6 +275,7 @@ __global__ __launch_bounds__(kMoveThreads) void cache_append_token_kernel(ficoco
   int e = block_exponent(top);
   e = e > old ? e : old;
   uint8_t* pool = side.pool + (block << shift) * D + 8 * g;
+  if (e == kExpTop) keep_finite(v);
   const uint2 q = to_e4m3(v, exp_inverse(e));
   *(uint2*)(pool + slot * D) = q;
   if (e != old && slot > 0) {

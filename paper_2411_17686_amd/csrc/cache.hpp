@@ -9,6 +9,8 @@ constexpr int kMaxSlots = 8192;      // slots of a cache (their owners in a call
 constexpr int kMaxCall = 1024;       // sequences of a call that hands out pages: one thread each
 constexpr int kExpBias = 127, kExpMin = 17;
 constexpr float kE4m3Max = 448.0f;
+constexpr int kExpTop = 247;         // byte of the largest floats: 2^120, in units of which they lie below 256
+constexpr float kTopFinite = 240.0f * 0x1p120f;      // the largest E4M3 number of such a block that is read back as a finite one
 
 // Workspace of a compaction: {first new page, pages, tokens, -} of every sequence, then the rows of the table before it.
 inline size_t compact_workspace(const ficoco_cache& c, int n) {
@@ -37,6 +39,15 @@ __device__ __forceinline__ int block_exponent(float amax) {
 __device__ __forceinline__ float finite_magnitude(float x) {
   const float a = fabsf(x);
   return a <= 3.402823466e38f ? a : 0.0f;        // (false for NaN too)
+}
+
+// Values of a block with byte kExpTop: finite ones from 248 * 2^120 on would be rounded to 2^128, which is read back as infinity.
+__device__ __forceinline__ void keep_finite(float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float a = fabsf(x[i]);
+    x[i] = a > kTopFinite && a <= 3.402823466e38f ? copysignf(kTopFinite, x[i]) : x[i];
+  }
 }
 
 // Eight values to E4M3, times `inv`: beyond the largest number the largest; NaN becomes the positive NaN (the conversion's own does not

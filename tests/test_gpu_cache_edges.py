@@ -1,9 +1,11 @@
 """Calls of the cache and its attention that the header allows and that lie at an edge of it."""
+import numpy as np
 import pytest
 import torch
 
 from paper_2411_17686_amd import ficoco as fc
-from tests.test_gpu_cache import i32
+from tests import cache_ref as R
+from tests.test_gpu_cache import append, i32, pair, reserve, same
 from tests.test_gpu_cache_attention import check, dense, filled
 
 pytestmark = pytest.mark.gpu
@@ -61,3 +63,48 @@ def test_more_queries_announced_than_given(ctx, n_q, group, d, window, sinks):
         O = torch.full_like(Q, 7.0)
         fc.ficoco_window_attention(ctx, Q, K, V, O, q_len=q_len, window=window, sinks=sinks)
         check(O, Q, K.double().cpu().numpy(), V.double().cpu().numpy(), [90] * 3, d ** -0.5, [90 - n_q] * 3, [n_q] * 3, window, sinks, group)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n_new", [1, 16])
+def test_the_largest_numbers_stay_finite(ctx, monkeypatch, dtype, n_new):
+    """From 248 * 2^120 on the nearest E4M3 number of a block with the largest byte (247) would be 2^128, infinity: 240 * 2^120 is the largest that a finite
+    value is stored as there.  One token, a block of tokens, an exponent raised to 247, and blocks rewritten."""
+    plain, most = R.encode, 240.0 * 2.0 ** 120
+    monkeypatch.setattr(R, "encode", lambda x, e: plain(np.where(np.abs(x) < 2.0 ** 128, np.clip(x, -most, most), x) if e == 247 else x, e))
+    g, h = pair(1, 20, 16, 1, 64, 4, 2)
+    top, largest = torch.finfo(torch.float32).max, torch.finfo(torch.bfloat16).max
+    K, V = (torch.randn(4, 1, 17, 64, generator=torch.Generator().manual_seed(s)) for s in (1, 2))
+    K[0, 0, n_new - 1, 3], K[0, 0, n_new - 1, 4] = largest, -largest
+    V[0, 0, n_new - 1, 5], V[0, 0, n_new - 1, 6] = -float("inf"), largest
+    V[0, 0, n_new - 1, 7] = float("nan")
+    K[1, 0, n_new - 1, :6] = torch.tensor([247.0, 248.0, 249.0, 255.0, -252.0, 231.0]) * 2.0 ** 120
+    V[1, 0, 0] = 2.0 ** 119
+    V[2, 0, n_new - 1, ::2] = 1.74 * 2.0 ** 127
+    V[2, 0, 0, 1] = float("inf")                           # (byte 246: 448 is a finite number)
+    K[3, 0, n_new - 1, 0] = 1.75 * 2.0 ** 127              # the largest value of a block with byte 246: 448 * 2^119
+    if dtype == torch.float32:
+        K[2, 0, n_new - 1, 9], V[3, 0, n_new - 1, 9] = top, -top
+    K, V = K.to(dtype), V.to(dtype)
+    seq = [0, 1, 2, 3]
+    for first, stop in ((0, n_new), (n_new, 17)):          # (the second call finds pages begun, or begins the next one)
+        start, at = reserve(ctx, g, h, seq, [stop - first] * 4)
+        append(ctx, g, h, 0, K[:, :, first:stop], V[:, :, first:stop], at, [stop - first] * 4, seq)
+        same(g, h)
+    assert h.e["k"][0, h.table[0, 0], 0] == 247 and h.e["k"][0, h.table[3, 0], 0] == 246
+    # a louder token raises a quiet page to the largest byte
+    done = i32([0] * 4)
+    keep = np.array([[0, 1, 2, 3, 5, 6, 7, 8]] * 4, np.int32)
+    fc.ficoco_cache_compact(ctx, g, 0, 1, i32(seq), i32(seq), 4, 13, torch.from_numpy(keep).cuda(), done, fc.cache_workspace(g, 4))
+    assert done.tolist() == h.compact([0], seq, seq, 4, 13, keep)
+    same(g, h)
+    for step in range(2):
+        start, at = reserve(ctx, g, h, seq, [1] * 4)
+        k1 = torch.full((4, 1, 1, 64), (1.0, float(largest))[step]).to(dtype)
+        append(ctx, g, h, 0, k1, -k1, at, [1] * 4, seq)
+        same(g, h)
+    for dt in (torch.bfloat16, torch.float32):
+        k, v = (torch.zeros(4, 1, 14, 64, dtype=dt, device="cuda") for _ in range(2))
+        fc.ficoco_cache_read(ctx, g, 0, k, v)
+        assert torch.isfinite(k).all()
+        assert torch.isinf(v).nonzero().tolist() == ([[0, 0, 0, 5]] if n_new == 1 else [])      # (where an infinity was put, and stayed)
