@@ -462,7 +462,8 @@ int ficoco_cache_read(ficoco_ctx *ctx, const ficoco_cache *c, int32_t layer, con
 
 /* Sequence dst[b] continues src[b]: it shares its whole pages and has a copy, in all layers, of the page that is not full, or of every
  * page (whole != 0).  done[b], out: 1, or 0 and nothing changes where a slot is out of range, dst[b] is not empty or named before in this
- * call, src[b] is a dst of this call, or pages run out (as ficoco_cache_reserve). */
+ * call, src[b] is a dst of this call, or pages run out (as ficoco_cache_reserve; counted for every position).  Positions of src[b] that
+ * have no page have none in dst[b]. */
 int ficoco_cache_fork(ficoco_ctx *ctx, const ficoco_cache *c, int32_t n, const int32_t *src, const int32_t *dst,
                       int32_t whole, int32_t *done, void *stream);
 

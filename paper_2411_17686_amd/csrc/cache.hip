@@ -347,7 +347,8 @@ __global__ __launch_bounds__(NT) void cache_fork_kernel(ficoco_cache c, int n, c
 }
 
 // Whole pages of all layers, as they are.  Workgroups of one sequence, layer, head and K / V walk its copied pages; one of a sequence's has its
-// shared ones entered (by the plan's one workgroup: 128 sequences of ten pages 27 us instead of 22).
+// shared ones entered (by the plan's one workgroup: 128 sequences of ten pages 27 us instead of 22).  Where src has no page to copy, dst gets none: the one
+// that the plan entered is given back by the workgroups of the first layer and head (the others have no use for the entry).
 __global__ __launch_bounds__(kMoveThreads) void cache_copy_kernel(ficoco_cache c, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
                                                                   int whole, const int32_t* __restrict__ done) {
   const int b = blockIdx.z >> 1;
@@ -365,8 +366,15 @@ __global__ __launch_bounds__(kMoveThreads) void cache_copy_kernel(ficoco_cache c
   uint8_t* exps = blockIdx.z & 1 ? c.v_exp : c.k_exp;
   const int block_bytes = c.page_size * c.d_head;
   for (int i = (whole ? 0 : len / c.page_size) + blockIdx.x; i < pages; i += gridDim.x) {
-    const int p = c.table[(int64_t)from * c.max_pages + i], q = c.table[(int64_t)to * c.max_pages + i];
-    if (!page_ok(c, p) || !page_ok(c, q)) continue;
+    int32_t* at = c.table + (int64_t)to * c.max_pages + i;
+    const int p = c.table[(int64_t)from * c.max_pages + i], q = *at;
+    if (!page_ok(c, p) || !page_ok(c, q)) {
+      if (!page_ok(c, p) && page_ok(c, q) && (blockIdx.y | blockIdx.z & 1) == 0 && threadIdx.x == 0) {
+        c.refs[q] = 0;
+        *at = -1;
+      }
+      continue;
+    }
     const int64_t bp = ((int64_t)layer * c.n_pages + p) * c.heads + h, bq = ((int64_t)layer * c.n_pages + q) * c.heads + h;
     const uint4* x = (const uint4*)(pool + bp * block_bytes);
     uint4* y = (uint4*)(pool + bq * block_bytes);

@@ -108,3 +108,51 @@ def test_the_largest_numbers_stay_finite(ctx, monkeypatch, dtype, n_new):
         fc.ficoco_cache_read(ctx, g, 0, k, v)
         assert torch.isfinite(k).all()
         assert torch.isinf(v).nonzero().tolist() == ([[0, 0, 0, 5]] if n_new == 1 else [])      # (where an infinity was put, and stayed)
+
+
+@pytest.mark.parametrize("whole", [False, True])
+@pytest.mark.parametrize("layers,heads", [(1, 1), (3, 2)])
+def test_fork_of_a_sequence_with_positions_that_have_no_page(ctx, whole, layers, heads):
+    """What has no page in src has none in dst, in the pages that are shared and in those that are copied."""
+    n, P, d = 90, 16, 64
+    g, h = pair(layers, 60, P, heads, d, 6, 8)
+    start, at = reserve(ctx, g, h, [0, 1, 2], [n] * 3)
+    for layer in range(layers):
+        K, V = (rows(10 * layer + i, 3, heads, n, d).cpu() for i in (1, 2))
+        append(ctx, g, h, layer, K, V, at, [n] * 3, [0, 1, 2])
+    for s, i, bad in ((0, 5, -1), (1, 0, -1), (1, 2, 60), (1, 5, 2 ** 31 - 1), (2, 1, -9)):
+        h.refs[h.table[s, i]] -= 1
+        h.table[s, i] = bad
+    g.table.copy_(torch.from_numpy(h.table))
+    g.refs.copy_(torch.from_numpy(h.refs))
+    taken, src, dst = h.refs.copy(), [0, 1, 1, 2], [3, 4, 0, 5]      # (0 is not empty)
+    done = i32([7] * 4)
+    fc.ficoco_cache_fork(ctx, g, i32(src), i32(dst), done, whole=whole)
+    # 0 is a dst of the call: entry 0 may not read it
+    assert done.tolist() == [0, 1, 0, 1]
+    table, refs = g.table.cpu().numpy(), g.refs.cpu().numpy()
+    want = taken.copy()
+    for s, t in ((1, 4), (2, 5)):
+        assert int(g.len[t]) == n
+        for i in range(6):
+            p, q = h.table[s, i], table[t, i]
+            if not 0 <= p < 60:
+                assert not 0 <= q < 60
+            elif i < 5 and not whole:
+                assert p == q
+                want[p] += 1
+            else:
+                assert taken[q] == 0
+                want[q] += 1
+                for x in "kv":
+                    assert torch.equal(getattr(g, x)[:, q], getattr(g, x)[:, p]) and torch.equal(getattr(g, x + "_exp")[:, q], getattr(g, x + "_exp")[:, p])
+    assert np.array_equal(refs, want) and (table[3] == -1).all() and np.array_equal(table[:3], h.table[:3])
+    # attended to alike
+    for n_q in (1, 40):
+        Q = rows(3, 2, heads, n_q, d)
+        out = [torch.zeros_like(Q) for _ in range(2)]
+        for o, seq in zip(out, ([1, 2], [4, 5])):
+            fc.ficoco_cache_attention(ctx, g, layers - 1, Q, o, fc.attention_workspace(g, Q, o), seq=i32(seq))
+        assert torch.equal(*out) and out[0].any()
+    fc.ficoco_cache_free(ctx, g, i32([0, 1, 2, 4, 5]))
+    assert not g.refs.any() and (g.table < 0).all()
