@@ -473,7 +473,7 @@ int ficoco_cache_fork(ficoco_ctx *ctx, const ficoco_cache *c, int32_t n, const i
  * before the first token that moves are kept (shared); the others are written anew into free pages, each
  * block with the exponent of what it holds, and src's own are given back if it is replaced.  Other layers of the new
  * pages are void.  done[b], out: as ficoco_cache_fork (a src may be replaced, not read, by another entry), also 0 where src[b] has fewer than
- * vis_begin + N tokens.  ws: ficoco_cache_workspace_bytes, 256-byte aligned. */
+ * vis_begin + N tokens or a token that would go into a new page has no page.  ws: ficoco_cache_workspace_bytes, 256-byte aligned. */
 int ficoco_cache_workspace_bytes(const ficoco_cache *c, int32_t n, size_t *out_bytes);
 int ficoco_cache_compact(ficoco_ctx *ctx, const ficoco_cache *c, int32_t layer_begin, int32_t n_layers, int32_t n, const int32_t *src,
                          const int32_t *dst, int32_t vis_begin, int32_t N, int32_t n_keep, const int32_t *keep_idx,

@@ -432,9 +432,33 @@ __global__ __launch_bounds__(NT) void cache_compact_plan_kernel(ficoco_cache c, 
     need = ok ? pages - f : 0;
   }
   __syncthreads();
-  for (int e = threadIdx.x / kWave; e < n; e += NT / kWave)
-    for (int i = lane; i < had[e]; i += kWave) rows[(int64_t)e * c.max_pages + i] = c.table[(int64_t)from[e] * c.max_pages + i];
+  // A token that has no page cannot move.  Whether page i of entry e, which has none, holds one that is preserved (keep_idx ascends):
+  auto in_use = [&](int e, int i) {
+    const int64_t lo = (int64_t)i * c.page_size - vis_begin, hi = min(lo + c.page_size, (int64_t)c.len[from[e]] - vis_begin);
+    if (lo < 0 || hi > N) return true;
+    const int32_t* k = keep_idx + (int64_t)e * n_keep;
+    int x = 0, y = n_keep;
+    while (x < y) {
+      const int mid = (x + y) / 2;
+      if (k[mid] < lo) x = mid + 1; else y = mid;
+    }
+    return x < n_keep && k[x] < hi;
+  };
+  for (int e = threadIdx.x / kWave; e < n; e += NT / kWave) {
+    bool stuck = false;
+    for (int i = lane; i < had[e]; i += kWave) {
+      const int page = c.table[(int64_t)from[e] * c.max_pages + i];
+      rows[(int64_t)e * c.max_pages + i] = page;
+      if (!page_ok(c, page) && i >= first[e]) stuck |= in_use(e, i);
+    }
+    stuck = __any(stuck);
+    if (lane == 0) moved[e] = stuck;                       // (its value so far has served)
+  }
   __syncthreads();                                         // the rows are saved before new pages go into them
+  if (b < n && moved[b]) {
+    ok = false;
+    need = 0;
+  }
   const bool served = ok & hand_out<NT>(c, l, n, need, first_mask, [&](int e, int k, int page) {
     c.table[(int64_t)to[e] * c.max_pages + first[e] + k] = page;
     c.refs[page] = 1;
@@ -523,7 +547,7 @@ __global__ __launch_bounds__(kMoveThreads) void cache_compact_kernel(ficoco_cach
         p = rows[(int64_t)b * c.max_pages + (t >> shift)];
         if (!page_ok(c, p)) p = -1;
       }
-      from_page[threadIdx.x] = r < m.tokens ? p : -2;       // -1: zeros, -2: behind the last token, left as it is
+      from_page[threadIdx.x] = r < m.tokens ? p : -2;       // -1: zeros (keep_idx out of order alone), -2: behind the last token, left as it is
       from_slot[threadIdx.x] = (int)(t & (P - 1));
     }
     __syncthreads();

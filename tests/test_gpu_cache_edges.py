@@ -156,3 +156,66 @@ def test_fork_of_a_sequence_with_positions_that_have_no_page(ctx, whole, layers,
         assert torch.equal(*out) and out[0].any()
     fc.ficoco_cache_free(ctx, g, i32([0, 1, 2, 4, 5]))
     assert not g.refs.any() and (g.table < 0).all()
+
+
+@pytest.mark.parametrize("n", [4, 9])                      # plans by 256 threads and by 1024
+@pytest.mark.parametrize("in_place", [True, False])
+def test_compact_of_a_sequence_with_positions_that_have_no_page(ctx, n, in_place):
+    """A token that has no page cannot move: such a sequence is left as it is.  In the pages that are kept it changes nothing."""
+    P, d, length, v, N = 16, 64, 100, 40, 30
+    g, h = pair(2, 200, P, 2, d, 2 * n, 8)
+    seq = list(range(n))
+    start, at = reserve(ctx, g, h, seq, [length] * n)
+    K, V = rows(1, n, 2, length, d).cpu(), rows(2, n, 2, length, d).cpu()
+    for layer in (0, 1):
+        append(ctx, g, h, layer, K, V, at, [length] * n, seq)
+    for s, i, bad in ((0, 2, -1), (1, 6, 200), (2, 1, -1)):          # tokens 32 .. 47, the last page, a page in front of what moves
+        h.refs[h.table[s, i]] -= 1
+        h.table[s, i] = bad
+    g.table.copy_(torch.from_numpy(h.table))
+    g.refs.copy_(torch.from_numpy(h.refs))
+    keep = np.tile(np.arange(3, 30, 2, dtype=np.int32), (n, 1))
+    dst = seq if in_place else [n + s for s in seq]
+    done = i32([7] * n)
+    fc.ficoco_cache_compact(ctx, g, 0, 2, i32(seq), i32(dst), v, N, torch.from_numpy(keep).cuda(), done, fc.cache_workspace(g, n))
+    assert done.tolist() == [0, 0] + [1] * (n - 2)
+    ok = seq[2:]
+    before = h.table[2].copy()
+    h.table[2, 1] = h.n_pages - 1                          # (the model counts the pages kept: one that nobody has)
+    h.refs[h.n_pages - 1] = 1
+    assert h.compact([0, 1], ok, dst[2:], v, N, keep[2:]) == [1] * (n - 2)
+    h.refs[h.n_pages - 1] = 0
+    h.table[2, 1] = before[1]
+    h.table[dst[2], 1] = before[1]
+    same(g, h)
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_compact_drops_tokens_that_have_no_page(ctx, in_place):
+    """Pages of which no token is preserved need not be there; the first and the last token of such a page preserved, they have to."""
+    P, d, length, v, N, n = 16, 64, 85, 20, 65, 5              # the span ends with the sequence: tokens 20 .. 84, pages 1 .. 5
+    g, h = pair(1, 60, P, 1, d, 2 * n, 8)
+    seq = list(range(n))
+    start, at = reserve(ctx, g, h, seq, [length] * n)
+    K, V = rows(1, n, 1, length, d).cpu(), rows(2, n, 1, length, d).cpu()
+    append(ctx, g, h, 0, K, V, at, [length] * n, seq)
+    for s in seq:
+        for i in (2, 3, 5):                                    # tokens 32 .. 63, 80 .. 84
+            h.refs[h.table[s, i]] -= 1
+            h.table[s, i] = -1
+    g.table.copy_(torch.from_numpy(h.table))
+    g.refs.copy_(torch.from_numpy(h.refs))
+    keep = np.array([[21, 30, 64, 70], [21, 32, 64, 70], [21, 31, 63, 70], [22, 31, 64, 79], [22, 31, 64, 80]], np.int32) - v
+    dst = seq if in_place else [n + s for s in seq]
+    done = i32([7] * n)
+    fc.ficoco_cache_compact(ctx, g, 0, 1, i32(seq), i32(dst), v, N, torch.from_numpy(keep).cuda(), done, fc.cache_workspace(g, n))
+    assert done.tolist() == [1, 0, 0, 1, 0]
+    spare = h.n_pages - 1                                      # (the model counts pages: one that nobody has)
+    for s in (0, 3):
+        for i in (2, 3, 5):
+            h.table[s, i] = spare
+            h.refs[spare] += 1
+    assert h.compact([0], [0, 3], [dst[0], dst[3]], v, N, keep[[0, 3]]) == [1, 1]
+    h.table[h.table == spare] = -1
+    h.refs[spare] = 0
+    same(g, h)
