@@ -13,7 +13,8 @@
  *     thread's current device (checked: FICOCO_EINVAL otherwise).  The library allocates no
  *     device memory and frees nothing of the caller's.  Outputs must not alias inputs
  *     (X_out overlapping X or the workspace is rejected with FICOCO_EINVAL; the small index
- *     and edge outputs are not checked).  The arrays of a ficoco_cache are read and changed in place.
+ *     and edge outputs are not checked).  The arrays of a ficoco_cache are read and changed in place; other
+ *     outputs and workspaces that overlap them are rejected as well.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  All work is
  *     enqueued on it asynchronously; no call synchronises the device or copies to the host.
  *   - Return value: a ficoco_status.  Argument errors are found on the host before anything

@@ -62,6 +62,21 @@ int check_count(ficoco_ctx* ctx, const ficoco_cache& c, int32_t n, const char* f
   return FICOCO_OK;
 }
 
+// Bytes from a tensor's first to its last element.
+size_t extent(int64_t b, int64_t h, int64_t n, int64_t sb, int64_t sh, int64_t sn, int64_t d, size_t es) {
+  return b > 0 && h > 0 && n > 0 ? (size_t)((b - 1) * sb + (h - 1) * sh + (n - 1) * sn + d) * es : 0;
+}
+size_t pool_bytes(const ficoco_cache& c) {
+  return (size_t)c.layers * c.n_pages * c.heads * c.page_size * c.d_head;
+}
+// Whether [p, p + n) shares bytes with an array of the cache.
+bool reaches_into(const ficoco_cache& c, const void* p, size_t n) {
+  const size_t exps = (size_t)c.layers * c.n_pages * c.heads;
+  return ranges_overlap(p, n, c.k, pool_bytes(c)) || ranges_overlap(p, n, c.v, pool_bytes(c)) || ranges_overlap(p, n, c.k_exp, exps) ||
+         ranges_overlap(p, n, c.v_exp, exps) || ranges_overlap(p, n, c.table, (size_t)c.n_seqs * c.max_pages * sizeof(int32_t)) ||
+         ranges_overlap(p, n, c.len, (size_t)c.n_seqs * sizeof(int32_t)) || ranges_overlap(p, n, c.refs, (size_t)c.n_pages * sizeof(int32_t));
+}
+
 int check_tokens(ficoco_ctx* ctx, const ficoco_cache& c, int32_t layer, const ficoco_tokens* t, bool write, const char* fn) {
   if (!t) return fail(ctx, FICOCO_EINVAL, fn, "tokens is NULL");
   if (layer < 0 || layer >= c.layers) return fail(ctx, FICOCO_EINVAL, fn, "no such layer");
@@ -79,16 +94,12 @@ int check_tokens(ficoco_ctx* ctx, const ficoco_cache& c, int32_t layer, const fi
     if ((t->K && rows_collide(c.d_head, {{{t->k_stride_b, t->n}, {t->k_stride_h, c.heads}, {t->k_stride_n, t->n_max}}})) ||
         (t->V && rows_collide(c.d_head, {{{t->v_stride_b, t->n}, {t->v_stride_h, c.heads}, {t->v_stride_n, t->n_max}}})) || t->K == t->V)
       return fail(ctx, FICOCO_EINVAL, fn, "rows that are written overlap");
+    const size_t es = t->dtype == FICOCO_BF16 ? 2 : 4;
+    if (reaches_into(c, t->K, extent(t->n, c.heads, t->n_max, t->k_stride_b, t->k_stride_h, t->k_stride_n, c.d_head, es)) ||
+        reaches_into(c, t->V, extent(t->n, c.heads, t->n_max, t->v_stride_b, t->v_stride_h, t->v_stride_n, c.d_head, es)))
+      return fail(ctx, FICOCO_EINVAL, fn, "K or V overlaps the cache");
   }
   return FICOCO_OK;
-}
-
-// Bytes from a tensor's first to its last element.
-size_t extent(int64_t b, int64_t h, int64_t n, int64_t sb, int64_t sh, int64_t sn, int64_t d, size_t es) {
-  return b > 0 && h > 0 && n > 0 ? (size_t)((b - 1) * sb + (h - 1) * sh + (n - 1) * sn + d) * es : 0;
-}
-size_t pool_bytes(const ficoco_cache& c) {
-  return (size_t)c.layers * c.n_pages * c.heads * c.page_size * c.d_head;
 }
 
 // paged: with a cache (its heads), else dense keys and values
@@ -218,6 +229,8 @@ int ficoco_cache_compact(ficoco_ctx* ctx, const ficoco_cache* c, int32_t layer_b
   if ((int64_t)n_layers * c->heads > kMaxGridY) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "more than 65535 heads in all layers");
   if (!ws || ((uintptr_t)ws & 255)) return fail(ctx, FICOCO_EINVAL, fn, "workspace is NULL or not 256-byte aligned");
   if (ws_bytes < compact_workspace(*c, n)) return fail(ctx, FICOCO_ENOMEM, fn, "workspace smaller than ficoco_cache_workspace_bytes()");
+  if (reaches_into(*c, ws, compact_workspace(*c, n)) || ranges_overlap(ws, compact_workspace(*c, n), keep_idx, (size_t)n * n_keep * sizeof(int32_t)))
+    return fail(ctx, FICOCO_EINVAL, fn, "the workspace overlaps the cache or keep_idx");
   launch_cache_compact(*c, layer_begin, n_layers, n, src, dst, vis_begin, N, n_keep, keep_idx, done, (char*)ws, (hipStream_t)stream);
   return finish(ctx, fn);
 }
@@ -253,9 +266,10 @@ int ficoco_cache_attention(ficoco_ctx* ctx, const ficoco_cache* c, int32_t layer
   if (!ws || ((uintptr_t)ws & 255)) return fail(ctx, FICOCO_EINVAL, fn, "workspace is NULL or not 256-byte aligned");
   if (ws_bytes < pl.total) return fail(ctx, FICOCO_ENOMEM, fn, "workspace smaller than ficoco_cache_attention_workspace_bytes()");
   const size_t out = extent(a->B, a->H, a->n_q, a->o_stride_b, a->o_stride_h, a->o_stride_n, a->d_head, 2);
-  if (ranges_overlap(a->O, out, ws, pl.total)) return fail(ctx, FICOCO_EINVAL, fn, "O overlaps the workspace");
-  if (ranges_overlap(a->O, out, c->k, pool_bytes(*c)) || ranges_overlap(a->O, out, c->v, pool_bytes(*c)))
-    return fail(ctx, FICOCO_EINVAL, fn, "O overlaps the pages");
+  if (ranges_overlap(a->O, out, ws, pl.total) ||
+      ranges_overlap(a->Q, extent(a->B, a->H, a->n_q, a->q_stride_b, a->q_stride_h, a->q_stride_n, a->d_head, 2), ws, pl.total))
+    return fail(ctx, FICOCO_EINVAL, fn, "Q or O overlaps the workspace");
+  if (reaches_into(*c, a->O, out) || reaches_into(*c, ws, pl.total)) return fail(ctx, FICOCO_EINVAL, fn, "O or the workspace overlaps the cache");
   if ((int64_t)a->B * c->heads * std::max<int64_t>((int64_t)pl.row_tiles * pl.splits, (int64_t)a->n_q * (a->H / c->heads)) > kMaxGridX)
     return fail(ctx, FICOCO_EUNSUPPORTED, fn, "too many rows in one call");
   AttendArgs x = arguments(*a, c->heads, pl, (char*)ws);

@@ -219,3 +219,52 @@ def test_compact_drops_tokens_that_have_no_page(ctx, in_place):
     h.table[h.table == spare] = -1
     h.refs[spare] = 0
     same(g, h)
+
+
+def test_outputs_and_workspaces_that_reach_into_the_cache_are_refused(ctx):
+    c = fc.Cache.empty(1, 400, 16, 2, 64, 4, 100)
+    start = i32([0, 0])
+    fc.ficoco_cache_reserve(ctx, c, start, 20, seq=i32([0, 1]))
+    K, V = rows(1, 2, 2, 20, 64), rows(2, 2, 2, 20, 64)
+    fc.ficoco_cache_append(ctx, c, 0, K, V, start)
+    names = ("k", "v", "k_exp", "v_exp", "table", "len", "refs")
+    torch.cuda.synchronize()
+    before = [getattr(c, name).clone() for name in names]
+    Q, O = rows(3, 2, 4, 1, 64), torch.zeros(2, 4, 1, 64, dtype=torch.bfloat16, device="cuda")
+    ws, cws = fc.attention_workspace(c, Q, O), fc.cache_workspace(c, 2)
+    keep, two, done = i32([[0, 1]] * 2), i32([0, 1]), i32([5, 5])
+
+    def into(t, numel, dtype=torch.bfloat16):
+        flat = t.view(-1).view(dtype)
+        return flat[:numel] if flat.numel() >= numel else None
+
+    def space(t, of):
+        w = fc.Workspace(of.bytes, "cuda")
+        w.ptr = -(-t.data_ptr() // 256) * 256
+        return w
+
+    calls = []
+    for name in names:
+        t = getattr(c, name)
+        rows_of = into(t, 2 * 2 * 64)
+        if rows_of is not None:
+            out = rows_of.view(2, 2, 1, 64)
+            calls += [lambda out=out: fc.ficoco_cache_read(ctx, c, 0, out, None), lambda out=out: fc.ficoco_cache_read(ctx, c, 0, None, out)]
+        rows_of = into(t, 2 * 64)
+        if rows_of is not None:
+            out = rows_of.view(1, 2, 1, 64)
+            calls.append(lambda out=out: fc.ficoco_cache_attention(ctx, c, 0, Q[:1, :2], out, ws))
+        if t.numel() * t.element_size() >= 1024:
+            calls += [lambda t=t: fc.ficoco_cache_attention(ctx, c, 0, Q, O, space(t, ws)),
+                      lambda t=t: fc.ficoco_cache_compact(ctx, c, 0, 1, two, two, 0, 4, keep, done, space(t, cws))]
+    big = fc.Workspace(ws.bytes, "cuda")
+    calls.append(lambda: fc.ficoco_cache_attention(ctx, c, 0, big.t[big.ptr - big.t.data_ptr():][:1024].view(torch.bfloat16).view(2, 4, 1, 64), O, big))
+    assert len(calls) > 20
+    for i, call in enumerate(calls):
+        with pytest.raises(fc.FicocoError) as err:
+            call()
+        assert err.value.code == fc.EINVAL, i
+    torch.cuda.synchronize()
+    for name, t in zip(names, before):
+        assert torch.equal(getattr(c, name), t), name
+    assert done.tolist() == [5, 5] and not O.any()
