@@ -86,13 +86,17 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
   };
 
   // ---- through registers
+  // (load j: row my_row + RJ * j, for which the swizzles are the same, so that one address serves all; addresses of their own cost heads of 128 ten
+  // spilled registers, 1319 us instead of 1158 for 16384 tokens)
+  const int my_row = tid / CH, my_chunk = tid % CH;
+  static_assert(RJ % 16 == 0, "swizzles look at four bits of a row at most");
   auto load_dense = [&](TileRaw<D>& raw, const bf16_t* base, int64_t sn, int step) {
-    const int key0 = blocks.block(step) * kTileKeys;
+    const int key0 = blocks.block(step) * kTileKeys + my_row;
+    const bf16_t* from = base + (int64_t)key0 * sn + 8 * my_chunk;
 #pragma unroll
     for (int j = 0; j < NL; ++j) {
-      const int at = tid + j * kTileThreads, key = key0 + at / CH;
       raw.x[j] = uint4{0, 0, 0, 0};
-      if (step < end && wanted(key)) __builtin_memcpy(&raw.x[j], base + (int64_t)key * sn + 8 * (at % CH), 16);
+      if (step < end && wanted(key0 + RJ * j)) __builtin_memcpy(&raw.x[j], from + j * RJ * sn, 16);
     }
   };
   const bf16_t* Kb = a.K + (int64_t)b * a.k_sb + (int64_t)h * a.k_sh;
@@ -119,12 +123,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
   };
   auto store = [&](const TileRaw<D>& raw, bf16_t* to, bool keys) {
     if constexpr (SRC != kDenseDirect) {
+      uint4* r = (uint4*)to + my_row * CH + (my_chunk ^ (keys ? key_swizzle<D>(my_row) : value_swizzle<D>(my_row)));
 #pragma unroll
-      for (int j = 0; j < NL; ++j) {
-        const int at = tid + j * kTileThreads, row = at / CH, ch = at % CH, swizzle = keys ? key_swizzle<D>(row) : value_swizzle<D>(row);
-        uint4* r = (uint4*)to + row * CH;
-        r[ch ^ swizzle] = raw.x[j];
-      }
+      for (int j = 0; j < NL; ++j) r[j * RJ * CH] = raw.x[j];
     }
   };
   auto arrived = [&]() {
@@ -292,7 +293,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
 
 void launch_dense_rows(const AttendArgs& a, int d_head, hipStream_t s) {
   const dim3 grid((unsigned)(a.B * a.H_kv * a.row_tiles)), threads(kTileThreads);
-  // (straight into LDS: no registers, and no waiting for them.  16384 tokens 922 us, through registers 1229; two prompts of 675 tokens 19.9, 27.1)
+  // (straight into LDS: no registers, and no waiting for them.  16384 tokens 920 us, through registers 1110; two prompts of 675 tokens 19.6, 23.6.  Rows at odd
+  // elements, which have to go through registers: 1158 and 25.8)
   const bool direct = (((uintptr_t)a.K | (uintptr_t)a.V) & 15) == 0 && ((a.k_sb | a.k_sh | a.k_sn | a.v_sb | a.v_sh | a.v_sn) & 7) == 0 &&
                       a.k_sn < (1 << 23) && a.v_sn < (1 << 23);
   if (d_head == 128) {
