@@ -12,6 +12,7 @@ using namespace ficoco;
 namespace {
 
 constexpr int64_t kMaxGridY = 65535, kMaxGridX = 0x7fffffff;
+constexpr int64_t kMaxRows = 0x7fffffff;
 constexpr int64_t kMaxTokens = 1 << 30;      // (a block behind the last token, too, is named by 32 bits)
 
 // Whether rows of d elements may share elements: none do where every stride steps over all that the smaller ones span.
@@ -127,6 +128,7 @@ const char* attention_fault(const ficoco_attention& a, int heads, int d_head, bo
   *code = FICOCO_EUNSUPPORTED;
   if (d_head != 64 && d_head != 128) return "d_head must be 64 or 128";
   if ((int64_t)a.n_q * (a.H / heads) > 0x3fffffff) return "more than 2^30 rows of one key / value head";
+  if ((__int128)a.B * a.H * a.n_q > kMaxRows) return "2^31 rows or more in one call";      // (three times 2^31 pass 64 bits)
   if (!paged && a.n_k > kMaxTokens) return "more than 2^30 keys";
   *code = FICOCO_EINVAL;
   if (rows_collide(d_head, {{{a.o_stride_b, a.B}, {a.o_stride_h, a.H}, {a.o_stride_n, a.n_q}}})) return "rows of O overlap";
