@@ -399,7 +399,8 @@ int ficoco_v_step_static(ficoco_ctx *ctx, const ficoco_problem *p, void *X_out, 
  * entries that are out of range, or that name a slot a second time where that has no meaning, are left out as each
  * function says; page numbers out of range are taken for -1.  Limits: page_size 16, 32, 64 or 128; d_head 64 or 128
  * (others FICOCO_EUNSUPPORTED); n_seqs <= 8192; at most 2^30 tokens in a sequence or a call, at most 1024 sequences in a call of
- * reserve, fork or compact, whose rows of the table have room for less than 2^31 pages together.
+ * reserve, fork or compact, whose rows of the table have room for less than 2^31 pages together.  A call whose kernel would take 2^32
+ * threads along one axis (from some 10^8 tokens of a sequence or 10^9 rows of queries on) is FICOCO_EUNSUPPORTED.
  */
 typedef struct {
   int32_t layers, n_pages, page_size, heads, d_head, n_seqs, max_pages;
@@ -441,7 +442,8 @@ typedef struct {
   float scale;
   int32_t window, sinks;
   int32_t max_len; /* ficoco_cache_attention: about how many tokens the longest sequence has, 0 = as many as the
-                      table has room for.  It decides how the work is cut, never the result's meaning. */
+                      table has room for.  It decides how the work is cut, never the result's meaning.  A workspace for one
+                      max_len serves every smaller one. */
 } ficoco_attention;
 
 /* Pages for n_new[b] more tokens of each sequence (n_new NULL: n_each), the free ones with the lowest numbers, in the

@@ -13,7 +13,6 @@ namespace {
 
 constexpr int kMaxPlanThreads = kMaxCall;
 constexpr int kNone = 0x7fffffff;
-constexpr int kMoveThreads = 256;
 
 struct PlanLds {
   int owner[kMaxSlots];      // the first entry of the call that names a slot
@@ -652,8 +651,7 @@ void append_groups(const ficoco_cache& c, int layer, const ficoco_tokens& t, hip
     else hipLaunchKernelGGL((cache_append_token_kernel<T, 64>), grid, dim3(kMoveThreads), 0, s, c, lp, k, v, (int)items, t.seq, t.start, t.n_new);
     return;
   }
-  const int touched = (t.n_max + c.page_size - 2) / c.page_size + 1;
-  const dim3 grid(touched, c.heads, 2 * t.n);
+  const dim3 grid(append_pages(c, t.n_max), c.heads, 2 * t.n);
   const int groups = c.page_size * c.d_head / 16;
   // (no threads without tokens: 16 prompts of 1000, 4 heads of 64, pages of 16, written and read back 23 us with 256, 18 with 64)
   if (groups <= 256) hipLaunchKernelGGL((cache_append_kernel<T, 1>), grid, dim3(groups), 0, s, c, lp, k, v, t.n_max, t.seq, t.start, t.n_new);

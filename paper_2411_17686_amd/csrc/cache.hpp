@@ -7,6 +7,7 @@ namespace ficoco {
 
 constexpr int kMaxSlots = 8192;      // slots of a cache (their owners in a call are kept in LDS)
 constexpr int kMaxCall = 1024;       // sequences of a call that hands out pages: one thread each
+constexpr int kMoveThreads = 256;    // of a workgroup that moves tokens or pages
 constexpr int kExpBias = 127, kExpMin = 17;
 constexpr float kE4m3Max = 448.0f;
 constexpr int kExpTop = 247;         // byte of the largest floats: 2^120, in units of which they lie below 256
@@ -15,6 +16,13 @@ constexpr float kTopFinite = 240.0f * 0x1p120f;      // the largest E4M3 number 
 // Workspace of a compaction: {first new page, pages, tokens, -} of every sequence, then the rows of the table before it.
 inline size_t compact_workspace(const ficoco_cache& c, int n) {
   return ((size_t)n * 4 * sizeof(int32_t) + (size_t)n * c.max_pages * sizeof(int32_t) + 255) / 256 * 256;
+}
+
+// Threads of an append (write) or a read along the tokens of a sequence.
+inline int append_pages(const ficoco_cache& c, int n_max) { return (n_max + c.page_size - 2) / c.page_size + 1; }
+inline int64_t token_threads(const ficoco_cache& c, int n_max, bool write) {
+  const int rows = kMoveThreads / (c.d_head / 8), pieces = c.page_size * c.d_head / 16;
+  return write ? (int64_t)append_pages(c, n_max) * (pieces < kMoveThreads ? pieces : kMoveThreads) : ((int64_t)n_max + rows - 1) / rows * kMoveThreads;
 }
 
 void launch_cache_reserve(const ficoco_cache& c, int n, const int32_t* seq, const int32_t* n_new, int n_each, int32_t* start, hipStream_t s);

@@ -11,8 +11,8 @@ using namespace ficoco;
 
 namespace {
 
-constexpr int64_t kMaxGridY = 65535, kMaxGridX = 0x7fffffff;
-constexpr int64_t kMaxRows = 0x7fffffff;
+constexpr int64_t kMaxGridY = 65535, kMaxRows = 0x7fffffff;
+constexpr int64_t kMaxThreads = 0xffffffff;      // of a launch, along one axis
 constexpr int64_t kMaxTokens = 1 << 30;      // (a block behind the last token, too, is named by 32 bits)
 
 // Whether rows of d elements may share elements: none do where every stride steps over all that the smaller ones span.
@@ -89,6 +89,7 @@ int check_tokens(ficoco_ctx* ctx, const ficoco_cache& c, int32_t layer, const fi
   if (((uintptr_t)t->K | (uintptr_t)t->V) & align) return fail(ctx, FICOCO_EINVAL, fn, "K or V is not aligned to its elements");
   if (t->n_max > kMaxTokens) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "more than 2^30 tokens of a sequence");
   if (2 * (int64_t)t->n > kMaxGridY) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "more than 32767 sequences in a call");
+  if (token_threads(c, t->n_max, write) > kMaxThreads) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "n_max takes more than 2^32 threads");
   if (t->k_stride_b < 0 || t->k_stride_h < 0 || t->k_stride_n < 0 || t->v_stride_b < 0 || t->v_stride_h < 0 || t->v_stride_n < 0)
     return fail(ctx, FICOCO_EINVAL, fn, "a stride is negative");
   if (!write) {
@@ -243,6 +244,7 @@ int ficoco_cache_free(ficoco_ctx* ctx, const ficoco_cache* c, int32_t n, const i
   if (rc != FICOCO_OK) return rc;
   if (n < 0) return fail(ctx, FICOCO_EINVAL, fn, "n is negative");
   if (n == 0) return FICOCO_OK;
+  if ((int64_t)n * kMoveThreads > kMaxThreads) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "more than 2^24 sequences in a call");
   launch_cache_free(*c, n, seq, (hipStream_t)stream);
   return finish(ctx, fn);
 }
@@ -272,7 +274,7 @@ int ficoco_cache_attention(ficoco_ctx* ctx, const ficoco_cache* c, int32_t layer
       ranges_overlap(a->Q, extent(a->B, a->H, a->n_q, a->q_stride_b, a->q_stride_h, a->q_stride_n, a->d_head, 2), ws, pl.total))
     return fail(ctx, FICOCO_EINVAL, fn, "Q or O overlaps the workspace");
   if (reaches_into(*c, a->O, out) || reaches_into(*c, ws, pl.total)) return fail(ctx, FICOCO_EINVAL, fn, "O or the workspace overlaps the cache");
-  if ((int64_t)a->B * c->heads * std::max<int64_t>((int64_t)pl.row_tiles * pl.splits, (int64_t)a->n_q * (a->H / c->heads)) > kMaxGridX)
+  if ((int64_t)a->B * c->heads * pl.row_tiles * pl.splits * kTileThreads > kMaxThreads)
     return fail(ctx, FICOCO_EUNSUPPORTED, fn, "too many rows in one call");
   AttendArgs x = arguments(*a, c->heads, pl, (char*)ws);
   const int64_t blocks = (int64_t)layer * c->n_pages * c->heads;
@@ -299,7 +301,7 @@ int ficoco_window_attention(ficoco_ctx* ctx, const ficoco_attention* a, void* st
   if (const char* why = attention_fault(*a, a->H_kv, a->d_head, false, &code)) return fail(ctx, code, fn, why);
   if (a->B == 0 || a->n_q == 0) return FICOCO_OK;
   const AttendPlan pl = attend_plan(*a, a->H_kv, a->n_k, false);
-  if ((int64_t)a->B * a->H_kv * pl.row_tiles > kMaxGridX) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "too many rows in one call");
+  if ((int64_t)a->B * a->H_kv * pl.row_tiles * kTileThreads > kMaxThreads) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "too many rows in one call");
   launch_dense_rows(arguments(*a, a->H_kv, pl, nullptr), a->d_head, (hipStream_t)stream);
   return finish(ctx, fn);
 }

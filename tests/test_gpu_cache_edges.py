@@ -268,3 +268,29 @@ def test_outputs_and_workspaces_that_reach_into_the_cache_are_refused(ctx):
     for name, t in zip(names, before):
         assert torch.equal(getattr(c, name), t), name
     assert done.tolist() == [5, 5] and not O.any()
+
+
+def test_calls_beyond_the_threads_of_a_launch_are_refused(ctx):
+    """Along one axis a launch has less than 2^32 threads."""
+    c = fc.Cache.empty(1, 4, 16, 1, 64, 2, 4)
+    wide = rows(1, 1, 1, 1, 64).expand(1, 1, 1 << 30, 64)
+    for n, refused in (((1 << 30) - 1, True), (1 << 30, True), (1 << 20, False)):
+        call = lambda: fc.ficoco_cache_append(ctx, c, 0, wide[:, :, :n], wide[:, :, :n], i32([0]))
+        if refused:
+            with pytest.raises(fc.FicocoError) as err:
+                call()
+            assert err.value.code == fc.EUNSUPPORTED
+        else:
+            call()                                         # (positions that have no page: nothing to write)
+    # 2^31 rows of queries, that many sequences freed, 2^29 tokens read: described, not there
+    L, stream = fc.lib(), ctx.raw_stream()
+    p = 1 << 40
+    far = fc._ATTENTION.pack(1 << 16, 1, 1, 1 << 15, 0, 64, p, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 2 * p, 1 << 22, 1 << 21, 64, 0, 0, 0, 0, 0.1, 0, 0, 0)
+    assert L.ficoco_window_attention(ctx._h, far, stream) == fc.EUNSUPPORTED
+    ws = fc.Workspace(256, "cuda")
+    assert L.ficoco_cache_attention(ctx._h, c._p, 0, far, ws.ptr, ws.bytes, stream) == fc.EUNSUPPORTED
+    assert L.ficoco_cache_free(ctx._h, c._p, 1 << 24, None, stream) == fc.EUNSUPPORTED
+    tokens = fc._TOKENS.pack(1, 1 << 29, fc.BF16, 0, 0, 0, p, 0, 1 << 40, 1 << 40, 64, 0, 0, 0)
+    assert L.ficoco_cache_read(ctx._h, c._p, 0, tokens, stream) == fc.EUNSUPPORTED
+    torch.cuda.synchronize()
+    assert not c.k.any() and not c.refs.any() and not c.len.any()
