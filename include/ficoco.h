@@ -454,7 +454,8 @@ int ficoco_cache_reserve(ficoco_ctx *ctx, const ficoco_cache *c, int32_t n, cons
                          int32_t n_each, int32_t *start, void *stream);
 
 /* Writes the tokens of one layer into their pages.  A page that is begun inside keeps what lies before: it takes the larger of
- * its exponent and that of the new tokens, the older ones rewritten to it (exactly, but for E4M3's denormals).  What lies behind
+ * its exponent and that of the new tokens, the older ones rewritten to it (exactly, but for E4M3's denormals): what lies before has to have been
+ * written in this layer, or its exponent, which counts all the same, be one that the new tokens can bear.  What lies behind
  * the new tokens in a page is void.  Sequences with start[b] < 0 are left out, and so are positions that have no page.  Two entries
  * of a call must not write one page (the starts of ficoco_cache_reserve see to it). */
 int ficoco_cache_append(ficoco_ctx *ctx, const ficoco_cache *c, int32_t layer, const ficoco_tokens *t, void *stream);
@@ -475,7 +476,8 @@ int ficoco_cache_fork(ficoco_ctx *ctx, const ficoco_cache *c, int32_t n, const i
  * visual span is [vis_begin, vis_begin + N).  dst[b] = src[b] replaces the sequence; otherwise dst[b] must be empty.  Whole pages
  * before the first token that moves are kept (shared); the others are written anew into free pages, each
  * block with the exponent of what it holds, and src's own are given back if it is replaced.  Other layers of the new
- * pages are void.  done[b], out: as ficoco_cache_fork (a src may be replaced, not read, by another entry), also 0 where src[b] has fewer than
+ * pages are void, also where they held earlier tokens of the sequence: what is appended to such a layer begins at the first of these pages.  All
+ * layers share one length: a decoder that reduces at several layers and keeps the layers before longer has a ficoco_cache for each length.  done[b], out: as ficoco_cache_fork (a src may be replaced, not read, by another entry), also 0 where src[b] has fewer than
  * vis_begin + N tokens or a token that would go into a new page has no page.  ws: ficoco_cache_workspace_bytes, 256-byte aligned. */
 int ficoco_cache_workspace_bytes(const ficoco_cache *c, int32_t n, size_t *out_bytes);
 int ficoco_cache_compact(ficoco_ctx *ctx, const ficoco_cache *c, int32_t layer_begin, int32_t n_layers, int32_t n, const int32_t *src,

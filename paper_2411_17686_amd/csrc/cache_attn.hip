@@ -39,10 +39,13 @@ __device__ __forceinline__ float quarters_sum(float v) {
 //   O^T[feature][row] += V^T P^T   contraction over 32 keys in the order in which a lane holds its logits, so that the weights
 //                                  stay where they are; operand A eight keys of one feature, out of a byte transposition
 // 8 bits become bfloat16 (exactly, the block's scale with them) in front of the products.  A row's maximum is the reference of its
-// exponentials as long as no logit lies more than 2^8 above it.
+// exponentials as long as no logit lies more than 8 (units of log2) above it: a weight then stays below 2^8.  Weights are rounded to bfloat16 for the second
+// product (half a step, 2^-9 to 2^-8 of each; their sum is of the unrounded ones): single precision has a sixteenth of its rate, and two parts of bfloat16 would
+// double it.  Against 64 bits results are off by 0.0021 of their size, the plain form by 0.0017, which is the rounding of the results.
 //
-// Bound by memory: 2 d_head bytes a token and head.  4 sequences of 40000 .. 65536 tokens, 32 heads on 8: 86 us with the join, 5.3 TB/s (5.7 without: a
-// plain read's rate); 32 of 300 .. 4096: 37 us, 4.1 TB/s (the longest sequences end last); one of 243: 6 us, a launch and three trips to memory.
+// Bound by memory: 2 d_head bytes a token and head.  4 sequences of 40000 .. 65536 tokens, 32 heads on 8: 80 us, 5.7 TB/s, a plain read's rate; with the join 86 .. 89;
+// 32 of 300 .. 4096: 37 us with the join, 4.1 TB/s (the longest sequences end last); one of 243: 6 us, a launch and three trips to memory.  24 sequences,
+// 28 heads of 64 on 4, behind a window of 1 .. 32 tokens 5.2 us, of 2048 9.4, 4096 13.3, 8192 21.3: such a start, then 6.3 TB/s.
 template <int D>
 __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendArgs a) {
   constexpr int L = D / 64;                  // 16-byte loads of a key
@@ -349,7 +352,15 @@ AttendPlan attend_plan(const ficoco_attention& a, int heads, int64_t max_keys, b
   const int64_t rows = (int64_t)a.n_q * (a.H / heads), bh = (int64_t)a.B * heads;
   // Workgroups of 16 rows that stream the keys, or of 128 that have them in LDS.  One of 16: 4 rows of 243 tokens 6 us, the other way 11; of 40000 .. 65536 86 and 155.
   // Up to four of them, as long as there are few enough to have every key read and converted that often: 64 heads of 2400 tokens, 32 rows 17 and 25, 64 rows
-  // 23 and 27; 512 heads of 1000 .. 2000, 32 rows 71 and 75; 128 heads, 64 rows 28 and 33; but 1024 heads, 32 rows 150 and 133; 256 heads, 64 rows 56 and 51.
+  // 23 and 27.  1000 .. 2000 tokens, heads of 128 (of 64), this way and the other:
+  //   heads   32 rows                       48 rows                       64 rows
+  //   128     21 and 32 us (16 and 23)      27 and 32 (20 and 23)         27 and 33 (20 and 24)
+  //   256     27 and 46 (20 and 34)         45 and 48 (24 and 34)         54 and 49 (29 and 35): the other way
+  //   344     46 and 66 (23 and 48)         65 and 67 (33 and 49): 1032, the other way    77 and 68 (40 and 49): the other way
+  //   512     66 and 71 (32 and 50)         93 and 72 (48 and 51): the other way          120 and 73 (61 and 52): the other way
+  //   1024    151 and 137 (64 and 93): the other way for all
+  // The line is drawn for heads of 128 and a few thousand tokens.  Beyond it heads of 64 take up to 1.6 times what they could (344 heads behind 300 .. 600, 48 rows:
+  // 13 and 21 us), and short of it long sequences up to 1.3 times: behind 6000 .. 9000, 128 heads of 128, 48 rows 107 and 86 us, 256 heads 211 and 163; 512 heads, 32 rows 347 and 294.
   const int64_t tiles = (rows + kFewRows - 1) / kFewRows;
   pl.few = paged && (tiles <= 1 || (tiles <= 4 && bh * tiles <= (tiles <= 3 ? 1024 : 512)));
   pl.rows = pl.few ? kFewRows : kTileRows;

@@ -27,9 +27,9 @@ template <int D> struct TileRaw { uint4 x[D / 32]; };       // a thread's share 
 // turns.  So keys are in LDS a step ahead of the values; either in two buffers, what comes next on its way while a step is computed.
 //
 // Bound by LDS, out of which four SIMDs at their full rate would take 128 bytes a cycle, all it gives, while the loads write to it, and by the matrix cores at the
-// clock that they leave (1.9 GHz): 16384 tokens, window of 4096, 32 heads of 128 on 8: 910 .. 940 us, 1.03 PFLOP/s of
-// products (a large library product reaches 1.2); without its loads it would take 714, without exponentials 843.  Two prompts of 675 tokens, 32 heads: 20 us, of
-// which 5 before the first step.
+// clock that they leave (1.9 GHz): 16384 tokens, window of 4096, 32 heads of 128 on 8: 920 .. 960 us on different cards, 1.00 .. 1.05 PFLOP/s of
+// products (a large library product reaches 1.2); without its loads it would take 714, without exponentials 843 (where it takes 920).  Two prompts of 675 tokens,
+// 32 heads: 19 .. 20 us, of which 5 before the first step.  Weights are rounded to bfloat16 for the second product, as in few_rows_kernel (cache_attn.hip).
 template <int D, TileSource SRC>
 __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a) {
   constexpr int DT = D / 32, KS = D / 16, CH = D / 8;
