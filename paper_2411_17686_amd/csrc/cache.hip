@@ -247,7 +247,7 @@ __global__ __launch_bounds__(kMoveThreads) void cache_append_kernel(ficoco_cache
 // One token a sequence (a decoder's step): eight values a lane, so a row of 16 lanes (heads of 64: half of one) holds the token of one head, K or V.
 // Older tokens of the page are touched only where the new one raises the exponent: one by one, a trip to memory each, by the lanes of that block.  48 sequences, 32
 // heads, pages of 64: 3.3 us where no exponent rises, a launch and its trips (with the kernel above, a workgroup per block, 8.5 us).  A decoder's new tokens
-// raise some of the 3072 blocks in most steps: 256 steps with normal keys and values 19 us at the median, 29 for a tenth of them, 34 at most; every block raised by
+// raise some block in most steps: 256 steps with normal keys and values 19 us at the median, 29 for a tenth of them, 34 at most; every block raised by
 // the last token of a page of 128 57 us.
 template <typename T, int D>
 __global__ __launch_bounds__(kMoveThreads) void cache_append_token_kernel(ficoco_cache c, int64_t layer_pages, TokenSide ks, TokenSide vs, int items,

@@ -564,7 +564,7 @@ def _attention(Q, O, K, V, scale, window, sinks, q_len, k_len, q_start, seq, max
 
 
 def attention_workspace(cache, Q, O, window=0, sinks=0, max_len=0):
-    """Workspace of ficoco_cache_attention for calls of these shapes."""
+    """Workspace of ficoco_cache_attention for calls of these shapes, with this max_len or a smaller one (0 = the largest)."""
     out = C.c_size_t()
     rc = lib().ficoco_cache_attention_workspace_bytes(
         cache._p, _attention(Q, O, None, None, None, window, sinks, None, None, None, None, max_len), C.byref(out))
