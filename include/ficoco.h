@@ -496,6 +496,76 @@ int ficoco_cache_attention(ficoco_ctx *ctx, const ficoco_cache *c, int32_t layer
 /* Attention of dense prompts (k_len NULL = n_k), with or without a window.  Keys that no query of a block sees are not read. */
 int ficoco_window_attention(ficoco_ctx *ctx, const ficoco_attention *a, void *stream);
 
+/* ---- Queries and keys on their way from a projection -------------------------------------------------
+ *
+ * Norm of each head and rotation to the token's position, in one pass, in single precision, rounded once to the outputs' type.
+ *
+ *   norm      y = x / sqrt(mean(x^2) + eps), or (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps), times the weight, plus the bias, over all
+ *             d_head features of a head.  The sum of the squares has to stay inside single precision.
+ *   rotation  pair i of the rotated features becomes (a cos - b sin, b cos + a sin) * amplitude with the angle f[i] * (position of the
+ *             token on axis[i]).  Features in front of rot_begin and from rot_begin + rot_dim on keep the value that the norm gave.
+ *
+ * Angles are counted in turns, as 64-bit fractions: position * turns[i] modulo 2^64 is the fraction of a turn, whatever the position (within
+ * 2^-33 of a turn at position 2^31; a negative position turns backwards, so that -p undoes p where amplitude is 1 and there is no norm).  Sines and cosines are within 2^-23. */
+typedef enum {
+  FICOCO_ROTARY_HALVES = 0, /* pair i: features rot_begin + i and rot_begin + i + rot_dim / 2 */
+  FICOCO_ROTARY_PAIRS = 1   /* pair i: features rot_begin + 2 i and rot_begin + 2 i + 1       */
+} ficoco_rotary_layout;
+typedef enum { FICOCO_NORM_NONE = 0, FICOCO_NORM_RMS = 1, FICOCO_NORM_LAYER = 2 } ficoco_norm;
+
+/* Frequencies in radians a token: f[i] = base^(-2 i / rot_dim) / divisors[i] (divisors NULL: ones).  For contexts longer than those trained by `factor`:
+ * length = 0: every f[i] is divided by factor; otherwise f[i] (s + (1 - s) / factor), s = (length f[i] / 2 pi - low) / (high - low), at least 0 and at most 1:
+ * frequencies of fewer than `low` turns over `length` tokens are divided, those of more than `high` kept.  (A base that grows with the context: give that base.)
+ * turns [rot_dim / 2], out: f[i] / 2 pi modulo 1 in units of 2^-64.  Host arithmetic on host memory; the table is copied to the device once. */
+typedef struct {
+  int32_t rot_dim;
+  double base, factor, length, low, high;
+  const double *divisors; /* [rot_dim / 2], host memory, or NULL */
+} ficoco_frequencies;
+int ficoco_rotary_turns(const ficoco_frequencies *f, uint64_t *turns);
+
+/* What a model fixes for all of its calls. */
+typedef struct {
+  int32_t d_head;                     /* 1 .. 512                                                */
+  int32_t rot_begin, rot_dim, layout; /* rotated features of a head (rot_dim even, 0 = none); ficoco_rotary_layout */
+  int32_t norm, weight_dtype, per_head; /* ficoco_norm; ficoco_dtype of weights and biases; one row for all heads, or (per_head) one each */
+  float eps, amplitude;
+  const uint64_t *turns;              /* [rot_dim / 2]                                           */
+  const uint8_t *axis;                /* [rot_dim / 2], NULL = axis 0; an axis that a call has no positions for counts as 0 */
+  const void *q_weight, *k_weight;    /* [d_head] or [heads][d_head]; NULL = ones                */
+  const void *q_bias, *k_bias;        /* the same; NULL = zeros                                  */
+} ficoco_rotary;
+
+/* Rows of a call: token t < n_rows[b] <= n of sequence b, all heads.  Rows behind them are left as they are.  Strides in elements, d_head contiguous, any
+ * element alignment.  An output is its input (same address, type and strides: in place) or shares no element with any of them; views
+ * of one packed projection are told apart where their strides allow it. */
+typedef struct {
+  int32_t B, H, H_kv, n;
+  int32_t dtype, out_dtype; /* ficoco_dtype of Q and K, of Q_out and K_out */
+  const void *Q;            /* [B][H][n][d_head], or NULL                  */
+  int64_t q_stride_b, q_stride_h, q_stride_n;
+  const void *K;            /* [B][H_kv][n][d_head], or NULL               */
+  int64_t k_stride_b, k_stride_h, k_stride_n;
+  void *Q_out;
+  int64_t qo_stride_b, qo_stride_h, qo_stride_n;
+  void *K_out;
+  int64_t ko_stride_b, ko_stride_h, ko_stride_n;
+  const int32_t *pos;       /* [axes][B][n] positions, the last axis contiguous; NULL = start[b] + t on all axes */
+  int64_t pos_stride_axis, pos_stride_b;
+  int32_t axes;             /* 1 .. 256 */
+  const int32_t *start;     /* [B], NULL = 0 */
+  const int32_t *n_rows;    /* [B], NULL = n */
+} ficoco_rotation;
+
+int ficoco_rotate(ficoco_ctx *ctx, const ficoco_rotary *r, const ficoco_rotation *x, void *stream);
+
+/* ficoco_rotate of the keys and ficoco_cache_append in one pass: a key goes from single precision into its page, rounded once, the values as in
+ * ficoco_cache_append, and the rows are what ficoco_cache_append says of t.  Queries (x->Q may be NULL) come out as by ficoco_rotate, those of entries that are
+ * left out (start < 0, a slot out of range) not at all.  x->pos NULL = the tokens' positions in the cache; of x, B and n are those of t, and H_kv, K, K_out, start and n_rows
+ * are not read.  Heads of 64 and 128, rot_begin a multiple of 8 and rot_dim of 16 (others FICOCO_EUNSUPPORTED). */
+int ficoco_cache_append_rotated(ficoco_ctx *ctx, const ficoco_cache *c, int32_t layer, const ficoco_rotary *r, const ficoco_tokens *t,
+                                const ficoco_rotation *x, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -13,7 +13,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libficoco.so")
 SOURCES = ["api.hip", "attn_reduce.hip", "attn_qk.hip", "select.hip", "correlate.hip", "compress.hip", "features.hip", "schedule.hip",
-           "cache_api.hip", "cache.hip", "cache_attn.hip", "page_attn.hip", "tile_attn.hip"]
+           "cache_api.hip", "cache.hip", "cache_attn.hip", "page_attn.hip", "tile_attn.hip", "rotary.hip",
+           "rotary_cache.hip", "rotary_api.hip"]
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "-shared", "--offload-arch=gfx950",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-command-line-argument", "-Wno-unknown-warning-option"]

@@ -21,10 +21,6 @@ struct PlanLds {
   int served;
 };
 
-__device__ __forceinline__ bool slot_ok(const ficoco_cache& c, int s) { return s >= 0 && s < c.n_seqs; }
-__device__ __forceinline__ bool page_ok(const ficoco_cache& c, int p) { return p >= 0 && p < c.n_pages; }
-__device__ __forceinline__ int pages_of(const ficoco_cache& c, int64_t tokens) { return (int)((tokens + c.page_size - 1) / c.page_size); }
-
 // owner[s] = the first entry b of the call with slot(b) == s
 template <int NT, typename F>
 __device__ __forceinline__ void find_owners(const ficoco_cache& c, PlanLds& l, int n, F slot) {
@@ -131,51 +127,6 @@ __global__ __launch_bounds__(NT) void cache_reserve_kernel(ficoco_cache c, int n
 }
 
 // ---- tokens in and out of blocks ----------------------------------------------------------------------------
-__device__ __forceinline__ void load8f(const bf16_t* p, float (&x)[8]) {
-  uint4 r;
-  __builtin_memcpy(&r, p, 16);
-  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void load8f(const float* p, float (&x)[8]) { __builtin_memcpy(x, p, 32); }
-__device__ __forceinline__ void store8f(float* p, const float (&x)[8]) { __builtin_memcpy(p, x, 32); }
-__device__ __forceinline__ void store8f(bf16_t* p, const float (&x)[8]) {      // (exact: three mantissa bits)
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = (__float_as_uint(x[2 * i]) >> 16) | (__float_as_uint(x[2 * i + 1]) & 0xffff0000u);
-  __builtin_memcpy(p, w, 16);
-}
-
-struct TokenSide {       // K or V of a call
-  const void* x;
-  int64_t sb, sh, sn;
-  uint8_t* pool;
-  uint8_t* exps;
-};
-
-__device__ __forceinline__ float block_max(float v, float* scratch) {
-  v = wave_reduce(v, [](float a, float b) { return fmaxf(a, b); });
-  const int nw = blockDim.x / kWave;
-  __syncthreads();
-  if (threadIdx.x % kWave == 0) scratch[threadIdx.x / kWave] = v;
-  __syncthreads();
-  for (int w = 0; w < nw; ++w) v = fmaxf(v, scratch[w]);
-  return v;
-}
-
-// What a call writes to one sequence: positions [first, stop) of slot `slot`, none where first < 0.
-struct Span { int slot, first; int64_t stop; };
-__device__ __forceinline__ Span span_of(const ficoco_cache& c, int b, int n_max, const int32_t* seq, const int32_t* start, const int32_t* n_new) {
-  const int s = seq ? seq[b] : b, first = start[b];
-  int n = n_new ? n_new[b] : n_max;
-  n = n < n_max ? n : n_max;
-  return slot_ok(c, s) && first >= 0 && n > 0 ? Span{s, first, (int64_t)first + n} : Span{0, -1, -1};
-}
-
 // One workgroup per touched page, head, sequence and K / V: the new tokens' largest magnitude, then all of them.  GPT: groups of
 // sixteen values a thread.  The tokens are on their way before the page is looked up.
 //
@@ -621,11 +572,6 @@ __global__ __launch_bounds__(kMoveThreads) void cache_free_kernel(ficoco_cache c
     if (page_ok(c, page)) atomicSub(&c.refs[page], 1);
   }
   if (threadIdx.x == 0) c.len[s] = 0;
-}
-
-TokenSide side_of(const ficoco_tokens& t, const ficoco_cache& c, bool v) {
-  return v ? TokenSide{t.V, t.v_stride_b, t.v_stride_h, t.v_stride_n, (uint8_t*)c.v, c.v_exp}
-           : TokenSide{t.K, t.k_stride_b, t.k_stride_h, t.k_stride_n, (uint8_t*)c.k, c.k_exp};
 }
 
 // Whether a plan is made by 256 threads instead of 1024: pages that these see at one look, and no more entries than `most`.  Four wavefronts wait less for

@@ -1,0 +1,213 @@
+// Norm and rotation of queries and keys: what the kernel of dense rows (rotary.hip) and those that write into pages (rotary_cache.hip) share.
+#pragma once
+#include "cache.hpp"
+
+namespace ficoco {
+
+struct RotaryArgs {
+  const uint64_t* turns;
+  const uint8_t* axis;
+  const int32_t* pos;
+  int64_t pos_sa, pos_sb;
+  const int32_t* start;
+  const void *q_weight, *k_weight, *q_bias, *k_bias;
+  int axes, d, begin, rot, pairs, norm, weight_f32, per_head;      // pairs: neighbours turn together, else the two halves
+  float eps, amplitude, inv_d;
+};
+RotaryArgs rotary_args(const ficoco_rotary& r, const ficoco_rotation& x);
+
+// A head's features as slots of two chunks of W: the two chunks of a slot hold W pairs that turn together (halves: features W i of either half; neighbours: 2 W
+// features in a row), and behind these slots come the features that do not turn, in their order, two chunks each.
+template <int W>
+struct Slot {
+  int a, b;            // first features of the chunks, -1: no such chunk
+  int turn;            // first frequency, -1: not turned
+};
+template <int W>
+__device__ __forceinline__ Slot<W> slot_of(const RotaryArgs& r, int i) {
+  const int turned = r.rot / (2 * W);
+  if (i < turned) {
+    const int a = r.begin + (r.pairs ? 2 * W : W) * i;
+    return Slot<W>{a, r.pairs ? a + W : a + r.rot / 2, W * i};
+  }
+  const int rest = r.d - r.rot, at = 2 * W * (i - turned);
+  auto place = [&](int f) { return f >= rest ? -1 : f < r.begin ? f : f + r.rot; };
+  return Slot<W>{place(at), place(at + W), -1};
+}
+inline int slots_of(int d, int rot, int w) { return rot / (2 * w) + ((d - rot) / w + 1) / 2; }
+
+// Where token t of sequence b stands: on every axis there where positions are given, else `own`.
+struct Place {
+  const int32_t* pos;
+  int64_t own, step;
+};
+__device__ __forceinline__ Place place_of(const RotaryArgs& r, int b, int64_t t, int64_t own) {
+  return Place{r.pos ? r.pos + (int64_t)b * r.pos_sb + t : nullptr, own, r.pos_sa};
+}
+
+// sin and cos of `angle` turns / 2^32, times `amplitude`: a quarter turn by its two top bits (rounded), the rest |x| <= pi / 4 by the first terms of their series (what is left
+// out is below 2^-29).
+__device__ __forceinline__ void sin_cos(uint32_t angle, float amplitude, float& s, float& c) {
+  const uint32_t q = angle + 0x20000000u;
+  const float x = (float)(int32_t)(angle - (q & 0xc0000000u)) * 1.46291807926715968105e-9f, y = x * x;      // 2 pi / 2^32
+  float u = fmaf(y, 2.7557319224e-6f, -1.9841269841e-4f);
+  u = fmaf(y, u, 8.3333333333e-3f);
+  u = fmaf(y, u, -1.6666666667e-1f);
+  u = fmaf(x * y, u, x);
+  float v = fmaf(y, -2.7557319224e-7f, 2.4801587302e-5f);
+  v = fmaf(y, v, -1.3888888889e-3f);
+  v = fmaf(y, v, 4.1666666667e-2f);
+  v = fmaf(y, v, -0.5f);
+  v = fmaf(y, v, 1.0f);
+  const bool odd = q & 0x40000000u;
+  s = (odd ? v : u) * __uint_as_float(__float_as_uint(amplitude) ^ (q & 0x80000000u));
+  c = (odd ? u : v) * __uint_as_float(__float_as_uint(amplitude) ^ ((q ^ q << 1) & 0x80000000u));
+}
+
+template <int W>
+struct Angles { float s[W], c[W]; };
+template <int W>
+__device__ __forceinline__ void angles_of(const RotaryArgs& r, const Slot<W>& slot, const Place& p, Angles<W>& x) {
+  if (slot.turn < 0) return;
+  uint64_t turns[W];
+  __builtin_memcpy(turns, r.turns + slot.turn, sizeof(turns));
+  if (!p.pos || r.axes == 1 || !r.axis) {
+    const int64_t at = p.pos ? (int64_t)p.pos[0] : p.own;
+#pragma unroll
+    for (int i = 0; i < W; ++i) sin_cos((uint32_t)((uint64_t)at * turns[i] >> 32), r.amplitude, x.s[i], x.c[i]);
+  } else {
+    uint8_t axis[W];
+    __builtin_memcpy(axis, r.axis + slot.turn, W);
+    int32_t at[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) at[i] = p.pos[(axis[i] < r.axes ? axis[i] : 0) * p.step];
+#pragma unroll
+    for (int i = 0; i < W; ++i) sin_cos((uint32_t)((uint64_t)(int64_t)at[i] * turns[i] >> 32), r.amplitude, x.s[i], x.c[i]);
+  }
+}
+template <int W>
+__device__ __forceinline__ void turn(const RotaryArgs& r, const Slot<W>& slot, const Angles<W>& x, float (&v)[2 * W]) {
+  if (slot.turn < 0) return;
+  if (r.pairs) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      const float a = v[2 * i], b = v[2 * i + 1];
+      v[2 * i] = fmaf(a, x.c[i], -(b * x.s[i]));
+      v[2 * i + 1] = fmaf(b, x.c[i], a * x.s[i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      const float a = v[i], b = v[W + i];
+      v[i] = fmaf(a, x.c[i], -(b * x.s[i]));
+      v[W + i] = fmaf(b, x.c[i], a * x.s[i]);
+    }
+  }
+}
+
+template <int W>
+__device__ __forceinline__ void load_chunk(const bf16_t* p, float* x) {
+  if constexpr (W == 8) {
+    load8f(p, *(float(*)[8])x);
+  } else {
+    uint16_t h[W];
+    __builtin_memcpy(h, p, sizeof(h));
+#pragma unroll
+    for (int i = 0; i < W; ++i) x[i] = __uint_as_float((uint32_t)h[i] << 16);
+  }
+}
+template <int W>
+__device__ __forceinline__ void load_chunk(const float* p, float* x) { __builtin_memcpy(x, p, W * sizeof(float)); }
+template <int W>
+__device__ __forceinline__ void store_chunk(float* p, const float* x) { __builtin_memcpy(p, x, W * sizeof(float)); }
+template <int W>
+__device__ __forceinline__ void store_chunk(bf16_t* p, const float* x) {
+  __bf16 h[W];
+#pragma unroll
+  for (int i = 0; i < W; ++i) h[i] = (__bf16)x[i];
+  __builtin_memcpy(p, h, sizeof(h));
+}
+template <int W>
+__device__ __forceinline__ void load_weights(const void* w, int f32, int64_t at, float* x) {
+  if (f32) load_chunk<W>((const float*)w + at, x);
+  else load_chunk<W>((const bf16_t*)w + at, x);
+}
+
+// Sum over `lanes` (a power of two) neighbouring lanes.
+__device__ __forceinline__ float group_sum(float v, int lanes) {
+  if (lanes > 1) v += dpp_move<0xB1>(v);
+  if (lanes > 2) v += dpp_move<0x4E>(v);
+  if (lanes > 4) v += dpp_move<0x141>(v);
+  if (lanes > 8) v += dpp_move<0x140>(v);
+  if (lanes > 16) v += __shfl_xor(v, 16);
+  if (lanes > 32) v += __shfl_xor(v, 32);
+  return v;
+}
+
+// The norm of a head's row in NS slots a lane, `lanes` lanes; chunks that do not exist hold zeros.
+template <int W, int NS>
+__device__ __forceinline__ void normalise(const RotaryArgs& r, const Slot<W> (&slot)[NS], int lanes, const void* weight, const void* bias, int h, float (&v)[NS][2 * W]) {
+#pragma clang fp contract(off)      // (a row gives the same numbers in every kernel that normalises it)
+  if (r.norm == FICOCO_NORM_NONE) return;
+  float mean = 0.0f;
+  if (r.norm == FICOCO_NORM_LAYER) {
+#pragma unroll
+    for (int k = 0; k < NS; ++k) {
+#pragma unroll
+      for (int i = 0; i < 2 * W; ++i) mean += v[k][i];
+    }
+    mean = group_sum(mean, lanes) * r.inv_d;
+  }
+  float square = 0.0f;
+#pragma unroll
+  for (int k = 0; k < NS; ++k) {
+#pragma unroll
+    for (int i = 0; i < 2 * W; ++i) {
+      const float x = (i < W ? slot[k].a : slot[k].b) >= 0 ? v[k][i] - mean : 0.0f;
+      v[k][i] = x;
+      square = fmaf(x, x, square);
+    }
+  }
+  const float inv = 1.0f / sqrtf(fmaf(group_sum(square, lanes), r.inv_d, r.eps));
+  const int64_t at = r.per_head ? (int64_t)h * r.d : 0;
+#pragma unroll
+  for (int k = 0; k < NS; ++k) {
+    float w[2 * W], o[2 * W];
+#pragma unroll
+    for (int i = 0; i < 2 * W; ++i) {
+      w[i] = 1.0f;
+      o[i] = 0.0f;
+    }
+    if (weight) {
+      if (slot[k].a >= 0) load_weights<W>(weight, r.weight_f32, at + slot[k].a, w);
+      if (slot[k].b >= 0) load_weights<W>(weight, r.weight_f32, at + slot[k].b, w + W);
+    }
+    if (bias) {
+      if (slot[k].a >= 0) load_weights<W>(bias, r.weight_f32, at + slot[k].a, o);
+      if (slot[k].b >= 0) load_weights<W>(bias, r.weight_f32, at + slot[k].b, o + W);
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * W; ++i) v[k][i] = fmaf(v[k][i] * inv, w[i], o[i]);
+  }
+}
+
+struct HeadRows {       // queries or keys of a call
+  const void* x;
+  void* out;
+  int64_t sb, sh, sn, ob, oh, on;
+  int heads;
+};
+struct RotateArgs {
+  RotaryArgs r;
+  HeadRows q, k;
+  int B, n;
+  const int32_t *n_rows;
+  // of an append: rows of entries that it leaves out are left out
+  const int32_t *seq, *first;
+  int n_seqs;
+};
+void launch_rotate(const RotateArgs& a, int dtype, int out_dtype, hipStream_t s);
+int64_t rotate_threads(const RotateArgs& a);
+void launch_append_rotated(const ficoco_cache& c, int layer, const ficoco_tokens& t, const RotateArgs& q, int out_dtype, hipStream_t s);
+
+}  // namespace ficoco

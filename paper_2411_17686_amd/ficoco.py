@@ -23,6 +23,8 @@ PROBE_REDUCE, PROBE_GRAM, PROBE_GRAM_X16 = 0, 1, 2
 PROBE_REPEAT = 16
 K_ADAPTIVE, K_FIXED, K_CONVERGENT = 0, 1, 2
 COMPRESS_SELF, COMPRESS_AVERAGE = 0, 1
+ROTARY_HALVES, ROTARY_PAIRS = 0, 1
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 
 EXPORTS = ["ficoco_create", "ficoco_destroy", "ficoco_last_error", "ficoco_version",
            "ficoco_set_probe", "ficoco_workspace_bytes", "ficoco_out_rows", "ficoco_reduce", "ficoco_score",
@@ -30,7 +32,8 @@ EXPORTS = ["ficoco_create", "ficoco_destroy", "ficoco_last_error", "ficoco_versi
            "ficoco_l_step", "ficoco_schedule", "ficoco_gather_tokens", "ficoco_v_step_static",
            "ficoco_cache_reserve", "ficoco_cache_append", "ficoco_cache_read", "ficoco_cache_fork",
            "ficoco_cache_workspace_bytes", "ficoco_cache_compact", "ficoco_cache_free",
-           "ficoco_cache_attention_workspace_bytes", "ficoco_cache_attention", "ficoco_window_attention"]
+           "ficoco_cache_attention_workspace_bytes", "ficoco_cache_attention", "ficoco_window_attention",
+           "ficoco_rotary_turns", "ficoco_rotate", "ficoco_cache_append_rotated"]
 STATIC_SCRATCH_BYTES = 32 << 20
 
 
@@ -100,6 +103,31 @@ class AttentionProblem(C.Structure):
                 ("scale", C.c_float), ("window", C.c_int32), ("sinks", C.c_int32), ("max_len", C.c_int32)]
 
 
+class FrequenciesProblem(C.Structure):
+    """Mirror of `ficoco_frequencies`."""
+    _fields_ = [("rot_dim", C.c_int32), ("base", C.c_double), ("factor", C.c_double), ("length", C.c_double), ("low", C.c_double),
+                ("high", C.c_double), ("divisors", C.c_void_p)]
+
+
+class RotaryProblem(C.Structure):
+    """Mirror of `ficoco_rotary`."""
+    _fields_ = [("d_head", C.c_int32), ("rot_begin", C.c_int32), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("norm", C.c_int32),
+                ("weight_dtype", C.c_int32), ("per_head", C.c_int32), ("eps", C.c_float), ("amplitude", C.c_float),
+                ("turns", C.c_void_p), ("axis", C.c_void_p), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p),
+                ("q_bias", C.c_void_p), ("k_bias", C.c_void_p)]
+
+
+class RotationProblem(C.Structure):
+    """Mirror of `ficoco_rotation`."""
+    _fields_ = [("B", C.c_int32), ("H", C.c_int32), ("H_kv", C.c_int32), ("n", C.c_int32), ("dtype", C.c_int32), ("out_dtype", C.c_int32),
+                ("Q", C.c_void_p), ("q_stride_b", C.c_int64), ("q_stride_h", C.c_int64), ("q_stride_n", C.c_int64),
+                ("K", C.c_void_p), ("k_stride_b", C.c_int64), ("k_stride_h", C.c_int64), ("k_stride_n", C.c_int64),
+                ("Q_out", C.c_void_p), ("qo_stride_b", C.c_int64), ("qo_stride_h", C.c_int64), ("qo_stride_n", C.c_int64),
+                ("K_out", C.c_void_p), ("ko_stride_b", C.c_int64), ("ko_stride_h", C.c_int64), ("ko_stride_n", C.c_int64),
+                ("pos", C.c_void_p), ("pos_stride_axis", C.c_int64), ("pos_stride_b", C.c_int64), ("axes", C.c_int32),
+                ("start", C.c_void_p), ("n_rows", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -144,6 +172,9 @@ def lib():
         L.ficoco_cache_attention_workspace_bytes.argtypes = [cp, ap, C.POINTER(C.c_size_t)]
         L.ficoco_cache_attention.argtypes = [vp, cp, i32, ap, vp, C.c_size_t, vp]
         L.ficoco_window_attention.argtypes = [vp, ap, vp]
+        L.ficoco_rotary_turns.argtypes = [C.POINTER(FrequenciesProblem), vp]
+        L.ficoco_rotate.argtypes = [vp, vp, vp, vp]
+        L.ficoco_cache_append_rotated.argtypes = [vp, cp, i32, vp, vp, vp, vp]
         for name in EXPORTS:
             getattr(L, name)            # fail loudly here if the build lacks a symbol
         _lib = L
@@ -589,5 +620,125 @@ def ficoco_window_attention(ctx, Q, K, V, O, scale=None, window=0, sinks=0, q_le
     _same_device(ctx, Q.get_device())
     rc = lib().ficoco_window_attention(ctx._h, _attention(Q, O, K, V, scale, window, sinks, q_len, k_len, q_start, None, 0),
                                        ctx.raw_stream())
+    if rc:
+        ctx.check(rc)
+
+
+# ---- queries and keys on their way from a projection ---------------------------------------------
+# `ficoco_rotary` and `ficoco_rotation` as packed bytes, as above.
+_ROTARY = struct.Struct("@7i2f6P")
+_ROTATION = struct.Struct("@6iP3qP3qP3qP3qP2qi2P")
+_NO_ROWS = (0, 0, 0, 0)
+
+
+def rotary_turns(rot_dim, base=10000.0, factor=1.0, length=0.0, low=1.0, high=32.0, divisors=None):
+    """The frequencies of ficoco_rotary_turns as int64 [rot_dim / 2] (their 64 bits) on the host; divisors: floats, or None."""
+    half = max(rot_dim // 2, 0)
+    if divisors is not None:
+        if len(divisors) != half:
+            raise TypeError("divisors must be %d numbers" % half)
+        divisors = (C.c_double * max(half, 1))(*divisors)
+    turns = torch.zeros(half, dtype=torch.int64)
+    f = FrequenciesProblem(rot_dim, base, factor, length, low, high, C.cast(divisors, C.c_void_p) if divisors is not None else None)
+    rc = lib().ficoco_rotary_turns(C.byref(f), turns.data_ptr() or None)
+    if rc != OK:
+        raise FicocoError(rc, "ficoco_rotary_turns rejected the arguments")
+    return turns
+
+
+class Rotary:
+    """A `ficoco_rotary`: what a model fixes of its rotation and norm, and its tensors, on one device.  turns: int64 [rot_dim / 2] of rotary_turns(); axis:
+    uint8 of the same shape; weights and biases [d_head], or all of them [heads][d_head]."""
+
+    def __init__(self, d_head, turns, layout=ROTARY_HALVES, rot_begin=0, axis=None, amplitude=1.0, norm=NORM_NONE, eps=1e-6, q_weight=None,
+                 k_weight=None, q_bias=None, k_bias=None):
+        if turns.dtype != torch.int64 or turns.dim() != 1 or not turns.is_contiguous():
+            raise TypeError("turns must be contiguous int64 [rot_dim / 2]")
+        self.index, self.d_head = turns.get_device(), d_head
+        if axis is not None and (axis.dtype != torch.uint8 or axis.shape != turns.shape or not axis.is_contiguous() or axis.get_device() != self.index):
+            raise TypeError("axis must be contiguous uint8 of the shape of turns, on its device")
+        given = [t for t in (q_weight, k_weight, q_bias, k_bias) if t is not None]
+        rows = given[0].dim() if given else 1
+        for t in given:
+            if t.dtype != given[0].dtype or t.dim() != rows or rows not in (1, 2) or t.shape[-1] != d_head or not t.is_contiguous() or t.get_device() != self.index:
+                raise TypeError("weights and biases are contiguous, of one type, all [d_head] or all [heads][d_head], on the device of turns")
+        self.heads = [{t.shape[0] for t in side if t is not None and rows == 2} for side in ((q_weight, q_bias), (k_weight, k_bias))]
+        self.kept = (turns, axis, q_weight, k_weight, q_bias, k_bias)
+        at = [0 if t is None else t.data_ptr() for t in self.kept]
+        self.packed = _ROTARY.pack(d_head, rot_begin, 2 * turns.numel(), layout, norm, _dtype_code(given[0]) if given else F32, int(rows == 2), eps,
+                                   amplitude, *at)
+
+    def check_heads(self, H, H_kv):
+        if (H is not None and not self.heads[0] <= {H}) or (H_kv is not None and not self.heads[1] <= {H_kv}):
+            raise TypeError("weights of each head do not have the heads of the rows")
+
+
+def _head_rows(t, d, index, name):
+    """Address and strides of [B][heads][n][d_head] rows."""
+    sb, sh, sn, s1 = t.stride()
+    if t.shape[3] != d or (s1 != 1 and d > 1) or t.get_device() != index:
+        raise TypeError("%s must be [B][heads][n][d_head], d_head contiguous, on device %d" % (name, index))
+    return t.data_ptr(), sb, sh, sn
+
+
+def _rotation(rotary, Q, K, Q_out, K_out, pos, start, n_rows):
+    some = K if Q is None else Q
+    if some is None:
+        raise TypeError("Q and K are both None")
+    d, index = rotary.d_head, rotary.index
+    B, _, n, _ = some.shape
+    out = K_out if Q is None else Q_out
+    H = H_kv = None
+    q = k = qo = ko = _NO_ROWS
+    if Q is not None:
+        H = Q.shape[1]
+        q, qo = _head_rows(Q, d, index, "Q"), _head_rows(Q_out, d, index, "Q_out")
+        if Q_out.shape != Q.shape:
+            raise TypeError("Q_out has not the shape of Q")
+    if K is not None:
+        H_kv = K.shape[1]
+        k, ko = _head_rows(K, d, index, "K"), _head_rows(K_out, d, index, "K_out")
+        if K_out.shape != K.shape or K.shape[0] != B or K.shape[2] != n or K.dtype != some.dtype or K_out.dtype != out.dtype:
+            raise TypeError("Q and K, and their outputs, are of the same sequences and types")
+    rotary.check_heads(H, H_kv)
+    return _ROTATION.pack(B, H or 0, H_kv or 0, n, _dtype_code(some), _dtype_code(out), *q, *k, *qo, *ko, *_positions(pos, B, n, index),
+                          0 if start is None else _i32(start, B, "start", index), 0 if n_rows is None else _i32(n_rows, B, "n_rows", index))
+
+
+def _positions(pos, B, n, index):
+    if pos is None:
+        return 0, 0, 0, 1
+    shape, stride = pos.shape, pos.stride()
+    if pos.dtype != torch.int32 or shape[-2:] != (B, n) or len(shape) not in (2, 3) or (stride[-1] != 1 and n > 1) or pos.get_device() != index:
+        raise TypeError("pos must be int32 [B][n] or [axes][B][n], the last axis contiguous, on device %d" % index)
+    return pos.data_ptr(), stride[0] if len(shape) == 3 else 0, stride[-2], shape[0] if len(shape) == 3 else 1
+
+
+def ficoco_rotate(ctx, rotary, Q, K, Q_out=None, K_out=None, pos=None, start=None, n_rows=None):
+    """Q and K (either may be None) [B][heads][n][d_head]; outputs None = in place.  pos: int32 [B][n], or [axes][B][n]."""
+    _same_device(ctx, rotary.index)
+    rc = lib().ficoco_rotate(ctx._h, rotary.packed, _rotation(rotary, Q, K, Q if Q_out is None else Q_out, K if K_out is None else K_out, pos, start, n_rows),
+                             ctx.raw_stream())
+    if rc:
+        ctx.check(rc)
+
+
+def ficoco_cache_append_rotated(ctx, cache, layer, rotary, Q, Q_out, K, V, start, pos=None, n_new=None, seq=None):
+    """Queries into Q_out (None = in place; Q may be None), keys and values into their pages; pos as in ficoco_rotate, None = start[b] + t."""
+    _same_device(ctx, rotary.index)
+    if K is None or V is None:
+        raise TypeError("K or V is None")
+    tokens = _tokens(ctx, cache, K, V, start, n_new, seq)
+    B, H_kv, n, _ = K.shape
+    if Q is None:
+        rotary.check_heads(None, H_kv)
+        code = _dtype_code(K)
+        rows = _ROTATION.pack(B, 0, 0, n, code, code, *_NO_ROWS, *_NO_ROWS, *_NO_ROWS, *_NO_ROWS, *_positions(pos, B, n, rotary.index), 0, 0)
+    else:
+        if Q.shape[0] != B or Q.shape[2] != n:
+            raise TypeError("Q is not of the sequences of K")
+        rotary.check_heads(None, H_kv)
+        rows = _rotation(rotary, Q, None, Q if Q_out is None else Q_out, None, pos, None, None)
+    rc = lib().ficoco_cache_append_rotated(ctx._h, cache._p, layer, rotary.packed, tokens, rows, ctx.raw_stream())
     if rc:
         ctx.check(rc)
