@@ -10,21 +10,6 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
-// n / d without a division: m = floor(2^(31 + l) / d) + 1 with 2^l >= d, and n m / 2^(31 + l) is above n / d by less than 1 / d for n < 2^31.
-struct Divisor {
-  uint32_t d, m, s;
-  Divisor() = default;
-  explicit Divisor(int64_t by) : d((uint32_t)by), m(0), s(0) {
-    int l = 0;
-    while ((int64_t)1 << l < by) ++l;
-    if (l > 0) {
-      m = (uint32_t)(((uint64_t)1 << (31 + l)) / (uint64_t)by + 1);
-      s = (uint32_t)(l - 1);
-    }
-  }
-  __device__ __forceinline__ int of(int n) const { return d == 1 ? n : (int)(__umulhi((uint32_t)n, m) >> s); }
-};
-
 // A key / value head serves `group` query heads; their rows are taken together, row r = query r / group of head
 // r % group, so that a block's keys are read once for all of them.
 struct AttendArgs {

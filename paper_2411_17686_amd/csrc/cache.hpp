@@ -13,6 +13,21 @@ constexpr float kE4m3Max = 448.0f;
 constexpr int kExpTop = 247;         // byte of the largest floats: 2^120, in units of which they lie below 256
 constexpr float kTopFinite = 240.0f * 0x1p120f;      // the largest E4M3 number of such a block that is read back as a finite one
 
+// n / d without a division: m = floor(2^(31 + l) / d) + 1 with 2^l >= d, and n m / 2^(31 + l) is above n / d by less than 1 / d for n < 2^31.
+struct Divisor {
+  uint32_t d, m, s;
+  Divisor() = default;
+  explicit Divisor(int64_t by) : d((uint32_t)by), m(0), s(0) {
+    int l = 0;
+    while ((int64_t)1 << l < by) ++l;
+    if (l > 0) {
+      m = (uint32_t)(((uint64_t)1 << (31 + l)) / (uint64_t)by + 1);
+      s = (uint32_t)(l - 1);
+    }
+  }
+  __device__ __forceinline__ int of(int n) const { return d == 1 ? n : (int)(__umulhi((uint32_t)n, m) >> s); }
+};
+
 // Workspace of a compaction: {first new page, pages, tokens, -} of every sequence, then the rows of the table before it.
 inline size_t compact_workspace(const ficoco_cache& c, int n) {
   return ((size_t)n * 4 * sizeof(int32_t) + (size_t)n * c.max_pages * sizeof(int32_t) + 255) / 256 * 256;

@@ -1,4 +1,5 @@
 // Norm and rotation of queries and keys, and the frequencies that it goes by.
+#include <algorithm>
 #include <cmath>
 
 #include "rotary.hpp"
@@ -8,104 +9,138 @@ namespace {
 
 constexpr int kRotateThreads = 256;
 
-// How rows are laid over lanes: 2^shift lanes a row, `per_token` items a token, HPT heads an item (per_token apart).
-struct RowShape { int shift, per_token; };
+constexpr int kAtOnce = 2;           // heads of a lane whose loads are on their way together
 
-// A lane holds NS slots of a head (slot_of()) and turns them in HPT heads by the same angles.  All loads of a lane are on their way before the angles are formed.
+enum NormForm { kNoNorm, kPlainNorm, kAnyNorm };      // (none; root mean square without a bias; whatever the call says)
+
+// How rows are laid over lanes: `lanes` lanes a row, items of up to `heads` heads of one token, q_items of queries and k_items of keys.
+struct RowShape {
+  int lanes, heads, q_items, k_items;
+  Divisor by_lanes, by_items, by_rows;
+};
+
+// A lane holds NS slots of a head (slot_of()) and turns them by the same angles in all heads of its item.
 //
 // Bound by memory.
-template <typename T, typename TO, int W, int NS, int HPT>
+template <typename T, typename TO, int W, int NS, NormForm NORM>
 __global__ __launch_bounds__(kRotateThreads) void rotate_kernel(RotateArgs a, RowShape shape) {
-  const uint32_t at = blockIdx.x * kRotateThreads + threadIdx.x, item = at >> shape.shift, token = item / (uint32_t)shape.per_token;
-  const int lanes = 1 << shape.shift, i = at & (lanes - 1), h0 = item - token * shape.per_token, b = token / (uint32_t)a.n;
-  const int t = token - (uint32_t)b * a.n;
+  const int at = blockIdx.x * kRotateThreads + threadIdx.x, all = shape.by_lanes.of(at), token = shape.by_items.of(all), b = shape.by_rows.of(token);
+  const int i = at - all * shape.lanes, t = token - b * a.n, in = all - token * (shape.q_items + shape.k_items);
   if (b >= a.B) return;
+  const bool key = in >= shape.q_items;
+  const HeadRows& x = key ? a.k : a.q;
+  const int first = key ? in - shape.q_items : in, step = key ? shape.k_items : shape.q_items;      // heads first, first + step ..
   int rows = a.n;
   if (a.n_rows) rows = a.n_rows[b] < rows ? a.n_rows[b] : rows;
   bool there = t < rows;
   int64_t own = t;
   if (a.first) {
-    const int s = a.seq ? a.seq[b] : b, first = a.first[b];
-    there &= s >= 0 && s < a.n_seqs && first >= 0;
-    own += first;
+    const int s = a.seq ? a.seq[b] : b, from = a.first[b];
+    there &= s >= 0 && s < a.n_seqs && from >= 0;
+    own += from;
   } else if (a.r.start) {
     own += a.r.start[b];
   }
+  if (!there) return;                                      // (all lanes of a row)
   Slot<W> slot[NS];
 #pragma unroll
-  for (int k = 0; k < NS; ++k) slot[k] = slot_of<W>(a.r, i + k * lanes);
-  const int heads = a.q.heads + a.k.heads;
-  float v[HPT][NS][2 * W];
+  for (int k = 0; k < NS; ++k) slot[k] = slot_of<W>(a.r, i + k * shape.lanes);
+  Angles<W> angle[NS];
+  Weights<W, NS> weights;
+  const void *weight = key ? a.r.k_weight : a.r.q_weight, *bias = key ? a.r.k_bias : a.r.q_bias;
+  const T* from = (const T*)x.x + (int64_t)b * x.sb + (int64_t)t * x.sn;
+  TO* to = (TO*)x.out + (int64_t)b * x.ob + (int64_t)t * x.on;
+  for (int h0 = first; h0 < x.heads; h0 += kAtOnce * step) {
+    Raw<T, W> raw[kAtOnce][NS][2];
 #pragma unroll
-  for (int j = 0; j < HPT; ++j) {
-    const int h = h0 + j * shape.per_token;
-    const bool key = h >= a.q.heads;
-    const HeadRows& x = key ? a.k : a.q;
-    const T* p = (const T*)x.x + (int64_t)b * x.sb + (int64_t)(key ? h - a.q.heads : h) * x.sh + (int64_t)t * x.sn;
+    for (int j = 0; j < kAtOnce; ++j) {
+      const int h = h0 + j * step;
+      if (h < x.heads) {
+        const T* p = from + (int64_t)h * x.sh;
 #pragma unroll
-    for (int k = 0; k < NS; ++k) {
+        for (int k = 0; k < NS; ++k) {
+          if (slot[k].a >= 0) __builtin_memcpy(&raw[j][k][0], p + slot[k].a, sizeof(raw[j][k][0]));
+          if (slot[k].b >= 0) __builtin_memcpy(&raw[j][k][1], p + slot[k].b, sizeof(raw[j][k][1]));
+        }
+      }
+    }
+    if (h0 == first) {
+      const Place place = place_of(a.r, b, t, own);
 #pragma unroll
-      for (int e = 0; e < 2 * W; ++e) v[j][k][e] = 0.0f;
-      if (there && h < heads) {
-        if (slot[k].a >= 0) load_chunk<W>(p + slot[k].a, v[j][k]);
-        if (slot[k].b >= 0) load_chunk<W>(p + slot[k].b, v[j][k] + W);
+      for (int k = 0; k < NS; ++k) angles_of<W>(a.r, slot[k], place, angle[k]);
+      if (NORM != kNoNorm && !a.r.per_head) weights_of<W, NS>(a.r, slot, weight, bias, 0, weights);
+    }
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      const int h = h0 + j * step;
+      if (h >= x.heads) break;
+      float v[NS][2 * W];
+#pragma unroll
+      for (int k = 0; k < NS; ++k) {
+#pragma unroll
+        for (int e = 0; e < 2 * W; ++e) v[k][e] = 0.0f;
+        if (slot[k].a >= 0) widen<W>(raw[j][k][0], v[k]);
+        if (slot[k].b >= 0) widen<W>(raw[j][k][1], v[k] + W);
+      }
+      if (NORM != kNoNorm && (NORM == kPlainNorm || a.r.norm != FICOCO_NORM_NONE)) {
+        if (a.r.per_head) weights_of<W, NS>(a.r, slot, weight, bias, h, weights);
+        normalise<W, NS, NORM == kPlainNorm>(a.r, slot, shape.lanes, weights, v);
+      }
+      TO* p = to + (int64_t)h * x.oh;
+#pragma unroll
+      for (int k = 0; k < NS; ++k) {
+        turn<W>(a.r, slot[k], angle[k], v[k]);
+        if (slot[k].a >= 0) store_chunk<W>(p + slot[k].a, v[k]);
+        if (slot[k].b >= 0) store_chunk<W>(p + slot[k].b, v[k] + W);
       }
     }
   }
-  if (!there) return;                                      // (all lanes of a row)
-  Angles<W> angle[NS];
-  const Place place = place_of(a.r, b, t, own);
-#pragma unroll
-  for (int k = 0; k < NS; ++k) angles_of<W>(a.r, slot[k], place, angle[k]);
-#pragma unroll
-  for (int j = 0; j < HPT; ++j) {
-    const int h = h0 + j * shape.per_token;
-    if (h >= heads) break;
-    const bool key = h >= a.q.heads;
-    const HeadRows& x = key ? a.k : a.q;
-    const int hh = key ? h - a.q.heads : h;
-    normalise<W, NS>(a.r, slot, lanes, key ? a.r.k_weight : a.r.q_weight, key ? a.r.k_bias : a.r.q_bias, hh, v[j]);
-    TO* p = (TO*)x.out + (int64_t)b * x.ob + (int64_t)hh * x.oh + (int64_t)t * x.on;
-#pragma unroll
-    for (int k = 0; k < NS; ++k) {
-      turn<W>(a.r, slot[k], angle[k], v[j][k]);
-      if (slot[k].a >= 0) store_chunk<W>(p + slot[k].a, v[j][k]);
-      if (slot[k].b >= 0) store_chunk<W>(p + slot[k].b, v[j][k] + W);
-    }
-  }
 }
 
-// The widest chunk that the rotated features begin and end with.
-int chunk_width(const RotaryArgs& r) {
-  for (int w = 8; w > 1; w /= 2)
+// The widest chunk that the rotated features begin and end with, of 16 bytes at most: lanes next to each other then load what lies next to each other (float rows of
+// 80 by chunks of 8 55 us, of 4 ).
+int chunk_width(const RotaryArgs& r, int most) {
+  for (int w = most; w > 1; w /= 2)
     if (r.d % w == 0 && r.begin % w == 0 && r.rot % (2 * w) == 0) return w;
   return 1;
 }
-RowShape shape_of(const RotateArgs& a, int width, int hpt) {
-  const int slots = slots_of(a.r.d, a.r.rot, width);
-  int shift = 0;
-  while (shift < 6 && 1 << shift < slots) ++shift;
-  const int heads = a.q.heads + a.k.heads;
-  return RowShape{shift, (heads + hpt - 1) / hpt};
+RowShape shape_of(const RotateArgs& a, int width) {
+  const int slots = std::max(1, slots_of(a.r.d, a.r.rot, width));
+  RowShape s{};
+  // A norm is a sum over lanes of one wavefront, a power of two of them; without one a row takes what lanes it needs.
+  s.lanes = slots;
+  if (a.r.norm != FICOCO_NORM_NONE || slots > kWave)
+    for (s.lanes = 1; s.lanes < kWave && s.lanes < slots;) s.lanes *= 2;
+  // Several heads an item where there are rows enough to fill the chip that way.
+  s.heads = (int64_t)a.B * a.n * (a.q.heads + a.k.heads) * a.r.d >= 1 << 23 ? 4 : 1;
+  s.q_items = (a.q.heads + s.heads - 1) / s.heads;
+  s.k_items = (a.k.heads + s.heads - 1) / s.heads;
+  s.by_lanes = Divisor(s.lanes);
+  s.by_items = Divisor((int64_t)s.q_items + s.k_items);
+  s.by_rows = Divisor(a.n);
+  return s;
 }
-// Several heads a lane where there are rows enough to fill the chip that way.
-int heads_a_lane(const RotateArgs& a) { return (int64_t)a.B * a.n * (a.q.heads + a.k.heads) * a.r.d >= 1 << 23 ? 4 : 1; }
 
-template <typename T, typename TO, int W, int NS>
+template <typename T, typename TO, int W, int NS, NormForm NORM>
 void launch_rows(const RotateArgs& a, hipStream_t s) {
-  const int hpt = heads_a_lane(a);
-  const RowShape shape = shape_of(a, W, hpt);
-  const dim3 grid((unsigned)(((((int64_t)a.B * a.n * shape.per_token) << shape.shift) + kRotateThreads - 1) / kRotateThreads));
-  if (hpt == 4) hipLaunchKernelGGL((rotate_kernel<T, TO, W, NS, 4>), grid, dim3(kRotateThreads), 0, s, a, shape);
-  else hipLaunchKernelGGL((rotate_kernel<T, TO, W, NS, 1>), grid, dim3(kRotateThreads), 0, s, a, shape);
+  const RowShape shape = shape_of(a, W);
+  const int64_t threads = (int64_t)a.B * a.n * (shape.q_items + shape.k_items) * shape.lanes;
+  hipLaunchKernelGGL((rotate_kernel<T, TO, W, NS, NORM>), dim3((unsigned)((threads + kRotateThreads - 1) / kRotateThreads)), dim3(kRotateThreads), 0, s, a, shape);
+}
+template <typename T, typename TO, int W>
+void launch_norm(const RotateArgs& a, hipStream_t s) {
+  if (a.r.norm == FICOCO_NORM_NONE) launch_rows<T, TO, W, 1, kNoNorm>(a, s);
+  else if (a.r.norm == FICOCO_NORM_RMS && !a.r.q_bias && !a.r.k_bias) launch_rows<T, TO, W, 1, kPlainNorm>(a, s);
+  else launch_rows<T, TO, W, 1, kAnyNorm>(a, s);
 }
 template <typename T, typename TO>
 void launch_width(const RotateArgs& a, hipStream_t s) {
-  switch (chunk_width(a.r)) {
-    case 8: launch_rows<T, TO, 8, 1>(a, s); break;
-    case 4: launch_rows<T, TO, 4, 1>(a, s); break;
-    case 2: launch_rows<T, TO, 2, 2>(a, s); break;
-    default: launch_rows<T, TO, 1, 4>(a, s); break;
+  constexpr int most = sizeof(T) == 2 && sizeof(TO) == 2 ? 8 : 4;
+  switch (chunk_width(a.r, most)) {
+    case 8: if constexpr (most == 8) launch_norm<T, TO, 8>(a, s); break;
+    case 4: launch_norm<T, TO, 4>(a, s); break;
+    case 2: launch_rows<T, TO, 2, 2, kAnyNorm>(a, s); break;
+    default: launch_rows<T, TO, 1, 4, kAnyNorm>(a, s); break;
   }
 }
 
@@ -125,9 +160,9 @@ RotaryArgs rotary_args(const ficoco_rotary& r, const ficoco_rotation& x) {
   return y;
 }
 
-int64_t rotate_threads(const RotateArgs& a) {
-  const RowShape shape = shape_of(a, chunk_width(a.r), heads_a_lane(a));
-  const __int128 n = ((__int128)a.B * a.n * shape.per_token) << shape.shift;
+int64_t rotate_threads(const RotateArgs& a, int dtype, int out_dtype) {
+  const RowShape s = shape_of(a, chunk_width(a.r, dtype == FICOCO_BF16 && out_dtype == FICOCO_BF16 ? 8 : 4));
+  const __int128 n = (__int128)a.B * a.n * ((int64_t)s.q_items + s.k_items) * s.lanes;
   return n > INT64_MAX ? INT64_MAX : (int64_t)n;
 }
 

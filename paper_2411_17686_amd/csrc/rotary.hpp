@@ -1,5 +1,7 @@
 // Norm and rotation of queries and keys: what the kernel of dense rows (rotary.hip) and those that write into pages (rotary_cache.hip) share.
 #pragma once
+#include <type_traits>
+
 #include "cache.hpp"
 
 namespace ficoco {
@@ -64,6 +66,11 @@ __device__ __forceinline__ void sin_cos(uint32_t angle, float amplitude, float& 
   c = (odd ? u : v) * __uint_as_float(__float_as_uint(amplitude) ^ ((q ^ q << 1) & 0x80000000u));
 }
 
+// The fraction of a turn, in 2^-32, of `turns` at position p, -2^31 <= p < 2^32: bits 32 .. 63 of their product.
+__device__ __forceinline__ uint32_t turned_by(int64_t p, uint64_t turns) {
+  const uint32_t low = (uint32_t)turns;
+  return (uint32_t)p * (uint32_t)(turns >> 32) + __umulhi((uint32_t)p, low) - (low & (uint32_t)(p >> 63));
+}
 template <int W>
 struct Angles { float s[W], c[W]; };
 template <int W>
@@ -74,15 +81,18 @@ __device__ __forceinline__ void angles_of(const RotaryArgs& r, const Slot<W>& sl
   if (!p.pos || r.axes == 1 || !r.axis) {
     const int64_t at = p.pos ? (int64_t)p.pos[0] : p.own;
 #pragma unroll
-    for (int i = 0; i < W; ++i) sin_cos((uint32_t)((uint64_t)at * turns[i] >> 32), r.amplitude, x.s[i], x.c[i]);
+    for (int i = 0; i < W; ++i) sin_cos(turned_by(at, turns[i]), r.amplitude, x.s[i], x.c[i]);
   } else {
-    uint8_t axis[W];
-    __builtin_memcpy(axis, r.axis + slot.turn, W);
+    uint64_t axis = 0;
+    __builtin_memcpy(&axis, r.axis + slot.turn, W);
     int32_t at[W];
 #pragma unroll
-    for (int i = 0; i < W; ++i) at[i] = p.pos[(axis[i] < r.axes ? axis[i] : 0) * p.step];
+    for (int i = 0; i < W; ++i) {
+      const int on = (int)(axis >> 8 * i) & 255;
+      at[i] = p.pos[(on < r.axes ? on : 0) * p.step];
+    }
 #pragma unroll
-    for (int i = 0; i < W; ++i) sin_cos((uint32_t)((uint64_t)(int64_t)at[i] * turns[i] >> 32), r.amplitude, x.s[i], x.c[i]);
+    for (int i = 0; i < W; ++i) sin_cos(turned_by(at[i], turns[i]), r.amplitude, x.s[i], x.c[i]);
   }
 }
 template <int W>
@@ -105,19 +115,31 @@ __device__ __forceinline__ void turn(const RotaryArgs& r, const Slot<W>& slot, c
   }
 }
 
+// A chunk as it comes out of memory, in whole words where it has any: the compiler otherwise gives every half word a register of its own.
+template <typename T, int W>
+struct Raw {
+  static constexpr int WORDS = W * (int)sizeof(T) / 4;
+  typename std::conditional<WORDS == 0, uint16_t, uint32_t>::type x[WORDS == 0 ? W : WORDS];
+};
 template <int W>
-__device__ __forceinline__ void load_chunk(const bf16_t* p, float* x) {
-  if constexpr (W == 8) {
-    load8f(p, *(float(*)[8])x);
-  } else {
-    uint16_t h[W];
-    __builtin_memcpy(h, p, sizeof(h));
+__device__ __forceinline__ void widen(const Raw<bf16_t, W>& r, float* x) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) x[i] = __uint_as_float((uint32_t)h[i] << 16);
+  for (int i = 0; i < W; ++i) {
+    if constexpr (W == 1) x[i] = __uint_as_float((uint32_t)r.x[i] << 16);
+    else x[i] = __uint_as_float(i % 2 ? r.x[i / 2] & 0xffff0000u : r.x[i / 2] << 16);
   }
 }
 template <int W>
-__device__ __forceinline__ void load_chunk(const float* p, float* x) { __builtin_memcpy(x, p, W * sizeof(float)); }
+__device__ __forceinline__ void widen(const Raw<float, W>& r, float* x) {
+#pragma unroll
+  for (int i = 0; i < W; ++i) x[i] = __uint_as_float(r.x[i]);
+}
+template <int W, typename T>
+__device__ __forceinline__ void load_chunk(const T* p, float* x) {
+  Raw<T, W> r;
+  __builtin_memcpy(&r, p, sizeof(r));
+  widen<W>(r, x);
+}
 template <int W>
 __device__ __forceinline__ void store_chunk(float* p, const float* x) { __builtin_memcpy(p, x, W * sizeof(float)); }
 template <int W>
@@ -144,50 +166,74 @@ __device__ __forceinline__ float group_sum(float v, int lanes) {
   return v;
 }
 
-// The norm of a head's row in NS slots a lane, `lanes` lanes; chunks that do not exist hold zeros.
+// Weights and biases of a lane's slots; those of chunks that do not exist do not matter.
 template <int W, int NS>
-__device__ __forceinline__ void normalise(const RotaryArgs& r, const Slot<W> (&slot)[NS], int lanes, const void* weight, const void* bias, int h, float (&v)[NS][2 * W]) {
-#pragma clang fp contract(off)      // (a row gives the same numbers in every kernel that normalises it)
-  if (r.norm == FICOCO_NORM_NONE) return;
-  float mean = 0.0f;
-  if (r.norm == FICOCO_NORM_LAYER) {
-#pragma unroll
-    for (int k = 0; k < NS; ++k) {
-#pragma unroll
-      for (int i = 0; i < 2 * W; ++i) mean += v[k][i];
-    }
-    mean = group_sum(mean, lanes) * r.inv_d;
-  }
-  float square = 0.0f;
-#pragma unroll
-  for (int k = 0; k < NS; ++k) {
-#pragma unroll
-    for (int i = 0; i < 2 * W; ++i) {
-      const float x = (i < W ? slot[k].a : slot[k].b) >= 0 ? v[k][i] - mean : 0.0f;
-      v[k][i] = x;
-      square = fmaf(x, x, square);
-    }
-  }
-  const float inv = 1.0f / sqrtf(fmaf(group_sum(square, lanes), r.inv_d, r.eps));
+struct Weights { float w[NS][2 * W], o[NS][2 * W]; };
+template <int W, int NS>
+__device__ __forceinline__ void weights_of(const RotaryArgs& r, const Slot<W> (&slot)[NS], const void* weight, const void* bias, int h, Weights<W, NS>& x) {
   const int64_t at = r.per_head ? (int64_t)h * r.d : 0;
 #pragma unroll
   for (int k = 0; k < NS; ++k) {
-    float w[2 * W], o[2 * W];
 #pragma unroll
     for (int i = 0; i < 2 * W; ++i) {
-      w[i] = 1.0f;
-      o[i] = 0.0f;
+      x.w[k][i] = 1.0f;
+      x.o[k][i] = 0.0f;
     }
     if (weight) {
-      if (slot[k].a >= 0) load_weights<W>(weight, r.weight_f32, at + slot[k].a, w);
-      if (slot[k].b >= 0) load_weights<W>(weight, r.weight_f32, at + slot[k].b, w + W);
+      if (slot[k].a >= 0) load_weights<W>(weight, r.weight_f32, at + slot[k].a, x.w[k]);
+      if (slot[k].b >= 0) load_weights<W>(weight, r.weight_f32, at + slot[k].b, x.w[k] + W);
     }
     if (bias) {
-      if (slot[k].a >= 0) load_weights<W>(bias, r.weight_f32, at + slot[k].a, o);
-      if (slot[k].b >= 0) load_weights<W>(bias, r.weight_f32, at + slot[k].b, o + W);
+      if (slot[k].a >= 0) load_weights<W>(bias, r.weight_f32, at + slot[k].a, x.o[k]);
+      if (slot[k].b >= 0) load_weights<W>(bias, r.weight_f32, at + slot[k].b, x.o[k] + W);
     }
+  }
+}
+
+// The sum of f(v) over the chunks of a slot.  Chunks of 8 are added as the two slots of 4 that they consist of, so that the sum over a row is the same number
+// for either width.
+template <int W, typename F>
+__device__ __forceinline__ float slot_sum(bool halves, const float (&v)[2 * W], F f) {
+#pragma clang fp contract(off)
+  float s = 0.0f;
+  if constexpr (W == 8) {
+    float z = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 2 * W; ++i) v[k][i] = fmaf(v[k][i] * inv, w[i], o[i]);
+    for (int i = 0; i < 8; ++i) {
+      s = f(i < 4 ? v[i] : halves ? v[4 + i] : v[i], s);
+      z = f(i < 4 ? (halves ? v[4 + i] : v[8 + i]) : v[8 + i], z);
+    }
+    return s + z;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2 * W; ++i) s = f(v[i], s);
+    return s;
+  }
+}
+
+// The norm of a head's row in NS slots a lane, `lanes` lanes; chunks that do not exist hold zeros.  PLAIN: a root mean square without a bias, decided by the caller.
+template <int W, int NS, bool PLAIN = false>
+__device__ __forceinline__ void normalise(const RotaryArgs& r, const Slot<W> (&slot)[NS], int lanes, const Weights<W, NS>& x, float (&v)[NS][2 * W]) {
+#pragma clang fp contract(off)      // (a row gives the same numbers in every kernel that normalises it)
+  if (!PLAIN && r.norm == FICOCO_NORM_LAYER) {
+    float mean = 0.0f;
+#pragma unroll
+    for (int k = 0; k < NS; ++k) mean += slot_sum<W>(slot[k].turn >= 0 && !r.pairs, v[k], [](float a, float s) { return a + s; });
+    mean = group_sum(mean, lanes) * r.inv_d;
+#pragma unroll
+    for (int k = 0; k < NS; ++k) {
+#pragma unroll
+      for (int i = 0; i < 2 * W; ++i) v[k][i] = (i < W ? slot[k].a : slot[k].b) >= 0 ? v[k][i] - mean : 0.0f;
+    }
+  }
+  float square = 0.0f;
+#pragma unroll
+  for (int k = 0; k < NS; ++k) square += slot_sum<W>(slot[k].turn >= 0 && !r.pairs, v[k], [](float a, float s) { return fmaf(a, a, s); });
+  const float inv = 1.0f / sqrtf(fmaf(group_sum(square, lanes), r.inv_d, r.eps));
+#pragma unroll
+  for (int k = 0; k < NS; ++k) {
+#pragma unroll
+    for (int i = 0; i < 2 * W; ++i) v[k][i] = PLAIN ? v[k][i] * inv * x.w[k][i] : fmaf(v[k][i] * inv, x.w[k][i], x.o[k][i]);
   }
 }
 
@@ -207,7 +253,7 @@ struct RotateArgs {
   int n_seqs;
 };
 void launch_rotate(const RotateArgs& a, int dtype, int out_dtype, hipStream_t s);
-int64_t rotate_threads(const RotateArgs& a);
+int64_t rotate_threads(const RotateArgs& a, int dtype, int out_dtype);
 void launch_append_rotated(const ficoco_cache& c, int layer, const ficoco_tokens& t, const RotateArgs& q, int out_dtype, hipStream_t s);
 
 }  // namespace ficoco

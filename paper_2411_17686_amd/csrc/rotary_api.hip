@@ -128,7 +128,7 @@ int ficoco_rotate(ficoco_ctx* ctx, const ficoco_rotary* r, const ficoco_rotation
   const bool one_type = x->dtype == x->out_dtype;
   if ((!(one_type && same(q, qo)) && may_meet(q, qo)) || (!(one_type && same(k, ko)) && may_meet(k, ko)) || may_meet(qo, k) || may_meet(ko, q) || may_meet(qo, ko))
     return fail(ctx, FICOCO_EINVAL, fn, "an output shares elements with another tensor");
-  if (rotate_threads(a) > kMaxThreads - 256) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "too many rows in one call");
+  if (rotate_threads(a, x->dtype, x->out_dtype) > kMaxRows - 256) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "too many rows in one call");
   launch_rotate(a, x->dtype, x->out_dtype, (hipStream_t)stream);
   return finish(ctx, fn);
 }
@@ -163,7 +163,7 @@ int ficoco_cache_append_rotated(ficoco_ctx* ctx, const ficoco_cache* c, int32_t 
     if ((!(x->dtype == x->out_dtype && same(q, qo)) && may_meet(q, qo)) || may_meet(qo, k) || may_meet(qo, v))
       return fail(ctx, FICOCO_EINVAL, fn, "Q_out shares elements with another tensor");
     if (reaches_into(*c, x->Q_out, (size_t)qo.bytes())) return fail(ctx, FICOCO_EINVAL, fn, "Q_out overlaps the cache");
-    if (rotate_threads(a) > kMaxThreads - 256) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "too many rows in one call");
+    if (rotate_threads(a, x->dtype, x->out_dtype) > kMaxRows - 256) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "too many rows in one call");
   }
   launch_append_rotated(*c, layer, *t, a, x->out_dtype, (hipStream_t)stream);
   return finish(ctx, fn);

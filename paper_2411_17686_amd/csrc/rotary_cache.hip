@@ -43,7 +43,11 @@ __global__ __launch_bounds__(kMoveThreads) void append_rotated_kernel(ficoco_cac
 #pragma unroll
     for (int j = 0; j < GPT; ++j) {
       const int64_t pos = pos0 + ((threadIdx.x + j * kMoveThreads) >> row_shift);
-      normalise<8, 1>(r, slot, 1 << row_shift, r.k_weight, r.k_bias, h, v[j]);
+      if (r.norm != FICOCO_NORM_NONE) {
+        Weights<8, 1> weights;
+        weights_of<8, 1>(r, slot, r.k_weight, r.k_bias, h, weights);
+        normalise<8, 1>(r, slot, 1 << row_shift, weights, v[j]);
+      }
       if (pos >= sp.first && pos < sp.stop) {
         Angles<8> angle;
         angles_of<8>(r, slot[0], place_of(r, b, pos - sp.first, pos), angle);
@@ -116,7 +120,11 @@ __global__ __launch_bounds__(kMoveThreads) void append_rotated_token_kernel(fico
   const int64_t block = ok ? (layer_pages + page) * c.heads + h : 0;
   const int old = ok && place > 0 ? side.exps[block] : 0;
   if (!value) {
-    normalise<8, 1>(a.r, slot, L, query ? a.r.q_weight : a.r.k_weight, query ? a.r.q_bias : a.r.k_bias, h, v);
+    if (a.r.norm != FICOCO_NORM_NONE) {
+      Weights<8, 1> weights;
+      weights_of<8, 1>(a.r, slot, query ? a.r.q_weight : a.r.k_weight, query ? a.r.q_bias : a.r.k_bias, h, weights);
+      normalise<8, 1>(a.r, slot, L, weights, v);
+    }
     if (live) {
       Angles<8> angle;
       angles_of<8>(a.r, slot[0], place_of(a.r, b, 0, sp.first), angle);
