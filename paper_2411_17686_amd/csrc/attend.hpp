@@ -64,25 +64,27 @@ __device__ __forceinline__ Sight sight_of(const AttendArgs& a, int b, int& slot)
   return s;
 }
 
-// Blocks of KEYS keys that queries at positions lo .. hi of a sequence see: `head` blocks from key 0 on (the first tokens),
-// then the blocks from `near` on.
+// Blocks of KEYS keys, of those from key `from` (a multiple of KEYS) to `keys`, that queries at positions lo .. hi of a sequence see: `head` blocks from `from` on (the first
+// tokens), then the blocks from `near` on.
 template <int KEYS>
 struct Blocks {
-  int head, near, count;
+  int head, near, count, start;
   int near_key, first_keys;       // keys below near_key are seen by no row unless they are below first_keys
   int end;                        // keys behind the last one seen
-  __device__ __forceinline__ Blocks(const AttendArgs& a, const Sight& s, int lo, int hi) {
-    end = hi < s.keys ? hi + 1 : s.keys;
-    end = end > 0 ? end : 0;
+  __device__ __forceinline__ Blocks(const AttendArgs& a, int keys, int lo, int hi, int from = 0) {
+    end = hi < keys ? hi + 1 : keys;
+    end = end > from ? end : from;
     near_key = a.window > 0 && lo >= a.window ? lo - a.window + 1 : 0;
     near_key = near_key < end ? near_key : end;
     first_keys = a.sinks < near_key ? a.sinks : near_key;
-    near = near_key / KEYS;
+    start = from / KEYS;
+    near = (near_key > from ? near_key : from) / KEYS;
     head = (first_keys + KEYS - 1) / KEYS;
-    head = head < near ? head : near;
+    head = (head < near ? head : near) - start;
+    head = head > 0 ? head : 0;
     count = head + (end + KEYS - 1) / KEYS - near;
   }
-  __device__ __forceinline__ int block(int i) const { return i < head ? i : near + (i - head); }
+  __device__ __forceinline__ int block(int i) const { return i < head ? start + i : near + (i - head); }
 };
 
 // The keys that one row sees: [lo, lo + span], and those below `first`.

@@ -47,7 +47,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_rows_kernel(AttendArgs a
   const int rows = s.queries * a.group, row0 = tile * kTileRows;
   if (s.queries <= 0 || row0 >= rows) return;
   auto pos_of = [&](int r) { return s.first + a.by_group.of(r < rows ? r : rows - 1); };
-  const Blocks<kTileKeys> blocks(a, s, pos_of(row0), pos_of(row0 + kTileRows - 1));
+  const Blocks<kTileKeys> blocks(a, s.keys, pos_of(row0), pos_of(row0 + kTileRows - 1));
   const int begin = 0, end = blocks.count;
 
   const int r = row0 + 32 * wv + c32, my_r = r < rows ? r : rows - 1;
