@@ -14,7 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libficoco.so")
 SOURCES = ["api.hip", "attn_reduce.hip", "attn_qk.hip", "select.hip", "correlate.hip", "compress.hip", "features.hip", "schedule.hip",
            "cache_api.hip", "cache.hip", "cache_attn.hip", "page_attn.hip", "tile_attn.hip", "rotary.hip",
-           "rotary_cache.hip", "rotary_api.hip"]
+           "rotary_cache.hip", "rotary_api.hip", "share.hip", "share_attn.hip"]
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "-shared", "--offload-arch=gfx950",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-command-line-argument", "-Wno-unknown-warning-option"]

@@ -4,25 +4,26 @@
 
 #include "attend.hpp"
 #include "checks.hpp"
+#include "share.hpp"
 
 using namespace ficoco;
 
 namespace {
 
-// paged: with a cache (its heads), else dense keys and values
-const char* attention_fault(const ficoco_attention& a, int heads, int d_head, bool paged, int* code) {
+// paged: with a cache (its heads), else dense keys and values; shapes: of a plan, which needs no tensors
+const char* attention_fault(const ficoco_attention& a, int heads, int d_head, bool paged, int* code, bool shapes = false) {
   *code = FICOCO_EINVAL;
   if (a.B < 0 || a.n_q < 0 || a.H < 1 || heads < 1) return "a size is negative, or there are no heads";
   if (a.H % heads != 0) return "H is not a multiple of the key / value heads";
   if (a.d_head != d_head) return "d_head is not that of the cache";
   if (a.window < 0 || a.sinks < 0 || a.max_len < 0) return "window, sinks or max_len is negative";
-  if (!(a.scale > 0.0f) || !std::isfinite(a.scale)) return "scale must be positive and finite";
+  if (!shapes && (!(a.scale > 0.0f) || !std::isfinite(a.scale))) return "scale must be positive and finite";
   if (!paged && a.n_k < 0) return "a size is negative";
   const int64_t st[4][3] = {{a.q_stride_b, a.q_stride_h, a.q_stride_n}, {a.o_stride_b, a.o_stride_h, a.o_stride_n},
                             {a.k_stride_b, a.k_stride_h, a.k_stride_n}, {a.v_stride_b, a.v_stride_h, a.v_stride_n}};
-  for (int i = 0; i < (paged ? 2 : 4); ++i)
+  for (int i = 0; i < (shapes ? 0 : paged ? 2 : 4); ++i)
     if (st[i][0] < 0 || st[i][1] < 0 || st[i][2] < 0) return "a stride is negative";
-  if (a.B > 0 && a.n_q > 0) {
+  if (!shapes && a.B > 0 && a.n_q > 0) {
     if (!a.Q || !a.O || (!paged && a.n_k > 0 && (!a.K || !a.V))) return "a pointer is NULL";
     if (((uintptr_t)a.Q | (uintptr_t)a.O | (paged ? 0 : (uintptr_t)a.K | (uintptr_t)a.V)) & 1) return "a tensor is not aligned to its elements";
     const size_t out = extent(a.B, a.H, a.n_q, a.o_stride_b, a.o_stride_h, a.o_stride_n, d_head, 2);
@@ -37,7 +38,7 @@ const char* attention_fault(const ficoco_attention& a, int heads, int d_head, bo
   if ((__int128)a.B * a.H * a.n_q > kMaxRows) return "2^31 rows or more in one call";      // (three times 2^31 pass 64 bits)
   if (!paged && a.n_k > kMaxTokens) return "more than 2^30 keys";
   *code = FICOCO_EINVAL;
-  if (rows_collide(d_head, {{{a.o_stride_b, a.B}, {a.o_stride_h, a.H}, {a.o_stride_n, a.n_q}}})) return "rows of O overlap";
+  if (!shapes && rows_collide(d_head, {{{a.o_stride_b, a.B}, {a.o_stride_h, a.H}, {a.o_stride_n, a.n_q}}})) return "rows of O overlap";
   *code = FICOCO_OK;
   return nullptr;
 }
@@ -65,6 +66,51 @@ AttendArgs arguments(const ficoco_attention& a, int heads, const AttendPlan& pl,
   x.part_ms = (float2*)(ws + pl.part_ms);
   x.part_o = (float*)(ws + pl.part_o);
   return x;
+}
+
+// The pages of a layer.
+void layer_pages(AttendArgs& x, const ficoco_cache& c, int32_t layer) {
+  const int64_t blocks = (int64_t)layer * c.n_pages * c.heads;
+  x.k = (const uint8_t*)c.k + blocks * c.page_size * c.d_head;
+  x.v = (const uint8_t*)c.v + blocks * c.page_size * c.d_head;
+  x.k_exp = c.k_exp + blocks;
+  x.v_exp = c.v_exp + blocks;
+  x.table = c.table; x.len = c.len;
+  x.n_pages = c.n_pages; x.n_seqs = c.n_seqs; x.max_pages = c.max_pages;
+  x.page_shift = __builtin_ctz((unsigned)c.page_size);
+}
+
+// ---- sequences that share pages -------------------------------------------------------------------------------
+const char* share_fault(const ficoco_cache& c, const ficoco_attention& a, bool shapes, SharePlan* pl, int* code) {
+  if (const char* why = attention_fault(a, c.heads, c.d_head, true, code, shapes)) return why;
+  *code = FICOCO_EUNSUPPORTED;
+  if (a.B > kMaxCall) return "more than 1024 sequences in a call";
+  // (three times the rows, and the pieces of a tile: see share_plan())
+  if (4 * (int64_t)a.B * a.n_q * (a.H / c.heads) + 1024 * kTileRows > kMaxRows) return "too many rows in one call";
+  *pl = share_plan(c, a);
+  if ((int64_t)pl->items * c.heads * kTileThreads > kMaxThreads || (int64_t)a.B * a.H * a.n_q * (a.d_head / 4) * 8 > kMaxThreads) return "too many rows in one call";
+  *code = FICOCO_OK;
+  return nullptr;
+}
+
+ShareArgs share_arguments(const ficoco_cache& c, const ficoco_attention& a, const SharePlan& pl, void* plan, char* ws) {
+  ShareArgs s{};
+  AttendPlan none{};
+  none.splits = 1;
+  none.part_ms = pl.part_ms; none.part_o = pl.part_o;
+  s.a = arguments(a, c.heads, none, ws);
+  layer_pages(s.a, c, 0);
+  // what the plan's numbers depend on
+  uint64_t mark = 0x9e3779b97f4a7c15ull;
+  for (const int64_t x : {(int64_t)a.B, (int64_t)a.H, (int64_t)c.heads, (int64_t)a.n_q, (int64_t)a.d_head, (int64_t)a.window, (int64_t)a.sinks, (int64_t)c.page_size, (int64_t)c.n_pages,
+                          (int64_t)c.n_seqs, (int64_t)c.max_pages, (int64_t)pl.items, (int64_t)pl.pieces})
+    mark = (mark ^ (uint64_t)x) * 0x100000001b3ull + (mark >> 29);
+  s.mark = mark;
+  s.plan = (char*)plan;
+  s.by_rows = Divisor((int64_t)a.n_q * (a.H / c.heads));
+  s.own_tile = pl.own_tile; s.own_tiles = pl.own_tiles; s.pieces = pl.pieces; s.items = pl.items;
+  s.entries = pl.entries; s.members = pl.members; s.items_at = pl.items_at;
+  return s;
 }
 
 }  // namespace
@@ -182,17 +228,67 @@ int ficoco_cache_attention(ficoco_ctx* ctx, const ficoco_cache* c, int32_t layer
   if ((int64_t)a->B * c->heads * pl.row_tiles * pl.splits * kTileThreads > kMaxThreads)
     return fail(ctx, FICOCO_EUNSUPPORTED, fn, "too many rows in one call");
   AttendArgs x = arguments(*a, c->heads, pl, (char*)ws);
-  const int64_t blocks = (int64_t)layer * c->n_pages * c->heads;
-  x.k = (const uint8_t*)c->k + blocks * c->page_size * c->d_head;
-  x.v = (const uint8_t*)c->v + blocks * c->page_size * c->d_head;
-  x.k_exp = c->k_exp + blocks;
-  x.v_exp = c->v_exp + blocks;
-  x.table = c->table; x.len = c->len;
-  x.n_pages = c->n_pages; x.n_seqs = c->n_seqs; x.max_pages = c->max_pages;
-  x.page_shift = __builtin_ctz((unsigned)c->page_size);
+  layer_pages(x, *c, layer);
   if (pl.few) launch_few_rows(x, a->d_head, (hipStream_t)stream);
   else launch_page_rows(x, a->d_head, (hipStream_t)stream);
   if (pl.splits > 1) launch_join_rows(x, a->d_head, (hipStream_t)stream);
+  return finish(ctx, fn);
+}
+
+int ficoco_cache_share_bytes(const ficoco_cache* c, const ficoco_attention* a, size_t* plan_bytes, size_t* ws_bytes) {
+  if (!c || !a || !plan_bytes || !ws_bytes) return FICOCO_EINVAL;
+  int code;
+  SharePlan pl;
+  if (cache_fault(*c, &code) || share_fault(*c, *a, true, &pl, &code)) return code;
+  *plan_bytes = pl.bytes;
+  *ws_bytes = pl.ws_bytes;
+  return FICOCO_OK;
+}
+
+int ficoco_cache_share(ficoco_ctx* ctx, const ficoco_cache* c, const ficoco_attention* a, const int32_t* group, void* plan, size_t plan_bytes, void* stream) {
+  const char* fn = "ficoco_cache_share";
+  const int rc = begin(ctx, c, fn);
+  if (rc != FICOCO_OK) return rc;
+  if (!a) return fail(ctx, FICOCO_EINVAL, fn, "attention is NULL");
+  int code;
+  SharePlan pl;
+  if (const char* why = share_fault(*c, *a, true, &pl, &code)) return fail(ctx, code, fn, why);
+  if (a->B == 0 || a->n_q == 0) return FICOCO_OK;
+  if (!plan || ((uintptr_t)plan & 255)) return fail(ctx, FICOCO_EINVAL, fn, "plan is NULL or not 256-byte aligned");
+  if (plan_bytes < pl.bytes) return fail(ctx, FICOCO_ENOMEM, fn, "plan smaller than ficoco_cache_share_bytes()");
+  if (reaches_into(*c, plan, pl.bytes)) return fail(ctx, FICOCO_EINVAL, fn, "the plan overlaps the cache");
+  for (const int32_t* p : {group, a->seq, a->q_len, a->k_len, a->q_start})
+    if (ranges_overlap(p, (size_t)a->B * sizeof(int32_t), plan, pl.bytes)) return fail(ctx, FICOCO_EINVAL, fn, "the plan overlaps an input");
+  ShareArgs s = share_arguments(*c, *a, pl, plan, nullptr);
+  s.group = group;
+  launch_share(s, (hipStream_t)stream);
+  return finish(ctx, fn);
+}
+
+int ficoco_cache_shared_attention(ficoco_ctx* ctx, const ficoco_cache* c, int32_t layer, const ficoco_attention* a, const void* plan, size_t plan_bytes, void* ws, size_t ws_bytes,
+                                  void* stream) {
+  const char* fn = "ficoco_cache_shared_attention";
+  const int rc = begin(ctx, c, fn);
+  if (rc != FICOCO_OK) return rc;
+  if (!a) return fail(ctx, FICOCO_EINVAL, fn, "attention is NULL");
+  if (layer < 0 || layer >= c->layers) return fail(ctx, FICOCO_EINVAL, fn, "no such layer");
+  int code;
+  SharePlan pl;
+  if (const char* why = share_fault(*c, *a, false, &pl, &code)) return fail(ctx, code, fn, why);
+  if (a->B == 0 || a->n_q == 0) return FICOCO_OK;
+  if (!plan || ((uintptr_t)plan & 255)) return fail(ctx, FICOCO_EINVAL, fn, "plan is NULL or not 256-byte aligned");
+  if (plan_bytes < pl.bytes) return fail(ctx, FICOCO_ENOMEM, fn, "plan smaller than ficoco_cache_share_bytes()");
+  if (!ws || ((uintptr_t)ws & 255)) return fail(ctx, FICOCO_EINVAL, fn, "workspace is NULL or not 256-byte aligned");
+  if (ws_bytes < pl.ws_bytes) return fail(ctx, FICOCO_ENOMEM, fn, "workspace smaller than ficoco_cache_share_bytes()");
+  const size_t out = extent(a->B, a->H, a->n_q, a->o_stride_b, a->o_stride_h, a->o_stride_n, a->d_head, 2);
+  const size_t in = extent(a->B, a->H, a->n_q, a->q_stride_b, a->q_stride_h, a->q_stride_n, a->d_head, 2);
+  if (ranges_overlap(a->O, out, ws, pl.ws_bytes) || ranges_overlap(a->Q, in, ws, pl.ws_bytes) || ranges_overlap(plan, pl.bytes, ws, pl.ws_bytes) ||
+      ranges_overlap(a->O, out, plan, pl.bytes))
+    return fail(ctx, FICOCO_EINVAL, fn, "Q, O, the plan and the workspace overlap");
+  if (reaches_into(*c, a->O, out) || reaches_into(*c, ws, pl.ws_bytes)) return fail(ctx, FICOCO_EINVAL, fn, "O or the workspace overlaps the cache");
+  ShareArgs s = share_arguments(*c, *a, pl, (void*)plan, (char*)ws);
+  layer_pages(s.a, *c, layer);
+  launch_share_rows(s, a->d_head, (hipStream_t)stream);
   return finish(ctx, fn);
 }
 

@@ -33,7 +33,8 @@ EXPORTS = ["ficoco_create", "ficoco_destroy", "ficoco_last_error", "ficoco_versi
            "ficoco_cache_reserve", "ficoco_cache_append", "ficoco_cache_read", "ficoco_cache_fork",
            "ficoco_cache_workspace_bytes", "ficoco_cache_compact", "ficoco_cache_free",
            "ficoco_cache_attention_workspace_bytes", "ficoco_cache_attention", "ficoco_window_attention",
-           "ficoco_rotary_turns", "ficoco_rotate", "ficoco_cache_append_rotated"]
+           "ficoco_rotary_turns", "ficoco_rotate", "ficoco_cache_append_rotated",
+           "ficoco_cache_share_bytes", "ficoco_cache_share", "ficoco_cache_shared_attention"]
 STATIC_SCRATCH_BYTES = 32 << 20
 
 
@@ -172,6 +173,9 @@ def lib():
         L.ficoco_cache_attention_workspace_bytes.argtypes = [cp, ap, C.POINTER(C.c_size_t)]
         L.ficoco_cache_attention.argtypes = [vp, cp, i32, ap, vp, C.c_size_t, vp]
         L.ficoco_window_attention.argtypes = [vp, ap, vp]
+        L.ficoco_cache_share_bytes.argtypes = [cp, ap, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
+        L.ficoco_cache_share.argtypes = [vp, cp, ap, i32p, vp, C.c_size_t, vp]
+        L.ficoco_cache_shared_attention.argtypes = [vp, cp, i32, ap, vp, C.c_size_t, vp, C.c_size_t, vp]
         L.ficoco_rotary_turns.argtypes = [C.POINTER(FrequenciesProblem), vp]
         L.ficoco_rotate.argtypes = [vp, vp, vp, vp]
         L.ficoco_cache_append_rotated.argtypes = [vp, cp, i32, vp, vp, vp, vp]
@@ -611,6 +615,51 @@ def ficoco_cache_attention(ctx, cache, layer, Q, O, ws, scale=None, window=0, si
     rc = lib().ficoco_cache_attention(ctx._h, cache._p, layer,
                                       _attention(Q, O, None, None, scale, window, sinks, q_len, k_len, q_start, seq, max_len),
                                       ws.ptr, ws.bytes, ctx.raw_stream())
+    if rc:
+        ctx.check(rc)
+
+
+class Share:
+    """Plan and workspace of a batch of B sequences, H query heads and n_q queries each, that ficoco_cache_share fills and
+    ficoco_cache_shared_attention goes by."""
+
+    def __init__(self, cache, B, H, n_q, window=0, sinks=0, max_len=0):
+        self.shape, self.index = (B, H, n_q, cache.d_head), cache.index
+        self.how = window, sinks, max_len
+        sizes = C.c_size_t(), C.c_size_t()
+        rc = lib().ficoco_cache_share_bytes(cache._p, self.describe(), C.byref(sizes[0]), C.byref(sizes[1]))
+        if rc != OK:
+            raise FicocoError(rc, "ficoco_cache_share_bytes rejected the arguments")
+        self.plan, self.ws = (Workspace(n.value, cache.device) for n in sizes)
+        self.plan.t.zero_()                 # no plan yet
+
+    def describe(self, Q=0, q=(0, 0, 0), O=0, o=(0, 0, 0), arrays=(0, 0, 0, 0), scale=1.0):
+        B, H, n_q, d = self.shape
+        return _ATTENTION.pack(B, H, 0, n_q, 0, d, Q, *q, 0, 0, 0, 0, 0, 0, 0, 0, O, *o, *arrays, scale, *self.how)
+
+
+def ficoco_cache_share(ctx, cache, share, group=None, seq=None, q_len=None, k_len=None, q_start=None):
+    """The plan of a step's attention; group: int32 [B]."""
+    B, d = share.shape[0], share.index
+    _same_device(ctx, cache.index, d)
+    arrays = [_i32(t, B, name, d) for t, name in ((seq, "seq"), (q_len, "q_len"), (k_len, "k_len"), (q_start, "q_start"))]
+    rc = lib().ficoco_cache_share(ctx._h, cache._p, share.describe(arrays=arrays), _i32(group, B, "group", d), share.plan.ptr, share.plan.bytes,
+                                  ctx.raw_stream())
+    if rc:
+        ctx.check(rc)
+
+
+def ficoco_cache_shared_attention(ctx, cache, layer, share, Q, O, scale=None):
+    """Into O, by the plan in `share`; scale None = d_head ** -0.5."""
+    d = share.index
+    _same_device(ctx, cache.index, d)
+    qb, qh, qn, q1 = Q.stride()
+    ob, oh, on, o1 = O.stride()
+    if Q.shape != share.shape or O.shape != share.shape or Q.dtype != torch.bfloat16 or O.dtype != torch.bfloat16 or q1 != 1 or o1 != 1 \
+            or Q.get_device() != d or O.get_device() != d:
+        raise TypeError("Q and O are bfloat16 %s, d_head contiguous, on device %d" % (list(share.shape), d))
+    a = share.describe(Q.data_ptr(), (qb, qh, qn), O.data_ptr(), (ob, oh, on), scale=share.shape[3] ** -0.5 if scale is None else scale)
+    rc = lib().ficoco_cache_shared_attention(ctx._h, cache._p, layer, a, share.plan.ptr, share.plan.bytes, share.ws.ptr, share.ws.bytes, ctx.raw_stream())
     if rc:
         ctx.check(rc)
 
