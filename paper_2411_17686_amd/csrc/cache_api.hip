@@ -86,7 +86,7 @@ const char* share_fault(const ficoco_cache& c, const ficoco_attention& a, bool s
   *code = FICOCO_EUNSUPPORTED;
   if (a.B > kMaxCall) return "more than 1024 sequences in a call";
   // (three times the rows, and the pieces of a tile: see share_plan())
-  if (4 * (int64_t)a.B * a.n_q * (a.H / c.heads) + 1024 * kTileRows > kMaxRows) return "too many rows in one call";
+  if (4 * (int64_t)a.B * a.n_q * (a.H / c.heads) + 2048 * kTileRows > kMaxRows) return "too many rows in one call";
   *pl = share_plan(c, a);
   if ((int64_t)pl->items * c.heads * kTileThreads > kMaxThreads || (int64_t)a.B * a.H * a.n_q * (a.d_head / 4) * 8 > kMaxThreads) return "too many rows in one call";
   *code = FICOCO_OK;
@@ -109,7 +109,7 @@ ShareArgs share_arguments(const ficoco_cache& c, const ficoco_attention& a, cons
   s.plan = (char*)plan;
   s.by_rows = Divisor((int64_t)a.n_q * (a.H / c.heads));
   s.own_tile = pl.own_tile; s.own_tiles = pl.own_tiles; s.pieces = pl.pieces; s.items = pl.items;
-  s.entries = pl.entries; s.members = pl.members; s.items_at = pl.items_at;
+  s.entries = pl.entries; s.members = pl.members; s.owners = pl.owners; s.items_at = pl.items_at;
   return s;
 }
 

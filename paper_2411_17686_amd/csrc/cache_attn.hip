@@ -8,6 +8,12 @@ namespace ficoco {
 namespace {
 
 template <int D>
+struct FewLds {
+  float o[kFewWaves][kFewRows][D + 4], top[kFewWaves * kFewRows], sum[kFewWaves * kFewRows];
+  __device__ __forceinline__ float* at(int w, int row, int feature) { return &o[w][row][feature]; }
+};
+
+template <int D>
 __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendArgs a) {
   __shared__ FewLds<D> lds;
   const int at = a.by_splits.of(blockIdx.x), split = blockIdx.x - at * a.splits, tile = a.by_all.of(at), bh = at - tile * a.B * a.H_kv;

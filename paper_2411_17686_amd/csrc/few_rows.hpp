@@ -30,12 +30,6 @@ __device__ __forceinline__ float quarters_sum(float v) {
   return v + __shfl_xor(v, 32);
 }
 
-template <int D>
-struct FewLds {
-  float o[kFewWaves][kFewRows][D + 4];
-  float top[kFewWaves][kFewRows], sum[kFewWaves][kFewRows];
-};
-
 // o = sum_j softmax_j(scale q . k_j) v_j for 16 rows, in one pass with a running maximum and sum.  Every wavefront takes steps of
 // 32 keys of its own, straight from memory into registers, the next step's loads in flight while one is computed:
 //   S^T[key][row] = K Q^T      operand A a lane's 32 bytes of key lane % 16 (the features of a lane are not in order: Q has them alike)
@@ -52,10 +46,11 @@ struct FewLds {
 //
 // A lane's row (lane % 16) has its queries at q and sees `sight`; `rows` of the 16 rows count.  Keys of head h are those of blocks begin .. end - 1 and of the table's `row`;
 // lo, hi: the rows' first and last position, keys: how many keys each of them has at least.  put(r, feature, x, top, sum): eight features of
-// row r, relative to the row's maximum, and its sum.
-template <int D, typename Put>
-__device__ __forceinline__ void few_rows(const AttendArgs& a, FewLds<D>& lds, int h, const bf16_t* q, const RowSight& sight, int rows, int lo, int hi, int keys,
-                                         const int32_t* row, const Blocks<kFewKeys>& blocks, int begin, int end, Put put) {
+// row r, relative to the row's maximum, and its sum.  lds: where the wavefronts' parts meet: at(w, row, feature), eight features from a multiple of eight on next to each other, and top, sum
+// [kFewWaves * kFewRows].
+template <int D, typename Lds, typename Steps, typename Put>
+__device__ __forceinline__ void few_rows(const AttendArgs& a, Lds& lds, int h, const bf16_t* q, const RowSight& sight, int rows, int lo, int hi, int keys,
+                                         const int32_t* row, const Steps& blocks, int begin, int end, Put put) {
   constexpr int L = D / 64;                  // 16-byte loads of a key
   constexpr int M = D / 16;                  // blocks of 16 features; features of a lane's value load
   const int lane = threadIdx.x % kWave, wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -148,8 +143,8 @@ __device__ __forceinline__ void few_rows(const AttendArgs& a, FewLds<D>& lds, in
     products_settle();
     const int last = key0 + kFewKeys - 1;
     const bool all_seen = there && last < keys && last <= lo && (a.window <= 0 || (int64_t)key0 > (int64_t)hi - a.window || last < a.sinks);
-    S[0] *= a.scale_log2e;
-    S[1] *= a.scale_log2e;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) S[i / 4][i % 4] *= a.scale_log2e;
     if (!all_seen) {                                      // (uniform)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -221,28 +216,28 @@ __device__ __forceinline__ void few_rows(const AttendArgs& a, FewLds<D>& lds, in
   // the wavefronts' parts
   const float total_here = quarters_sum(sum);
   if (q4 == 0) {
-    lds.top[wv][c16] = top;
-    lds.sum[wv][c16] = total_here;
+    lds.top[wv * kFewRows + c16] = top;
+    lds.sum[wv * kFewRows + c16] = total_here;
   }
 #pragma unroll
   for (int m = 0; m < M; ++m) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) lds.o[wv][c16][(4 * q4 + i) * M + m] = o[m][i];
+    for (int i = 0; i < 4; ++i) *lds.at(wv, c16, (4 * q4 + i) * M + m) = o[m][i];
   }
   __syncthreads();
   for (int j = threadIdx.x; j < kFewRows * D / 8; j += kFewWaves * kWave) {
     const int r = j / (D / 8), d = j % (D / 8) * 8;
     if (r >= rows) continue;
-    float m = lds.top[0][r];
+    float m = lds.top[r];
 #pragma unroll
-    for (int w = 1; w < kFewWaves; ++w) m = fmaxf(m, lds.top[w][r]);
+    for (int w = 1; w < kFewWaves; ++w) m = fmaxf(m, lds.top[w * kFewRows + r]);
     float total = 0.0f, x[8] = {};
 #pragma unroll
     for (int w = 0; w < kFewWaves; ++w) {
-      const float f = __builtin_amdgcn_exp2f(lds.top[w][r] - m);
-      total += f * lds.sum[w][r];
+      const float f = __builtin_amdgcn_exp2f(lds.top[w * kFewRows + r] - m);
+      total += f * lds.sum[w * kFewRows + r];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] += f * lds.o[w][r][d + i];
+      for (int i = 0; i < 8; ++i) x[i] += f * lds.at(w, r, d)[i];
     }
     put(r, d, x, m, total);
   }

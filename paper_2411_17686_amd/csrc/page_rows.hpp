@@ -19,6 +19,20 @@ typedef __attribute__((address_space(3))) i32x2_t* lds_i32x2_t;
 template <int D> __device__ __forceinline__ int key_swizzle(int row) { return D == 128 ? row >> 1 & 7 : row >> 2 & 3; }
 template <int D> __device__ __forceinline__ int value_swizzle(int row) { return D == 128 ? (row & 2) | (row >> 1 & 4) : row >> 2 & 2; }
 
+// Arrays of their own, so that the compiler can tell loads into one from reads of another; what else a kernel has to do may use them too.
+template <int D>
+struct PageLds {
+  template <int I>
+  static __device__ __forceinline__ uint8_t* array() {
+    __shared__ __align__(16) uint8_t x[kTileKeys * D];
+    return x;
+  }
+  static __device__ __forceinline__ int2* meta() {
+    __shared__ int2 x[2 * kChunk * kGroups];
+    return x;
+  }
+};
+
 // As tile_rows_kernel (tile_attn.hip): 128 rows a workgroup, 32 a wavefront, 64 keys a step, 32 x 32 x 16 products, a step's weights formed
 // beside the products of the next step's logits.  Pages go straight into LDS as bytes, three steps ahead, and become bfloat16 (exactly, with
 // their block's scale) in front of the products, in every wavefront: that costs 128 conversions of 2 ns a step and saves the registers and
@@ -39,9 +53,9 @@ __device__ __forceinline__ void page_rows(const AttendArgs& a, int h, const bf16
   constexpr int DT = D / 32, KS = D / 16, CH = D / 16;
   constexpr int NL = D / 64;                       // loads into LDS of a wavefront, keys and values each
   constexpr int RL = 64 / CH;                      // rows of a load
-  __shared__ __align__(16) uint8_t k0[kTileKeys * D], k1[kTileKeys * D], k2[kTileKeys * D], k3[kTileKeys * D];
-  __shared__ __align__(16) uint8_t v0[kTileKeys * D], v1[kTileKeys * D], v2[kTileKeys * D], v3[kTileKeys * D];
-  __shared__ int2 meta[2 * kChunk * kGroups];      // page (or -1) and exponents (keys, values << 8, kHole) of the groups
+  uint8_t *const k0 = PageLds<D>::template array<0>(), *const k1 = PageLds<D>::template array<1>(), *const k2 = PageLds<D>::template array<2>(), *const k3 = PageLds<D>::template array<3>();
+  uint8_t *const v0 = PageLds<D>::template array<4>(), *const v1 = PageLds<D>::template array<5>(), *const v2 = PageLds<D>::template array<6>(), *const v3 = PageLds<D>::template array<7>();
+  int2* const meta = PageLds<D>::meta();           // page (or -1) and exponents (keys, values << 8, kHole) of the groups
   const int tid = threadIdx.x, lane = tid % kWave, wv = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int c32 = lane % 32, half = lane / 32;
   // a lane's 16 bytes of a key are features 32 l + 16 half .. + 16, for two products

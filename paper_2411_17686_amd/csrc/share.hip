@@ -6,154 +6,237 @@
 namespace ficoco {
 namespace {
 
-constexpr int kPlanThreads = kMaxCall;
 constexpr int kShareLeast = 2 * kShareAlign;     // common keys below which a group's members attend for themselves
-constexpr int kLeastBlocks = 4;                  // blocks of 64 keys of a piece
-constexpr int kMostPieces = 256;
+constexpr int kLeastBlocks = 4;                  // blocks of a workgroup
+constexpr int kMostPieces = 512;                 // workgroups for a head: two a compute unit (see attend_plan())
 constexpr int kFewGroup = 64;                    // rows of a group up to which its tiles have 16
 
+// Sums over the threads before this one, and over all.
+struct Sums { long long blocks; int cut, whole, parts, members; };
+__device__ __forceinline__ Sums add(const Sums& x, const Sums& y) { return Sums{x.blocks + y.blocks, x.cut + y.cut, x.whole + y.whole, x.parts + y.parts, x.members + y.members}; }
+template <int NT>
+__device__ __forceinline__ Sums sums_before(const Sums& mine, Sums* scratch, Sums& all) {
+  const int lane = threadIdx.x % kWave, wv = threadIdx.x / kWave;
+  Sums x = mine;
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) {
+    const Sums y{__shfl_up(x.blocks, d), __shfl_up(x.cut, d), __shfl_up(x.whole, d), __shfl_up(x.parts, d), __shfl_up(x.members, d)};
+    if (lane >= d) x = add(x, y);
+  }
+  if (lane == kWave - 1) scratch[wv] = x;
+  __syncthreads();
+  Sums before{0, 0, 0, 0, 0};
+  all = before;
+  for (int w = 0; w < NT / kWave; ++w) {
+    if (w < wv) before = add(before, scratch[w]);
+    all = add(all, scratch[w]);
+  }
+  before = add(before, x);
+  return Sums{before.blocks - mine.blocks, before.cut - mine.cut, before.whole - mine.whole, before.parts - mine.parts, before.members - mine.members};
+}
+
+// The last of n ascending numbers that is not above x.
+template <typename T>
+__device__ __forceinline__ int last_below(const T* at, int n, T x) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (at[mid] <= x) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
 // One workgroup, a thread a sequence.  Every number is the same in every run: groups are in the order of their first members, members in that of the call.
-__global__ __launch_bounds__(kPlanThreads) void share_plan_kernel(ShareArgs s) {
-  __shared__ int group[kMaxCall], keys[kMaxCall], slots[kMaxCall];
-  __shared__ int common[kMaxCall], lows[kMaxCall], highs[kMaxCall];      // of the group whose first member is b
-  __shared__ int scratch[kPlanThreads / kWave];
+template <int NT>
+__global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
+  __shared__ int group[NT], slots[NT];
+  __shared__ int common[NT], lows[NT], highs[NT];          // of the group whose first member is b
+  __shared__ long long at_blocks[2 * NT];                  // of owner i (group 2 b, sequence 2 b + 1): blocks, and tiles, that are cut before it
+  __shared__ int at_cut[2 * NT];
+  __shared__ int begins[kMostPieces];
+  __shared__ Sums scratch[NT / kWave];
   __shared__ unsigned long long total;
   const AttendArgs& a = s.a;
-  const int b = threadIdx.x, P = 1 << a.page_shift, R = a.n_q * a.group;
+  const int b = threadIdx.x, R = a.n_q * a.group;
   ShareEntry* entries = (ShareEntry*)(s.plan + s.entries);
   ShareMember* members = (ShareMember*)(s.plan + s.members);
+  ShareOwner* owners = (ShareOwner*)(s.plan + s.owners);
   ShareItem* items = (ShareItem*)(s.plan + s.items_at);
   Sight sight{0, 0, 0};
   int slot = 0, g = -1;
   if (b < a.B) {
+    const int named = a.seq ? a.seq[b] : b;
+    if (s.group) g = s.group[b];
     sight = sight_of<true>(a, b, slot);
     sight.queries = sight.queries > 0 ? sight.queries : 0;
-    const int named = a.seq ? a.seq[b] : b;
-    if (s.group && sight.queries > 0 && named >= 0 && named < a.n_seqs) g = s.group[b];
-    if (g < 0 || g >= a.B) g = -1;
+    if (sight.queries == 0 || named < 0 || named >= a.n_seqs || g < 0 || g >= a.B) g = -1;
   }
   group[b] = g;
-  keys[b] = sight.keys;
   slots[b] = slot;
+  common[b] = 0x7fffffff;
+  lows[b] = 0x7fffffff;
+  highs[b] = -0x7fffffff - 1;
   if (b == 0) total = 0;
   __syncthreads();
   // members before this one, all of them, and the first
   int rank = 0, count = 0, leader = b;
   if (g >= 0) {
+#pragma unroll 8
     for (int i = a.B - 1; i >= 0; --i) {
       const bool same = group[i] == g;
       count += same;
       rank += same && i < b;
       leader = same ? i : leader;
     }
-  }
-  common[b] = 0x7fffffff;
-  lows[b] = 0x7fffffff;
-  highs[b] = -0x7fffffff - 1;
-  __syncthreads();
-  if (g >= 0) {
     atomicMin(&common[leader], sight.keys >> a.page_shift);
     atomicMin(&lows[leader], sight.first);
     atomicMax(&highs[leader], sight.first + sight.queries - 1);
-    group[b] = leader;                                     // (nobody looks for equal numbers any more; -1 elsewhere)
   }
   __syncthreads();
-  // the pages that all members of a group hold: a wavefront a member, against the first one's
+  group[b] = g >= 0 ? leader : -1;
+  __syncthreads();
+  // the pages that all members of a group hold: a wavefront a member, four at a time, against the first one's
   const int lane = threadIdx.x % kWave, wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  for (int e = wv; e < a.B; e += kPlanThreads / kWave) {
-    const int first = group[e];
-    if (first < 0 || first == e || slots[first] == slots[e]) continue;
-    const int32_t *x = a.table + (int64_t)slots[first] * a.max_pages, *y = a.table + (int64_t)slots[e] * a.max_pages;
-    for (int i0 = 0; i0 < common[first]; i0 += 4 * kWave) {
-      const int till = common[first];
-      int differ = 0x7fffffff;
+  constexpr int WAVES = NT / kWave;
+  for (int e0 = wv; e0 < a.B; e0 += 4 * WAVES) {
+    int first[4], till[4], most = 0;
 #pragma unroll
-      for (int k = 3; k >= 0; --k) {
-        const int i = i0 + k * kWave + lane;
-        if (i < till && x[i] != y[i]) differ = i;
+    for (int k = 0; k < 4; ++k) {
+      const int e = e0 + k * WAVES;
+      first[k] = e < a.B ? group[e] : -1;
+      if (first[k] == e || (first[k] >= 0 && slots[first[k]] == slots[e])) first[k] = -1;
+      till[k] = first[k] >= 0 ? common[first[k]] : 0;      // (what others have found meanwhile may be less, and then decides)
+      most = till[k] > most ? till[k] : most;
+    }
+    for (int i0 = 0; i0 < most; i0 += 2 * kWave) {
+      int differ[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        differ[k] = 0x7fffffff;
+        const int64_t x = first[k] >= 0 ? (int64_t)slots[first[k]] * a.max_pages : 0, y = first[k] >= 0 ? (int64_t)slots[e0 + k * WAVES] * a.max_pages : 0;
+#pragma unroll
+        for (int j = 1; j >= 0; --j) {
+          const int i = i0 + j * kWave + lane;
+          if (i < till[k] && a.table[x + i] != a.table[y + i]) differ[k] = i;
+        }
       }
-      const uint64_t any = __ballot(differ != 0x7fffffff);
-      if (any) {
-        differ = wave_reduce(differ, [](int u, int v) { return u < v ? u : v; });
-        if (lane == 0) atomicMin(&common[first], differ);
-        break;
+      most = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (__any(differ[k] != 0x7fffffff)) {
+          const int at = wave_reduce(differ[k], [](int u, int v) { return u < v ? u : v; });
+          if (lane == 0) atomicMin(&common[first[k]], at);
+          till[k] = 0;
+        }
+        most = till[k] > most ? till[k] : most;
       }
     }
   }
   __syncthreads();
   const int from = g >= 0 && count > 1 ? (int)(((int64_t)common[leader] << a.page_shift) & ~(int64_t)(kShareAlign - 1)) : 0;
   const bool shared = from >= kShareLeast, leads = shared && leader == b;
-  // owners: a sequence with its own keys, and, with its first member, a group with the common ones
-  const Blocks<kTileKeys> own(a, sight.keys, sight.first, sight.first + sight.queries - 1, shared ? from : 0);
-  const int own_tiles = sight.queries > 0 ? (sight.queries * a.group + s.own_tile - 1) / s.own_tile : 0;
-  int group_blocks = 0, group_tiles = 0;
-  const int group_rows = count * R;                        // (the host has seen to 32 bits)
-  const int group_tile = group_rows <= kFewGroup ? 16 : kTileRows;
+  ShareOwner own{}, all{};
+  own.owner = b; own.slot = all.slot = slot;
+  own.from = shared ? from : 0; own.keys = sight.keys;
+  own.lo = sight.first; own.hi = sight.first + sight.queries - 1;
+  own.rows = sight.queries * a.group; own.few = s.own_tile == 16;
+  own.tiles = (own.rows + s.own_tile - 1) / s.own_tile;
+  own.blocks = own.tiles ? Blocks<kTileKeys>(a, own.keys, own.lo, own.hi, own.from).count : 0;
+  own.part_rows = R < s.own_tile ? R : s.own_tile;
+  const int group_rows = count * R, group_tile = group_rows <= kFewGroup ? 16 : kTileRows;       // (the host has seen to 32 bits)
+  all.part_rows = group_rows < group_tile ? group_rows : group_tile;
   if (leads) {
-    group_blocks = Blocks<kTileKeys>(a, from, lows[b], highs[b]).count;
-    group_tiles = (group_rows + group_tile - 1) / group_tile;
+    all.keys = from;
+    all.lo = lows[b]; all.hi = highs[b];
+    all.rows = group_rows; all.few = group_tile == 16;
+    all.tiles = (group_rows + group_tile - 1) / group_tile;
+    all.blocks = Blocks<kTileKeys>(a, from, all.lo, all.hi).count;
   }
-  atomicAdd(&total, (unsigned long long)own.count * own_tiles + (unsigned long long)group_blocks * group_tiles);
+  if (own.tiles + all.tiles) atomicAdd(&total, (unsigned long long)own.blocks * own.tiles + (unsigned long long)all.blocks * all.tiles);
   __syncthreads();
-  const unsigned long long all = (total + s.pieces - 1) / s.pieces;
-  const int unit = (int)(all > kLeastBlocks ? all < 0x3fffffff ? all : 0x3fffffff : kLeastBlocks);
-  auto pieces_of = [&](int blocks) {
-    const int n = (blocks + unit - 1) / unit;
-    return n < 1 ? 1 : n < kMostPieces ? n : kMostPieces;
+  const unsigned long long each = (total + s.pieces - 1) / s.pieces;
+  const int unit = (int)(each > kLeastBlocks ? each < 0x3fffffff ? each : 0x3fffffff : kLeastBlocks);
+  auto cut_up = [&](ShareOwner& o) {
+    o.cut = o.blocks > unit;
+    o.part_pieces = o.cut ? o.blocks / unit + 2 : 1;
   };
-  const int own_pieces = own_tiles ? pieces_of(own.count) : 0, group_pieces = leads ? pieces_of(group_blocks) : 0;
-  const int own_part_rows = R < s.own_tile ? R : s.own_tile, group_part_rows = group_rows < group_tile ? group_rows : group_tile;
-  const bool direct = !shared && own_pieces <= 1;
-  // items: the groups', then the sequences'; rows of parts in the same order
-  int n_group, n_own, p_group, p_own;
-  const int my_group = group_tiles * group_pieces, my_own = own_tiles * own_pieces;
-  const int at_group = block_scan_inclusive(my_group, scratch, &n_group) - my_group;
-  const int at_own = block_scan_inclusive(my_own, scratch, &n_own) - my_own + n_group;
-  const int rows_group = my_group * group_part_rows, rows_own = direct ? 0 : my_own * own_part_rows;
-  const int part_group = block_scan_inclusive(rows_group, scratch, &p_group) - rows_group;
-  const int part_own = block_scan_inclusive(rows_own, scratch, &p_own) - rows_own + p_group;
-  int n_members;
-  const int members_at = block_scan_inclusive(leads ? count : 0, scratch, &n_members) - (leads ? count : 0);
-  // (common, lows and highs of a first member have served)
-  const int low = g >= 0 ? lows[leader] : 0, high = g >= 0 ? highs[leader] : 0;
-  __syncthreads();
-  if (leads) {
-    common[b] = members_at;
-    lows[b] = part_group;
-    highs[b] = group_pieces;
+  cut_up(own);
+  cut_up(all);
+  const bool direct = !shared && !own.cut;
+  const long long blocks_all = all.cut ? (long long)all.blocks * all.tiles : 0, blocks_own = own.cut ? (long long)own.blocks * own.tiles : 0;
+  const int parts_all = all.tiles * all.part_pieces * all.part_rows, parts_own = direct ? 0 : own.tiles * own.part_pieces * own.part_rows;
+  Sums sum;
+  const Sums before = sums_before<NT>(Sums{blocks_all + blocks_own, (all.cut ? all.tiles : 0) + (own.cut ? own.tiles : 0), (all.cut ? 0 : all.tiles) + (own.cut ? 0 : own.tiles), parts_all + parts_own,
+                                           leads ? count : 0}, scratch, sum);
+  all.owner = -2 - before.members;
+  all.part = before.parts;
+  own.part = direct ? -1 : before.parts + parts_all;
+  at_blocks[2 * b] = before.blocks;
+  at_blocks[2 * b + 1] = before.blocks + blocks_all;
+  at_cut[2 * b] = before.cut;
+  at_cut[2 * b + 1] = before.cut + (all.cut ? all.tiles : 0);
+  if (b < a.B) {
+    owners[2 * b] = all;
+    owners[2 * b + 1] = own;
+    int at = 2 * s.pieces + before.whole;
+    auto whole = [&](const ShareOwner& o) {
+      for (int t = 0; !o.cut && t < o.tiles; ++t, ++at) items[at] = ShareItem{o, t, 0, 0x3fffffff, o.part < 0 ? -1 : o.part + t * o.part_rows, {0, 0, 0, 0}};
+    };
+    whole(all);
+    whole(own);
   }
   __syncthreads();
   if (b < a.B) {
     ShareEntry e{};
     e.queries = sight.queries;
     e.direct = direct;
-    e.own_part = part_own; e.own_pieces = own_pieces; e.own_rows = own_part_rows; e.own_tile = s.own_tile;
+    e.own = ShareParts{(double)at_blocks[2 * b + 1], own.blocks, own.part, own.part_rows, own.tiles ? own.part_pieces : 0, s.own_tile, own.cut};
     if (shared) {
-      e.group_part = lows[leader]; e.group_pieces = highs[leader]; e.group_rows = group_part_rows; e.group_tile = group_tile;
+      const ShareOwner o = owners[2 * leader];
+      e.group = ShareParts{(double)at_blocks[2 * leader], o.blocks, o.part, o.part_rows, o.part_pieces, group_tile, o.cut};
       e.row0 = rank * R;
-      members[common[leader] + rank] = ShareMember{b, sight.first, sight.queries, sight.keys};
+      members[-2 - o.owner + rank] = ShareMember{b, sight.first, sight.queries, sight.keys};
     }
     entries[b] = e;
   }
-  auto put = [&](int at, int i, ShareItem x, int part) {   // item i of an owner
-    x.tile = i / x.pieces;
-    x.piece = i - x.tile * x.pieces;
-    x.part = part < 0 ? -1 : part + i * x.part_rows;
-    items[at + i] = x;
-  };
-  if (my_own > 0) {
-    const ShareItem x{b, 0, 0, own_pieces, slot, shared ? from : 0, sight.keys, sight.first, sight.first + sight.queries - 1, sight.queries * a.group, s.own_tile == 16, 0, own_part_rows, {0, 0, 0}};
-    for (int i = 0; i < my_own; ++i) put(at_own, i, x, direct ? -1 : part_own);
+  // workgroups of the owners that are cut
+  for (int w = b; w < s.pieces; w += NT) {
+    const long long at = (long long)w * unit;
+    if (at >= sum.blocks) {
+      items[w].o.owner = -1;
+      continue;
+    }
+    const int i = last_below(at_blocks, 2 * a.B, at);
+    const ShareOwner o = owners[i];
+    const long long in = at - at_blocks[i];
+    const int tile = (int)(in / o.blocks), i0 = (int)(in - (long long)tile * o.blocks), i1 = i0 + unit < o.blocks ? i0 + unit : o.blocks;
+    const int piece = w - (int)((at_blocks[i] + (long long)tile * o.blocks) / unit);
+    items[w] = ShareItem{o, tile, i0, i1, o.part + (tile * o.part_pieces + piece) * o.part_rows, {0, 0, 0, 0}};
   }
-  if (leads) {
-    const ShareItem x{-2 - members_at, 0, 0, group_pieces, slot, 0, from, low, high, group_rows, group_tile == 16, 0, group_part_rows, {0, 0, 0}};
-    for (int i = 0; i < my_group; ++i) put(at_group, i, x, part_group);
+  // Beginnings of tiles, the longest first: they take the places of the workgroups that end first, which are the ends of tiles before them.
+  for (int c = b; c < s.pieces; c += NT) {
+    items[s.pieces + c].o.owner = -1;
+    if (c < sum.cut) {
+      const int i = last_below(at_cut, 2 * a.B, c);
+      const int behind = (int)((at_blocks[i] + (long long)(c - at_cut[i]) * owners[i].blocks) % unit);      // (a tile has more than `unit` blocks)
+      begins[c] = behind ? unit - behind : 0;              // 0: a workgroup of the first kind begins with it
+    }
   }
-  for (int i = n_group + n_own + b; i < s.items; i += kPlanThreads) items[i].owner = -1;
+  __syncthreads();
+  for (int c = b; c < sum.cut; c += NT) {
+    const int mine = begins[c];
+    if (mine == 0) continue;
+    int rank = 0;
+    for (int k = 0; k < sum.cut; ++k) rank += begins[k] > mine || (begins[k] == mine && k < c);
+    const int i = last_below(at_cut, 2 * a.B, c), tile = c - at_cut[i];
+    const ShareOwner o = owners[i];
+    items[s.pieces + rank] = ShareItem{o, tile, 0, mine, o.part + tile * o.part_pieces * o.part_rows, {0, 0, 0, 0}};
+  }
+  for (int i = 2 * s.pieces + sum.whole + b; i < s.items; i += NT) items[i].o.owner = -1;
   if (b == 0) {
     ShareHead* head = (ShareHead*)s.plan;
     head->mark = s.mark;
-    head->items = n_group + n_own;
+    head->unit = unit;
   }
 }
 
@@ -161,25 +244,25 @@ __global__ __launch_bounds__(kPlanThreads) void share_plan_kernel(ShareArgs s) {
 
 SharePlan share_plan(const ficoco_cache& c, const ficoco_attention& a) {
   SharePlan pl{};
-  const int64_t heads = c.heads, group = a.H / heads, R = a.n_q * group, B = a.B;
+  const int64_t heads = c.heads, R = (int64_t)a.n_q * (a.H / heads), B = a.B;
   // own rows as in attend_plan()
   const int64_t few_tiles = (R + 15) / 16;
   pl.own_tile = few_tiles <= 1 || (few_tiles <= 4 && B * heads * few_tiles <= (few_tiles <= 3 ? 1024 : 512)) ? 16 : kTileRows;
   pl.own_tiles = (int)((R + pl.own_tile - 1) / pl.own_tile);
-  // Two workgroups a compute unit (see attend_plan()).
-  pl.pieces = (int)std::max<int64_t>(1, 512 / heads);
   const int64_t room = (int64_t)c.max_pages * c.page_size, longest = a.max_len > 0 ? std::min<int64_t>(room, a.max_len) : room;
-  pl.pieces = (int)std::max<int64_t>(1, std::min<int64_t>(pl.pieces, B * std::max(1, pl.own_tiles) * ((longest + 255) / 256)));
-  // Pieces beyond one a tile are as many as pl.pieces at most; a group has two members at least, and a last tile that is not full.
+  pl.pieces = (int)std::max<int64_t>(1, std::min<int64_t>(std::max<int64_t>(1, kMostPieces / heads), B * std::max(1, pl.own_tiles) * ((longest + 255) / 256)));
+  // A group has two members at least, and a last tile that is not full.
   const int64_t most_groups = B / 2, own_items = B * pl.own_tiles, group_items = B * R / 16 + most_groups;
-  pl.items = (int)std::min<int64_t>(0x7fffffff, pl.pieces + own_items + group_items);
-  // Rows of parts: tiles of own rows, of groups in tiles of 16 (64 rows at most) or of 128 (more than 64 rows), and the pieces beyond one a tile.
+  pl.items = (int)std::min<int64_t>(0x3fffffff, 2 * pl.pieces + own_items + group_items);
+  // Rows of parts: tiles of own rows, of groups in tiles of 16 (64 rows at most) or of 128 (more than 64 rows); of tiles that are cut (there are less than pl.pieces, of more blocks than a
+  // workgroup's), two parts more than whole workgroups.
   const int64_t own_rows = own_items * std::min<int64_t>(R, pl.own_tile), group_rows = B * R + 16 * most_groups + B * R / kFewGroup * 128;
-  const int64_t parts = (own_rows + group_rows + (int64_t)pl.pieces * kTileRows) * heads;
+  const int64_t parts = (own_rows + group_rows + 3 * (int64_t)pl.pieces * kTileRows) * heads;
   auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   pl.entries = 256;
   pl.members = pl.entries + up((size_t)B * sizeof(ShareEntry));
-  pl.items_at = pl.members + up((size_t)B * sizeof(ShareMember));
+  pl.owners = pl.members + up((size_t)B * sizeof(ShareMember));
+  pl.items_at = pl.owners + up((size_t)B * 2 * sizeof(ShareOwner));
   pl.bytes = pl.items_at + up((size_t)pl.items * sizeof(ShareItem));
   pl.part_ms = 0;
   pl.part_o = up((size_t)parts * sizeof(float2));
@@ -188,7 +271,8 @@ SharePlan share_plan(const ficoco_cache& c, const ficoco_attention& a) {
 }
 
 void launch_share(const ShareArgs& s, hipStream_t stream) {
-  hipLaunchKernelGGL(share_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, s);
+  if (s.a.B <= 256) hipLaunchKernelGGL(share_plan_kernel<256>, dim3(1), dim3(256), 0, stream, s);
+  else hipLaunchKernelGGL(share_plan_kernel<kMaxCall>, dim3(1), dim3(kMaxCall), 0, stream, s);
 }
 
 }  // namespace ficoco

@@ -4,35 +4,44 @@
 
 namespace ficoco {
 
-constexpr int kShareAlign = 64;              // common keys are counted in whole steps of either kind of workgroup
+// Common keys are counted in whole blocks of 64, the steps of a tile of 128 rows; a tile of 16 takes two steps of 32.
+constexpr int kShareAlign = kTileKeys;
 
-// One workgroup's rows and keys, for each key / value head: tile `tile` of an owner's rows (a sequence's own ones, or all of a group's), piece `piece` of `pieces` of the owner's keys from `from` on.
-struct ShareItem {
-  int owner;                                 // the sequence, or -2 - the group's first member record; -1: nothing to do
-  int tile, piece, pieces;
+// An owner of rows: a sequence with its own keys, or a group with the common ones.  Its rows are cut into tiles, each of which sees all of its keys.
+struct ShareOwner {
+  int owner;                                 // the sequence, or -2 - the group's first member record
   int slot;                                  // whose row of the table
-  int from, keys;
-  int lo, hi;                                // positions of the owner's rows
-  int rows;                                  // of the owner
-  int few;                                   // 16 rows, else 128
-  int part;                                  // first of its rows of parts (times the key / value heads); -1: straight into the result
-  int part_rows;                             // rows of parts of a tile
-  int pad[3];
+  int from, keys;                            // keys [from, keys)
+  int lo, hi;                                // positions of the rows
+  int rows, few;                             // rows; tiles of 16 of them, else of 128
+  int blocks, tiles;                         // of 64 keys; of rows
+  int part, part_rows, part_pieces;          // first row of parts (-1: straight into the result), rows of a tile's part, parts of a tile that there is room for
+  int cut;                                   // whether its blocks are cut over workgroups (else one workgroup a tile)
+  int pad[2];
+};
+// What a workgroup does, for one key / value head: blocks [i0, i1) of one tile.
+struct ShareItem {
+  ShareOwner o;                              // owner -1: nothing to do
+  int tile, i0, i1, part, pad[4];            // part: its first row of parts
 };
 // A sequence: where the parts of its rows are, its own and its group's.
+struct ShareParts {
+  double at;                                 // where the owner's blocks begin among all that are cut
+  int blocks, part, rows, pieces, tile, cut; // of the owner: part_rows, part_pieces (0: no such owner); tile: rows of one
+};
 struct ShareEntry {
-  int queries, direct;
-  int own_part, own_pieces, own_rows, own_tile;          // first row of parts, pieces, rows of parts of a tile, rows of a tile
-  int group_part, group_pieces, group_rows, group_tile;  // pieces 0: no group
-  int row0;                                  // its first row among the group's
-  int pad[5];
+  ShareParts own, group;
+  int queries, direct, row0, pad;            // row0: its first row among the group's
 };
 struct ShareMember { int b, first, queries, keys; };
-struct ShareHead { uint64_t mark; int items, pad[13]; };
+struct ShareHead { uint64_t mark; int unit, pad[13]; };        // unit: blocks of a workgroup
 
+// The blocks of all tiles of the owners that are cut, one tile after the other, are cut every `unit` blocks, and where a tile ends: as many workgroups of `unit` blocks as are resident at once, and
+// shorter ones that take the places that become free.  Items: [0, pieces) those that begin at a multiple of `unit`, [pieces, 2 pieces) beginnings of tiles that lie between, [2 pieces, items) tiles that
+// are not cut.
 struct SharePlan {
-  int own_tile, own_tiles, pieces, items;    // rows of a tile of own rows; tiles of a sequence; pieces that the keys are cut into, about; most items
-  size_t entries, members, items_at, bytes;  // offsets and size of the plan
+  int own_tile, own_tiles, pieces, items;    // rows of a tile of own rows; tiles of a sequence
+  size_t entries, members, owners, items_at, bytes;      // offsets and size of the plan
   size_t part_ms, part_o, ws_bytes;          // of the workspace
 };
 SharePlan share_plan(const ficoco_cache& c, const ficoco_attention& a);
@@ -44,7 +53,7 @@ struct ShareArgs {
   const int32_t* group;
   Divisor by_rows;                           // n_q * group
   int own_tile, own_tiles, pieces, items;
-  size_t entries, members, items_at;
+  size_t entries, members, owners, items_at;
 };
 void launch_share(const ShareArgs& s, hipStream_t stream);
 void launch_share_rows(const ShareArgs& s, int d_head, hipStream_t stream);

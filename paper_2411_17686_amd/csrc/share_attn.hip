@@ -9,17 +9,9 @@
 namespace ficoco {
 namespace {
 
-// What one workgroup does: its item, or nothing.
-__device__ __forceinline__ bool item_of(const ShareArgs& s, bool few, ShareItem& it, int& h) {
-  const int i = s.a.by_heads.of(blockIdx.x);
-  h = blockIdx.x - i * s.a.H_kv;
-  if (((const ShareHead*)s.plan)->mark != s.mark) return false;      // (a plan for something else: nothing of it means anything)
-  it = ((const ShareItem*)(s.plan + s.items_at))[i];
-  return it.owner != -1 && (it.few != 0) == few;
-}
 // Row r of an item's owner: the sequence, the query and the head of the group that it is of, where it stands and whether it counts.
 struct OwnerRow { int b, t, g, pos; bool live; };
-__device__ __forceinline__ OwnerRow owner_row(const ShareArgs& s, const ShareItem& it, int r) {
+__device__ __forceinline__ OwnerRow owner_row(const ShareArgs& s, const ShareOwner& it, int r) {
   OwnerRow x{it.owner, 0, 0, it.lo, true};
   int queries = 0x7fffffff;
   if (it.owner < -1) {
@@ -52,54 +44,85 @@ __device__ __forceinline__ RowSight sight_of_row(const AttendArgs& a, const Owne
   return sight;
 }
 
+// Blocks of 64 keys as steps of 32.
+struct HalfBlocks : Blocks<kTileKeys> {
+  __device__ __forceinline__ explicit HalfBlocks(const Blocks<kTileKeys>& b) : Blocks<kTileKeys>(b) {}
+  __device__ __forceinline__ int block(int i) const { return 2 * Blocks<kTileKeys>::block(i >> 1) + (i & 1); }
+};
+
+// The LDS of few_rows() inside that of page_rows(): 16 rows of a wavefront fill one of its arrays, each row turned by eight features a row, so that the rows of one feature
+// lie on different banks.
 template <int D>
-__global__ __launch_bounds__(kFewWaves * kWave, 2) void share_few_kernel(ShareArgs s) {
-  __shared__ FewLds<D> lds;
-  ShareItem it;
-  int h;
-  if (!item_of(s, true, it, h)) return;
+struct FewInPages {
+  float *top, *sum;
+  __device__ __forceinline__ float* at(int w, int row, int feature) const {
+    float* o = (float*)(w < 2 ? w == 0 ? PageLds<D>::template array<0>() : PageLds<D>::template array<1>() : w == 2 ? PageLds<D>::template array<2>() : PageLds<D>::template array<3>());
+    return o + row * D + ((feature + 8 * row) & (D - 1));
+  }
+};
+
+// The work of one item: 16 rows straight from memory (few_rows()) or 128 (page_rows()).
+template <int D, bool FEW>
+__device__ __forceinline__ void share_tile(const ShareArgs& s, const ShareItem& it, int h) {
+  constexpr int TILE = FEW ? kFewRows : kTileRows;
   const AttendArgs& a = s.a;
-  const bool own = it.owner >= 0;
-  const int row0 = it.tile * kFewRows, rows = it.rows - row0 < kFewRows ? it.rows - row0 : kFewRows;
-  const int lo = own ? it.lo + a.by_group.of(row0) : it.lo, hi = own ? it.lo + a.by_group.of(row0 + rows - 1) : it.hi;
-  const Blocks<kFewKeys> blocks(a, it.keys, lo, hi, it.from);
-  int per = (blocks.count + it.pieces - 1) / it.pieces;
-  per = (per + kFewWaves - 1) / kFewWaves * kFewWaves;
-  const int begin = it.piece * per, end = begin + per < blocks.count ? begin + per : blocks.count;
-  const int c16 = threadIdx.x % kFewRows;
-  const OwnerRow mine = owner_row(s, it, row0 + (c16 < rows ? c16 : rows - 1));
-  few_rows<D>(a, lds, h, query_at(a, mine, h), sight_of_row(a, mine, it.keys), rows, lo, hi, it.keys, a.table + (int64_t)it.slot * a.max_pages, blocks, begin, end,
-              [&](int r, int d, const float (&x)[8], float m, float total) {
-    if (it.part >= 0) {
-      const int64_t at = (int64_t)it.part * a.H_kv + (int64_t)h * it.part_rows + r;
-      if (d == 0) a.part_ms[at] = float2{m, total};
-      __builtin_memcpy(a.part_o + at * D + d, x, 32);
-    } else {
-      put_row(result_at(a, owner_row(s, it, row0 + r), h) + d, x, total);
-    }
-  });
+  const ShareOwner& o = it.o;
+  const int row0 = it.tile * TILE, rows = o.rows - row0 < TILE ? o.rows - row0 : TILE;
+  auto pos_of = [&](int r) { return o.lo + a.by_group.of(r < o.rows ? r : o.rows - 1); };
+  // (pieces of a tile have to be pieces of the same blocks as those of the others: of all that the owner sees)
+  const bool narrow = o.owner >= 0 && !o.cut;
+  const int lo = narrow ? pos_of(row0) : o.lo, hi = narrow ? pos_of(row0 + rows - 1) : o.hi;
+  const Blocks<kTileKeys> blocks(a, o.keys, lo, hi, o.from);
+  const int i0 = it.i0, i1 = it.i1 < blocks.count ? it.i1 : blocks.count;
+  const int32_t* table = a.table + (int64_t)o.slot * a.max_pages;
+  const int64_t part = (int64_t)it.part * a.H_kv + (int64_t)h * o.part_rows;
+  const bool parts = it.part >= 0;
+  if constexpr (FEW) {
+    float* ms = (float*)PageLds<D>::meta();
+    FewInPages<D> lds{ms, ms + kFewWaves * kFewRows};
+    const int c16 = threadIdx.x % kFewRows;
+    const OwnerRow mine = owner_row(s, o, row0 + (c16 < rows ? c16 : rows - 1));
+    few_rows<D>(a, lds, h, query_at(a, mine, h), sight_of_row(a, mine, o.keys), rows, lo, hi, o.keys, table, HalfBlocks(blocks), 2 * i0, 2 * i1,
+                [&](int r, int d, const float (&x)[8], float m, float total) {
+      if (parts) {
+        if (d == 0) a.part_ms[part + r] = float2{m, total};
+        __builtin_memcpy(a.part_o + (part + r) * D + d, x, 32);
+      } else {
+        put_row(result_at(a, owner_row(s, o, row0 + r), h) + d, x, total);
+      }
+    });
+  } else {
+    const int first = 32 * __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), mine_at = first + (int)(threadIdx.x % 32);
+    const OwnerRow mine = owner_row(s, o, row0 + (mine_at < rows ? mine_at : rows - 1));
+    page_rows<D>(a, h, query_at(a, mine, h), sight_of_row(a, mine, o.keys), narrow ? pos_of(row0 + first) : lo, narrow ? pos_of(row0 + first + 31) : hi, o.keys, table, blocks, i0, i1, parts,
+                 mine_at < rows ? a.part_ms + part + mine_at : nullptr,
+                 [&](int row, int piece) -> void* { return first + row < rows ? a.part_o + (part + first + row) * D + 4 * piece : nullptr; },
+                 [&](int row, int piece) -> void* { return first + row < rows ? result_at(a, owner_row(s, o, row0 + first + row), h) + 8 * piece : nullptr; });
+  }
 }
 
 template <int D>
-__global__ __launch_bounds__(kTileThreads, 2) void share_tile_kernel(ShareArgs s) {
-  ShareItem it;
-  int h;
-  if (!item_of(s, false, it, h)) return;
-  const AttendArgs& a = s.a;
-  const bool own = it.owner >= 0;
-  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c32 = threadIdx.x % 32;
-  const int row0 = it.tile * kTileRows, first_row = row0 + 32 * wv, rows = it.rows;
-  auto pos_of = [&](int r) { return it.lo + a.by_group.of(r < rows ? r : rows - 1); };
-  const Blocks<kTileKeys> blocks(a, it.keys, own ? pos_of(row0) : it.lo, own ? pos_of(row0 + kTileRows - 1) : it.hi, it.from);
-  const int per = (blocks.count + it.pieces - 1) / it.pieces;
-  const int begin = it.piece * per, end = begin + per < blocks.count ? begin + per : blocks.count;
-  const int r = first_row + c32;
-  const OwnerRow mine = owner_row(s, it, r < rows ? r : rows - 1);
-  const int64_t at = (int64_t)it.part * a.H_kv + (int64_t)h * it.part_rows + 32 * wv;
-  page_rows<D>(a, h, query_at(a, mine, h), sight_of_row(a, mine, it.keys), own ? pos_of(first_row) : it.lo, own ? pos_of(first_row + 31) : it.hi, it.keys,
-               a.table + (int64_t)it.slot * a.max_pages, blocks, begin, end, it.part >= 0, r < rows ? a.part_ms + at + c32 : nullptr,
-               [&](int row, int piece) -> void* { return first_row + row < rows ? a.part_o + (at + row) * D + 4 * piece : nullptr; },
-               [&](int row, int piece) -> void* { return first_row + row < rows ? result_at(a, owner_row(s, it, first_row + row), h) + 8 * piece : nullptr; });
+__global__ __launch_bounds__(kTileThreads, 2) void share_rows_kernel(ShareArgs s) {
+  static_assert(kTileThreads == kFewWaves * kWave && kFewKeys * 2 == kTileKeys, "either kind of tile");
+  const int i = s.a.by_heads.of(blockIdx.x), h = blockIdx.x - i * s.a.H_kv;
+  if (((const ShareHead*)s.plan)->mark != s.mark) return;            // (a plan for something else: nothing of it means anything)
+  const ShareItem it = ((const ShareItem*)(s.plan + s.items_at))[i];
+  if (it.o.owner == -1) return;
+  if (it.o.few) share_tile<D, true>(s, it, h);
+  else share_tile<D, false>(s, it, h);
+}
+
+// The parts of row `r` of an owner: the first, and how many, one after the other `step` rows apart.
+struct PartsOf { int64_t first, step; int count; };
+__device__ __forceinline__ PartsOf parts_of(const ShareParts& p, int r, int h, int heads, int unit) {
+  const int tile = p.tile == 16 ? r / 16 : r / kTileRows;
+  int count = p.pieces > 0 ? 1 : 0;
+  if (p.cut) {                                             // (quotients of whole numbers below 2^53: exact)
+    const double at = p.at + (double)tile * p.blocks, per = (double)unit;
+    count = (int)((at + (p.blocks - 1)) / per) - (int)(at / per) + 1;
+  }
+  const int64_t step = (int64_t)p.rows * heads;
+  return PartsOf{((int64_t)p.part + (int64_t)tile * p.pieces * p.rows) * heads + (int64_t)h * p.rows + (r - tile * p.tile), step, count};
 }
 
 // Rows that have parts: those of their own keys and of their group's, relative to their largest maximum, eight at a time; D / 4 lanes a row and group of parts, the
@@ -116,12 +139,11 @@ __global__ __launch_bounds__(kFewWaves * kWave) void share_join_kernel(ShareArgs
   const bool there = at < (int64_t)R * a.B * a.H_kv;
   const int bh = there ? s.by_rows.of((int)at) : 0, r = there ? (int)at - bh * R : 0, b = a.by_heads.of(bh), h = bh - b * a.H_kv;
   const int t = a.by_group.of(r);
-  const ShareEntry e = ((const ShareEntry*)(s.plan + s.entries))[b];
+  const ShareEntry& e = ((const ShareEntry*)(s.plan + s.entries))[b];
   const bool wanted = there && !e.direct && t < e.queries;
-  const int own_tile = e.own_tile == 16 ? r / 16 : r / kTileRows, shared_row = e.row0 + r, group_tile = e.group_tile == 16 ? shared_row / 16 : shared_row / kTileRows;
-  const int64_t own0 = ((int64_t)e.own_part + (int64_t)own_tile * e.own_pieces * e.own_rows) * a.H_kv + (int64_t)h * e.own_rows + (r - own_tile * e.own_tile);
-  const int64_t group0 = ((int64_t)e.group_part + (int64_t)group_tile * e.group_pieces * e.group_rows) * a.H_kv + (int64_t)h * e.group_rows + (shared_row - group_tile * e.group_tile);
-  const int parts = e.own_pieces + e.group_pieces;
+  const int unit = ((const ShareHead*)s.plan)->unit;
+  const PartsOf own = parts_of(e.own, r, h, a.H_kv, unit), common = parts_of(e.group, e.row0 + r, h, a.H_kv, unit);
+  const int parts = own.count + common.count;
   float m = kNoLogit, total = 0.0f;
   f32x4_t x = {0, 0, 0, 0};
   for (int i = group * AT_ONCE; wanted && i < parts; i += GROUPS * AT_ONCE) {
@@ -133,7 +155,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void share_join_kernel(ShareArgs
       v[k] = f32x4_t{0, 0, 0, 0};
       const int j = i + k;
       if (j < parts) {
-        const int64_t p = j < e.own_pieces ? own0 + (int64_t)j * e.own_rows * a.H_kv : group0 + (int64_t)(j - e.own_pieces) * e.group_rows * a.H_kv;
+        const int64_t p = j < own.count ? own.first + j * own.step : common.first + (j - own.count) * common.step;
         ms[k] = a.part_ms[p];
         v[k] = *(const f32x4_t*)(a.part_o + p * D + 4 * piece);
       }
@@ -186,8 +208,7 @@ void launch_join(const ShareArgs& s, hipStream_t stream) {
 template <int D>
 void launch_rows(const ShareArgs& s, hipStream_t stream) {
   const dim3 grid((unsigned)((int64_t)s.items * s.a.H_kv));
-  hipLaunchKernelGGL(share_tile_kernel<D>, grid, dim3(kTileThreads), 0, stream, s);
-  hipLaunchKernelGGL(share_few_kernel<D>, grid, dim3(kFewWaves * kWave), 0, stream, s);
+  hipLaunchKernelGGL(share_rows_kernel<D>, grid, dim3(kTileThreads), 0, stream, s);
   if (s.pieces > 8) launch_join<D, 8>(s, stream); else launch_join<D, 1>(s, stream);
 }
 
