@@ -49,13 +49,14 @@ __device__ __forceinline__ int last_below(const T* at, int n, T x) {
 // One workgroup, a thread a sequence.  Every number is the same in every run: groups are in the order of their first members, members in that of the call.
 template <int NT>
 __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
-  __shared__ int group[NT], slots[NT];
+  __shared__ __align__(16) int group[NT];
+  __shared__ int slots[NT];
   __shared__ int common[NT], lows[NT], highs[NT];          // of the group whose first member is b
   __shared__ long long at_blocks[2 * NT];                  // of owner i (group 2 b, sequence 2 b + 1): blocks, and tiles, that are cut before it
   __shared__ int at_cut[2 * NT];
   __shared__ int begins[kMostPieces];
   __shared__ Sums scratch[NT / kWave];
-  __shared__ unsigned long long total;
+  __shared__ unsigned long long totals[NT / kWave];
   const AttendArgs& a = s.a;
   const int b = threadIdx.x, R = a.n_q * a.group;
   ShareEntry* entries = (ShareEntry*)(s.plan + s.entries);
@@ -76,17 +77,20 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
   common[b] = 0x7fffffff;
   lows[b] = 0x7fffffff;
   highs[b] = -0x7fffffff - 1;
-  if (b == 0) total = 0;
   __syncthreads();
   // members before this one, all of them, and the first
   int rank = 0, count = 0, leader = b;
   if (g >= 0) {
-#pragma unroll 8
-    for (int i = a.B - 1; i >= 0; --i) {
-      const bool same = group[i] == g;
-      count += same;
-      rank += same && i < b;
-      leader = same ? i : leader;
+    for (int i = (a.B - 1) / 4 * 4; i >= 0; i -= 4) {      // (behind the last one: -1)
+      const int4 x = *(const int4*)&group[i];
+      const int y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int k = 3; k >= 0; --k) {
+        const bool same = y[k] == g;
+        count += same;
+        rank += same && i + k < b;
+        leader = same ? i + k : leader;
+      }
     }
     atomicMin(&common[leader], sight.keys >> a.page_shift);
     atomicMin(&lows[leader], sight.first);
@@ -108,17 +112,32 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
       till[k] = first[k] >= 0 ? common[first[k]] : 0;      // (what others have found meanwhile may be less, and then decides)
       most = till[k] > most ? till[k] : most;
     }
-    for (int i0 = 0; i0 < most; i0 += 2 * kWave) {
-      int differ[4];
+    for (int i0 = 0; i0 < most; i0 += 8 * kWave) {         // eight pages a lane
+      int x[4][8], y[4][8], differ[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int32_t* p = a.table + (first[k] >= 0 ? (int64_t)slots[first[k]] * a.max_pages : 0);
+        const int32_t* q = a.table + (first[k] >= 0 ? (int64_t)slots[e0 + k * WAVES] * a.max_pages : 0);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int i = i0 + 4 * (j * kWave + lane);
+          if (i + 4 <= till[k]) {
+            __builtin_memcpy(&x[k][4 * j], p + i, 16);
+            __builtin_memcpy(&y[k][4 * j], q + i, 16);
+          } else {
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+              x[k][4 * j + m] = i + m < till[k] ? p[i + m] : 0;
+              y[k][4 * j + m] = i + m < till[k] ? q[i + m] : 0;
+            }
+          }
+        }
+      }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         differ[k] = 0x7fffffff;
-        const int64_t x = first[k] >= 0 ? (int64_t)slots[first[k]] * a.max_pages : 0, y = first[k] >= 0 ? (int64_t)slots[e0 + k * WAVES] * a.max_pages : 0;
 #pragma unroll
-        for (int j = 1; j >= 0; --j) {
-          const int i = i0 + j * kWave + lane;
-          if (i < till[k] && a.table[x + i] != a.table[y + i]) differ[k] = i;
-        }
+        for (int j = 7; j >= 0; --j) differ[k] = x[k][j] != y[k][j] ? i0 + 4 * (j / 4 * kWave + lane) + j % 4 : differ[k];
       }
       most = 0;
 #pragma unroll
@@ -140,7 +159,7 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
   own.from = shared ? from : 0; own.keys = sight.keys;
   own.lo = sight.first; own.hi = sight.first + sight.queries - 1;
   own.rows = sight.queries * a.group; own.few = s.own_tile == 16;
-  own.tiles = (own.rows + s.own_tile - 1) / s.own_tile;
+  own.tiles = s.own_tile == 16 ? (own.rows + 15) / 16 : (own.rows + kTileRows - 1) / kTileRows;
   own.blocks = own.tiles ? Blocks<kTileKeys>(a, own.keys, own.lo, own.hi, own.from).count : 0;
   own.part_rows = R < s.own_tile ? R : s.own_tile;
   const int group_rows = count * R, group_tile = group_rows <= kFewGroup ? 16 : kTileRows;       // (the host has seen to 32 bits)
@@ -149,11 +168,16 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
     all.keys = from;
     all.lo = lows[b]; all.hi = highs[b];
     all.rows = group_rows; all.few = group_tile == 16;
-    all.tiles = (group_rows + group_tile - 1) / group_tile;
+    all.tiles = all.few ? (group_rows + 15) / 16 : (group_rows + kTileRows - 1) / kTileRows;
     all.blocks = Blocks<kTileKeys>(a, from, all.lo, all.hi).count;
   }
-  if (own.tiles + all.tiles) atomicAdd(&total, (unsigned long long)own.blocks * own.tiles + (unsigned long long)all.blocks * all.tiles);
+  unsigned long long total = (unsigned long long)own.blocks * own.tiles + (unsigned long long)all.blocks * all.tiles;
+#pragma unroll
+  for (int d = kWave / 2; d > 0; d /= 2) total += __shfl_xor(total, d);
+  if (lane == 0) totals[wv] = total;
   __syncthreads();
+  total = 0;
+  for (int w = 0; w < WAVES; ++w) total += totals[w];
   const unsigned long long each = (total + s.pieces - 1) / s.pieces;
   const int unit = (int)(each > kLeastBlocks ? each < 0x3fffffff ? each : 0x3fffffff : kLeastBlocks);
   auto cut_up = [&](ShareOwner& o) {
@@ -271,7 +295,8 @@ SharePlan share_plan(const ficoco_cache& c, const ficoco_attention& a) {
 }
 
 void launch_share(const ShareArgs& s, hipStream_t stream) {
-  if (s.a.B <= 256) hipLaunchKernelGGL(share_plan_kernel<256>, dim3(1), dim3(256), 0, stream, s);
+  // As many wavefronts as compare four members each at once, at least; fewer wait less for each other.
+  if (s.a.B <= 16) hipLaunchKernelGGL(share_plan_kernel<256>, dim3(1), dim3(256), 0, stream, s);
   else hipLaunchKernelGGL(share_plan_kernel<kMaxCall>, dim3(1), dim3(kMaxCall), 0, stream, s);
 }
 

@@ -209,7 +209,9 @@ template <int D>
 void launch_rows(const ShareArgs& s, hipStream_t stream) {
   const dim3 grid((unsigned)((int64_t)s.items * s.a.H_kv));
   hipLaunchKernelGGL(share_rows_kernel<D>, grid, dim3(kTileThreads), 0, stream, s);
-  if (s.pieces > 8) launch_join<D, 8>(s, stream); else launch_join<D, 1>(s, stream);
+  // Parts of a tile, if all rows were of one group: more than one batch of them by eight groups of lanes.
+  const int64_t tiles = std::max<int64_t>(1, (int64_t)s.a.B * s.by_rows.d / kTileRows);
+  if (s.pieces / tiles > 8) launch_join<D, 8>(s, stream); else launch_join<D, 1>(s, stream);
 }
 
 }  // namespace
