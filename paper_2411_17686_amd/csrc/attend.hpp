@@ -128,9 +128,9 @@ __device__ __forceinline__ float halves_max(float v) { return fmaxf(v, __shfl_xo
 // LDS of its own, so that lanes next to each other store 16 bytes next to each other: with 8 bytes a lane and two lanes a row the
 // stores of a workgroup took 1.6 us.  to(row, piece): where piece (16 bytes) of row 0 .. 31 goes, null for nowhere.
 template <int D, typename F>
-__device__ __forceinline__ void rows_out(const f32x16_t (&o)[D / 32], float inv, uint8_t* lds, F to) {
+__device__ __forceinline__ void rows_out(const f32x16_t (&o)[D / 32], float inv, uint8_t* lds, F to, int lane = threadIdx.x % kWave) {
   constexpr int CH = D / 8;
-  const int lane = threadIdx.x % kWave, row = lane % 32, half = lane / 32;
+  const int row = lane % 32, half = lane / 32;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
 #pragma unroll
@@ -147,9 +147,9 @@ __device__ __forceinline__ void rows_out(const f32x16_t (&o)[D / 32], float inv,
 }
 // The same in single precision, half of the features at a time; pieces 0 .. D / 4 - 1.
 template <int D, typename F>
-__device__ __forceinline__ void float_rows_out(const f32x16_t (&o)[D / 32], uint8_t* lds, F to) {
+__device__ __forceinline__ void float_rows_out(const f32x16_t (&o)[D / 32], uint8_t* lds, F to, int lane = threadIdx.x % kWave) {
   constexpr int CH = D / 8, DH = D / 64;
-  const int lane = threadIdx.x % kWave, row = lane % 32, half = lane / 32;
+  const int row = lane % 32, half = lane / 32;
 #pragma unroll
   for (int part = 0; part < 2; ++part) {
 #pragma unroll

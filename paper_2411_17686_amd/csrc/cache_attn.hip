@@ -29,7 +29,7 @@ __global__ __launch_bounds__(kFewWaves * kWave, 2) void few_rows_kernel(AttendAr
   const int begin = split * per, end = begin + per < blocks.count ? begin + per : blocks.count;
   const int c16 = threadIdx.x % kFewRows, my_r = row0 + (c16 < rows ? c16 : rows - 1), my_t = a.by_group.of(my_r);
   const bf16_t* q = a.Q + (int64_t)b * a.q_sb + (int64_t)(h * a.group + my_r - my_t * a.group) * a.q_sh + (int64_t)my_t * a.q_sn;
-  few_rows<D>(a, lds, h, q, RowSight(a, s.first + my_t, s.keys), rows, lo, hi, s.keys, a.table + (int64_t)slot * a.max_pages, blocks, begin, end,
+  few_rows<D>(a, threadIdx.x, lds, h, q, RowSight(a, s.first + my_t, s.keys), rows, lo, hi, s.keys, a.table + (int64_t)slot * a.max_pages, blocks, begin, end,
               [&](int r, int d, const float (&x)[8], float m, float total) {
     if (a.splits > 1) {
       const int64_t at = ((int64_t)bh * a.splits + split) * a.part_rows + row0 + r;

@@ -44,16 +44,16 @@ __device__ __forceinline__ float quarters_sum(float v) {
 // 32 of 300 .. 4096: 37 us with the join, 4.1 TB/s (the longest sequences end last); one of 243: 6 us, a launch and three trips to memory.  24 sequences,
 // 28 heads of 64 on 4, behind a window of 1 .. 32 tokens 5.2 us, of 2048 9.4, 4096 13.3, 8192 21.3: such a start, then 6.3 TB/s.
 //
-// A lane's row (lane % 16) has its queries at q and sees `sight`; `rows` of the 16 rows count.  Keys of head h are those of blocks begin .. end - 1 and of the table's `row`;
+// tid: the thread.  A lane's row (lane % 16) has its queries at q and sees `sight`; `rows` of the 16 rows count.  Keys of head h are those of blocks begin .. end - 1 and of the table's `row`;
 // lo, hi: the rows' first and last position, keys: how many keys each of them has at least.  put(r, feature, x, top, sum): eight features of
 // row r, relative to the row's maximum, and its sum.  lds: where the wavefronts' parts meet: at(w, row, feature), eight features from a multiple of eight on next to each other, and top, sum
 // [kFewWaves * kFewRows].
 template <int D, typename Lds, typename Steps, typename Put>
-__device__ __forceinline__ void few_rows(const AttendArgs& a, Lds& lds, int h, const bf16_t* q, const RowSight& sight, int rows, int lo, int hi, int keys,
+__device__ __forceinline__ void few_rows(const AttendArgs& a, int tid, Lds& lds, int h, const bf16_t* q, const RowSight& sight, int rows, int lo, int hi, int keys,
                                          const int32_t* row, const Steps& blocks, int begin, int end, Put put) {
   constexpr int L = D / 64;                  // 16-byte loads of a key
   constexpr int M = D / 16;                  // blocks of 16 features; features of a lane's value load
-  const int lane = threadIdx.x % kWave, wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int lane = tid % kWave, wv = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int c16 = lane % 16, q4 = lane / 16;
   // queries: features 64 l + 16 q4 + 8 u .. + 8
   bf16x8_t qf[L][2];
@@ -225,7 +225,7 @@ __device__ __forceinline__ void few_rows(const AttendArgs& a, Lds& lds, int h, c
     for (int i = 0; i < 4; ++i) *lds.at(wv, c16, (4 * q4 + i) * M + m) = o[m][i];
   }
   __syncthreads();
-  for (int j = threadIdx.x; j < kFewRows * D / 8; j += kFewWaves * kWave) {
+  for (int j = tid; j < kFewRows * D / 8; j += kFewWaves * kWave) {
     const int r = j / (D / 8), d = j % (D / 8) * 8;
     if (r >= rows) continue;
     float m = lds.top[r];

@@ -44,11 +44,11 @@ struct PageLds {
 // but nothing then fills its waits for LDS and barriers: 57 us instead of 40 with the queries in LDS (73 without, for lack of registers), and with heads of 64, where nothing is
 // short of registers, 102 instead of 69 behind 9600 tokens.
 //
-// A lane's row (lane % 32 of its wavefront's) has its queries at q and sees `sight`.  Keys of head h are those of blocks begin .. end - 1 and of `table`; lo, hi: first and last
+// tid: the thread.  A lane's row (lane % 32 of its wavefront's) has its queries at q and sees `sight`.  Keys of head h are those of blocks begin .. end - 1 and of `table`; lo, hi: first and last
 // position of the wavefront's rows, keys: how many keys each of them has at least.  part_ms (the lane's, null for none): where maxima and sums of parts go; part(row, piece) and out(row, piece): the
 // places of 16 bytes of row 0 .. 31 of the wavefront as floats, relative to the maximum, or as bfloat16, null for nowhere.
 template <int D, typename Part, typename Out>
-__device__ __forceinline__ void page_rows(const AttendArgs& a, int h, const bf16_t* q, const RowSight& sight, int lo, int hi, int keys, const int32_t* table,
+__device__ __forceinline__ void page_rows(const AttendArgs& a, int tid, int h, const bf16_t* q, const RowSight& sight, int lo, int hi, int keys, const int32_t* table,
                                           const Blocks<kTileKeys>& blocks, int begin, int end, bool parts, float2* part_ms, Part part, Out out) {
   constexpr int DT = D / 32, KS = D / 16, CH = D / 16;
   constexpr int NL = D / 64;                       // loads into LDS of a wavefront, keys and values each
@@ -56,7 +56,7 @@ __device__ __forceinline__ void page_rows(const AttendArgs& a, int h, const bf16
   uint8_t *const k0 = PageLds<D>::template array<0>(), *const k1 = PageLds<D>::template array<1>(), *const k2 = PageLds<D>::template array<2>(), *const k3 = PageLds<D>::template array<3>();
   uint8_t *const v0 = PageLds<D>::template array<4>(), *const v1 = PageLds<D>::template array<5>(), *const v2 = PageLds<D>::template array<6>(), *const v3 = PageLds<D>::template array<7>();
   int2* const meta = PageLds<D>::meta();           // page (or -1) and exponents (keys, values << 8, kHole) of the groups
-  const int tid = threadIdx.x, lane = tid % kWave, wv = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int lane = tid % kWave, wv = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int c32 = lane % 32, half = lane / 32;
   // a lane's 16 bytes of a key are features 32 l + 16 half .. + 16, for two products
   bf16x8_t qf[KS];
@@ -271,10 +271,10 @@ __device__ __forceinline__ void page_rows(const AttendArgs& a, int h, const bf16
   uint8_t* rows = wv < 2 ? wv == 0 ? k0 : k1 : wv == 2 ? k2 : k3;
   if (parts) {
     if (half == 0 && part_ms) *part_ms = float2{top, sum};
-    float_rows_out<D>(o, rows, part);
+    float_rows_out<D>(o, rows, part, lane);
     return;
   }
-  rows_out<D>(o, sum > 0.0f ? 1.0f / sum : 0.0f, rows, out);
+  rows_out<D>(o, sum > 0.0f ? 1.0f / sum : 0.0f, rows, out, lane);
 }
 
 }  // namespace ficoco

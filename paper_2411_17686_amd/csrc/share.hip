@@ -54,9 +54,8 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
   __shared__ int common[NT], lows[NT], highs[NT];          // of the group whose first member is b
   __shared__ long long at_blocks[2 * NT];                  // of owner i (group 2 b, sequence 2 b + 1): blocks, and tiles, that are cut before it
   __shared__ int at_cut[2 * NT];
-  __shared__ int begins[kMostPieces];
   __shared__ Sums scratch[NT / kWave];
-  __shared__ unsigned long long totals[NT / kWave];
+  __shared__ unsigned long long totals[NT / kWave], needs[2][NT / kWave];
   const AttendArgs& a = s.a;
   const int b = threadIdx.x, R = a.n_q * a.group;
   ShareEntry* entries = (ShareEntry*)(s.plan + s.entries);
@@ -179,15 +178,37 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
   total = 0;
   for (int w = 0; w < WAVES; ++w) total += totals[w];
   const unsigned long long each = (total + s.pieces - 1) / s.pieces;
-  const int unit = (int)(each > kLeastBlocks ? each < 0x3fffffff ? each : 0x3fffffff : kLeastBlocks);
+  int unit = (int)(each > kLeastBlocks ? each < 0x3fffffff ? each : 0x3fffffff : kLeastBlocks);
+  // Whether every tile can begin with a workgroup of its own, if these take a little more each: a workgroup that begins a second tile takes as long as 5 blocks, or an eighth of them, more.
+  const int larger = unit + (unit / 8 > 5 ? unit / 8 : 5);
+  auto whole_pieces = [](const ShareOwner& o, int u) { return o.blocks > u ? (unsigned long long)o.tiles * ((o.blocks + u - 1) / u) : 0ull; };
+  unsigned long long need = whole_pieces(all, unit) + whole_pieces(own, unit), need_larger = whole_pieces(all, larger) + whole_pieces(own, larger);
+#pragma unroll
+  for (int d = kWave / 2; d > 0; d /= 2) {
+    need += __shfl_xor(need, d);
+    need_larger += __shfl_xor(need_larger, d);
+  }
+  if (lane == 0) {
+    needs[0][wv] = need;
+    needs[1][wv] = need_larger;
+  }
+  __syncthreads();
+  need = need_larger = 0;
+  for (int w = 0; w < WAVES; ++w) {
+    need += needs[0][w];
+    need_larger += needs[1][w];
+  }
+  const bool apart = need <= (unsigned)s.pieces || need_larger <= (unsigned)s.pieces;
+  if (need > (unsigned)s.pieces && apart) unit = larger;
   auto cut_up = [&](ShareOwner& o) {
     o.cut = o.blocks > unit;
     o.part_pieces = o.cut ? o.blocks / unit + 2 : 1;
+    o.stride = apart ? (o.blocks + unit - 1) / unit * unit : o.blocks;
   };
   cut_up(own);
   cut_up(all);
   const bool direct = !shared && !own.cut;
-  const long long blocks_all = all.cut ? (long long)all.blocks * all.tiles : 0, blocks_own = own.cut ? (long long)own.blocks * own.tiles : 0;
+  const long long blocks_all = all.cut ? (long long)all.stride * all.tiles : 0, blocks_own = own.cut ? (long long)own.stride * own.tiles : 0;
   const int parts_all = all.tiles * all.part_pieces * all.part_rows, parts_own = direct ? 0 : own.tiles * own.part_pieces * own.part_rows;
   Sums sum;
   const Sums before = sums_before<NT>(Sums{blocks_all + blocks_own, (all.cut ? all.tiles : 0) + (own.cut ? own.tiles : 0), (all.cut ? 0 : all.tiles) + (own.cut ? 0 : own.tiles), parts_all + parts_own,
@@ -204,7 +225,7 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
     owners[2 * b + 1] = own;
     int at = 2 * s.pieces + before.whole;
     auto whole = [&](const ShareOwner& o) {
-      for (int t = 0; !o.cut && t < o.tiles; ++t, ++at) items[at] = ShareItem{o, t, 0, 0x3fffffff, o.part < 0 ? -1 : o.part + t * o.part_rows, {0, 0, 0, 0}};
+      for (int t = 0; !o.cut && t < o.tiles; ++t, ++at) items[at] = ShareItem{o, t, 0, 0x3fffffff, o.part < 0 ? -1 : o.part + t * o.part_rows, -1, {0, 0, 0}};
     };
     whole(all);
     whole(own);
@@ -214,10 +235,10 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
     ShareEntry e{};
     e.queries = sight.queries;
     e.direct = direct;
-    e.own = ShareParts{(double)at_blocks[2 * b + 1], own.blocks, own.part, own.part_rows, own.tiles ? own.part_pieces : 0, s.own_tile, own.cut};
+    e.own = ShareParts{(double)at_blocks[2 * b + 1], own.blocks, own.part, own.part_rows, own.tiles ? own.part_pieces : 0, s.own_tile, own.cut, own.stride, 0};
     if (shared) {
       const ShareOwner o = owners[2 * leader];
-      e.group = ShareParts{(double)at_blocks[2 * leader], o.blocks, o.part, o.part_rows, o.part_pieces, group_tile, o.cut};
+      e.group = ShareParts{(double)at_blocks[2 * leader], o.blocks, o.part, o.part_rows, o.part_pieces, group_tile, o.cut, o.stride, 0};
       e.row0 = rank * R;
       members[-2 - o.owner + rank] = ShareMember{b, sight.first, sight.queries, sight.keys};
     }
@@ -233,28 +254,15 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
     const int i = last_below(at_blocks, 2 * a.B, at);
     const ShareOwner o = owners[i];
     const long long in = at - at_blocks[i];
-    const int tile = (int)(in / o.blocks), i0 = (int)(in - (long long)tile * o.blocks), i1 = i0 + unit < o.blocks ? i0 + unit : o.blocks;
-    const int piece = w - (int)((at_blocks[i] + (long long)tile * o.blocks) / unit);
-    items[w] = ShareItem{o, tile, i0, i1, o.part + (tile * o.part_pieces + piece) * o.part_rows, {0, 0, 0, 0}};
+    const int tile = (int)(in / o.stride), i0 = (int)(in - (long long)tile * o.stride), i1 = i0 + unit < o.blocks ? i0 + unit : o.blocks;
+    const int piece = w - (int)((at_blocks[i] + (long long)tile * o.stride) / unit), after = at_cut[i] + tile + 1;
+    items[w] = ShareItem{o, tile, i0, i1, o.part + (tile * o.part_pieces + piece) * o.part_rows, !apart && i1 - i0 < unit && after < sum.cut ? s.pieces + after : -1, {0, 0, 0}};
   }
-  // Beginnings of tiles, the longest first: they take the places of the workgroups that end first, which are the ends of tiles before them.
-  for (int c = b; c < s.pieces; c += NT) {
-    items[s.pieces + c].o.owner = -1;
-    if (c < sum.cut) {
-      const int i = last_below(at_cut, 2 * a.B, c);
-      const int behind = (int)((at_blocks[i] + (long long)(c - at_cut[i]) * owners[i].blocks) % unit);      // (a tile has more than `unit` blocks)
-      begins[c] = behind ? unit - behind : 0;              // 0: a workgroup of the first kind begins with it
-    }
-  }
-  __syncthreads();
-  for (int c = b; c < sum.cut; c += NT) {
-    const int mine = begins[c];
-    if (mine == 0) continue;
-    int rank = 0;
-    for (int k = 0; k < sum.cut; ++k) rank += begins[k] > mine || (begins[k] == mine && k < c);
-    const int i = last_below(at_cut, 2 * a.B, c), tile = c - at_cut[i];
+  for (int c = b; !apart && c < sum.cut; c += NT) {
+    const int i = last_below(at_cut, 2 * a.B, c);
     const ShareOwner o = owners[i];
-    items[s.pieces + rank] = ShareItem{o, tile, 0, mine, o.part + tile * o.part_pieces * o.part_rows, {0, 0, 0, 0}};
+    const int tile = c - at_cut[i], behind = (int)((at_blocks[i] + (long long)tile * o.blocks) % unit);      // (a tile has more than `unit` blocks)
+    if (behind != 0) items[s.pieces + c] = ShareItem{o, tile, 0, unit - behind, o.part + tile * o.part_pieces * o.part_rows, -1, {0, 0, 0}};
   }
   for (int i = 2 * s.pieces + sum.whole + b; i < s.items; i += NT) items[i].o.owner = -1;
   if (b == 0) {

@@ -17,17 +17,19 @@ struct ShareOwner {
   int blocks, tiles;                         // of 64 keys; of rows
   int part, part_rows, part_pieces;          // first row of parts (-1: straight into the result), rows of a tile's part, parts of a tile that there is room for
   int cut;                                   // whether its blocks are cut over workgroups (else one workgroup a tile)
-  int pad[2];
+  int stride;                                // blocks from the beginning of a tile to that of the next, among all that are cut
+  int pad;
 };
-// What a workgroup does, for one key / value head: blocks [i0, i1) of one tile.
+// What a workgroup does, for one key / value head: blocks [i0, i1) of one tile, then item `next`, if that is not -1.
 struct ShareItem {
   ShareOwner o;                              // owner -1: nothing to do
-  int tile, i0, i1, part, pad[4];            // part: its first row of parts
+  int tile, i0, i1, part, next, pad[3];      // part: its first row of parts
 };
 // A sequence: where the parts of its rows are, its own and its group's.
 struct ShareParts {
   double at;                                 // where the owner's blocks begin among all that are cut
   int blocks, part, rows, pieces, tile, cut; // of the owner: part_rows, part_pieces (0: no such owner); tile: rows of one
+  int stride, pad;
 };
 struct ShareEntry {
   ShareParts own, group;
@@ -36,9 +38,9 @@ struct ShareEntry {
 struct ShareMember { int b, first, queries, keys; };
 struct ShareHead { uint64_t mark; int unit, pad[13]; };        // unit: blocks of a workgroup
 
-// The blocks of all tiles of the owners that are cut, one tile after the other, are cut every `unit` blocks, and where a tile ends: as many workgroups of `unit` blocks as are resident at once, and
-// shorter ones that take the places that become free.  Items: [0, pieces) those that begin at a multiple of `unit`, [pieces, 2 pieces) beginnings of tiles that lie between, [2 pieces, items) tiles that
-// are not cut.
+// The blocks of all tiles of the owners that are cut, one tile after the other, go to workgroups `unit` at a time: as many as are resident at once, and they end together.  A workgroup that comes to the
+// end of a tile goes on with the next one, or, where there are workgroups enough for that, every tile begins with one of its own.  (As workgroups of their own such beginnings wait, while others have ended, for a place on the shader engine whose turn it is: 8 sequences of 16484 tokens 48 us
+// so.)  Items: [0, pieces) where these workgroups begin, [pieces, 2 pieces) beginnings of tiles that they come to, [2 pieces, items) tiles that are not cut.
 struct SharePlan {
   int own_tile, own_tiles, pieces, items;    // rows of a tile of own rows; tiles of a sequence
   size_t entries, members, owners, items_at, bytes;      // offsets and size of the plan

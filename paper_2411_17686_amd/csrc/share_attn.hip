@@ -63,7 +63,7 @@ struct FewInPages {
 
 // The work of one item: 16 rows straight from memory (few_rows()) or 128 (page_rows()).
 template <int D, bool FEW>
-__device__ __forceinline__ void share_tile(const ShareArgs& s, const ShareItem& it, int h) {
+__device__ __forceinline__ void share_tile(const ShareArgs& s, const ShareItem& it, int tid, int h) {
   constexpr int TILE = FEW ? kFewRows : kTileRows;
   const AttendArgs& a = s.a;
   const ShareOwner& o = it.o;
@@ -80,9 +80,9 @@ __device__ __forceinline__ void share_tile(const ShareArgs& s, const ShareItem& 
   if constexpr (FEW) {
     float* ms = (float*)PageLds<D>::meta();
     FewInPages<D> lds{ms, ms + kFewWaves * kFewRows};
-    const int c16 = threadIdx.x % kFewRows;
+    const int c16 = tid % kFewRows;
     const OwnerRow mine = owner_row(s, o, row0 + (c16 < rows ? c16 : rows - 1));
-    few_rows<D>(a, lds, h, query_at(a, mine, h), sight_of_row(a, mine, o.keys), rows, lo, hi, o.keys, table, HalfBlocks(blocks), 2 * i0, 2 * i1,
+    few_rows<D>(a, tid, lds, h, query_at(a, mine, h), sight_of_row(a, mine, o.keys), rows, lo, hi, o.keys, table, HalfBlocks(blocks), 2 * i0, 2 * i1,
                 [&](int r, int d, const float (&x)[8], float m, float total) {
       if (parts) {
         if (d == 0) a.part_ms[part + r] = float2{m, total};
@@ -92,9 +92,9 @@ __device__ __forceinline__ void share_tile(const ShareArgs& s, const ShareItem& 
       }
     });
   } else {
-    const int first = 32 * __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), mine_at = first + (int)(threadIdx.x % 32);
+    const int first = 32 * __builtin_amdgcn_readfirstlane(tid / kWave), mine_at = first + tid % 32;
     const OwnerRow mine = owner_row(s, o, row0 + (mine_at < rows ? mine_at : rows - 1));
-    page_rows<D>(a, h, query_at(a, mine, h), sight_of_row(a, mine, o.keys), narrow ? pos_of(row0 + first) : lo, narrow ? pos_of(row0 + first + 31) : hi, o.keys, table, blocks, i0, i1, parts,
+    page_rows<D>(a, tid, h, query_at(a, mine, h), sight_of_row(a, mine, o.keys), narrow ? pos_of(row0 + first) : lo, narrow ? pos_of(row0 + first + 31) : hi, o.keys, table, blocks, i0, i1, parts,
                  mine_at < rows ? a.part_ms + part + mine_at : nullptr,
                  [&](int row, int piece) -> void* { return first + row < rows ? a.part_o + (part + first + row) * D + 4 * piece : nullptr; },
                  [&](int row, int piece) -> void* { return first + row < rows ? result_at(a, owner_row(s, o, row0 + first + row), h) + 8 * piece : nullptr; });
@@ -104,12 +104,20 @@ __device__ __forceinline__ void share_tile(const ShareArgs& s, const ShareItem& 
 template <int D>
 __global__ __launch_bounds__(kTileThreads, 2) void share_rows_kernel(ShareArgs s) {
   static_assert(kTileThreads == kFewWaves * kWave && kFewKeys * 2 == kTileKeys, "either kind of tile");
-  const int i = s.a.by_heads.of(blockIdx.x), h = blockIdx.x - i * s.a.H_kv;
+  const int wg = s.a.by_heads.of(blockIdx.x), h = blockIdx.x - wg * s.a.H_kv;
   if (((const ShareHead*)s.plan)->mark != s.mark) return;            // (a plan for something else: nothing of it means anything)
-  const ShareItem it = ((const ShareItem*)(s.plan + s.items_at))[i];
-  if (it.o.owner == -1) return;
-  if (it.o.few) share_tile<D, true>(s, it, h);
-  else share_tile<D, false>(s, it, h);
+  const ShareItem* items = (const ShareItem*)(s.plan + s.items_at);
+  int next = wg < s.pieces ? wg : wg + s.pieces;
+  if (items[next].o.owner == -1) return;
+  do {
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));                                    // (or what follows from it is kept over the loop, in more registers than there are)
+    const ShareItem it = items[next];
+    if (it.o.few) share_tile<D, true>(s, it, tid, h);
+    else share_tile<D, false>(s, it, tid, h);
+    next = it.next;
+    __syncthreads();                                                 // LDS is free again
+  } while (next >= 0);
 }
 
 // The parts of row `r` of an owner: the first, and how many, one after the other `step` rows apart.
@@ -118,7 +126,7 @@ __device__ __forceinline__ PartsOf parts_of(const ShareParts& p, int r, int h, i
   const int tile = p.tile == 16 ? r / 16 : r / kTileRows;
   int count = p.pieces > 0 ? 1 : 0;
   if (p.cut) {                                             // (quotients of whole numbers below 2^53: exact)
-    const double at = p.at + (double)tile * p.blocks, per = (double)unit;
+    const double at = p.at + (double)tile * p.stride, per = (double)unit;
     count = (int)((at + (p.blocks - 1)) / per) - (int)(at / per) + 1;
   }
   const int64_t step = (int64_t)p.rows * heads;
@@ -207,7 +215,7 @@ void launch_join(const ShareArgs& s, hipStream_t stream) {
 
 template <int D>
 void launch_rows(const ShareArgs& s, hipStream_t stream) {
-  const dim3 grid((unsigned)((int64_t)s.items * s.a.H_kv));
+  const dim3 grid((unsigned)((int64_t)(s.items - s.pieces) * s.a.H_kv));
   hipLaunchKernelGGL(share_rows_kernel<D>, grid, dim3(kTileThreads), 0, stream, s);
   // Parts of a tile, if all rows were of one group: more than one batch of them by eight groups of lanes.
   const int64_t tiles = std::max<int64_t>(1, (int64_t)s.a.B * s.by_rows.d / kTileRows);
