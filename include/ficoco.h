@@ -497,13 +497,14 @@ int ficoco_cache_attention(ficoco_ctx *ctx, const ficoco_cache *c, int32_t layer
  * are read once for all of them.  ficoco_cache_share makes a plan, once for all layers of a decoder's step (the pages in common are found by the rows of the
  * table, whatever the caller says: group decides how the work is cut, never the result's meaning); ficoco_cache_shared_attention computes one layer by it.
  *   group [B]: sequences with the same number 0 .. B - 1 are taken together, all others for themselves; NULL = all of them for themselves.
+ *   always: 0 = where the plan finds that to take less time (few sequences behind a short prompt are faster for themselves), else wherever there are common keys.
  *   a: as for ficoco_cache_attention.  For the plan, Q, O, their strides and scale do not count; for the attention, seq and the arrays of lengths and positions do not: they, the
  *   lengths of the cache and its table are those that the plan found.  All other sizes, window, sinks and max_len have to be the same for both (with others, or without a plan, nothing is written).
  * A plan holds until the lengths of its sequences or their rows of the table change; whoever changes them makes another.  B <= 1024 (FICOCO_EUNSUPPORTED otherwise).  Plan
  * and workspace: 256-byte aligned, the workspace for one call at a time, the plan for any number of them. */
 int ficoco_cache_share_bytes(const ficoco_cache *c, const ficoco_attention *a, size_t *plan_bytes, size_t *ws_bytes);
-int ficoco_cache_share(ficoco_ctx *ctx, const ficoco_cache *c, const ficoco_attention *a, const int32_t *group, void *plan, size_t plan_bytes,
-                       void *stream);
+int ficoco_cache_share(ficoco_ctx *ctx, const ficoco_cache *c, const ficoco_attention *a, const int32_t *group, int32_t always, void *plan,
+                       size_t plan_bytes, void *stream);
 int ficoco_cache_shared_attention(ficoco_ctx *ctx, const ficoco_cache *c, int32_t layer, const ficoco_attention *a, const void *plan, size_t plan_bytes,
                                   void *ws, size_t ws_bytes, void *stream);
 

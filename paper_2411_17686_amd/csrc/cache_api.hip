@@ -85,8 +85,8 @@ const char* share_fault(const ficoco_cache& c, const ficoco_attention& a, bool s
   if (const char* why = attention_fault(a, c.heads, c.d_head, true, code, shapes)) return why;
   *code = FICOCO_EUNSUPPORTED;
   if (a.B > kMaxCall) return "more than 1024 sequences in a call";
-  // (three times the rows, and the pieces of a tile: see share_plan())
-  if (4 * (int64_t)a.B * a.n_q * (a.H / c.heads) + 2048 * kTileRows > kMaxRows) return "too many rows in one call";
+  // (six times the rows, and the pieces of a tile: see share_plan())
+  if (8 * (int64_t)a.B * a.n_q * (a.H / c.heads) + 2048 * kTileRows > kMaxRows) return "too many rows in one call";
   *pl = share_plan(c, a);
   if ((int64_t)pl->items * c.heads * kTileThreads > kMaxThreads || (int64_t)a.B * a.H * a.n_q * (a.d_head / 4) * 8 > kMaxThreads) return "too many rows in one call";
   *code = FICOCO_OK;
@@ -109,6 +109,7 @@ ShareArgs share_arguments(const ficoco_cache& c, const ficoco_attention& a, cons
   s.plan = (char*)plan;
   s.by_rows = Divisor((int64_t)a.n_q * (a.H / c.heads));
   s.own_tile = pl.own_tile; s.own_tiles = pl.own_tiles; s.pieces = pl.pieces; s.items = pl.items;
+  s.d_head = a.d_head;
   s.entries = pl.entries; s.members = pl.members; s.owners = pl.owners; s.items_at = pl.items_at;
   return s;
 }
@@ -245,7 +246,7 @@ int ficoco_cache_share_bytes(const ficoco_cache* c, const ficoco_attention* a, s
   return FICOCO_OK;
 }
 
-int ficoco_cache_share(ficoco_ctx* ctx, const ficoco_cache* c, const ficoco_attention* a, const int32_t* group, void* plan, size_t plan_bytes, void* stream) {
+int ficoco_cache_share(ficoco_ctx* ctx, const ficoco_cache* c, const ficoco_attention* a, const int32_t* group, int32_t always, void* plan, size_t plan_bytes, void* stream) {
   const char* fn = "ficoco_cache_share";
   const int rc = begin(ctx, c, fn);
   if (rc != FICOCO_OK) return rc;
@@ -261,6 +262,7 @@ int ficoco_cache_share(ficoco_ctx* ctx, const ficoco_cache* c, const ficoco_atte
     if (ranges_overlap(p, (size_t)a->B * sizeof(int32_t), plan, pl.bytes)) return fail(ctx, FICOCO_EINVAL, fn, "the plan overlaps an input");
   ShareArgs s = share_arguments(*c, *a, pl, plan, nullptr);
   s.group = group;
+  s.always = always != 0;
   launch_share(s, (hipStream_t)stream);
   return finish(ctx, fn);
 }

@@ -23,7 +23,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void page_rows_kernel(AttendArgs a
   const int t = a.by_group.of(my_r), g = my_r - t * a.group;
   const bf16_t* q = a.Q + (int64_t)b * a.q_sb + (int64_t)(h * a.group + g) * a.q_sh + (int64_t)t * a.q_sn;
   const int64_t at = ((int64_t)bh * a.splits + split) * a.part_rows + first_row;
-  page_rows<D>(a, threadIdx.x, h, q, RowSight(a, s.first + t, s.keys), pos_of(first_row), pos_of(first_row + 31), s.keys, a.table + (int64_t)slot * a.max_pages, blocks, begin, end,
+  page_rows<D>(a, threadIdx.x, h, [&] { return TileRow{q, RowSight(a, s.first + t, s.keys)}; }, pos_of(first_row), pos_of(first_row + 31), s.keys, a.table + (int64_t)slot * a.max_pages, blocks, begin, end,
                a.splits > 1, r < rows ? a.part_ms + at + c32 : nullptr,
                [&](int row, int piece) -> void* { return first_row + row < rows ? a.part_o + (at + row) * D + 4 * piece : nullptr; },
                [&](int row, int piece) -> void* {

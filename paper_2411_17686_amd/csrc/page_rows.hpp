@@ -44,11 +44,15 @@ struct PageLds {
 // but nothing then fills its waits for LDS and barriers: 57 us instead of 40 with the queries in LDS (73 without, for lack of registers), and with heads of 64, where nothing is
 // short of registers, 102 instead of 69 behind 9600 tokens.
 //
-// tid: the thread.  A lane's row (lane % 32 of its wavefront's) has its queries at q and sees `sight`.  Keys of head h are those of blocks begin .. end - 1 and of `table`; lo, hi: first and last
+// tid: the thread.  A lane's row (lane % 32 of its wavefront's) has its queries at q and sees `sight`: rows_of() says both.  Keys of head h are those of blocks begin .. end - 1 and of `table`; lo, hi: first and last
 // position of the wavefront's rows, keys: how many keys each of them has at least.  part_ms (the lane's, null for none): where maxima and sums of parts go; part(row, piece) and out(row, piece): the
 // places of 16 bytes of row 0 .. 31 of the wavefront as floats, relative to the maximum, or as bfloat16, null for nowhere.
-template <int D, typename Part, typename Out>
-__device__ __forceinline__ void page_rows(const AttendArgs& a, int tid, int h, const bf16_t* q, const RowSight& sight, int lo, int hi, int keys, const int32_t* table,
+struct TileRow {
+  const bf16_t* q;
+  RowSight sight;
+};
+template <int D, typename Rows, typename Part, typename Out>
+__device__ __forceinline__ void page_rows(const AttendArgs& a, int tid, int h, Rows rows_of, int lo, int hi, int keys, const int32_t* table,
                                           const Blocks<kTileKeys>& blocks, int begin, int end, bool parts, float2* part_ms, Part part, Out out) {
   constexpr int DT = D / 32, KS = D / 16, CH = D / 16;
   constexpr int NL = D / 64;                       // loads into LDS of a wavefront, keys and values each
@@ -58,10 +62,6 @@ __device__ __forceinline__ void page_rows(const AttendArgs& a, int tid, int h, c
   int2* const meta = PageLds<D>::meta();           // page (or -1) and exponents (keys, values << 8, kHole) of the groups
   const int lane = tid % kWave, wv = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int c32 = lane % 32, half = lane / 32;
-  // a lane's 16 bytes of a key are features 32 l + 16 half .. + 16, for two products
-  bf16x8_t qf[KS];
-#pragma unroll
-  for (int k = 0; k < KS; ++k) __builtin_memcpy(&qf[k], q + 16 * half + 32 * (k / 2) + 8 * (k % 2), 16);
   f32x16_t o[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i) o[i] = f32x16_t{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
@@ -69,23 +69,34 @@ __device__ __forceinline__ void page_rows(const AttendArgs& a, int tid, int h, c
 
   // ---- pages of a chunk of steps, a group a thread
   auto wanted = [&](int key) { return key < blocks.end && (key >= blocks.near_key || key < blocks.first_keys); };
-  auto look_up = [&](int chunk) {
+  auto page_of = [&](int chunk) {                  // of a group: its page, -1 where none is needed, -2 where there is none
     const int step = begin + chunk * kChunk + tid / kGroups;
-    int2 m = {-1, 0};
+    int p = -1;
     if (step < end) {
       const int key = blocks.block(step) * kTileKeys + tid % kGroups * kGroup;
       if (key < blocks.end && (key + kGroup > blocks.near_key || key < blocks.first_keys)) {     // (then key lies inside the row: see sight_of)
-        const int p = table[key >> a.page_shift];
-        if (p >= 0 && p < a.n_pages) {
-          const int64_t block = (int64_t)p * a.H_kv + h;
-          m = int2{p, a.k_exp[block] | a.v_exp[block] << 8};
-        } else {
-          m.y = kHole;
-        }
+        p = table[key >> a.page_shift];
+        p = p >= 0 && p < a.n_pages ? p : -2;
       }
     }
-    return m;
+    return p;
   };
+  auto exps_of = [&](int p) {
+    const int64_t block = (int64_t)p * a.H_kv + h;
+    return p >= 0 ? a.k_exp[block] | a.v_exp[block] << 8 : p == -2 ? kHole : 0;
+  };
+  auto look_up = [&](int chunk) {
+    const int p = page_of(chunk);
+    return int2{p < 0 ? -1 : p, exps_of(p)};
+  };
+  // What does not wait for each other is on its way at once: the first pages and what rows_of() reads; queries, exponents, and the keys and values that the pages hold.
+  const int first_page = page_of(0);
+  const TileRow mine = rows_of();
+  const RowSight sight = mine.sight;
+  // a lane's 16 bytes of a key are features 32 l + 16 half .. + 16, for two products
+  bf16x8_t qf[KS];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) __builtin_memcpy(&qf[k], mine.q + 16 * half + 32 * (k / 2) + 8 * (k % 2), 16);
   auto meta_at = [&](int step) { return (step - begin) % (2 * kChunk) * kGroups; };
 
   // ---- a step's keys and values into LDS.  Keys that no row of the workgroup sees become zeros (loads behind the end of their buffer): their
@@ -237,21 +248,21 @@ __device__ __forceinline__ void page_rows(const AttendArgs& a, int tid, int h, c
   static_assert(kChunk * kGroups == kTileThreads, "a group a thread");
 
   f32x16_t S0[2], S1[2];
-  if (begin < end) {
-    meta[tid] = look_up(0);
-    meta[kChunk * kGroups + tid] = int2{-1, 0};
-  }
+  meta[tid].x = first_page < 0 ? -1 : first_page;
+  const int first_exps = exps_of(first_page);
   __syncthreads();
   if (begin < end) {
     read_pages(begin);
     load(k0, v0, begin);
     load(k1, v1, begin + 1);
     load(k2, v2, begin + 2);
-    read_exps(exps, begin);
   }
+  meta[tid].y = first_exps;
+  meta[kChunk * kGroups + tid] = int2{-1, 0};
   __builtin_amdgcn_s_waitcnt(0x0f70);
   __syncthreads();
   if (begin < end) {
+    read_exps(exps, begin);
 #pragma unroll
     for (int n = 0; n < 2 * KS; ++n) {
       const bf16x8_t kf = widen_key(*(const uint4*)(k0 + n / KS * 32 * D + k_at[n % KS / 2]), n % 2, key_scale(exps, n / KS));

@@ -54,7 +54,7 @@ struct ShareArgs {
   char* plan;
   const int32_t* group;
   Divisor by_rows;                           // n_q * group
-  int own_tile, own_tiles, pieces, items;
+  int own_tile, own_tiles, pieces, items, d_head, always;
   size_t entries, members, owners, items_at;
 };
 void launch_share(const ShareArgs& s, hipStream_t stream);

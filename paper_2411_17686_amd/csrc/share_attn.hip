@@ -93,8 +93,11 @@ __device__ __forceinline__ void share_tile(const ShareArgs& s, const ShareItem& 
     });
   } else {
     const int first = 32 * __builtin_amdgcn_readfirstlane(tid / kWave), mine_at = first + tid % 32;
-    const OwnerRow mine = owner_row(s, o, row0 + (mine_at < rows ? mine_at : rows - 1));
-    page_rows<D>(a, tid, h, query_at(a, mine, h), sight_of_row(a, mine, o.keys), narrow ? pos_of(row0 + first) : lo, narrow ? pos_of(row0 + first + 31) : hi, o.keys, table, blocks, i0, i1, parts,
+    auto row_of = [&] {
+      const OwnerRow mine = owner_row(s, o, row0 + (mine_at < rows ? mine_at : rows - 1));
+      return TileRow{query_at(a, mine, h), sight_of_row(a, mine, o.keys)};
+    };
+    page_rows<D>(a, tid, h, row_of, narrow ? pos_of(row0 + first) : lo, narrow ? pos_of(row0 + first + 31) : hi, o.keys, table, blocks, i0, i1, parts,
                  mine_at < rows ? a.part_ms + part + mine_at : nullptr,
                  [&](int row, int piece) -> void* { return first + row < rows ? a.part_o + (part + first + row) * D + 4 * piece : nullptr; },
                  [&](int row, int piece) -> void* { return first + row < rows ? result_at(a, owner_row(s, o, row0 + first + row), h) + 8 * piece : nullptr; });
@@ -105,10 +108,11 @@ template <int D>
 __global__ __launch_bounds__(kTileThreads, 2) void share_rows_kernel(ShareArgs s) {
   static_assert(kTileThreads == kFewWaves * kWave && kFewKeys * 2 == kTileKeys, "either kind of tile");
   const int wg = s.a.by_heads.of(blockIdx.x), h = blockIdx.x - wg * s.a.H_kv;
-  if (((const ShareHead*)s.plan)->mark != s.mark) return;            // (a plan for something else: nothing of it means anything)
   const ShareItem* items = (const ShareItem*)(s.plan + s.items_at);
   int next = wg < s.pieces ? wg : wg + s.pieces;
-  if (items[next].o.owner == -1) return;
+  const uint64_t mark = ((const ShareHead*)s.plan)->mark;
+  const int owner = items[next].o.owner;                             // (on its way with the mark)
+  if (mark != s.mark || owner == -1) return;                         // (another mark: a plan for something else, of which nothing means anything)
   do {
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));                                    // (or what follows from it is kept over the loop, in more registers than there are)

@@ -174,7 +174,7 @@ def lib():
         L.ficoco_cache_attention.argtypes = [vp, cp, i32, ap, vp, C.c_size_t, vp]
         L.ficoco_window_attention.argtypes = [vp, ap, vp]
         L.ficoco_cache_share_bytes.argtypes = [cp, ap, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
-        L.ficoco_cache_share.argtypes = [vp, cp, ap, i32p, vp, C.c_size_t, vp]
+        L.ficoco_cache_share.argtypes = [vp, cp, ap, i32p, i32, vp, C.c_size_t, vp]
         L.ficoco_cache_shared_attention.argtypes = [vp, cp, i32, ap, vp, C.c_size_t, vp, C.c_size_t, vp]
         L.ficoco_rotary_turns.argtypes = [C.POINTER(FrequenciesProblem), vp]
         L.ficoco_rotate.argtypes = [vp, vp, vp, vp]
@@ -638,12 +638,12 @@ class Share:
         return _ATTENTION.pack(B, H, 0, n_q, 0, d, Q, *q, 0, 0, 0, 0, 0, 0, 0, 0, O, *o, *arrays, scale, *self.how)
 
 
-def ficoco_cache_share(ctx, cache, share, group=None, seq=None, q_len=None, k_len=None, q_start=None):
-    """The plan of a step's attention; group: int32 [B]."""
+def ficoco_cache_share(ctx, cache, share, group=None, seq=None, q_len=None, k_len=None, q_start=None, always=False):
+    """The plan of a step's attention; group: int32 [B].  always: share wherever there are common keys, also where that takes longer."""
     B, d = share.shape[0], share.index
     _same_device(ctx, cache.index, d)
     arrays = [_i32(t, B, name, d) for t, name in ((seq, "seq"), (q_len, "q_len"), (k_len, "k_len"), (q_start, "q_start"))]
-    rc = lib().ficoco_cache_share(ctx._h, cache._p, share.describe(arrays=arrays), _i32(group, B, "group", d), share.plan.ptr, share.plan.bytes,
+    rc = lib().ficoco_cache_share(ctx._h, cache._p, share.describe(arrays=arrays), _i32(group, B, "group", d), int(always), share.plan.ptr, share.plan.bytes,
                                   ctx.raw_stream())
     if rc:
         ctx.check(rc)

@@ -52,13 +52,13 @@ def queries(B, H, n_q, d, seed=3):
     return (torch.randn(B, H, n_q, d, generator=g, device="cuda") * 2).to(torch.bfloat16)
 
 
-def run(ctx, c, Q, group, layer=1, window=0, sinks=0, max_len=0, scale=None, share=None, **arrays):  # noqa: F811
+def run(ctx, c, Q, group, layer=1, window=0, sinks=0, max_len=0, scale=None, share=None, always=True, **arrays):  # noqa: F811
     O = torch.full_like(Q, 77.0)
     if share is None:
         share = fc.Share(c, Q.shape[0], Q.shape[1], Q.shape[2], window=window, sinks=sinks, max_len=max_len)
         share.plan.t.fill_(255)
         share.ws.t.fill_(255)
-    fc.ficoco_cache_share(ctx, c, share, group=None if group is None else i32(group), **arrays)
+    fc.ficoco_cache_share(ctx, c, share, group=None if group is None else i32(group), always=always, **arrays)
     fc.ficoco_cache_shared_attention(ctx, c, layer, share, Q, O, scale=scale)
     return O
 
@@ -96,6 +96,8 @@ def test_families(ctx, case):  # noqa: F811
     for how in ([int(names[x]) for x in group], None, [0] * B, [-1 if i % 2 else 0 for i in range(B)]):      # right, none, all as one, some
         O = run(ctx, c, Q, how, window=window, sinks=sinks, max_len=max_len)
         check(O, Q, k, v, lens, d ** -0.5, starts, [n_q] * B, window, sinks, g)
+    O = run(ctx, c, Q, group, window=window, sinks=sinks, max_len=max_len, always=False)
+    check(O, Q, k, v, lens, d ** -0.5, starts, [n_q] * B, window, sinks, g)
     # in another order
     O = run(ctx, c, Q[torch.from_numpy(order).cuda()], [group[i] for i in order], window=window, sinks=sinks, max_len=max_len, seq=i32(order.tolist()))
     back = torch.empty_like(O)
@@ -191,7 +193,7 @@ def test_the_same_in_every_run_and_in_every_layer(ctx):  # noqa: F811
     s = torch.cuda.Stream()
     for i in range(3):
         with torch.cuda.stream(s if i == 1 else torch.cuda.current_stream()):
-            fc.ficoco_cache_share(ctx, c, share, group=i32(group))
+            fc.ficoco_cache_share(ctx, c, share, group=i32(group), always=True)
             O = [torch.empty_like(Q) for _ in range(2)]
             for layer in (0, 1):
                 fc.ficoco_cache_shared_attention(ctx, c, layer, share, Q, O[layer])
@@ -207,7 +209,7 @@ def test_a_plan_of_another_shape_writes_nothing(ctx):  # noqa: F811
     c, lens, group = family(ctx, 64, 2, 64, [(300, [310, 400])])
     Q = queries(2, 4, 1, 64)
     right, other = fc.Share(c, 2, 4, 1), fc.Share(c, 2, 4, 1, window=50)
-    fc.ficoco_cache_share(ctx, c, other, group=i32(group))
+    fc.ficoco_cache_share(ctx, c, other, group=i32(group), always=True)
     for share in (right, fc.Share(c, 2, 4, 1)):      # another's plan, none at all
         if share is right:
             share.plan = other.plan
@@ -223,9 +225,10 @@ def test_a_thousand_sequences(ctx):  # noqa: F811
     families += [(0, [int(r.randint(1, 60))]) for _ in range(1024 - sum(len(f[1]) for f in families))]
     c, lens, group = family(ctx, 32, 1, 64, families)
     Q = queries(1024, 2, 1, 64)
-    O = run(ctx, c, Q, group)
     k, v = dense(ctx, c, 1, max(lens))
-    check(O, Q, k, v, lens, 0.125, [n - 1 for n in lens], [1] * 1024, 0, 0, 2)
+    for always in (True, False):
+        O = run(ctx, c, Q, group, always=always)
+        check(O, Q, k, v, lens, 0.125, [n - 1 for n in lens], [1] * 1024, 0, 0, 2)
     with pytest.raises(fc.FicocoError) as e:
         fc.Share(c, 1025, 2, 1)
     assert e.value.code == fc.EUNSUPPORTED
@@ -253,7 +256,7 @@ def test_answers_step_by_step(ctx):  # noqa: F811
 
     def step():
         fc.ficoco_cache_reserve(ctx, c, start, 1)
-        fc.ficoco_cache_share(ctx, c, share, group=group)
+        fc.ficoco_cache_share(ctx, c, share, group=group, always=True)
         for l in range(layers):
             fc.ficoco_cache_append_rotated(ctx, c, l, rotary, q, Q, k, v, start)
             fc.ficoco_cache_shared_attention(ctx, c, l, share, Q, O[l])
@@ -281,7 +284,7 @@ def test_refused(ctx):  # noqa: F811
     c, lens, group = family(ctx, 64, 2, 64, [(300, [310, 400])])
     Q = queries(2, 4, 1, 64)
     share = fc.Share(c, 2, 4, 1)
-    fc.ficoco_cache_share(ctx, c, share, group=i32(group))
+    fc.ficoco_cache_share(ctx, c, share, group=i32(group), always=True)
     for kw, kind in ((dict(layer=2), fc.EINVAL), (dict(scale=0.0), fc.EINVAL), (dict(O=Q), fc.EINVAL), (dict(Q=Q.float()), TypeError), (dict(Q=Q[:1]), TypeError),
                      (dict(O=Q[:1].clone().expand(2, 4, 1, 64)), fc.EINVAL)):
         args = dict(layer=0, Q=Q, O=torch.empty_like(Q), scale=None)
@@ -305,3 +308,31 @@ def test_refused(ctx):  # noqa: F811
     empty = fc.Share(c, 0, 4, 1)
     fc.ficoco_cache_share(ctx, c, empty, group=i32([]))
     fc.ficoco_cache_shared_attention(ctx, c, 0, empty, Q[:0], Q[:0])
+
+
+LARGE = [  # prompt tokens, tokens of a sequence behind them, sequences, page, heads, query heads a head, d, n_q, window
+    (4096, 100, 64, 64, 8, 4, 128, 1, 0),      # tiles of 128 cut into workgroups that go on with the next tile
+    (6000, 77, 24, 32, 32, 1, 64, 1, 0),
+    (3000, 200, 16, 64, 4, 4, 128, 24, 0),
+    (3000, 200, 16, 16, 2, 7, 64, 24, 2500),
+    (9000, 64, 6, 128, 8, 4, 128, 1, 0),       # tiles of 16
+]
+
+
+@pytest.mark.parametrize("case", LARGE, ids=str)
+def test_large_families(ctx, case):  # noqa: F811
+    """A few of the rows against 64 bits, all of them against the attention of each sequence for itself."""
+    prompt, tail, n, page, heads, g, d, n_q, window = case
+    c, lens, group = family(ctx, page, heads, d, [(prompt, [prompt + tail + 3 * i for i in range(n)]), (prompt // 2, [prompt] * 3), (0, [prompt + 10])])
+    B = len(lens)
+    Q = queries(B, heads * g, n_q, d)
+    alone = torch.empty_like(Q)
+    ws = fc.attention_workspace(c, Q, alone, window=window, sinks=4)
+    fc.ficoco_cache_attention(ctx, c, 1, Q, alone, ws, window=window, sinks=4)
+    some = [0, n // 2, n - 1, n + 1, n + 3]
+    k, v = (t[some] for t in dense(ctx, c, 1, max(lens)))
+    for always in (True, False):
+        O = run(ctx, c, Q, group, window=window, sinks=4, always=always)
+        check(O[some], Q[some], k, v, [lens[i] for i in some], d ** -0.5, [lens[i] - n_q for i in some], [n_q] * len(some), window, 4, g)
+        # both are within 2^-7 of sum w |v| of the exact result (the weights' rounding, 2^-8, and some 2^-15 more), and rounded: |v| stays below 12
+        assert float((O.float() - alone.float()).abs().max()) <= 2 * (2.0 ** -8 * 1.1 + 2.0 ** -8) * 12
