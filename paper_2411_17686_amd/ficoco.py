@@ -712,6 +712,7 @@ class Rotary:
             if t.dtype != given[0].dtype or t.dim() != rows or rows not in (1, 2) or t.shape[-1] != d_head or not t.is_contiguous() or t.get_device() != self.index:
                 raise TypeError("weights and biases are contiguous, of one type, all [d_head] or all [heads][d_head], on the device of turns")
         self.heads = [{t.shape[0] for t in side if t is not None and rows == 2} for side in ((q_weight, q_bias), (k_weight, k_bias))]
+        self.per_head = rows == 2
         self.kept = (turns, axis, q_weight, k_weight, q_bias, k_bias)
         at = [0 if t is None else t.data_ptr() for t in self.kept]
         self.packed = _ROTARY.pack(d_head, rot_begin, 2 * turns.numel(), layout, norm, _dtype_code(given[0]) if given else F32, int(rows == 2), eps,
@@ -722,71 +723,96 @@ class Rotary:
             raise TypeError("weights of each head do not have the heads of the rows")
 
 
-def _head_rows(t, d, index, name):
-    """Address and strides of [B][heads][n][d_head] rows."""
-    sb, sh, sn, s1 = t.stride()
-    if t.shape[3] != d or (s1 != 1 and d > 1) or t.get_device() != index:
-        raise TypeError("%s must be [B][heads][n][d_head], d_head contiguous, on device %d" % (name, index))
-    return t.data_ptr(), sb, sh, sn
+_CODES = {torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _head_rows(t, out, d, index, name):
+    """Shape, then addresses and strides of [B][heads][n][d_head] rows and of their output."""
+    shape = t.shape
+    B, heads, n, width = shape
+    sb, sh, sn, s1 = stride = t.stride()
+    at = out_at = t.data_ptr()
+    ob, oh, on, o1 = stride
+    if out is not t:
+        ob, oh, on, o1 = out.stride()
+        out_at = out.data_ptr()
+        if out.shape != shape or out.get_device() != index:
+            raise TypeError("the output of %s must have its shape, on device %d" % (name, index))
+    if width != d or (s1 != 1 or o1 != 1) and d > 1 or t.get_device() != index:
+        raise TypeError("%s and its output must be [B][heads][n][d_head], d_head contiguous, on device %d" % (name, index))
+    return B, heads, n, (at, sb, sh, sn), (out_at, ob, oh, on)
 
 
 def _rotation(rotary, Q, K, Q_out, K_out, pos, start, n_rows):
-    some = K if Q is None else Q
-    if some is None:
-        raise TypeError("Q and K are both None")
     d, index = rotary.d_head, rotary.index
-    B, _, n, _ = some.shape
-    out = K_out if Q is None else Q_out
-    H = H_kv = None
+    H = H_kv = 0
     q = k = qo = ko = _NO_ROWS
     if Q is not None:
-        H = Q.shape[1]
-        q, qo = _head_rows(Q, d, index, "Q"), _head_rows(Q_out, d, index, "Q_out")
-        if Q_out.shape != Q.shape:
-            raise TypeError("Q_out has not the shape of Q")
+        B, H, n, q, qo = _head_rows(Q, Q_out, d, index, "Q")
+        dtype, out_dtype = Q.dtype, Q_out.dtype
     if K is not None:
-        H_kv = K.shape[1]
-        k, ko = _head_rows(K, d, index, "K"), _head_rows(K_out, d, index, "K_out")
-        if K_out.shape != K.shape or K.shape[0] != B or K.shape[2] != n or K.dtype != some.dtype or K_out.dtype != out.dtype:
+        B_k, H_kv, n_k, k, ko = _head_rows(K, K_out, d, index, "K")
+        if Q is None:
+            B, n, dtype, out_dtype = B_k, n_k, K.dtype, K_out.dtype
+        elif B_k != B or n_k != n or K.dtype != dtype or K_out.dtype != out_dtype:
             raise TypeError("Q and K, and their outputs, are of the same sequences and types")
-    rotary.check_heads(H, H_kv)
-    return _ROTATION.pack(B, H or 0, H_kv or 0, n, _dtype_code(some), _dtype_code(out), *q, *k, *qo, *ko, *_positions(pos, B, n, index),
+    elif Q is None:
+        raise TypeError("Q and K are both None")
+    code, out_code = _CODES.get(dtype), _CODES.get(out_dtype)
+    if code is None or out_code is None:
+        raise TypeError("queries and keys must be float32 or bfloat16")
+    if rotary.per_head:
+        rotary.check_heads(H or None, H_kv or None)
+    at, step, row, axes = (0, 0, 0, 1) if pos is None else _positions(pos, B, n, index)
+    return _ROTATION.pack(B, H, H_kv, n, code, out_code, *q, *k, *qo, *ko, at, step, row, axes,
                           0 if start is None else _i32(start, B, "start", index), 0 if n_rows is None else _i32(n_rows, B, "n_rows", index))
 
 
 def _positions(pos, B, n, index):
-    if pos is None:
-        return 0, 0, 0, 1
+    """Address, strides of an axis and of a sequence, axes."""
     shape, stride = pos.shape, pos.stride()
-    if pos.dtype != torch.int32 or shape[-2:] != (B, n) or len(shape) not in (2, 3) or (stride[-1] != 1 and n > 1) or pos.get_device() != index:
+    axes, step = 1, 0
+    if len(shape) == 3:
+        axes, b, m = shape
+        step, row, one = stride
+    elif len(shape) == 2:
+        b, m = shape
+        row, one = stride
+    else:
+        b = -1
+    if b != B or m != n or (one != 1 and n > 1) or pos.dtype != torch.int32 or pos.get_device() != index:
         raise TypeError("pos must be int32 [B][n] or [axes][B][n], the last axis contiguous, on device %d" % index)
-    return pos.data_ptr(), stride[0] if len(shape) == 3 else 0, stride[-2], shape[0] if len(shape) == 3 else 1
+    return pos.data_ptr(), step, row, axes
 
 
 def ficoco_rotate(ctx, rotary, Q, K, Q_out=None, K_out=None, pos=None, start=None, n_rows=None):
     """Q and K (either may be None) [B][heads][n][d_head]; outputs None = in place.  pos: int32 [B][n], or [axes][B][n]."""
-    _same_device(ctx, rotary.index)
-    rc = lib().ficoco_rotate(ctx._h, rotary.packed, _rotation(rotary, Q, K, Q if Q_out is None else Q_out, K if K_out is None else K_out, pos, start, n_rows),
-                             ctx.raw_stream())
+    if rotary.index != ctx.index:
+        _same_device(ctx, rotary.index)
+    rc = _lib.ficoco_rotate(ctx._h, rotary.packed, _rotation(rotary, Q, K, Q if Q_out is None else Q_out, K if K_out is None else K_out, pos, start, n_rows),
+                            ctx.raw_stream())
     if rc:
         ctx.check(rc)
 
 
 def ficoco_cache_append_rotated(ctx, cache, layer, rotary, Q, Q_out, K, V, start, pos=None, n_new=None, seq=None):
     """Queries into Q_out (None = in place; Q may be None), keys and values into their pages; pos as in ficoco_rotate, None = start[b] + t."""
-    _same_device(ctx, rotary.index)
+    if rotary.index != ctx.index:
+        _same_device(ctx, rotary.index)
     if K is None or V is None:
         raise TypeError("K or V is None")
     tokens = _tokens(ctx, cache, K, V, start, n_new, seq)
     B, H_kv, n, _ = K.shape
+    if rotary.per_head:
+        rotary.check_heads(None, H_kv)
     if Q is None:
-        rotary.check_heads(None, H_kv)
         code = _dtype_code(K)
-        rows = _ROTATION.pack(B, 0, 0, n, code, code, *_NO_ROWS, *_NO_ROWS, *_NO_ROWS, *_NO_ROWS, *_positions(pos, B, n, rotary.index), 0, 0)
+        rows = _ROTATION.pack(B, 0, 0, n, code, code, *_NO_ROWS, *_NO_ROWS, *_NO_ROWS, *_NO_ROWS,
+                              *((0, 0, 0, 1) if pos is None else _positions(pos, B, n, rotary.index)), 0, 0)
     else:
-        if Q.shape[0] != B or Q.shape[2] != n:
+        shape = Q.shape
+        if shape[0] != B or shape[2] != n:
             raise TypeError("Q is not of the sequences of K")
-        rotary.check_heads(None, H_kv)
         rows = _rotation(rotary, Q, None, Q if Q_out is None else Q_out, None, pos, None, None)
     rc = lib().ficoco_cache_append_rotated(ctx._h, cache._p, layer, rotary.packed, tokens, rows, ctx.raw_stream())
     if rc:
