@@ -9,8 +9,6 @@ namespace {
 
 constexpr int kRotateThreads = 256;
 
-constexpr int kAtOnce = 2;           // heads of a lane whose loads are on their way together
-
 enum NormForm { kNoNorm, kPlainNorm, kAnyNorm };      // (none; root mean square without a bias; whatever the call says)
 
 // How rows are laid over lanes: `lanes` lanes a row, items of up to `heads` heads of one token, q_items of queries and k_items of keys.
@@ -19,11 +17,16 @@ struct RowShape {
   Divisor by_lanes, by_items, by_rows;
 };
 
-// A lane holds NS slots of a head (slot_of()) and turns them by the same angles in all heads of its item.
+// A lane holds NS slots of a head (slot_of()) and turns them by the same angles in all heads of its item, each read and written once.
 //
-// Bound by memory.
+// Many rows are bound by memory: 32768 tokens, 32 heads of 128 features of which half turn, 537 MB of bfloat16, 104 us (5.1 TB/s, what a copy of 1 GiB reaches); a norm and
+// sines by three axes cost a little: 8 ragged prompts of up to 2979 tokens, 40 heads of 128, 356 MB, 79 us (4.5 TB/s).  Single precision by chunks of four: 576 patches of 16 images, 32 heads of 80,
+// 189 MB, 44 us (4.3 TB/s).  A few tokens take 3 to 5 us, a launch and two loads one after the other.
 template <typename T, typename TO, int W, int NS, NormForm NORM>
 __global__ __launch_bounds__(kRotateThreads) void rotate_kernel(RotateArgs a, RowShape shape) {
+  // Heads of a lane whose loads are on their way together: two (the 537 MB above 104 us, by one 108, by four 102; 2 prompts of 4100 tokens in single precision with a norm 36 us, 39 and 38), but one
+  // where weights and a norm of 16 features a lane need the registers (the 356 MB above 79 us, by two 82).  (The next heads' loads before these heads are done: 113 us and 99.)
+  constexpr int kAtOnce = NORM != kNoNorm && W == 8 ? 1 : 2;
   const int at = blockIdx.x * kRotateThreads + threadIdx.x, all = shape.by_lanes.of(at), token = shape.by_items.of(all), b = shape.by_rows.of(token);
   const int i = at - all * shape.lanes, t = token - b * a.n, in = all - token * (shape.q_items + shape.k_items);
   if (b >= a.B) return;
@@ -97,8 +100,8 @@ __global__ __launch_bounds__(kRotateThreads) void rotate_kernel(RotateArgs a, Ro
   }
 }
 
-// The widest chunk that the rotated features begin and end with, of 16 bytes at most: lanes next to each other then load what lies next to each other (float rows of
-// 80 by chunks of 8 55 us, of 4 ).
+// The widest chunk that the rotated features begin and end with, of 16 bytes at most: lanes next to each other then load what lies next to each other (16 images'
+// patches, heads of 80 in single precision: by chunks of eight 55 us, of four 44).
 int chunk_width(const RotaryArgs& r, int most) {
   for (int w = most; w > 1; w /= 2)
     if (r.d % w == 0 && r.begin % w == 0 && r.rot % (2 * w) == 0) return w;
@@ -111,8 +114,9 @@ RowShape shape_of(const RotateArgs& a, int width) {
   s.lanes = slots;
   if (a.r.norm != FICOCO_NORM_NONE || slots > kWave)
     for (s.lanes = 1; s.lanes < kWave && s.lanes < slots;) s.lanes *= 2;
-  // Several heads an item where there are rows enough to fill the chip that way.
-  s.heads = (int64_t)a.B * a.n * (a.q.heads + a.k.heads) * a.r.d >= 1 << 23 ? 4 : 1;
+  // Items of four heads share their angles, where there are rows enough to fill the chip that way: 40 heads of 128 with a norm, 400 tokens 6.9 us, by items of one head 5.2, 800 tokens 7.7 and 8.3,
+  // 20000 tokens 80 and 130; 32 heads of 64 in single precision, 800 tokens 5.0 and 4.9, 1600 tokens 6.3 and 7.2.  (The 537 MB of rotate_kernel() by items of two 102 us, of four 104, of eight 109; its 356 MB by eight 79 as by four.)
+  s.heads = (int64_t)a.B * a.n * (a.q.heads + a.k.heads) * a.r.d >= 3 << 20 ? 4 : 1;
   s.q_items = (a.q.heads + s.heads - 1) / s.heads;
   s.k_items = (a.k.heads + s.heads - 1) / s.heads;
   s.by_lanes = Divisor(s.lanes);
