@@ -553,7 +553,7 @@ typedef struct {
 
 /* Rows of a call: token t < n_rows[b] <= n of sequence b, all heads.  Rows behind them are left as they are.  Strides in elements, d_head contiguous, any
  * element alignment.  An output is its input (same address, type and strides: in place) or shares no element with any of them; views
- * of one packed projection are told apart where their strides allow it. */
+ * of one packed projection are told apart where their strides allow it.  Nor does an output share memory with anything else that the call reads. */
 typedef struct {
   int32_t B, H, H_kv, n;
   int32_t dtype, out_dtype; /* ficoco_dtype of Q and K, of Q_out and K_out */

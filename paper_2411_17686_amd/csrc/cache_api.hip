@@ -102,7 +102,7 @@ ShareArgs share_arguments(const ficoco_cache& c, const ficoco_attention& a, cons
   layer_pages(s.a, c, 0);
   // what the plan's numbers depend on
   uint64_t mark = 0x9e3779b97f4a7c15ull;
-  for (const int64_t x : {(int64_t)a.B, (int64_t)a.H, (int64_t)c.heads, (int64_t)a.n_q, (int64_t)a.d_head, (int64_t)a.window, (int64_t)a.sinks, (int64_t)c.page_size, (int64_t)c.n_pages,
+  for (const int64_t x : {(int64_t)a.B, (int64_t)a.H, (int64_t)c.heads, (int64_t)a.n_q, (int64_t)a.d_head, (int64_t)a.window, (int64_t)a.sinks, (int64_t)a.max_len, (int64_t)c.page_size, (int64_t)c.n_pages,
                           (int64_t)c.n_seqs, (int64_t)c.max_pages, (int64_t)pl.items, (int64_t)pl.pieces})
     mark = (mark ^ (uint64_t)x) * 0x100000001b3ull + (mark >> 29);
   s.mark = mark;

@@ -1,5 +1,6 @@
 // C-ABI layer of the rotation: argument checks and launches.  Host code only.
 #include <cmath>
+#include <initializer_list>
 
 #include "checks.hpp"
 #include "rotary.hpp"
@@ -95,6 +96,17 @@ Span3 target(const HeadRows& x, int64_t B, int64_t n, int64_t d, int dtype) {
   return span3(x.out, B, x.heads, n, x.ob, x.oh, x.on, d, dtype == FICOCO_BF16 ? 2 : 4);
 }
 
+// Whether rows that are written may be among what else a call reads: positions, lengths and slots (`lists`, of B each), frequencies and weights.
+bool into_inputs(const ficoco_rotary& r, const ficoco_rotation& x, int64_t B, int64_t n, std::initializer_list<const void*> lists, int64_t q_heads, int64_t k_heads, const Span3& out) {
+  if (out.empty()) return false;
+  auto meets = [&](const void* p, int64_t bytes) { return p && bytes > 0 && ranges_overlap(p, (size_t)bytes, (const void*)out.p, (size_t)out.bytes()); };
+  for (const void* p : lists)
+    if (meets(p, B * 4)) return true;
+  const int64_t row = (int64_t)r.d_head * (r.weight_dtype == FICOCO_F32 ? 4 : 2), q_row = r.per_head ? q_heads * row : row, k_row = r.per_head ? k_heads * row : row;
+  return meets(x.pos, ((x.axes - 1) * x.pos_stride_axis + (B - 1) * x.pos_stride_b + n) * 4) || meets(r.turns, (int64_t)r.rot_dim * 4) || meets(r.axis, r.rot_dim / 2) ||
+         meets(r.q_weight, q_row) || meets(r.q_bias, q_row) || meets(r.k_weight, k_row) || meets(r.k_bias, k_row);
+}
+
 }  // namespace
 
 extern "C" {
@@ -128,6 +140,8 @@ int ficoco_rotate(ficoco_ctx* ctx, const ficoco_rotary* r, const ficoco_rotation
   const bool one_type = x->dtype == x->out_dtype;
   if ((!(one_type && same(q, qo)) && may_meet(q, qo)) || (!(one_type && same(k, ko)) && may_meet(k, ko)) || may_meet(qo, k) || may_meet(ko, q) || may_meet(qo, ko))
     return fail(ctx, FICOCO_EINVAL, fn, "an output shares elements with another tensor");
+  for (const Span3& out : {qo, ko})
+    if (into_inputs(*r, *x, x->B, x->n, {x->start, x->n_rows}, a.q.heads, a.k.heads, out)) return fail(ctx, FICOCO_EINVAL, fn, "an output overlaps positions, lengths, frequencies or weights");
   if (rotate_threads(a, x->dtype, x->out_dtype) > kMaxRows - 256) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "too many rows in one call");
   launch_rotate(a, x->dtype, x->out_dtype, (hipStream_t)stream);
   return finish(ctx, fn);
@@ -162,6 +176,7 @@ int ficoco_cache_append_rotated(ficoco_ctx* ctx, const ficoco_cache* c, int32_t 
     const Span3 v = span3(t->V, t->n, c->heads, t->n_max, t->v_stride_b, t->v_stride_h, t->v_stride_n, d, es);
     if ((!(x->dtype == x->out_dtype && same(q, qo)) && may_meet(q, qo)) || may_meet(qo, k) || may_meet(qo, v))
       return fail(ctx, FICOCO_EINVAL, fn, "Q_out shares elements with another tensor");
+    if (into_inputs(*r, *x, t->n, t->n_max, {t->seq, t->start, t->n_new}, x->H, c->heads, qo)) return fail(ctx, FICOCO_EINVAL, fn, "Q_out overlaps positions, lengths, frequencies or weights");
     if (reaches_into(*c, x->Q_out, (size_t)qo.bytes())) return fail(ctx, FICOCO_EINVAL, fn, "Q_out overlaps the cache");
     if (rotate_threads(a, x->dtype, x->out_dtype) > kMaxRows - 256) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "too many rows in one call");
   }

@@ -1,4 +1,6 @@
 """Norm and rotation of queries and keys against 64 bits within the bound derived in tests/rotary_ref.py."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -239,3 +241,32 @@ def test_refused_calls_launch_nothing(ctx):
     assert e.value.code == fc.EUNSUPPORTED
     torch.cuda.synchronize()
     assert not x.any() and not K.any()
+
+
+def test_outputs_over_what_is_read(ctx):
+    """Positions, lengths, frequencies and weights that an output would change under the call; right beside them is allowed."""
+    n, heads, d = 3, 2, 64
+    size, small = heads * n * d, 4 * d * 4
+    memory = torch.zeros(4 * size + 3 * small, dtype=torch.uint8, device="cuda")
+    Qo = memory[small:small + 4 * size].view(torch.float32).view(1, heads, n, d)
+    Q = torch.ones_like(Qo)
+    ints = lambda at, *shape: memory[at:at + 4 * math.prod(shape)].view(torch.int32).view(shape)
+    floats = lambda at, *shape: ints(at, *shape).view(torch.float32)
+    turns = fc.rotary_turns(d).cuda()
+    end = small + 4 * size
+
+    def rotate(pos=None, start=None, n_rows=None, **kw):
+        fc.ficoco_rotate(ctx, fc.Rotary(d, kw.pop("turns", turns), **kw), Q, None, Qo, None, pos=pos, start=start, n_rows=n_rows)
+
+    norm = dict(norm=fc.NORM_RMS)
+    for kw in (dict(pos=ints(end - 4, 1, n)), dict(pos=ints(small - 8, 1, n)), dict(pos=ints(small - 4 * n, 2, 1, n)), dict(start=ints(small, 1)), dict(n_rows=ints(end - 4, 1)),
+               dict(turns=memory[end - 8:end + 4 * d - 8].view(torch.int64)), dict(axis=memory[small - 1:small + d // 2 - 1]),
+               dict(q_weight=floats(small - 4, d), **norm), dict(q_weight=floats(small - 4 * d - 4, heads, d), **norm), dict(q_bias=floats(end - 4, d), **norm)):
+        with pytest.raises(fc.FicocoError) as e:
+            rotate(**kw)
+        assert "overlaps" in str(e.value), kw
+    torch.cuda.synchronize()
+    assert not memory.any()
+    rotate(pos=ints(small - 4 * n, 1, n), start=ints(small - 4, 1), q_weight=floats(end, heads, d), k_weight=floats(small - 8 * d, heads, d), **norm)
+    torch.cuda.synchronize()
+    assert not memory.any()            # (a weight of zeros)
