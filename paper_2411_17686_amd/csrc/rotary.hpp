@@ -71,6 +71,7 @@ __device__ __forceinline__ uint32_t turned_by(int64_t p, uint64_t turns) {
   const uint32_t low = (uint32_t)turns;
   return (uint32_t)p * (uint32_t)(turns >> 32) + __umulhi((uint32_t)p, low) - (low & (uint32_t)(p >> 63));
 }
+constexpr int kFewAxes = 4;
 template <int W>
 struct Angles { float s[W], c[W]; };
 template <int W>
@@ -86,10 +87,23 @@ __device__ __forceinline__ void angles_of(const RotaryArgs& r, const Slot<W>& sl
     uint64_t axis = 0;
     __builtin_memcpy(&axis, r.axis + slot.turn, W);
     int32_t at[W];
+    if (r.axes <= kFewAxes) {                              // (uniform: a load for each axis, not for each pair)
+      int32_t on[kFewAxes];
 #pragma unroll
-    for (int i = 0; i < W; ++i) {
-      const int on = (int)(axis >> 8 * i) & 255;
-      at[i] = p.pos[(on < r.axes ? on : 0) * p.step];
+      for (int k = 0; k < kFewAxes; ++k) on[k] = p.pos[(k < r.axes ? k : 0) * p.step];
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const uint32_t which = (uint32_t)(axis >> 8 * i) & 255;
+        at[i] = on[0];
+#pragma unroll
+        for (int k = 1; k < kFewAxes; ++k) at[i] = which == (uint32_t)k ? on[k] : at[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const int on = (int)(axis >> 8 * i) & 255;
+        at[i] = p.pos[(on < r.axes ? on : 0) * p.step];
+      }
     }
 #pragma unroll
     for (int i = 0; i < W; ++i) sin_cos(turned_by(at[i], turns[i]), r.amplitude, x.s[i], x.c[i]);
