@@ -104,6 +104,11 @@ __device__ __forceinline__ void share_tile(const ShareArgs& s, const ShareItem& 
   }
 }
 
+// Bound by what few_rows() and page_rows() are bound by, common keys counted once for a group.  Heads of 128:
+//   8 answers behind 675 tokens, 32 heads            9.5 us  (9 MB) a launch, three trips to memory and the blocks of a workgroup
+//   64 answers behind 16384, 32 heads on 8          39 us    (17.4 GFLOP of products for the common keys, 13 MB of own keys) tiles of 128 rows: their 8 us of start, then 1.05 us a block
+//   16 questions of 48 behind 9000, 32 heads on 8  146 us    (113 GFLOP, 0.78 PFLOP/s) vector instructions beside the products, as page_rows()
+// and 48 sequences, 5 prompts of up to 24000, 28 heads of 64 on 4 32 us (82 MB, 2.6 TB/s).  Either kind of tile is in one launch, so that the one fills the places that the other leaves: a launch for each took 108 us instead of 102 for the last of these calls, 226 instead of 212 for the one before.
 template <int D>
 __global__ __launch_bounds__(kTileThreads, 2) void share_rows_kernel(ShareArgs s) {
   static_assert(kTileThreads == kFewWaves * kWave && kFewKeys * 2 == kTileKeys, "either kind of tile");
@@ -139,6 +144,8 @@ __device__ __forceinline__ PartsOf parts_of(const ShareParts& p, int r, int h, i
 
 // Rows that have parts: those of their own keys and of their group's, relative to their largest maximum, eight at a time; D / 4 lanes a row and group of parts, the
 // groups' sums meet in LDS (as join_rows_kernel).
+//
+// Bound by memory and latency: 64 sequences, 32 heads of 128 10 us, 16 questions of 48 queries 14 us (the parts once, 3 TB/s); 8 sequences 4 us, a launch and three trips.  One group of lanes a row where there are few parts.
 template <int D, int GROUPS>
 __global__ __launch_bounds__(kFewWaves * kWave) void share_join_kernel(ShareArgs s) {
   constexpr int L = D / 4, AT_ONCE = 8;
