@@ -13,24 +13,29 @@ constexpr int kMostPieces = 512;                 // workgroups for a head: two a
 // behind 2048 40.1 and 39.0, 8192 57.8 and 52.5; 32 rows 19.7 and 26 behind 16384; 112 rows of 4 heads of 64 behind 4096 11.7 and 13.9.
 constexpr long long kFewWork = 2100;
 
-// Sums over the threads before this one, and over all.
-struct Sums { long long blocks; int cut, whole, parts, members; };
+// Sums over the threads before this one, and over all, of which the first `waves` wavefronts have any.  Whole numbers below 2^53.
+struct Sums { double blocks; int cut, whole, parts, members; };
 __device__ __forceinline__ Sums add(const Sums& x, const Sums& y) { return Sums{x.blocks + y.blocks, x.cut + y.cut, x.whole + y.whole, x.parts + y.parts, x.members + y.members}; }
-template <int NT>
-__device__ __forceinline__ Sums sums_before(const Sums& mine, Sums* scratch, Sums& all) {
-  const int lane = threadIdx.x % kWave, wv = threadIdx.x / kWave;
-  Sums x = mine;
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const Sums y{__shfl_up(x.blocks, d), __shfl_up(x.cut, d), __shfl_up(x.whole, d), __shfl_up(x.parts, d), __shfl_up(x.members, d)};
-    if (lane >= d) x = add(x, y);
-  }
-  if (lane == kWave - 1) scratch[wv] = x;
+template <int CTRL>
+__device__ __forceinline__ double plus_shifted(double x) {
+  return x + __hiloint2double(dpp_move_or_zero<CTRL>(__double2hiint(x)), dpp_move_or_zero<CTRL>(__double2loint(x)));
+}
+__device__ __forceinline__ double scan_inclusive(double v) {      // (as wave_scan_inclusive())
+  v = plus_shifted<0x118>(plus_shifted<0x114>(plus_shifted<0x112>(plus_shifted<0x111>(v))));
+  const double r0 = lane_value(v, 15), r1 = lane_value(v, 31), r2 = lane_value(v, 47);
+  const int row = (int)(threadIdx.x % kWave) / 16;
+  return v + (row >= 1 ? r0 : 0.0) + (row >= 2 ? r1 : 0.0) + (row >= 3 ? r2 : 0.0);
+}
+__device__ __forceinline__ Sums sums_before(const Sums& mine, Sums* scratch, int waves, Sums& all) {
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  Sums x{0, 0, 0, 0, 0};
+  if (wv < waves) x = Sums{scan_inclusive(mine.blocks), wave_scan_inclusive(mine.cut), wave_scan_inclusive(mine.whole), wave_scan_inclusive(mine.parts), wave_scan_inclusive(mine.members)};
+  if (threadIdx.x % kWave == kWave - 1) scratch[wv] = x;
   __syncthreads();
   Sums before{0, 0, 0, 0, 0};
   all = before;
-#pragma unroll 4
-  for (int w = 0; w < NT / kWave; ++w) {
+#pragma unroll 2
+  for (int w = 0; w < waves; ++w) {
     if (w < wv) before = add(before, scratch[w]);
     all = add(all, scratch[w]);
   }
@@ -39,30 +44,18 @@ __device__ __forceinline__ Sums sums_before(const Sums& mine, Sums* scratch, Sum
 }
 
 // Sums over all threads.
-struct Six { unsigned long long x, y, z, w; int u, v; };
-template <int NT>
-__device__ __forceinline__ Six sum_of(Six p, Six* scratch) {
-#pragma unroll
-  for (int d = kWave / 2; d > 0; d /= 2) {
-    p.x += __shfl_xor(p.x, d);
-    p.y += __shfl_xor(p.y, d);
-    p.z += __shfl_xor(p.z, d);
-    p.w += __shfl_xor(p.w, d);
-    p.u += __shfl_xor(p.u, d);
-    p.v += __shfl_xor(p.v, d);
+struct Six { double x, y, z, w; int u, v; };
+__device__ __forceinline__ Six sum_of(Six p, Six* scratch, int waves) {
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  if (wv < waves) {
+    auto plus = [](auto a, auto b) { return a + b; };
+    p = Six{wave_reduce(p.x, plus), wave_reduce(p.y, plus), wave_reduce(p.z, plus), wave_reduce(p.w, plus), wave_reduce(p.u, plus), wave_reduce(p.v, plus)};
+    if (threadIdx.x % kWave == 0) scratch[wv] = p;
   }
-  if (threadIdx.x % kWave == 0) scratch[threadIdx.x / kWave] = p;
   __syncthreads();
-  p = Six{0, 0, 0, 0, 0, 0};
-#pragma unroll 4
-  for (int w = 0; w < NT / kWave; ++w) {
-    p.x += scratch[w].x;
-    p.y += scratch[w].y;
-    p.z += scratch[w].z;
-    p.w += scratch[w].w;
-    p.u += scratch[w].u;
-    p.v += scratch[w].v;
-  }
+  p = scratch[0];
+#pragma unroll 2
+  for (int w = 1; w < waves; ++w) p = Six{p.x + scratch[w].x, p.y + scratch[w].y, p.z + scratch[w].z, p.w + scratch[w].w, p.u + scratch[w].u, p.v + scratch[w].v};
   return p;
 }
 
@@ -71,22 +64,23 @@ __device__ __forceinline__ Six sum_of(Six p, Six* scratch) {
 // the parts at 3 TB/s and takes 1.5 us to begin.  It decides whether the common keys of the groups are worth it: 64 sequences, 32 heads on 8 of 128, behind 512 common tokens 16.4 us without, 20.3 with them; behind 1024 21.8
 // and 21.9, 4096 53.6 and 28; 8 behind 512 10.4 and 10.6, 4096 16.9 and 13.3; 16 questions of 48 tokens behind 512 37 and 41, 9000 163 and 138.
 struct Costs {
-  unsigned long long own, common, start;
+  int own, common, start;
   __device__ __forceinline__ Costs(const ShareArgs& s, bool few) : own(few ? 13 : 34), common(few ? 18 : 34), start(few ? 72 : 144) {
     if (s.d_head == 64) {
       common /= 2;
       own = few ? own : common;
     }
   }
-  __device__ __forceinline__ float time(const ShareArgs& s, unsigned long long work, unsigned long long blocks, int tiles, int part_rows) const {
+  __device__ __forceinline__ float time(const ShareArgs& s, double work, double blocks, int tiles, int part_rows) const {
     const float each = (float)work / (float)s.pieces, unit = fmaxf((float)kLeastBlocks, (float)blocks / (float)s.pieces), longest = (float)start + (float)own * unit + 72.0f * (ceilf((float)tiles / (float)s.pieces) - 1.0f);
     const float parts = fminf((float)s.pieces, (float)blocks / (float)kLeastBlocks) * (float)part_rows + (float)s.a.B * (float)(s.a.n_q * s.a.group);
     return fmaxf(each, longest) + 24.0f + parts * (float)s.a.H_kv * (float)(4 * s.d_head + 8) * (16.0f / 3e6f);
   }
 };
 
-// x / y of whole numbers, 0 <= x < 2^53: the quotient of the doubles lies on the same side of every whole number as the exact one (a division of 64-bit integers takes ten times as long).
-__device__ __forceinline__ long long quotient(long long x, int y) { return (long long)((double)x / (double)y); }
+// The whole part of x / y, whole numbers, 0 <= x < 2^53: the quotient of the doubles lies on the same side of every whole number as the exact one (a division of 64-bit integers takes ten times
+// as long).  It has to fit in an int.
+__device__ __forceinline__ int quotient(double x, int y) { return (int)(x / (double)y); }
 
 // The last of n ascending numbers that is not above x.
 template <typename T>
@@ -101,19 +95,19 @@ __device__ __forceinline__ int last_below(const T* at, int n, T x) {
 
 // One workgroup, a thread a sequence.  Every number is the same in every run: groups are in the order of their first members, members in that of the call.
 //
-// Bound by its chain: members of groups, rows of the table (read once, 16 bytes a lane, the bytes do not count), three sums over all threads, the items.  8 answers behind 675 tokens, pages of 64, 12 us;
-// 64 behind 16384 20; 48 in 5 groups behind 24000 at most, pages of 32, 22; once for all layers of a step.
+// Bound by its chain: members of groups, rows of the table (read once, 16 bytes a lane, the bytes do not count), three sums over all threads, the items.  8 answers behind 675 tokens, pages of 64, 8.6 us;
+// 64 behind 16384 13; 48 in 5 groups behind 24000 at most, pages of 32, 13.5; once for all layers of a step.
 template <int NT>
 __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
   __shared__ __align__(16) int group[NT];
   __shared__ int slots[NT];
   __shared__ int common[NT], lows[NT], highs[NT];          // of the group whose first member is b
-  __shared__ long long at_blocks[2 * NT];                  // of owner i (group 2 b, sequence 2 b + 1): blocks, and tiles, that are cut before it
+  __shared__ double at_blocks[2 * NT];                     // of owner i (group 2 b, sequence 2 b + 1): blocks, and tiles, that are cut before it
   __shared__ int at_cut[2 * NT];
   __shared__ Sums scratch[NT / kWave];
   __shared__ Six sixes[2][NT / kWave];
   const AttendArgs& a = s.a;
-  const int b = threadIdx.x, R = a.n_q * a.group;
+  const int b = threadIdx.x, R = a.n_q * a.group, waves = (a.B + kWave - 1) / kWave;
   ShareEntry* entries = (ShareEntry*)(s.plan + s.entries);
   ShareMember* members = (ShareMember*)(s.plan + s.members);
   ShareOwner* owners = (ShareOwner*)(s.plan + s.owners);
@@ -136,7 +130,7 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
   // members before this one, all of them, and the first
   int rank = 0, count = 0, leader = b;
   if (g >= 0) {
-    constexpr int STEP = NT > 512 ? 4 : 16;
+    constexpr int STEP = 16;
     for (int i = (a.B - 1) / STEP * STEP; i >= 0; i -= STEP) {      // (behind the last one: -1)
       int x[STEP];
 #pragma unroll
@@ -158,7 +152,7 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
   __syncthreads();
   // the pages that all members of a group hold: a wavefront a member, some at a time, against the first one's
   const int lane = threadIdx.x % kWave, wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  constexpr int WAVES = NT / kWave, AT_ONCE = NT > 512 ? 2 : 4;
+  constexpr int WAVES = NT / kWave, AT_ONCE = 4;
   for (int e0 = wv; e0 < a.B; e0 += AT_ONCE * WAVES) {
     int first[AT_ONCE], till[AT_ONCE], most = 0;
 #pragma unroll
@@ -178,10 +172,10 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const int i = i0 + 4 * (j * kWave + lane);
-          if (i + 4 <= till[k]) {
+          if (i < till[k] && i + 4 <= a.max_pages) {       // (what lies behind `till` in them does not count)
             __builtin_memcpy(&x[k][4 * j], p + i, 16);
             __builtin_memcpy(&y[k][4 * j], q + i, 16);
-          } else {
+          } else if (i < till[k]) {
 #pragma unroll
             for (int m = 0; m < 4; ++m) {
               x[k][4 * j + m] = i + m < till[k] ? p[i + m] : 0;
@@ -194,7 +188,10 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
       for (int k = 0; k < AT_ONCE; ++k) {
         differ[k] = 0x7fffffff;
 #pragma unroll
-        for (int j = 7; j >= 0; --j) differ[k] = x[k][j] != y[k][j] ? i0 + 4 * (j / 4 * kWave + lane) + j % 4 : differ[k];
+        for (int j = 7; j >= 0; --j) {
+          const int i = i0 + 4 * (j / 4 * kWave + lane) + j % 4;
+          differ[k] = i < till[k] && x[k][j] != y[k][j] ? i : differ[k];
+        }
       }
       most = 0;
 #pragma unroll
@@ -233,9 +230,10 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
   const int blocks_alone = own.tiles ? Blocks<kTileKeys>(a, own.keys, own.lo, own.hi).count : 0;
   const int blocks_beside = own.tiles ? Blocks<kTileKeys>(a, own.keys, own.lo, own.hi, held).count : 0;
   const Costs cost(s, own.few), group_cost(s, all.few);
-  const unsigned long long t = own.tiles, tg = all.tiles;
-  const Six work = sum_of<NT>(Six{t * (cost.own * blocks_alone + cost.start), t * (cost.own * blocks_beside + cost.start) + tg * (group_cost.common * all.blocks + group_cost.start),
-                                    t * blocks_alone, t * blocks_beside + tg * all.blocks, own.tiles, own.tiles + all.tiles}, sixes[0]);
+  const double t = own.tiles, tg = all.tiles;
+  auto takes = [](int each, int blocks, int start) { return (double)each * (double)blocks + (double)start; };
+  const Six work = sum_of(Six{t * takes(cost.own, blocks_alone, cost.start), t * takes(cost.own, blocks_beside, cost.start) + tg * takes(group_cost.common, all.blocks, group_cost.start),
+                              t * (double)blocks_alone, t * (double)blocks_beside + tg * (double)all.blocks, own.tiles, own.tiles + all.tiles}, sixes[0], waves);
   const bool tiles = __syncthreads_or(tg > 0 && !all.few), some = __syncthreads_or(tg > 0);
   const float alone = cost.time(s, work.x, work.z, work.u, own.part_rows), together = Costs(s, !tiles).time(s, work.y, work.w, work.v, tiles ? kTileRows : 16);
   const bool worth = some && (s.always || together < alone);
@@ -245,15 +243,14 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
   own.blocks = shared ? blocks_beside : blocks_alone;
   if (leads) all.keys = from;
   else all.tiles = all.blocks = 0;
-  const unsigned long long total = worth ? work.w : work.z;
-  const unsigned long long each = quotient(total + s.pieces - 1, s.pieces);
-  int unit = (int)(each > kLeastBlocks ? each < 0x3fffffff ? each : 0x3fffffff : kLeastBlocks);
+  const double each = ((worth ? work.w : work.z) + (double)(s.pieces - 1)) / (double)s.pieces;
+  int unit = (int)fmin(fmax(each, (double)kLeastBlocks), (double)0x3fffffff);
   // Whether every tile can begin with a workgroup of its own, if these take a little more each: a workgroup that begins a second tile takes as long as 5 blocks, or an eighth of them, more.
   const int larger = unit + (unit / 8 > 5 ? unit / 8 : 5);
-  auto whole_pieces = [](const ShareOwner& o, int u) { return o.blocks > u ? (unsigned long long)o.tiles * ((o.blocks + u - 1) / u) : 0ull; };
-  const Six need = sum_of<NT>(Six{whole_pieces(all, unit) + whole_pieces(own, unit), whole_pieces(all, larger) + whole_pieces(own, larger), 0, 0, 0, 0}, sixes[1]);
-  const bool apart = need.x <= (unsigned)s.pieces || need.y <= (unsigned)s.pieces;
-  if (need.x > (unsigned)s.pieces && apart) unit = larger;
+  auto whole_pieces = [](const ShareOwner& o, int u) { return o.blocks > u ? (double)o.tiles * (double)((o.blocks + u - 1) / u) : 0.0; };
+  const Six need = sum_of(Six{whole_pieces(all, unit) + whole_pieces(own, unit), whole_pieces(all, larger) + whole_pieces(own, larger), 0, 0, 0, 0}, sixes[1], waves);
+  const bool apart = need.x <= (double)s.pieces || need.y <= (double)s.pieces;
+  if (need.x > (double)s.pieces && apart) unit = larger;
   auto cut_up = [&](ShareOwner& o) {
     o.cut = o.blocks > unit;
     o.part_pieces = o.cut ? o.blocks / unit + 2 : 1;
@@ -262,11 +259,11 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
   cut_up(own);
   cut_up(all);
   const bool direct = !shared && !own.cut;
-  const long long blocks_all = all.cut ? (long long)all.stride * all.tiles : 0, blocks_own = own.cut ? (long long)own.stride * own.tiles : 0;
+  const double blocks_all = all.cut ? (double)all.stride * (double)all.tiles : 0.0, blocks_own = own.cut ? (double)own.stride * (double)own.tiles : 0.0;
   const int parts_all = all.tiles * all.part_pieces * all.part_rows, parts_own = direct ? 0 : own.tiles * own.part_pieces * own.part_rows;
   Sums sum;
-  const Sums before = sums_before<NT>(Sums{blocks_all + blocks_own, (all.cut ? all.tiles : 0) + (own.cut ? own.tiles : 0), (all.cut ? 0 : all.tiles) + (own.cut ? 0 : own.tiles), parts_all + parts_own,
-                                           leads ? count : 0}, scratch, sum);
+  const Sums before = sums_before(Sums{blocks_all + blocks_own, (all.cut ? all.tiles : 0) + (own.cut ? own.tiles : 0), (all.cut ? 0 : all.tiles) + (own.cut ? 0 : own.tiles), parts_all + parts_own,
+                                           leads ? count : 0}, scratch, waves, sum);
   all.owner = -2 - before.members;
   all.part = before.parts;
   own.part = direct ? -1 : before.parts + parts_all;
@@ -289,10 +286,10 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
     ShareEntry e{};
     e.queries = sight.queries;
     e.direct = direct;
-    e.own = ShareParts{(double)at_blocks[2 * b + 1], own.blocks, own.part, own.part_rows, own.tiles ? own.part_pieces : 0, s.own_tile, own.cut, own.stride, 0};
+    e.own = ShareParts{at_blocks[2 * b + 1], own.blocks, own.part, own.part_rows, own.tiles ? own.part_pieces : 0, s.own_tile, own.cut, own.stride, 0};
     if (shared) {
       const ShareOwner o = owners[2 * leader];
-      e.group = ShareParts{(double)at_blocks[2 * leader], o.blocks, o.part, o.part_rows, o.part_pieces, group_tile, o.cut, o.stride, 0};
+      e.group = ShareParts{at_blocks[2 * leader], o.blocks, o.part, o.part_rows, o.part_pieces, group_tile, o.cut, o.stride, 0};
       e.row0 = rank * R;
       members[-2 - o.owner + rank] = ShareMember{b, sight.first, sight.queries, sight.keys};
     }
@@ -300,23 +297,23 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
   }
   // workgroups of the owners that are cut
   for (int w = b; w < s.pieces; w += NT) {
-    const long long at = (long long)w * unit;
+    const double at = (double)w * (double)unit;
     if (at >= sum.blocks) {
       items[w].o.owner = -1;
       continue;
     }
     const int i = last_below(at_blocks, 2 * a.B, at);
     const ShareOwner o = owners[i];
-    const long long in = at - at_blocks[i];
-    const int tile = (int)quotient(in, o.stride), i0 = (int)(in - (long long)tile * o.stride), i1 = i0 + unit < o.blocks ? i0 + unit : o.blocks;
-    const int piece = w - (int)quotient(at_blocks[i] + (long long)tile * o.stride, unit), after = at_cut[i] + tile + 1;
+    const double in = at - at_blocks[i];
+    const int tile = quotient(in, o.stride), i0 = (int)(in - (double)tile * (double)o.stride), i1 = i0 + unit < o.blocks ? i0 + unit : o.blocks;
+    const int piece = w - quotient(at_blocks[i] + (double)tile * (double)o.stride, unit), after = at_cut[i] + tile + 1;
     items[w] = ShareItem{o, tile, i0, i1, o.part + (tile * o.part_pieces + piece) * o.part_rows, !apart && i1 - i0 < unit && after < sum.cut ? s.pieces + after : -1, {0, 0, 0}};
   }
   for (int c = b; !apart && c < sum.cut; c += NT) {
     const int i = last_below(at_cut, 2 * a.B, c);
     const ShareOwner o = owners[i];
-    const long long begins = at_blocks[i] + (long long)(c - at_cut[i]) * o.blocks;
-    const int tile = c - at_cut[i], behind = (int)(begins - quotient(begins, unit) * unit);      // (a tile has more than `unit` blocks)
+    const double begins = at_blocks[i] + (double)(c - at_cut[i]) * (double)o.blocks;
+    const int tile = c - at_cut[i], behind = (int)(begins - (double)quotient(begins, unit) * (double)unit);      // (a tile has more than `unit` blocks)
     if (behind != 0) items[s.pieces + c] = ShareItem{o, tile, 0, unit - behind, o.part + tile * o.part_pieces * o.part_rows, -1, {0, 0, 0}};
   }
   for (int i = 2 * s.pieces + sum.whole + b; i < s.items; i += NT) items[i].o.owner = -1;
@@ -358,9 +355,9 @@ SharePlan share_plan(const ficoco_cache& c, const ficoco_attention& a) {
 }
 
 void launch_share(const ShareArgs& s, hipStream_t stream) {
-  // Few wavefronts wait less for each other, but each compares four members at once: 64 members 19.9 us by 512 threads, 25.4 by 1024, 24.5 by 256; 16 of 141 pages 15.5 by 256.
+  // Few wavefronts wait less for each other, many compare more members at once: 64 members behind 256 pages 13 us by 1024 threads, 15 by 512, 19 by 256; 48 behind up to 750 13.5, 16 and 19; 8 behind 10
+  // 8.6 by 256, 10.6 by 512; 16 behind 140 13.6 and 15.
   if (s.a.B <= 16) hipLaunchKernelGGL(share_plan_kernel<256>, dim3(1), dim3(256), 0, stream, s);
-  else if (s.a.B <= 512) hipLaunchKernelGGL(share_plan_kernel<512>, dim3(1), dim3(512), 0, stream, s);
   else hipLaunchKernelGGL(share_plan_kernel<kMaxCall>, dim3(1), dim3(kMaxCall), 0, stream, s);
 }
 
