@@ -6,8 +6,10 @@
 namespace ficoco {
 namespace {
 
-constexpr int kLeastBlocks = 4;                  // blocks of a workgroup
-constexpr int kMostPieces = 512;                 // workgroups for a head: two a compute unit (see attend_plan())
+// Blocks of a workgroup: 4 at least (8 answers behind 675 tokens, plan and four layers: 61 us, by 2 59, by 8 71; longer prompts no difference).  Workgroups that all heads share: two a compute unit
+// (64 answers behind 16384 tokens, plan and two layers: 106 us, by 384 112, by 768 116, by 1024 128; 16 questions behind 9000 158, by 384 173).
+constexpr int kLeastBlocks = 4;
+constexpr int kMostPieces = 512;
 // Tiles of a group have 16 rows where 3 (tiles of 16) - 8 (tiles of 128), times its blocks, times the heads, is below this: three of the former take about as long for a block as one of the latter,
 // which take 4 us more to begin and end.  64 rows of 8 heads of 128: behind 512 common tokens 10.9 us and 15.2, 2048 13.6 and 16.7, 8192 20.9 and 21.6, 16384 28.0 and 28.4; of 32 heads
 // behind 2048 40.1 and 39.0, 8192 57.8 and 52.5; 32 rows 19.7 and 26 behind 16384; 112 rows of 4 heads of 64 behind 4096 11.7 and 13.9.
