@@ -4,6 +4,15 @@
 namespace ficoco {
 namespace {
 
+// to_e4m3() of values that are numbers and stay within the largest one.
+__device__ __forceinline__ uint2 numbers_to_e4m3(const float (&x)[8], float inv) {
+  int a = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, 0, false);
+  a = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, a, true);
+  int b = __builtin_amdgcn_cvt_pk_fp8_f32(x[4] * inv, x[5] * inv, 0, false);
+  b = __builtin_amdgcn_cvt_pk_fp8_f32(x[6] * inv, x[7] * inv, b, true);
+  return uint2{(uint32_t)a, (uint32_t)b};
+}
+
 // One workgroup per touched page, head, sequence and K / V, as cache_append_kernel (cache.hip); a lane holds the two chunks of a slot of a key, so that
 // pairs that turn together are in one lane and a key's norm takes D / 16 lanes.
 //
@@ -59,14 +68,30 @@ __global__ __launch_bounds__(kMoveThreads) void append_rotated_kernel(ficoco_cac
       }
     }
   }
+  // Magnitudes as whole numbers, in their order; those from infinity's on do not count, and a wavefront that has any looks at each value for itself.
+  uint32_t most = 0;
   float top = 0.0f;
 #pragma unroll
   for (int j = 0; j < GPT; ++j) {
     const int row = (threadIdx.x + j * kMoveThreads) >> row_shift;
     const int64_t pos = pos0 + row;
-    const bool fresh = row < P && pos >= sp.first && pos < sp.stop;
+    uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = fmaxf(top, fresh ? finite_magnitude(v[j][0][i]) : 0.0f);       // (a bias makes something of rows that are not there)
+    for (int i = 0; i < 16; ++i) m = max(m, __float_as_uint(v[j][0][i]) & 0x7fffffffu);
+    if (row < P && pos >= sp.first && pos < sp.stop) most = max(most, m);       // (a bias makes something of rows that are not there)
+  }
+  const bool numbers = __all(most < 0x7f800000u);
+  if (numbers) {
+    top = __uint_as_float(most);
+  } else {
+#pragma unroll
+    for (int j = 0; j < GPT; ++j) {
+      const int row = (threadIdx.x + j * kMoveThreads) >> row_shift;
+      const int64_t pos = pos0 + row;
+      const bool fresh = row < P && pos >= sp.first && pos < sp.stop;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, fresh ? finite_magnitude(v[j][0][i]) : 0.0f);
+    }
   }
   int e = block_exponent(block_max(top, scratch));
   e = e > old ? e : old;
@@ -85,6 +110,10 @@ __global__ __launch_bounds__(kMoveThreads) void append_rotated_kernel(ficoco_cac
       if (e == old) continue;
       from_e4m3(*to_a, exp_scale(old), a);
       from_e4m3(*to_b, exp_scale(old), z);
+    } else if (numbers && e != kExpTop) {                  // (uniform) no value is beyond the block's largest number
+      *to_a = numbers_to_e4m3(a, inv);
+      *to_b = numbers_to_e4m3(z, inv);
+      continue;
     } else if (e == kExpTop) {
       keep_finite(a);
       keep_finite(z);
