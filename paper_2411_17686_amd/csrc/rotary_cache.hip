@@ -16,9 +16,9 @@ __device__ __forceinline__ uint2 numbers_to_e4m3(const float (&x)[8], float inv)
 // One workgroup per touched page, head, sequence and K / V, as cache_append_kernel (cache.hip); a lane holds the two chunks of a slot of a key, so that
 // pairs that turn together are in one lane and a key's norm takes D / 16 lanes.
 //
-// 8 ragged prompts of up to 2979 tokens, 8 heads of 128, three axes, 111 MB: 43 us (2.6 TB/s), of which 10 are the sines (without any rotation 34, values alone 27 for all of it, which is
-// memory's): every head forms them again.  Two heads a workgroup, or four one after the other with one set of angles, take more registers or wait more often: 54 and 50 us.  A workgroup of 512 threads with one row each
-// 44 us, two wavefronts more a SIMD with what they leave of registers 50.
+// 8 ragged prompts of up to 2979 tokens, 8 heads of 128, three axes, 107 MB: 41 us (2.6 TB/s), some 9 of them for the sines, which every head forms again (values alone: 27 for as many bytes, as fast as memory
+// gives them).  Two heads a workgroup, or four one after the other with one set of angles, take more registers or wait more often: 54 and 50 us, where this took 43; angles in front of the
+// page 44; a workgroup of 512 threads with one row each 44, registers for two wavefronts more a SIMD 50.
 template <typename T, int GPT>
 __global__ __launch_bounds__(kMoveThreads) void append_rotated_kernel(ficoco_cache c, int64_t layer_pages, RotaryArgs r, TokenSide ks, TokenSide vs, int n_max,
                                                                       const int32_t* __restrict__ seq, const int32_t* __restrict__ start,
