@@ -270,3 +270,18 @@ def test_outputs_over_what_is_read(ctx):
     rotate(pos=ints(small - 4 * n, 1, n), start=ints(small - 4, 1), q_weight=floats(end, heads, d), k_weight=floats(small - 8 * d, heads, d), **norm)
     torch.cuda.synchronize()
     assert not memory.any()            # (a weight of zeros)
+
+
+@pytest.mark.parametrize("d,rot,begin", [(500, 500, 0), (260, 260, 0), (256, 252, 2), (300, 260, 20), (129, 128, 0), (128, 126, 1), (131, 2, 0)])
+@pytest.mark.parametrize("dtype,norm", [(BF, 0), (F, 1), (BF, 2)])
+def test_chunks_of_two_and_one_by_as_many_lanes_as_there_are(ctx, d, rot, begin, dtype, norm):
+    """Slots of one, two and four a lane: a wavefront's 64 lanes just hold them, or just do not."""
+    B, n, H, Hk = 2, 3, 2, 1
+    for layout in (H_, P_):
+        r = rotary(d, rot, norm, bias=norm == 2, layout=layout, rot_begin=begin)
+        Q, K = rows_of(B, H, n, d, dtype, 11), rows_of(B, Hk, n, d, dtype, 12)
+        Q0, K0 = Q.clone(), K.clone()
+        fc.ficoco_rotate(ctx, r, Q, K, start=i32([7, 60000]))
+        p = (np.array([7, 60000], np.int64)[:, None] + np.arange(n))[None]
+        check(r, Q0, Q, 0, p, [n] * B, Q)
+        check(r, K0, K, 1, p, [n] * B, K)
