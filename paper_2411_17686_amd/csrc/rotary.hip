@@ -25,8 +25,8 @@ struct RowShape {
 template <typename T, typename TO, int W, int NS, NormForm NORM>
 __global__ __launch_bounds__(kRotateThreads) void rotate_kernel(RotateArgs a, RowShape shape) {
   // Heads of a lane whose loads are on their way together: two (the 537 MB above 104 us, by one 108, by four 102; 2 prompts of 4100 tokens in single precision with a norm 36 us, 39 and 38), but one
-  // where weights and a norm of 16 features a lane need the registers (the 356 MB above 79 us, by two 82).  (The next heads' loads before these heads are done: 113 us and 99.)
-  constexpr int kAtOnce = NORM != kNoNorm && W == 8 ? 1 : 2;
+  // where a norm has more to do for each byte and registers for more wavefronts count (the 356 MB above 79 us, by two 82; 16720 tokens, 20 heads of 72, a root mean square 30 and 32, a mean taken out 38 and 42).  (The next heads' loads before these heads are done: 113 us and 99.)
+  constexpr int kAtOnce = NORM != kNoNorm && sizeof(T) == 2 ? 1 : 2;
   const int at = blockIdx.x * kRotateThreads + threadIdx.x, all = shape.by_lanes.of(at), token = shape.by_items.of(all), b = shape.by_rows.of(token);
   const int i = at - all * shape.lanes, t = token - b * a.n, in = all - token * (shape.q_items + shape.k_items);
   if (b >= a.B) return;
