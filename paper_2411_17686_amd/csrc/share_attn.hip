@@ -145,7 +145,7 @@ __device__ __forceinline__ PartsOf parts_of(const ShareParts& p, int r, int h, i
 // Rows that have parts: those of their own keys and of their group's, relative to their largest maximum, eight at a time; D / 4 lanes a row and group of parts, the
 // groups' sums meet in LDS (as join_rows_kernel).
 //
-// Bound by memory and latency: 64 sequences, 32 heads of 128 10 us, 16 questions of 48 queries 14 us (the parts once, 3 TB/s); 8 sequences 4 us, a launch and three trips.  One group of lanes a row where there are few parts.
+// Bound by memory and latency: 64 sequences, 32 heads of 128 8 us, 16 questions of 48 queries 14 us (the parts once, 3.6 and 4.5 TB/s); 8 sequences 4 us, a launch and three trips.
 template <int D, int GROUPS>
 __global__ __launch_bounds__(kFewWaves * kWave) void share_join_kernel(ShareArgs s) {
   constexpr int L = D / 4, AT_ONCE = 8;
@@ -228,9 +228,17 @@ template <int D>
 void launch_rows(const ShareArgs& s, hipStream_t stream) {
   const dim3 grid((unsigned)((int64_t)(s.items - s.pieces) * s.a.H_kv));
   hipLaunchKernelGGL(share_rows_kernel<D>, grid, dim3(kTileThreads), 0, stream, s);
-  // Parts of a tile, if all rows were of one group: more than one batch of them by eight groups of lanes.
-  const int64_t tiles = std::max<int64_t>(1, (int64_t)s.a.B * s.by_rows.d / kTileRows);
-  if (s.pieces / tiles > 8) launch_join<D, 8>(s, stream); else launch_join<D, 1>(s, stream);
+  // Groups of lanes a row: as many as take the parts of a tile at once, if all rows were of one group, and as fill the chip.  Rows and join, 16 rows of 60000 tokens by 8 groups 18.4 us, by 4 22.0, by 1 44; 64 of them
+  // 32.1, 32.9 and 39.1; 960 of 9000 by 8 28.4, by 4 27.8, by 2 27.6; 2048 of 16384 52.6, 50.7 and 50.6, by 1 51.4; 6400 of 3000 67.0, 62.0, 59.1 and 57.4.
+  const int64_t rows = (int64_t)s.a.B * s.by_rows.d, tiles = std::max<int64_t>(1, rows / kTileRows), threads = rows * s.a.H_kv * (D / 4);
+  int groups = 1;
+  while (groups < 8 && s.pieces / tiles > 8 * groups && 2 * groups * threads <= 1 << 17) groups *= 2;
+  switch (groups) {
+    case 8: launch_join<D, 8>(s, stream); break;
+    case 4: launch_join<D, 4>(s, stream); break;
+    case 2: launch_join<D, 2>(s, stream); break;
+    default: launch_join<D, 1>(s, stream); break;
+  }
 }
 
 }  // namespace
