@@ -7,7 +7,7 @@ namespace ficoco {
 namespace {
 
 // Blocks of a workgroup: 4 at least (8 answers behind 675 tokens, plan and four layers: 61 us, by 2 59, by 8 71; longer prompts no difference).  Workgroups that all heads share: two a compute unit
-// (64 answers behind 16384 tokens, plan and two layers: 106 us, by 384 112, by 768 116, by 1024 128; 16 questions behind 9000 158, by 384 173).
+// (64 answers behind 16384 tokens, plan and two layers: 101 us, by 384 108, by 768 113, by 1024 125; 16 questions behind 9000 153, by 384 169).
 constexpr int kLeastBlocks = 4;
 constexpr int kMostPieces = 512;
 // Tiles of a group have 16 rows where 3 (tiles of 16) - 8 (tiles of 128), times its blocks, times the heads, is below this: three of the former take about as long for a block as one of the latter,
