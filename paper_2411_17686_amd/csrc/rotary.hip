@@ -116,9 +116,10 @@ RowShape shape_of(const RotateArgs& a, int width) {
     for (s.lanes = 1; s.lanes < kWave && s.lanes < slots;) s.lanes *= 2;
   // Items of four heads share their angles, where there are rows enough to fill the chip that way: 40 heads of 128 with a norm, 400 tokens 6.9 us, by items of one head 5.2, 800 tokens 7.7 and 8.3,
   // 20000 tokens 80 and 130; 32 heads of 64 in single precision, 800 tokens 5.0 and 4.9, 1600 tokens 6.3 and 7.2.  (The 537 MB of rotate_kernel() by items of two 102 us, of four 104, of eight 109; its 356 MB by eight 79 as by four.)
-  s.heads = (int64_t)a.B * a.n * (a.q.heads + a.k.heads) * a.r.d >= 3 << 20 ? 4 : 1;
-  s.q_items = (a.q.heads + s.heads - 1) / s.heads;
-  s.k_items = (a.k.heads + s.heads - 1) / s.heads;
+  const int64_t q_heads = a.q.heads, k_heads = a.k.heads;      // (as many as 32 bits hold: what follows asks for more)
+  s.heads = (__int128)a.B * a.n * (q_heads + k_heads) * a.r.d >= 3 << 20 ? 4 : 1;
+  s.q_items = (int)((q_heads + s.heads - 1) / s.heads);
+  s.k_items = (int)((k_heads + s.heads - 1) / s.heads);
   s.by_lanes = Divisor(s.lanes);
   s.by_items = Divisor((int64_t)s.q_items + s.k_items);
   s.by_rows = Divisor(a.n);

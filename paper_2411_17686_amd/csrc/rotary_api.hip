@@ -49,6 +49,7 @@ bool same(const Span3& x, const Span3& y) {
 }
 
 constexpr int kMaxHead = 512;
+constexpr int64_t kMaxHeads = 0x3fffffff;      // of a call (a lane counts them in 32 bits, and beyond the last one)
 
 const char* rotary_fault(const ficoco_rotary& r) {
   if (r.d_head < 1) return "d_head is not positive";
@@ -125,7 +126,7 @@ int ficoco_rotate(ficoco_ctx* ctx, const ficoco_rotary* r, const ficoco_rotation
     return fail(ctx, FICOCO_EINVAL, fn, "unknown dtype");
   if (x->B == 0 || x->n == 0) return FICOCO_OK;
   if (!x->Q && !x->K) return fail(ctx, FICOCO_EINVAL, fn, "Q and K are both NULL");
-  if ((int64_t)(x->Q ? x->H : 0) + (x->K ? x->H_kv : 0) > 0x3fffffff) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "too many heads");
+  if ((int64_t)(x->Q ? x->H : 0) + (x->K ? x->H_kv : 0) > kMaxHeads) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "too many heads");
   RotateArgs a{};
   a.r = rotary_args(*r, *x);
   a.q = queries(*x);
@@ -161,6 +162,7 @@ int ficoco_cache_append_rotated(ficoco_ctx* ctx, const ficoco_cache* c, int32_t 
   if (x->Q && (x->dtype != t->dtype || (x->out_dtype != FICOCO_F32 && x->out_dtype != FICOCO_BF16)))
     return fail(ctx, FICOCO_EINVAL, fn, "Q must have the type of K, Q_out a known one");
   if (t->n == 0 || t->n_max == 0) return FICOCO_OK;
+  if (x->Q && x->H > kMaxHeads) return fail(ctx, FICOCO_EUNSUPPORTED, fn, "too many heads");
   RotateArgs a{};
   a.r = rotary_args(*r, *x);
   a.r.start = nullptr;

@@ -1,8 +1,9 @@
 // What a test may ask about the plan of a problem: where the block of approximate cosines, the unit rows, the text
 // profiles and their maxima lie in the workspace, how the block is cut, and the error its readers allow for; how the reduction
-// of the maps is cut; the order of causal tiles; the form of the feature passes.  (Host code only.)
+// of the maps is cut; the order of causal tiles; the form of the feature passes; the threads of a rotation.  (Host code only.)
 #include "../../paper_2411_17686_amd/csrc/common.hpp"
 #include "../../paper_2411_17686_amd/csrc/causal_tiles.hpp"
+#include "../../paper_2411_17686_amd/csrc/rotary.hpp"
 
 extern "C" {
 
@@ -46,6 +47,15 @@ int plan_hook_causal_live_first(int units, int k_tiles) { return ficoco::causal_
 // The order of all groups x k_tiles tiles: group and key tile of each.
 void plan_hook_causal_tiles(int groups, int k_tiles, int per, int full, int32_t* out) {
   for (int unit = 0; unit < groups * k_tiles; ++unit) ficoco::causal_tile(unit, groups, k_tiles, per, full, out[2 * unit], out[2 * unit + 1]);
+}
+
+// Threads of a call with `heads` query heads and `kv` key heads of d features, the first `rot` of them rotated by halves.
+int64_t plan_hook_rotate_threads(int B, int n, int heads, int kv, int d, int rot, int norm, int dtype, int out_dtype) {
+  ficoco::RotateArgs a{};
+  a.r.d = d; a.r.rot = rot; a.r.norm = norm;
+  a.q.heads = heads; a.k.heads = kv;
+  a.B = B; a.n = n;
+  return ficoco::rotate_threads(a, dtype, out_dtype);
 }
 
 }  // extern "C"

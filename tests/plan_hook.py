@@ -52,3 +52,9 @@ def causal_long_first(keys_of_first, keys_of_last):
 
 def unit_rows_summed(p):
     return bool(_lib().plan_hook_unit_rows_summed(C.byref(p)))
+
+
+def rotate_threads(B, n, heads, kv, d, rot, norm, dtype, out_dtype):
+    f = _lib().plan_hook_rotate_threads
+    f.restype = C.c_int64
+    return f(B, n, heads, kv, d, rot, norm, dtype, out_dtype)
