@@ -312,6 +312,7 @@ def test_refused(ctx):  # noqa: F811
 
 LARGE = [  # prompt tokens, tokens of a sequence behind them, sequences, page, heads, query heads a head, d, n_q, window
     (4096, 100, 64, 64, 8, 4, 128, 1, 0),      # tiles of 128 cut into workgroups that go on with the next tile
+    # (not so: each of its tiles begins with a workgroup of its own.  Workgroups that go on with another tile, of either kind: test_gpu_share_records.py)
     (6000, 77, 24, 32, 32, 1, 64, 1, 0),
     (3000, 200, 16, 64, 4, 4, 128, 24, 0),
     (3000, 200, 16, 16, 2, 7, 64, 24, 2500),
