@@ -520,8 +520,9 @@ int ficoco_window_attention(ficoco_ctx *ctx, const ficoco_attention *a, void *st
  *   rotation  pair i of the rotated features becomes (a cos - b sin, b cos + a sin) * amplitude with the angle f[i] * (position of the
  *             token on axis[i]).  Features in front of rot_begin and from rot_begin + rot_dim on keep the value that the norm gave.
  *
- * Angles are counted in turns, as 64-bit fractions: position * turns[i] modulo 2^64 is the fraction of a turn, whatever the position (within
- * 2^-33 of a turn at position 2^31; a negative position turns backwards, so that -p undoes p where amplitude is 1 and there is no norm).  Sines and cosines are within 2^-23. */
+ * Angles are counted in turns, as 64-bit fractions: position * turns[i] modulo 2^64 is the fraction of a turn, whatever the position (a negative position turns
+ * backwards, so that -p undoes p where amplitude is 1 and there is no norm).  Of it the upper 32 bits count, and their sines and cosines are within 2^-23: what is left out is
+ * below 2^-32 of a turn.  What turns[i] itself is off counts once a token: see ficoco_frequencies. */
 typedef enum {
   FICOCO_ROTARY_HALVES = 0, /* pair i: features rot_begin + i and rot_begin + i + rot_dim / 2 */
   FICOCO_ROTARY_PAIRS = 1   /* pair i: features rot_begin + 2 i and rot_begin + 2 i + 1       */
@@ -531,7 +532,9 @@ typedef enum { FICOCO_NORM_NONE = 0, FICOCO_NORM_RMS = 1, FICOCO_NORM_LAYER = 2 
 /* Frequencies in radians a token: f[i] = base^(-2 i / rot_dim) / divisors[i] (divisors NULL: ones).  For contexts longer than those trained by `factor`:
  * length = 0: every f[i] is divided by factor; otherwise f[i] (s + (1 - s) / factor), s = (length f[i] / 2 pi - low) / (high - low), at least 0 and at most 1:
  * frequencies of fewer than `low` turns over `length` tokens are divided, those of more than `high` kept.  (A base that grows with the context: give that base.)
- * turns [rot_dim / 2], out: f[i] / 2 pi modulo 1 in units of 2^-64.  Host arithmetic on host memory; the table is copied to the device once. */
+ * (The line is one over the number of turns.  One over the index of the pair, or any other rule: by divisors.)
+ * turns [rot_dim / 2], out: f[i] / 2 pi modulo 1 in units of 2^-64, by extended precision: within 4 units, 2^-31 of a turn at position 2^31, where base >= 1 and no f[i] passes one radian a
+ * token (and length >= 8 high^2 / (high - low)); within 3 + 2 max(f) units where base >= 1 and some do, by divisors or a factor below 1.  Host arithmetic on host memory; the table is copied to the device once. */
 typedef struct {
   int32_t rot_dim;
   double base, factor, length, low, high;
