@@ -108,7 +108,7 @@ ShareArgs share_arguments(const ficoco_cache& c, const ficoco_attention& a, cons
   s.mark = mark;
   s.plan = (char*)plan;
   s.by_rows = Divisor((int64_t)a.n_q * (a.H / c.heads));
-  s.own_tile = pl.own_tile; s.own_tiles = pl.own_tiles; s.pieces = pl.pieces; s.items = pl.items;
+  s.own_tile = pl.own_tile; s.pieces = pl.pieces; s.items = pl.items;
   s.d_head = a.d_head;
   s.entries = pl.entries; s.members = pl.members; s.owners = pl.owners; s.items_at = pl.items_at;
   return s;

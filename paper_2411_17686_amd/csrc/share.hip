@@ -293,7 +293,7 @@ __global__ __launch_bounds__(NT) void share_plan_kernel(ShareArgs s) {
       const ShareOwner o = owners[2 * leader];
       e.group = ShareParts{at_blocks[2 * leader], o.blocks, o.part, o.part_rows, o.part_pieces, group_tile, o.cut, o.stride, 0};
       e.row0 = rank * R;
-      members[-2 - o.owner + rank] = ShareMember{b, sight.first, sight.queries, sight.keys};
+      members[-2 - o.owner + rank] = ShareMember{b, sight.first, sight.queries, 0};
     }
     entries[b] = e;
   }

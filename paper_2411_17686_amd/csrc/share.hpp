@@ -35,7 +35,7 @@ struct ShareEntry {
   ShareParts own, group;
   int queries, direct, row0, pad;            // row0: its first row among the group's
 };
-struct ShareMember { int b, first, queries, keys; };
+struct ShareMember { int b, first, queries, pad; };
 struct ShareHead { uint64_t mark; int unit, pad[13]; };        // unit: blocks of a workgroup
 
 // The blocks of all tiles of the owners that are cut, one tile after the other, go to workgroups `unit` at a time: as many as are resident at once, and they end together.  A workgroup that comes to the
@@ -54,7 +54,7 @@ struct ShareArgs {
   char* plan;
   const int32_t* group;
   Divisor by_rows;                           // n_q * group
-  int own_tile, own_tiles, pieces, items, d_head, always;
+  int own_tile, pieces, items, d_head, always;
   size_t entries, members, owners, items_at;
 };
 void launch_share(const ShareArgs& s, hipStream_t stream);
