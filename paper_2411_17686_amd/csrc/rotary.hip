@@ -139,7 +139,8 @@ void launch_norm(const RotateArgs& a, hipStream_t s) {
   else launch_rows<T, TO, W, 1, kAnyNorm>(a, s);
 }
 // A slot a lane; several where there are more slots than a wavefront has lanes, of chunks of two beyond 256 features, of one beyond 128 (always room for several: 16 heads of 72 of which 36 turn, 35810 tokens of
-// bfloat16, 87 us instead of 44; of 66, 30000 tokens, 223 instead of 48).
+// bfloat16, 87 us instead of 44; of 66, 30000 tokens, 223 instead of 53).  Without a norm chunks of one, too, go by the form that has none, two heads at once (the 66 features 38 us, by the general form, one head at
+// once for a norm's sake, 53; 96 of which 50 turn 51 and 86); several slots a lane are better off with the general one (300 features, 15000 tokens, 122, by two heads at once 137; 201 of which 50 turn 165 and 261).
 template <typename T, typename TO>
 void launch_width(const RotateArgs& a, hipStream_t s) {
   constexpr int most = sizeof(T) == 2 && sizeof(TO) == 2 ? 8 : 4;
@@ -149,7 +150,10 @@ void launch_width(const RotateArgs& a, hipStream_t s) {
     case 8: if constexpr (most == 8) launch_norm<T, TO, 8>(a, s); break;
     case 4: launch_norm<T, TO, 4>(a, s); break;
     case 2: if (one) launch_norm<T, TO, 2>(a, s); else launch_rows<T, TO, 2, 2, kAnyNorm>(a, s); break;
-    default: if (one) launch_rows<T, TO, 1, 1, kAnyNorm>(a, s); else launch_rows<T, TO, 1, 4, kAnyNorm>(a, s); break;
+    default:
+      if (!one) launch_rows<T, TO, 1, 4, kAnyNorm>(a, s);
+      else if (a.r.norm == FICOCO_NORM_NONE) launch_rows<T, TO, 1, 1, kNoNorm>(a, s);
+      else launch_rows<T, TO, 1, 1, kAnyNorm>(a, s);
   }
 }
 
