@@ -498,6 +498,7 @@ int ficoco_cache_attention(ficoco_ctx *ctx, const ficoco_cache *c, int32_t layer
  * table, whatever the caller says: group decides how the work is cut, never the result's meaning); ficoco_cache_shared_attention computes one layer by it.
  *   group [B]: sequences with the same number 0 .. B - 1 are taken together, all others for themselves; NULL = all of them for themselves.
  *   always: 0 = where the plan finds that to take less time (few sequences behind a short prompt are faster for themselves), else wherever there are common keys.
+ *     Where little is shared, ficoco_cache_attention is faster than either by some microseconds a layer, and needs no plan.
  *   a: as for ficoco_cache_attention.  For the plan, Q, O, their strides and scale do not count; for the attention, seq and the arrays of lengths and positions do not: they, the
  *   lengths of the cache and its table are those that the plan found.  All other sizes, window, sinks and max_len have to be the same for both (with others, or without a plan, nothing is written).
  * A plan holds until the lengths of its sequences or their rows of the table change; whoever changes them makes another.  B <= 1024 (FICOCO_EUNSUPPORTED otherwise).  Plan

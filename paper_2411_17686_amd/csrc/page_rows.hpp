@@ -39,7 +39,7 @@ struct PageLds {
 // the second trip through LDS that a common conversion takes.
 //
 // Bound by the vector instructions beside the products: a step of a wavefront is 0.53 us of products and about as much of conversions, exponentials
-// and sums, and takes 1.05 us with two wavefronts a SIMD.  Questions of 64 tokens behind 1251 .. 2400, 8 sequences, 32 heads on 8: 33 us (a third of it
+// and sums, and takes 1.6 to 1.7 us beside another wavefront on its SIMD (workgroups of 54 steps 95 us at best).  Questions of 64 tokens behind 1251 .. 2400, 8 sequences, 32 heads on 8: 33 us (a third of it
 // before the first step and after the last), 7 more for the join.  Weights are rounded to bfloat16 for the second product, as in few_rows() (few_rows.hpp).  Sixty-four rows a wavefront, one wavefront a SIMD, halve the conversions,
 // but nothing then fills its waits for LDS and barriers: 57 us instead of 40 with the queries in LDS (73 without, for lack of registers), and with heads of 64, where nothing is
 // short of registers, 102 instead of 69 behind 9600 tokens.

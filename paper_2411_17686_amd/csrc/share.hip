@@ -6,7 +6,7 @@
 namespace ficoco {
 namespace {
 
-// Blocks of a workgroup: 4 at least (8 answers behind 675 tokens, plan and four layers: 61 us, by 2 59, by 8 71; longer prompts no difference).  Workgroups that all heads share: two a compute unit
+// Blocks of a workgroup: 4 at least (8 answers behind 675 tokens, plan and four layers: 61 us, by 2 59 to 65, by 8 71 to 73; 64 behind 16384 99 to 101 by either).  Workgroups that all heads share: two a compute unit
 // (64 answers behind 16384 tokens, plan and two layers: 101 us, by 384 108, by 768 113, by 1024 125; 16 questions behind 9000 153, by 384 169).
 constexpr int kLeastBlocks = 4;
 constexpr int kMostPieces = 512;
@@ -63,8 +63,9 @@ __device__ __forceinline__ Six sum_of(Six p, Six* scratch, int waves) {
 
 // What workgroups take, in sixteenths of a microsecond of one of two places of a compute unit (measured with heads of 128; of 64 as much for a sequence's own 16 rows, half of it for the others): a block of 64 keys for 16 rows
 // of a sequence 13, of a group 18, for 128 rows 34; to begin and end 72, or 144.  From these the time of a call: what all workgroups take over all places, or the longest of them and the beginnings of those that have to wait for a place, and the join, which reads and writes
-// the parts at 3 TB/s and takes 1.5 us to begin.  It decides whether the common keys of the groups are worth it: 64 sequences, 32 heads on 8 of 128, behind 512 common tokens 16.4 us without, 20.3 with them; behind 1024 21.8
-// and 21.9, 4096 53.6 and 28; 8 behind 512 10.4 and 10.6, 4096 16.9 and 13.3; 16 questions of 48 tokens behind 512 37 and 41, 9000 163 and 138.
+// the parts at 3 TB/s and takes 1.5 us to begin.  It decides whether the common keys of the groups are worth it, against this attention without them: 64 sequences, 32 heads on 8 of 128, behind 512 common tokens 15.6 us without,
+// 17.7 with them; behind 1024 20.6 and 16.4 (where the rule still does without), 4096 53.2 and 22.8; 8 behind 512 10.1 and 10.4, 4096 16.6 and 13.2; 16 questions of 48 tokens behind 512 37.8 and 41.2, 9000 162 and 138.
+// (ficoco_cache_attention, which needs no plan, launches what has work and joins only what is cut, in the same order: 12.3, 18.0, 52.5; 8.8, 14.2; 35.9, 159.  The rule does not know of it.)
 struct Costs {
   int own, common, start;
   __device__ __forceinline__ Costs(const ShareArgs& s, bool few) : own(few ? 13 : 34), common(few ? 18 : 34), start(few ? 72 : 144) {

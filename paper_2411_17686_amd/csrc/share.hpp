@@ -38,7 +38,8 @@ struct ShareEntry {
 struct ShareMember { int b, first, queries, pad; };
 struct ShareHead { uint64_t mark; int unit, pad[13]; };        // unit: blocks of a workgroup
 
-// The blocks of all tiles of the owners that are cut, one tile after the other, go to workgroups `unit` at a time: as many as are resident at once, and they end together.  A workgroup that comes to the
+// The blocks of all tiles of the owners that are cut, one tile after the other, go to workgroups `unit` at a time: as many as are resident at once.  They have equally many blocks, not equally much to do: a block of
+// a tile of 128 rows takes twice as long as one of 16 (22 blocks of the former 27 to 28 us, of the latter 13 to 18, in one launch of 30).  A workgroup that comes to the
 // end of a tile goes on with the next one, or, where there are workgroups enough for that, every tile begins with one of its own.  (As workgroups of their own such beginnings wait, while others have ended, for a place on the shader engine whose turn it is: 8 sequences of 16484 tokens 48 us
 // so.)  Items: [0, pieces) where these workgroups begin, [pieces, 2 pieces) beginnings of tiles that they come to, [2 pieces, items) tiles that are not cut.
 struct SharePlan {

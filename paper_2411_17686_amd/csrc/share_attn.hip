@@ -105,10 +105,11 @@ __device__ __forceinline__ void share_tile(const ShareArgs& s, const ShareItem& 
 }
 
 // Bound by what few_rows() and page_rows() are bound by, common keys counted once for a group.  Heads of 128:
-//   8 answers behind 675 tokens, 32 heads            9.5 us  (9 MB) a launch, three trips to memory and the blocks of a workgroup
-//   64 answers behind 16384, 32 heads on 8          39 us    (17.4 GFLOP of products for the common keys, 13 MB of own keys) tiles of 128 rows: their 8 us of start, then 1.05 us a block
-//   16 questions of 48 behind 9000, 32 heads on 8  146 us    (113 GFLOP, 0.78 PFLOP/s) vector instructions beside the products, as page_rows()
-// and 48 sequences, 5 prompts of up to 24000, 28 heads of 64 on 4 32 us (82 MB, 2.6 TB/s).  Either kind of tile is in one launch, so that the one fills the places that the other leaves: a launch for each took 108 us instead of 102 for the last of these calls, 226 instead of 212 for the one before.
+//   8 answers behind 675 tokens, 32 heads          8.8 .. 10.3 us (9 MB) a launch, three trips to memory and the blocks of a workgroup
+//   64 answers behind 16384, 32 heads on 8          39 us    (17.4 GFLOP of products for the common keys, 13 MB of own keys) tiles of 128 rows, two a compute unit: 11 blocks 24 to 32 us, 3 blocks 12 to 17, so
+//                                                            7 us to begin and end and 1.65 a block; then the own keys of the last sequences
+//   16 questions of 48 behind 9000, 32 heads on 8  143 .. 154 us (113 GFLOP, 0.74 to 0.79 PFLOP/s) vector instructions beside the products, as page_rows(): 54 blocks 95 to 136 us
+// and 48 sequences, 5 prompts of up to 24000, 28 heads of 64 on 4 31 us (82 MB, 2.6 TB/s).  (36 to 48 scalars go over lanes of a vector register, since both kinds of tile are in one kernel; none over memory.)  Either kind of tile is in one launch, so that the one fills the places that the other leaves: a launch for each took 108 us instead of 102 for the last of these calls, 226 instead of 212 for the one before.
 template <int D>
 __global__ __launch_bounds__(kTileThreads, 2) void share_rows_kernel(ShareArgs s) {
   static_assert(kTileThreads == kFewWaves * kWave && kFewKeys * 2 == kTileKeys, "either kind of tile");
