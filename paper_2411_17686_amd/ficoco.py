@@ -621,7 +621,8 @@ def ficoco_cache_attention(ctx, cache, layer, Q, O, ws, scale=None, window=0, si
 
 class Share:
     """Plan and workspace of a batch of B sequences, H query heads and n_q queries each, that ficoco_cache_share fills and
-    ficoco_cache_shared_attention goes by."""
+    ficoco_cache_shared_attention goes by.  The plan is cleared on the current stream: another one that uses it first waits for that, as for any
+    tensor made there.  Two calls at once need a Share each (the workspace serves one call at a time)."""
 
     def __init__(self, cache, B, H, n_q, window=0, sinks=0, max_len=0):
         self.shape, self.index = (B, H, n_q, cache.d_head), cache.index
